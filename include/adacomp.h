@@ -380,6 +380,136 @@ ADACOMP_API int adacomp_decode_values(const uint32_t* d_words, uint64_t words_pe
                                       const uint64_t* d_block_off, uint64_t pairs_per_worker,
                                       uint32_t n_workers, float* d_val_out, int device, void* cuda_stream);
 
+/* ---- element types ------------------------------------------------------------------------
+ * The operators below take half-precision tensors too (the selection and the server stay fp32). */
+enum {
+    ADACOMP_F32 = 0,                /* IEEE binary32 */
+    ADACOMP_BF16 = 1,               /* bfloat16 */
+    ADACOMP_F16 = 2                 /* IEEE binary16 */
+};
+enum {
+    ADACOMP_I32 = 0,                /* 32-bit token numbers */
+    ADACOMP_I64 = 1                 /* 64-bit token numbers */
+};
+
+/* ------------------------------------------------------------------------------------------
+ * Global gradient norm and clipping (what a worker does to its gradients before it selects; no counterpart in the
+ * paper, whose gradients are used as they come).
+ * ---------------------------------------------------------------------------------------- */
+
+/* One gradient tensor of a worker: n contiguous entries of grad_type at d_grad, and where its clipped entries go
+ * (n contiguous entries of out_type at d_out; not read by adacomp_grad_norm).  Both pointers are aligned to their
+ * element size, no more.  d_out is either d_grad itself with the same type (in place) or does not overlap any
+ * gradient of the call. */
+typedef struct {
+    const void* d_grad;
+    void* d_out;
+    uint64_t n;
+    int32_t grad_type;
+    int32_t out_type;
+} adacomp_grad_tensor_t;
+
+typedef struct adacomp_clip adacomp_clip_t;
+
+/* Workspace and handle for calls of up to max_workers workers (1 .. 65535).  The workspace holds partial sums only; it is
+ * 256-byte aligned device memory.  Creation is synchronous. */
+ADACOMP_API int adacomp_clip_workspace_bytes(uint32_t max_workers, size_t* bytes_out);
+ADACOMP_API int adacomp_clip_create(adacomp_clip_t** h, uint32_t max_workers, void* d_workspace, size_t workspace_bytes,
+                                    int device);
+
+/* Global norms: for every worker w, over all n_tensors tensors together,
+ *     d_norm_out[w] = |scale| * sqrt(sum of g^2),
+ * scale being what the stored entries still have to be multiplied by (1 / the loss scale of half-precision
+ * training; 1 otherwise).  Worker w's entries of tensor t start grad_stride * w elements behind h_tensors[t].d_grad
+ * (grad_stride is in elements of each tensor's own type; 0 is legal with one worker).  Squares are summed in fp32 inside
+ * groups of at most 64 entries and in 64 bits above that; groups whose sum would leave fp32's safe range are summed in 64
+ * bits altogether, so neither large nor tiny entries overflow or vanish.  The order of summation is fixed: the same
+ * call on the same device gives the same bits.  An infinity gives +Inf, a NaN gives NaN, no entries at all give 0.
+ * h_tensors is read before the call returns.  Errors: ADACOMP_ERR_INVALID (null pointer, unknown type, misaligned pointer,
+ * n >= 2^40, n_workers = 0 or > max_workers, scale not finite), ADACOMP_ERR_CUDA. */
+ADACOMP_API int adacomp_grad_norm(adacomp_clip_t* h, const adacomp_grad_tensor_t* h_tensors, uint32_t n_tensors,
+                                  uint64_t grad_stride, uint32_t n_workers, float scale, float* d_norm_out,
+                                  void* cuda_stream);
+
+/* Norm as above, and the clipped gradients:
+ *     c_w = scale * min(1, max_norm / (norm_w + 1e-6)),    out = g * c_w,
+ * c_w computed in 64 bits and rounded to fp32 once, the product rounded to fp32 and then to out_type.  max_norm > 0; +Inf
+ * means that nothing is clipped (the norm is still reported and scale still applied).  With a finite max_norm an infinite
+ * norm gives c_w = 0 (finite entries become zeros, infinite ones NaN) and a NaN norm makes every entry NaN.  Workers do not
+ * affect each other.  Where an in-place tensor meets c_w = 1 nothing is written.  out entries of worker w start
+ * out_stride * w elements behind d_out.  d_coef_out (NULL or [n_workers]) receives c_w: what selected
+ * pairs have to be multiplied by when the gradients themselves are left as they are. */
+ADACOMP_API int adacomp_clip(adacomp_clip_t* h, const adacomp_grad_tensor_t* h_tensors, uint32_t n_tensors,
+                             uint64_t grad_stride, uint64_t out_stride, uint32_t n_workers, float scale, float max_norm,
+                             float* d_norm_out, float* d_coef_out, void* cuda_stream);
+ADACOMP_API int adacomp_clip_destroy(adacomp_clip_t* h);
+
+/* ------------------------------------------------------------------------------------------
+ * Embedding tables: lookup with scaling, and the gradient by sorted tokens.  A table's gradient touches only the
+ * rows whose tokens the batch holds, so it comes in the form the server applies, without a selection (no counterpart in the
+ * paper, whose networks have no such layer).
+ * ---------------------------------------------------------------------------------------- */
+
+/* Rows somewhere in device memory: row r starts (r / group) * group_stride + (r % group) * row_stride elements behind d_data
+ * (group = 0: r * row_stride).  The elements of a row are contiguous.  For tokens a row is one number. */
+typedef struct {
+    void* d_data;
+    int32_t type;                   /* ADACOMP_F32 ...; for tokens ADACOMP_I32 / ADACOMP_I64 */
+    uint32_t group;
+    uint64_t row_stride;
+    uint64_t group_stride;
+} adacomp_rows_t;
+
+typedef struct adacomp_embed adacomp_embed_t;
+
+/* A handle for tables of `vocab` rows of `dim` entries; its gradient calls take up to max_tokens tokens (all workers
+ * together, 0: a handle for lookups alone) of up to max_workers workers.  padding_token: its gradient is left out (it is
+ * looked up like any other); UINT32_MAX: no such token.  Limits: vocab, dim and max_workers at least 1,
+ * vocab * max_workers <= 2^32 - 2, max_tokens < 2^31, dim < 2^31.  The workspace is 256-byte aligned device memory; creation
+ * is synchronous. */
+ADACOMP_API int adacomp_embed_workspace_bytes(uint32_t vocab, uint32_t dim, uint32_t max_tokens, uint32_t max_workers,
+                                              size_t* bytes_out);
+ADACOMP_API int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint32_t max_tokens,
+                                     uint32_t max_workers, uint32_t padding_token, void* d_workspace,
+                                     size_t workspace_bytes, int device);
+
+/* out[t] = table[token t] * scale for n_tokens tokens (any number below 2^31), the product in fp32 and then rounded to out's
+ * type.  table has `vocab` rows; table and out may be of any of the three types.  A token outside
+ * 0 .. vocab - 1 is not followed: its row of out is zeros, and adacomp_embed_last_error reports ADACOMP_ERR_INVALID. */
+ADACOMP_API int adacomp_embed_lookup(adacomp_embed_t* h, const adacomp_rows_t* table, const adacomp_rows_t* tokens,
+                                     uint32_t n_tokens, float scale, const adacomp_rows_t* out, void* cuda_stream);
+
+/* Gradient of the tables of n_workers workers from their n_tokens tokens each (worker w's are tokens
+ * w * n_tokens .. (w + 1) * n_tokens - 1) and the gradients of the looked-up rows, one row of `dim` entries per token:
+ *     sum[w][v] = scale * (sum over w's tokens equal to v of their gradient rows).
+ * Summands are added in fp32 along the order of the tokens in a fixed tree (the same call gives the same bits) and rounded
+ * once to the result's type.  Padding tokens and tokens outside 0 .. vocab - 1 contribute nothing; the latter are
+ * reported by adacomp_embed_last_error as ADACOMP_ERR_INVALID.  n_workers * n_tokens <= max_tokens.
+ *
+ * rows form: the distinct tokens, worker after worker, ascending within a worker:
+ *   d_row_begin_out  [n_workers + 1]: worker w's rows are entries d_row_begin_out[w] .. d_row_begin_out[w + 1] - 1 of the
+ *                    lists below (what adacomp_apply needs on the host, times dim, as pair_begin and pair_count);
+ *   d_rows_out       NULL or the tokens, room for n_workers * n_tokens; d_values_out: their sums, [.][dim] of values_type;
+ *   d_idx_out        NULL or [.][dim]: idx_offset + token * dim + column, the index of every value in the parameter vector
+ *                    whose entries idx_offset .. idx_offset + vocab * dim - 1 are the table (they must stay below 2^32):
+ *                    with fp32 values (d_idx_out, d_values_out) are updates as adacomp_apply takes them.
+ * What lies behind the last row is left as it was. */
+ADACOMP_API int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens,
+                                        uint32_t n_workers, const adacomp_rows_t* grad, float scale, uint32_t* d_rows_out,
+                                        uint64_t* d_row_begin_out, void* d_values_out, int values_type,
+                                        uint32_t* d_idx_out, uint64_t idx_offset, void* cuda_stream);
+
+/* dense form: the whole table of every worker; row v of worker w is row w * vocab + v of `out` (so group = vocab and
+ * group_stride = the distance between two workers' buffers place the tables inside the flat gradient buffers that
+ * adacomp_select reads).  accumulate = 0: rows without a token become zeros; accumulate = 1: the sums are added to what
+ * is there (in fp32, one rounding), rows without a token are not touched. */
+ADACOMP_API int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens,
+                                         uint32_t n_workers, const adacomp_rows_t* grad, float scale,
+                                         const adacomp_rows_t* out, int accumulate, void* cuda_stream);
+/* Waits for cuda_stream, returns and clears the first error recorded on the device. */
+ADACOMP_API int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream);
+ADACOMP_API int adacomp_embed_destroy(adacomp_embed_t* h);
+
 #ifdef __cplusplus
 }
 #endif

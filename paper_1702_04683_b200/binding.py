@@ -37,6 +37,21 @@ class Segment(ctypes.Structure):
     _fields_ = [("offset", ctypes.c_uint64), ("n", ctypes.c_uint32), ("k", ctypes.c_uint32)]
 
 
+class GradTensor(ctypes.Structure):
+    _fields_ = [("d_grad", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("n", ctypes.c_uint64),
+                ("grad_type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("d_data", ctypes.c_void_p), ("type", ctypes.c_int32), ("group", ctypes.c_uint32),
+                ("row_stride", ctypes.c_uint64), ("group_stride", ctypes.c_uint64)]
+
+
+#: element types of the operators that take more than fp32, and types of token numbers
+ELEMENT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+TOKEN_TYPES = {torch.int32: 0, torch.int64: 1}
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -86,6 +101,18 @@ def _load():
         "adacomp_server_debug_skip_positions": (i32, [vp, u64]),
         "adacomp_server_last_error": (i32, [vp, vp]),
         "adacomp_server_destroy": (i32, [vp]),
+        "adacomp_clip_workspace_bytes": (i32, [u32, P(ctypes.c_size_t)]),
+        "adacomp_clip_create": (i32, [P(vp), u32, vp, ctypes.c_size_t, i32]),
+        "adacomp_grad_norm": (i32, [vp, vp, u32, u64, u32, f32, vp, vp]),
+        "adacomp_clip": (i32, [vp, vp, u32, u64, u64, u32, f32, f32, vp, vp, vp]),
+        "adacomp_clip_destroy": (i32, [vp]),
+        "adacomp_embed_workspace_bytes": (i32, [u32, u32, u32, u32, P(ctypes.c_size_t)]),
+        "adacomp_embed_create": (i32, [P(vp), u32, u32, u32, u32, u32, vp, ctypes.c_size_t, i32]),
+        "adacomp_embed_lookup": (i32, [vp, vp, vp, u32, f32, vp, vp]),
+        "adacomp_embed_grad_rows": (i32, [vp, vp, u32, u32, vp, f32, vp, vp, vp, i32, vp, u64, vp]),
+        "adacomp_embed_grad_dense": (i32, [vp, vp, u32, u32, vp, f32, vp, i32, vp]),
+        "adacomp_embed_last_error": (i32, [vp, vp]),
+        "adacomp_embed_destroy": (i32, [vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -448,6 +475,329 @@ class Server:
     def close(self):
         if getattr(self, "_h", None):
             _lib.adacomp_server_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ----------------------------------------------------------------------------- clipping
+
+def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """An output tensor that belongs to the stream its kernels run on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _element_type(t: torch.Tensor, device: torch.device, name: str) -> int:
+    kind = ELEMENT_TYPES.get(t.dtype)
+    if kind is None or t.device != device:
+        raise TypeError(f"{name}: need a float32, bfloat16 or float16 tensor on {device}")
+    return kind
+
+
+def _is_dense(t: torch.Tensor) -> bool:
+    """Whether the tensor's entries fill one stretch of memory, in whatever order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    expect = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != expect:
+            return False
+        expect *= size
+    return True
+
+
+class GradList:
+    """One worker's gradient tensors, and where their clipped values go (``out``: one tensor for each, of any of the three
+    types and with the same shape and strides; None: in place).  Holds on to the tensors and only says where they are: a
+    program whose gradients stay in place makes the list once, values are read when a call runs."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]] = None):
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        if not self.grads:
+            raise ValueError("grads: need at least one tensor")
+        if len(self.out) != len(self.grads):
+            raise ValueError("out: need one tensor for each gradient")
+        self.device = self.grads[0].device
+        if self.device.type != "cuda":
+            raise TypeError("grads: need CUDA tensors")
+        self.table = (GradTensor * len(self.grads))()
+        spans = []                              # (begin, end, written)
+        for i, (g, o) in enumerate(zip(self.grads, self.out)):
+            kind, out_kind = _element_type(g, self.device, "grads"), _element_type(o, self.device, "out")
+            if o is not g and (o.shape != g.shape or (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous()))):
+                raise ValueError("out: need the shape and strides of the gradient")
+            if not _is_dense(g):
+                raise TypeError("grads: need tensors without gaps")
+            e, n, at, to = self.table[i], g.numel(), g.data_ptr(), o.data_ptr()
+            e.d_grad, e.d_out, e.n, e.grad_type, e.out_type = at, to, n, kind, out_kind
+            if n:
+                in_place = at == to and g.dtype == o.dtype
+                spans.append((at, at + n * g.element_size(), in_place))
+                if not in_place:
+                    spans.append((to, to + n * o.element_size(), True))
+        spans.sort()
+        reach = reach_written = 0               # how far the tensors before extend, and those of them that are written
+        for begin, end, written in spans:
+            if begin < reach_written or (written and begin < reach):
+                raise ValueError("out: overlaps a gradient or another output")
+            reach = max(reach, end)
+            if written:
+                reach_written = max(reach_written, end)
+
+
+class Clipper:
+    """Global gradient norm and clipping; owns its device workspace.  Gradients are a :class:`GradList`, a sequence of tensors
+    (one worker, any shapes), or a matrix [W, P] whose rows are the flat gradients of W workers."""
+
+    def __init__(self, max_workers: int = 1, device: Optional[torch.device] = None):
+        self.device = torch.device(device if device is not None else "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.max_workers = int(max_workers)
+        nbytes = ctypes.c_size_t(0)
+        _check(_lib.adacomp_clip_workspace_bytes(self.max_workers, ctypes.byref(nbytes)), "adacomp_clip_workspace_bytes")
+        self.workspace = torch.empty(max(int(nbytes.value), 256), dtype=torch.uint8, device=self.device)
+        h = ctypes.c_void_p()
+        _check(_lib.adacomp_clip_create(ctypes.byref(h), self.max_workers, self.workspace.data_ptr(), self.workspace.numel(),
+                                        self.device.index), "adacomp_clip_create")
+        self._h = h
+
+    def _given(self, grads, out=None):
+        """(table, tensors, workers, gradient stride, output stride, outputs)"""
+        if not isinstance(grads, (torch.Tensor, GradList)):
+            grads = GradList(grads, out)
+        elif out is not None and isinstance(grads, GradList):
+            raise ValueError("out: the list already says where its outputs go")
+        if isinstance(grads, GradList):
+            if grads.device != self.device:
+                raise TypeError(f"grads: need tensors on {self.device}")
+            return grads.table, len(grads.grads), 1, 0, 0, grads.out
+        out = grads if out is None else out
+        e = GradTensor()
+        e.grad_type, e.out_type = _element_type(grads, self.device, "grads"), _element_type(out, self.device, "out")
+        if grads.dim() != 2 or out.shape != grads.shape:
+            raise ValueError("grads: need a matrix [workers, entries], and out of the same shape")
+        W, n = grads.shape
+        for t in (grads, out):
+            if (n > 1 and t.stride(1) != 1) or (W > 1 and t.stride(0) < n):
+                raise TypeError("grads, out: need contiguous rows that do not overlap")
+        if out is not grads:
+            at, size, to, out_size = grads.data_ptr(), grads.element_size(), out.data_ptr(), out.element_size()
+            same = at == to and grads.dtype == out.dtype and (W == 1 or grads.stride(0) == out.stride(0))
+            if not same and n and at < to + ((W - 1) * out.stride(0) + n) * out_size and to < at + ((W - 1) * grads.stride(0) + n) * size:
+                raise ValueError("out: overlaps the gradients")
+        e.d_grad, e.d_out, e.n = grads.data_ptr(), out.data_ptr(), n
+        return ctypes.byref(e), 1, W, grads.stride(0) if W > 1 else 0, out.stride(0) if W > 1 else 0, out
+
+    def norm(self, grads, scale: float = 1.0, norm_out: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """|scale| times the norm over all of a worker's entries: float32 [W]."""
+        table, count, W, stride, _, _ = self._given(grads)
+        if norm_out is None:
+            norm_out = _empty((W,), torch.float32, self.device, stream)
+        elif norm_out.numel() != W:
+            raise ValueError("norm_out: need one entry per worker")
+        _check(_lib.adacomp_grad_norm(self._h, table, count, stride, W, float(scale), _dev(norm_out, torch.float32, "norm_out"),
+                                      _stream_ptr(stream)), "adacomp_grad_norm")
+        return norm_out
+
+    def clip(self, grads, max_norm: float, scale: float = 1.0, out=None, norm_out: Optional[torch.Tensor] = None,
+             coef_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """out = grads * scale * min(1, max_norm / (norm + 1e-6)) -> (out, norm [W]).  ``out`` defaults to the gradients
+        themselves; ``coef_out`` [W] receives the factors."""
+        table, count, W, stride, out_stride, out = self._given(grads, out)
+        if norm_out is None:
+            norm_out = _empty((W,), torch.float32, self.device, stream)
+        for t, name in ((norm_out, "norm_out"), (coef_out, "coef_out")):
+            if t is not None and t.numel() != W:
+                raise ValueError(f"{name}: need one entry per worker")
+        _check(_lib.adacomp_clip(self._h, table, count, stride, out_stride, W, float(scale), float(max_norm),
+                                 _dev(norm_out, torch.float32, "norm_out"),
+                                 _dev(coef_out, torch.float32, "coef_out") if coef_out is not None else None,
+                                 _stream_ptr(stream)), "adacomp_clip")
+        return out, norm_out
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.adacomp_clip_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ----------------------------------------------------------------------------- embedding tables
+
+def _rows(t: torch.Tensor, dims: int, kind: int, name: str) -> Rows:
+    """The first `dims` dimensions of a tensor as the numbering of its rows."""
+    r = Rows()
+    r.d_data, r.type = t.data_ptr(), kind
+    shape, strides = t.shape, t.stride()
+    if t.is_contiguous():
+        row = 1
+        for n in shape[dims:]:
+            row *= n
+        r.row_stride = row
+        return r
+    merged = []                                 # [rows, distance], outermost first; neighbours that make one run are joined
+    for n, st in zip(shape[:dims], strides[:dims]):
+        if n == 1:
+            continue
+        if merged and merged[-1][1] == n * st:
+            merged[-1] = [merged[-1][0] * n, st]
+        else:
+            merged.append([n, st])
+    if len(merged) > 2 or any(st < 0 for _, st in merged):
+        raise TypeError(f"{name}: rows need at most two distances between them")
+    if merged:
+        r.row_stride = merged[-1][1]
+    if len(merged) == 2:
+        r.group, r.group_stride = merged[1][0], merged[0][1]
+    return r
+
+
+class Embedding:
+    """Embedding tables of `vocab` rows of `dim` entries: lookup with scaling, and the gradient by sorted tokens; owns its
+    device workspace.  ``max_tokens`` bounds the tokens of a gradient call (0: lookups only)."""
+
+    def __init__(self, vocab: int, dim: int, max_tokens: int = 0, max_workers: int = 1, padding_idx: Optional[int] = None,
+                 device: Optional[torch.device] = None):
+        self.device = torch.device(device if device is not None else "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.vocab, self.dim, self.max_tokens, self.max_workers = int(vocab), int(dim), int(max_tokens), int(max_workers)
+        if padding_idx is not None and not 0 <= padding_idx < self.vocab:
+            raise ValueError("padding_idx: need a token of the vocabulary")
+        pad = 0xFFFFFFFF if padding_idx is None else int(padding_idx)
+        for n in (self.vocab, self.dim, self.max_tokens, self.max_workers):
+            if not 0 <= n < 1 << 32:
+                raise AdacompError(ERR_INVALID, "adacomp_embed_workspace_bytes")
+        nbytes = ctypes.c_size_t(0)
+        _check(_lib.adacomp_embed_workspace_bytes(self.vocab, self.dim, self.max_tokens, self.max_workers, ctypes.byref(nbytes)),
+               "adacomp_embed_workspace_bytes")
+        self.workspace = torch.empty(max(int(nbytes.value), 256), dtype=torch.uint8, device=self.device)
+        h = ctypes.c_void_p()
+        _check(_lib.adacomp_embed_create(ctypes.byref(h), self.vocab, self.dim, self.max_tokens, self.max_workers, pad,
+                                         self.workspace.data_ptr(), self.workspace.numel(), self.device.index),
+               "adacomp_embed_create")
+        self._h = h
+
+    def _tokens(self, tokens: torch.Tensor) -> Rows:
+        kind = TOKEN_TYPES.get(tokens.dtype)
+        if kind is None or tokens.device != self.device:
+            raise TypeError(f"tokens: need an int32 or int64 tensor on {self.device}")
+        if tokens.numel() >= 1 << 31:
+            raise ValueError("tokens: too many")
+        return _rows(tokens, tokens.dim(), kind, "tokens")
+
+    def _wide(self, t: torch.Tensor, name: str) -> Rows:
+        kind = _element_type(t, self.device, name)
+        if t.dim() == 0 or t.shape[-1] != self.dim or (self.dim > 1 and t.stride(-1) != 1):
+            raise TypeError(f"{name}: need contiguous rows of {self.dim} entries")
+        return _rows(t, t.dim() - 1, kind, name)
+
+    def lookup(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+               dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """table [vocab, dim], tokens of any shape -> [*tokens.shape, dim] = table[tokens] * scale, of ``dtype`` (the
+        table's by default)."""
+        if table.dim() != 2 or table.shape[0] != self.vocab:
+            raise ValueError(f"table: need {self.vocab} rows")
+        shape = (*tokens.shape, self.dim)
+        ids = self._tokens(tokens)
+        if out is None:
+            out = _empty(shape, dtype or table.dtype, self.device, stream)
+        elif out.shape != shape or (dtype is not None and out.dtype != dtype):
+            raise ValueError("out: need a row for every token, and the type asked for")
+        _check(_lib.adacomp_embed_lookup(self._h, ctypes.byref(self._wide(table, "table")), ctypes.byref(ids), tokens.numel(),
+                                         float(scale), ctypes.byref(self._wide(out, "out")), _stream_ptr(stream)),
+               "adacomp_embed_lookup")
+        return out
+
+    def _batch(self, tokens: torch.Tensor, grad: torch.Tensor, workers: int):
+        if workers < 1 or tokens.numel() % workers:
+            raise ValueError("tokens: need the same number for every worker")
+        if grad.numel() != tokens.numel() * self.dim:
+            raise ValueError("grad: need a row for every token")
+        return self._tokens(tokens), tokens.numel() // workers, self._wide(grad, "grad")
+
+    def _grad_rows(self, tokens, grad, scale, workers, rows_out, values_out, idx_out, offset, stream):
+        ids, per_worker, rows = self._batch(tokens, grad, workers)
+        n = tokens.numel()
+        for t, need, name in ((rows_out, n, "rows_out"), (values_out, n * self.dim, "values_out"), (idx_out, n * self.dim, "idx_out")):
+            if t is not None and t.numel() < need:
+                raise ValueError(f"{name}: too small")
+        begin = _empty((workers + 1,), torch.int64, self.device, stream)
+        kind = _element_type(values_out, self.device, "values_out")
+        _check(_lib.adacomp_embed_grad_rows(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
+                                            _dev(rows_out, torch.int32, "rows_out") if rows_out is not None else None,
+                                            begin.data_ptr(), _dev(values_out, values_out.dtype, "values_out"), kind,
+                                            _dev(idx_out, torch.int32, "idx_out") if idx_out is not None else None, int(offset),
+                                            _stream_ptr(stream)), "adacomp_embed_grad_rows")
+        return begin
+
+    def grad_rows(self, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, workers: int = 1,
+                  dtype: torch.dtype = torch.float32, rows_out: Optional[torch.Tensor] = None,
+                  values_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """Gradient of the table as its distinct rows -> (rows int32 [N], values [N, dim], row_begin int64 [workers + 1]) with
+        N = tokens.numel(): worker w's tokens (its share of the flattened ``tokens``) gave the entries row_begin[w] ..
+        row_begin[w + 1] of the two lists; what lies behind the last is left as it was."""
+        n = tokens.numel()
+        if rows_out is None:
+            rows_out = _empty((n,), torch.int32, self.device, stream)
+        if values_out is None:
+            values_out = _empty((n, self.dim), dtype, self.device, stream)
+        begin = self._grad_rows(tokens, grad, scale, workers, rows_out, values_out, None, 0, stream)
+        return rows_out, values_out, begin
+
+    def grad_update(self, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, workers: int = 1, offset: int = 0,
+                    idx_out: Optional[torch.Tensor] = None, val_out: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None):
+        """The same gradient as updates for :meth:`Server.apply` -> (idx int32 [N, dim] holding uint32, val float32 [N, dim],
+        row_begin int64 [workers + 1]); the table is entries offset .. offset + vocab * dim - 1 of the parameters.  Worker w's
+        update is pairs row_begin[w] * dim .. row_begin[w + 1] * dim - 1."""
+        n = tokens.numel()
+        if idx_out is None:
+            idx_out = _empty((n, self.dim), torch.int32, self.device, stream)
+        if val_out is None:
+            val_out = _empty((n, self.dim), torch.float32, self.device, stream)
+        elif val_out.dtype != torch.float32:
+            raise TypeError("val_out: updates are float32")
+        begin = self._grad_rows(tokens, grad, scale, workers, None, val_out, idx_out, offset, stream)
+        return idx_out, val_out, begin
+
+    def grad_dense(self, tokens: torch.Tensor, grad: torch.Tensor, out: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                   workers: int = 1, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The whole table's gradient into ``out`` [vocab, dim] or [workers, vocab, dim]; ``accumulate``: added to what is
+        there instead of replacing it."""
+        ids, per_worker, rows = self._batch(tokens, grad, workers)
+        want = (self.vocab, self.dim)
+        if tuple(out.shape) != (workers, *want) and not (workers == 1 and tuple(out.shape) == want):
+            raise ValueError("out: need a table for every worker")
+        if out.data_ptr() == grad.data_ptr() and grad.numel():
+            raise ValueError("out: overlaps the gradient")
+        _check(_lib.adacomp_embed_grad_dense(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
+                                             ctypes.byref(self._wide(out, "out")), int(accumulate), _stream_ptr(stream)),
+               "adacomp_embed_grad_dense")
+        return out
+
+    def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
+        """Waits for the stream; the first error the device recorded since the last call (a token outside the vocabulary)."""
+        return int(_lib.adacomp_embed_last_error(self._h, _stream_ptr(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.adacomp_embed_destroy(self._h)
             self._h = None
 
     def __del__(self):

@@ -1,0 +1,480 @@
+// Global gradient norm over many tensors, and clipping.
+//
+//   norm_w = |s| sqrt(sum_i g_i^2),   c_w = s min(1, max_norm / (norm_w + 1e-6)),   out_i = round(g_i c_w)
+//
+// Both kernels are one pass over the data (2 and 1 operations an entry): HBM bounds them.  The tensors of a call are cut
+// into units of 1024 vectors of 16 bytes; a block takes a run of consecutive units, so it looks a tensor up once and then walks on.
+// The second pass walks the same runs from the back: what the first pass read last is still in L2.
+#include <math.h>
+#include <new>
+#include <vector>
+
+#include "numeric.cuh"
+
+using namespace adacomp;
+
+struct adacomp_clip {
+    int device;
+    uint32_t max_workers;
+    uint32_t n_blocks;              // partial sums per worker
+    int n_sms;
+    double* d_partial;              // [max_workers][n_blocks]
+    uint32_t* d_done;               // [max_workers] blocks that have delivered their sum
+    float* d_coef;                  // [max_workers]
+};
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kVecsPerThread = 4;
+constexpr uint32_t kUnit = kThreads * kVecsPerThread;       // vectors of 16 bytes (norm) or items (write) per unit
+constexpr double kEps = 1e-6;
+
+struct Tensor {
+    const char* in;
+    char* out;
+    uint64_t n;
+    uint32_t first_unit;            // of this tensor among the call's units
+    uint8_t in_type, out_type;
+    uint16_t unused;
+};
+static_assert(sizeof(Tensor) == 32, "table entries are packed");
+
+// The tensors travel as kernel parameters: no upload, no buffer that a later call could overwrite, and the call can
+// be captured.  Parameters may take 32764 bytes; longer lists take several launches.
+template <int MAX> struct Table { Tensor t[MAX]; };
+constexpr int kFew = 64, kMany = 960;
+
+struct Job {
+    uint32_t n_tensors, n_units;
+    uint64_t in_stride, out_stride;
+    float scale;
+    float max_norm;
+    int first, last;                // of the call's launches
+    uint32_t n_blocks;
+    double* partial;
+    uint32_t* done;
+    float* norm_out;
+    float* coef;
+    float* coef_out;
+};
+
+// Position of a unit: the last tensor whose first unit is not behind it.
+template <int MAX> __device__ __forceinline__ uint32_t find_tensor(const Table<MAX>& tab, uint32_t n, uint32_t unit) {
+    uint32_t lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (tab.t[mid].first_unit <= unit) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ uint32_t or4(const uint4& v) { return v.x | v.y | v.z | v.w; }
+
+// Sum of the squares of what kVecsPerThread vectors hold.  In fp32 where that is safe (between 2^-100 and 2^100 no square
+// overflowed, and what underflowed is below 2^-20 of one unit in the last place), otherwise in 64 bits.
+template <typename T> __device__ __forceinline__ double sum_squares(const uint4 (&v)[kVecsPerThread]) {
+    constexpr int N = 16 / sizeof(T);
+    float s[2] = {0.f, 0.f};
+    uint32_t any = 0;
+#pragma unroll
+    for (int k = 0; k < kVecsPerThread; ++k) {
+        Packed<T, N> p;
+        p.v[0] = v[k];
+        float f[N];
+        p.unpack(f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[j & 1] = __fmaf_rn(f[j], f[j], s[j & 1]);
+        any |= or4(v[k]);
+    }
+    const float sum = s[0] + s[1];
+    if (sum >= 0x1p-100f && sum <= 0x1p100f) return static_cast<double>(sum);
+    if ((any & (sizeof(T) == 4 ? 0x7FFFFFFFu : 0x7FFF7FFFu)) == 0) return 0.0;
+    double d = 0.0;
+#pragma unroll
+    for (int k = 0; k < kVecsPerThread; ++k) {
+        Packed<T, N> p;
+        p.v[0] = v[k];
+        float f[N];
+        p.unpack(f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) d = __fma_rn(static_cast<double>(f[j]), static_cast<double>(f[j]), d);
+    }
+    return d;
+}
+
+// The vector at address a (16-byte aligned) of a tensor that occupies [p, end): elements outside read as zeros.
+template <typename T> __device__ __forceinline__ uint4 load_clamped(uintptr_t a, uintptr_t p, uintptr_t end) {
+    if (a >= p && a + 16 <= end) return load16(reinterpret_cast<const void*>(a));
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (a + 16 > p && a < end) {
+#pragma unroll
+        for (int j = 0; j < 16 / static_cast<int>(sizeof(T)); ++j) {
+            const uintptr_t e = a + j * sizeof(T);
+            if (e < p || e >= end) continue;
+            if constexpr (sizeof(T) == 4) w[j] = *reinterpret_cast<const uint32_t*>(e);
+            else w[j / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(e)) << (16 * (j & 1));
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename T>
+__device__ __forceinline__ double unit_squares(const char* base, uint64_t n, uint32_t unit) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(base), end = p + n * sizeof(T);
+    const uintptr_t a = (p & ~static_cast<uintptr_t>(15)) + (static_cast<uint64_t>(unit) * kUnit + threadIdx.x) * 16;
+    uint4 v[kVecsPerThread];
+#pragma unroll
+    for (int k = 0; k < kVecsPerThread; ++k) v[k] = load_clamped<T>(a + static_cast<uintptr_t>(k) * kThreads * 16, p, end);
+    return sum_squares<T>(v);
+}
+
+__device__ __forceinline__ double block_sum(double x, double* s_warp) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, d);
+    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double total = 0.0;
+    if (threadIdx.x == 0)
+        for (int i = 0; i < kThreads / 32; ++i) total += s_warp[i];
+    __syncthreads();
+    return total;                   // of thread 0
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(kThreads) k_grad_norm(const __grid_constant__ Table<MAX> tab, const Job job) {
+    __shared__ double s_warp[kThreads / 32];
+    __shared__ bool s_last;
+    const uint32_t w = blockIdx.y, b = blockIdx.x;
+    const uint32_t from = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * b / job.n_blocks);
+    const uint32_t to = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * (b + 1) / job.n_blocks);
+    double sum = 0.0;
+    uint32_t i = from < to ? find_tensor(tab, job.n_tensors, from) : 0;
+    for (uint32_t u = from; u < to; ++u) {
+        while (i + 1 < job.n_tensors && tab.t[i + 1].first_unit <= u) ++i;
+        const Tensor& t = tab.t[i];
+        const char* base = t.in + w * job.in_stride * type_size(t.in_type);
+        const uint32_t at = u - t.first_unit;
+        if (t.in_type == ADACOMP_F32) sum += unit_squares<float>(base, t.n, at);
+        else if (t.in_type == ADACOMP_BF16) sum += unit_squares<__nv_bfloat16>(base, t.n, at);
+        else sum += unit_squares<__half>(base, t.n, at);
+    }
+    sum = block_sum(sum, s_warp);
+    if (threadIdx.x == 0) {
+        double* slot = job.partial + static_cast<uint64_t>(w) * job.n_blocks + b;
+        *slot = job.first ? sum : *slot + sum;
+        s_last = false;
+        if (job.last) {
+            __threadfence();
+            s_last = atomicAdd(job.done + w, 1u) == job.n_blocks - 1;
+        }
+    }
+    __syncthreads();
+    if (!s_last) return;
+    // the worker's last block adds the partial sums, in their order
+    __threadfence();
+    double total = 0.0;
+    for (uint32_t k = threadIdx.x; k < job.n_blocks; k += kThreads)
+        total += __ldcg(job.partial + static_cast<uint64_t>(w) * job.n_blocks + k);
+    total = block_sum(total, s_warp);
+    if (threadIdx.x == 0) {
+        job.done[w] = 0;
+        const double norm = fabs(static_cast<double>(job.scale)) * sqrt(total);
+        job.norm_out[w] = static_cast<float>(norm);
+        if (job.coef) {
+            double c = static_cast<double>(job.max_norm) / (norm + kEps);
+            if (c > 1.0 || isinf(job.max_norm)) c = 1.0;        // a NaN stays one
+            const float f = static_cast<float>(c * static_cast<double>(job.scale));
+            job.coef[w] = f;
+            if (job.coef_out) job.coef_out[w] = f;
+        }
+    }
+}
+
+// Entries [e, e + N) of a tensor of n entries at `in` that does not sit on the 16-byte grid there: the vectors around them,
+// shifted into place, if all of those lie inside the tensor.
+template <typename A, int N>
+__device__ __forceinline__ Packed<A, N> load_shifted(const A* in, int64_t e, uint64_t n) {
+    constexpr int kVecs = Packed<A, N>::kVecs, kWords = 4 * (kVecs + 1);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(in + e), lo = a & ~static_cast<uintptr_t>(15);
+    const uintptr_t first = reinterpret_cast<uintptr_t>(in), end = first + n * sizeof(A);
+    Packed<A, N> p;
+    if (lo >= first && lo + 16 * (kVecs + 1) <= end) {
+        uint32_t w[kWords];
+#pragma unroll
+        for (int i = 0; i <= kVecs; ++i) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(lo + 16 * i));     // the neighbour reads it too
+            w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+        }
+        if (a & 8)
+#pragma unroll
+            for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
+        if (a & 4)
+#pragma unroll
+            for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
+        if (a & 2)
+#pragma unroll
+            for (int i = 0; i + 1 < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) p.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    } else {
+        float f[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) f[j] = to_float(in[e + j]);
+        p.pack(f);
+    }
+    return p;
+}
+
+template <typename A, typename B, int N>
+__device__ __forceinline__ void scale_store(const Packed<A, N>& p, B* out, float c) {
+    float f[N];
+    p.unpack(f);
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = __fmul_rn(f[j], c);
+    Packed<B, N> q;
+    q.pack(f);
+    q.store(out);
+}
+
+template <typename A, typename B>
+__device__ __forceinline__ void write_unit(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c) {
+    constexpr int N = kItemElems<A, B>;
+    const A* in = reinterpret_cast<const A*>(t.in) + w * job.in_stride;
+    B* out = reinterpret_cast<B*>(t.out) + w * job.out_stride;
+    const int64_t n = static_cast<int64_t>(t.n);
+    // items start on the output's 16-byte grid: item j holds entries [j N - skew, j N - skew + N)
+    const int64_t skew = static_cast<int64_t>((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(B));
+    const int64_t unit_at = static_cast<int64_t>(unit) * kUnit * N - skew, e0 = unit_at + threadIdx.x * N;
+    const bool on_grid = (reinterpret_cast<uintptr_t>(in + e0) & 15) == 0;
+    if (on_grid && unit_at >= 0 && unit_at + static_cast<int64_t>(kUnit) * N <= n) {
+        Packed<A, N> p[kVecsPerThread];
+#pragma unroll
+        for (int k = 0; k < kVecsPerThread; ++k) p[k].load(in + e0 + k * (kThreads * N));
+#pragma unroll
+        for (int k = 0; k < kVecsPerThread; ++k) scale_store<A, B, N>(p[k], out + e0 + k * (kThreads * N), c);
+        return;
+    }
+#pragma unroll 1
+    for (int k = 0; k < kVecsPerThread; ++k) {
+        const int64_t e = e0 + k * (kThreads * N);
+        if (e >= 0 && e + N <= n) {
+            Packed<A, N> p;
+            if (on_grid) p.load(in + e);
+            else p = load_shifted<A, N>(in, e, t.n);
+            scale_store<A, B, N>(p, out + e, c);
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < N; ++j)
+                if (e + j >= 0 && e + j < n) out[e + j] = from_float<B>(__fmul_rn(to_float(in[e + j]), c));
+        }
+    }
+}
+
+template <typename A>
+__device__ __forceinline__ void write_unit_from(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c) {
+    if (t.out_type == ADACOMP_F32) write_unit<A, float>(t, w, job, unit, c);
+    else if (t.out_type == ADACOMP_BF16) write_unit<A, __nv_bfloat16>(t, w, job, unit, c);
+    else write_unit<A, __half>(t, w, job, unit, c);
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(kThreads) k_clip_write(const __grid_constant__ Table<MAX> tab, const Job job) {
+    const uint32_t w = blockIdx.y, b = blockIdx.x;
+    const uint32_t from = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * b / job.n_blocks);
+    const uint32_t to = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * (b + 1) / job.n_blocks);
+    if (from >= to) return;
+    const float c = job.coef[w];
+    uint32_t i = find_tensor(tab, job.n_tensors, to - 1);
+    for (uint32_t u = to; u-- > from;) {
+        while (tab.t[i].first_unit > u) --i;
+        const Tensor& t = tab.t[i];
+        if (c == 1.0f && t.out == t.in) continue;           // in place, nothing to change
+        const uint32_t at = u - t.first_unit;
+        if (t.in_type == ADACOMP_F32) write_unit_from<float>(t, w, job, at, c);
+        else if (t.in_type == ADACOMP_BF16) write_unit_from<__nv_bfloat16>(t, w, job, at, c);
+        else write_unit_from<__half>(t, w, job, at, c);
+    }
+}
+
+// Units of a tensor: by its input's vectors (norm) or by its items on the output's grid (write), counted so that they
+// suffice wherever a worker's copy sits on the 16-byte grid.
+uint64_t units_of(const adacomp_grad_tensor_t& t, bool write) {
+    uint64_t vecs;
+    if (write) {
+        const uint64_t n_item = type_size(t.grad_type) == 4 && type_size(t.out_type) == 4 ? 4 : 8;
+        vecs = (t.n + 7 + n_item - 1) / n_item;
+    } else {
+        vecs = (t.n * type_size(t.grad_type) + 14 + 15) / 16;
+    }
+    return (vecs + kUnit - 1) / kUnit;
+}
+
+template <int MAX>
+int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, bool write, cudaStream_t stream) {
+    const dim3 grid(job.n_blocks, n_workers);
+    if (write) k_clip_write<MAX><<<grid, kThreads, 0, stream>>>(tab, job);
+    else k_grad_norm<MAX><<<grid, kThreads, 0, stream>>>(tab, job);
+    ADACOMP_LAUNCH_CHECK();
+    return ADACOMP_OK;
+}
+
+int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, bool write) {
+    if (!ts && n_tensors) return ADACOMP_ERR_INVALID;
+    for (uint32_t i = 0; i < n_tensors; ++i) {
+        const adacomp_grad_tensor_t& t = ts[i];
+        if (!known_type(t.grad_type) || t.n >= (1ull << 40)) return ADACOMP_ERR_INVALID;
+        if (t.n && (!t.d_grad || reinterpret_cast<uintptr_t>(t.d_grad) % type_size(t.grad_type))) return ADACOMP_ERR_INVALID;
+        if (!write) continue;
+        if (!known_type(t.out_type)) return ADACOMP_ERR_INVALID;
+        if (t.n && (!t.d_out || reinterpret_cast<uintptr_t>(t.d_out) % type_size(t.out_type))) return ADACOMP_ERR_INVALID;
+        if (t.n && t.d_out == t.d_grad && t.out_type != t.grad_type) return ADACOMP_ERR_INVALID;
+    }
+    return ADACOMP_OK;
+}
+
+// One pass over all tensors, in as many launches as the parameter space needs.
+int run_pass(const adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint32_t n_workers, Job job,
+             bool write, cudaStream_t stream) {
+    static thread_local Table<kMany> tab;
+    uint32_t at = 0;
+    bool first = true;
+    do {
+        uint32_t n = 0;
+        uint64_t units = 0;
+        for (; at < n_tensors && n < kMany; ++at) {
+            const adacomp_grad_tensor_t& t = ts[at];
+            if (t.n == 0) continue;
+            const uint64_t u = units_of(t, write);
+            if (units + u >= (1ull << 32)) {
+                if (n) break;
+                return ADACOMP_ERR_INVALID;
+            }
+            Tensor& e = tab.t[n++];
+            e.in = static_cast<const char*>(t.d_grad);
+            e.out = static_cast<char*>(t.d_out);
+            e.n = t.n;
+            e.first_unit = static_cast<uint32_t>(units);
+            e.in_type = static_cast<uint8_t>(t.grad_type);
+            e.out_type = static_cast<uint8_t>(t.out_type);
+            e.unused = 0;
+            units += u;
+        }
+        job.n_tensors = n;
+        job.n_units = static_cast<uint32_t>(units);
+        job.first = first;
+        job.last = at == n_tensors;
+        first = false;
+        if (write && n == 0) continue;
+        int rc;
+        if (n <= kFew) {
+            Table<kFew> few;
+            for (uint32_t k = 0; k < n; ++k) few.t[k] = tab.t[k];
+            rc = launch(few, job, n_workers, write, stream);
+        } else {
+            rc = launch(tab, job, n_workers, write, stream);
+        }
+        if (rc != ADACOMP_OK) return rc;
+    } while (at < n_tensors);
+    return ADACOMP_OK;
+}
+
+uint32_t blocks_per_worker(int n_sms) { return 6u * static_cast<uint32_t>(n_sms); }
+
+size_t carve(adacomp_clip_t* h, void* ws, uint32_t max_workers, uint32_t n_blocks) {
+    Carver c(ws);
+    double* partial = c.take<double>(static_cast<size_t>(max_workers) * n_blocks);
+    uint32_t* done = c.take<uint32_t>(max_workers);
+    float* coef = c.take<float>(max_workers);
+    if (h) {
+        h->d_partial = partial;
+        h->d_done = done;
+        h->d_coef = coef;
+    }
+    return c.used;
+}
+
+constexpr uint32_t kMaxBlocks = 1024;       // partial sums per worker the workspace has room for
+
+int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t in_stride, uint64_t out_stride,
+        uint32_t n_workers, float scale, float max_norm, float* d_norm, float* d_coef_out, bool write, void* cuda_stream) {
+    if (!h || !d_norm || n_workers == 0 || n_workers > h->max_workers || !isfinite(scale)) return ADACOMP_ERR_INVALID;
+    if (write && !(max_norm > 0.f)) return ADACOMP_ERR_INVALID;
+    int rc = check_tensors(ts, n_tensors, write);
+    if (rc != ADACOMP_OK) return rc;
+    DeviceGuard guard(h->device);
+    ADACOMP_CUDA(guard.err);
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    Job job = {};
+    job.in_stride = in_stride;
+    job.out_stride = out_stride;
+    job.scale = scale;
+    job.max_norm = max_norm;
+    // all blocks of a call are resident at once where there are fewer workers than that
+    job.n_blocks = blocks_per_worker(h->n_sms) / n_workers;
+    if (job.n_blocks < 1) job.n_blocks = 1;
+    if (job.n_blocks > kMaxBlocks) job.n_blocks = kMaxBlocks;
+    job.partial = h->d_partial;
+    job.done = h->d_done;
+    job.norm_out = d_norm;
+    job.coef = write ? h->d_coef : nullptr;
+    job.coef_out = d_coef_out;
+    rc = run_pass(h, ts, n_tensors, n_workers, job, false, stream);
+    if (rc != ADACOMP_OK || !write) return rc;
+    return run_pass(h, ts, n_tensors, n_workers, job, true, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int adacomp_clip_workspace_bytes(uint32_t max_workers, size_t* bytes_out) {
+    if (!bytes_out || max_workers == 0 || max_workers > 65535) return ADACOMP_ERR_INVALID;
+    *bytes_out = carve(nullptr, nullptr, max_workers, kMaxBlocks);
+    return ADACOMP_OK;
+}
+
+int adacomp_clip_create(adacomp_clip_t** h, uint32_t max_workers, void* d_workspace, size_t workspace_bytes, int device) {
+    if (!h) return ADACOMP_ERR_INVALID;
+    *h = nullptr;
+    size_t need = 0;
+    const int rc = adacomp_clip_workspace_bytes(max_workers, &need);
+    if (rc != ADACOMP_OK) return rc;
+    if (!d_workspace || (reinterpret_cast<uintptr_t>(d_workspace) % kAlign) != 0) return ADACOMP_ERR_INVALID;
+    if (need > workspace_bytes) return ADACOMP_ERR_ALLOC;
+    adacomp_clip_t* c = new (std::nothrow) adacomp_clip_t;
+    if (!c) return ADACOMP_ERR_ALLOC;
+    c->device = device;
+    c->max_workers = max_workers;
+    carve(c, d_workspace, max_workers, kMaxBlocks);
+    DeviceGuard guard(device);
+    cudaError_t e = guard.err;
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, device);
+    if (e == cudaSuccess) e = cudaMemset(c->d_done, 0, max_workers * sizeof(uint32_t));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+    if (e != cudaSuccess) {
+        delete c;
+        return cuda_fail(e);
+    }
+    *h = c;
+    return ADACOMP_OK;
+}
+
+int adacomp_grad_norm(adacomp_clip_t* h, const adacomp_grad_tensor_t* h_tensors, uint32_t n_tensors, uint64_t grad_stride,
+                      uint32_t n_workers, float scale, float* d_norm_out, void* cuda_stream) {
+    return run(h, h_tensors, n_tensors, grad_stride, 0, n_workers, scale, 1.f, d_norm_out, nullptr, false, cuda_stream);
+}
+
+int adacomp_clip(adacomp_clip_t* h, const adacomp_grad_tensor_t* h_tensors, uint32_t n_tensors, uint64_t grad_stride,
+                 uint64_t out_stride, uint32_t n_workers, float scale, float max_norm, float* d_norm_out,
+                 float* d_coef_out, void* cuda_stream) {
+    return run(h, h_tensors, n_tensors, grad_stride, out_stride, n_workers, scale, max_norm, d_norm_out, d_coef_out, true,
+               cuda_stream);
+}
+
+int adacomp_clip_destroy(adacomp_clip_t* h) {
+    delete h;
+    return ADACOMP_OK;
+}
+
+}  // extern "C"

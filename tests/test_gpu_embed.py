@@ -1,0 +1,378 @@
+"""Embedding lookup and the table's gradient (CUDA, through the C ABI) against plain sums in 64 bits.
+
+A lookup is one fp32 product and one rounding: compared bit for bit.  A sum of L gradient entries in fp32, in any order,
+is off by at most (L - 1) u sum|g| (u = 2^-24); with the product by the scale and the rounding of fp32 (2^-24 relative, and the
+smallest subnormal) that is the tolerance for fp32 results.  The order of a sum does not depend on the result's type, so
+the others, and what is added to a table, have to be the fp32 result's roundings bit for bit.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda", 0)
+U = 2.0 ** -24
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_1702_04683_b200 import binding as b
+    return b
+
+
+def gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def words(shape, vocab, seed, skew=True, dtype=torch.int64):
+    """Tokens of which a few are frequent."""
+    r = torch.rand(shape, device=DEV, generator=gen(seed), dtype=torch.float64)
+    return ((r ** 4 if skew else r) * vocab).long().clamp_(max=vocab - 1).to(dtype)
+
+
+def plain(tokens, grad, vocab, workers, scale, pad):
+    """Sums in 64 bits, sums of magnitudes, and counts of every worker's table: [W * V, D], [W * V, D], [W * V]"""
+    D = grad.shape[-1]
+    tok = tokens.reshape(workers, -1).long()
+    live = (tok >= 0) & (tok < vocab)
+    if pad is not None:
+        live &= tok != pad
+    key = (tok + torch.arange(workers, device=DEV).view(-1, 1) * vocab)[live]
+    rows = grad.reshape(-1, D)[live.reshape(-1)].double()
+    sums = torch.zeros((workers * vocab, D), dtype=torch.float64, device=DEV).index_add_(0, key, rows)
+    size = torch.zeros_like(sums).index_add_(0, key, rows.abs())
+    return sums * scale, size * abs(scale), torch.bincount(key, minlength=workers * vocab)
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a.float(), nan=123.0), torch.nan_to_num(b.float(), nan=123.0)) and a.dtype == b.dtype
+
+
+def near(got, want, size, count):
+    tol = (count.double().view(-1, 1) + 1) * U * size
+    tol = tol + U * (want.abs() + tol) + 2.0 ** -149
+    off = (got.double() - want).abs()
+    assert bool((off <= tol).all()), float((off - tol).max())
+
+
+def check_grad(binding, tokens, grad, vocab, workers=1, scale=1.0, pad=None, out_type=torch.float32, handle=None, bad=False):
+    """All three forms of one call against the plain sums."""
+    D, n = grad.shape[-1], tokens.numel()
+    h = handle or binding.Embedding(vocab, D, max_tokens=n, max_workers=workers, padding_idx=pad)
+    want, size, count = plain(tokens, grad, vocab, workers, scale, pad)
+    keys = count.nonzero().view(-1)
+    U_ = len(keys)
+    begin_want = [int((keys < w * vocab).sum()) for w in range(workers + 1)]
+    # rows
+    rows_out = torch.full((n,), -5, dtype=torch.int32, device=DEV)
+    values_out = torch.full((n, D), 7.0, dtype=out_type, device=DEV)
+    rows, values, begin = h.grad_rows(tokens, grad, scale=scale, workers=workers, rows_out=rows_out, values_out=values_out)
+    assert begin.tolist() == begin_want
+    assert torch.equal(rows[:U_].long(), keys % vocab) and bool((rows[U_:] == -5).all()) and bool((values[U_:] == 7).all())
+    exact = h.grad_rows(tokens, grad, scale=scale, workers=workers)[1][:U_]
+    near(exact, want[keys], size[keys], count[keys])
+    assert same(values[:U_], exact.to(out_type))
+    dense = torch.zeros((workers * vocab, D), device=DEV)
+    dense[keys] = exact
+    # update
+    offset = 1_001
+    idx, val, begin = h.grad_update(tokens, grad, scale=scale, workers=workers, offset=offset)
+    assert begin.tolist() == begin_want
+    assert torch.equal(idx[:U_].long() & 0xFFFFFFFF, (keys % vocab).view(-1, 1) * D + offset + torch.arange(D, device=DEV))
+    assert same(val[:U_], exact)
+    # dense, in buffers with gaps
+    stride = vocab * D + 13 * 8
+    buf = torch.full((workers, stride), 7.0, dtype=out_type, device=DEV)
+    table = buf[:, 8:8 + vocab * D].view(workers, vocab, D)
+    h.grad_dense(tokens, grad, table, scale=scale, workers=workers)
+    assert same(table.reshape(-1, D), dense.to(out_type))
+    assert bool((buf[:, :8] == 7).all()) and bool((buf[:, 8 + vocab * D:] == 7).all())
+    # added to what is there
+    base = torch.randn((workers, vocab, D), device=DEV, generator=gen(3)).to(out_type)
+    acc = base.clone()
+    h.grad_dense(tokens, grad, acc, scale=scale, workers=workers, accumulate=True)
+    added = torch.where((count > 0).view(-1, 1), (dense + base.view(-1, D).float()).to(out_type), base.view(-1, D))
+    assert same(acc.view(-1, D), added)
+    assert h.last_error() == (binding.ERR_INVALID if bad else 0)
+    assert h.last_error() == 0
+    return h
+
+
+# --------------------------------------------------------------------------------------------- lookup
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("dim,tokens", [(1, 5), (7, 33), (64, 1), (64, 1000), (513, 100), (1000, 65), (2048, 17), (5000, 3)])
+def test_lookup(binding, kind, out, dim, tokens):
+    vocab = 211
+    table = (torch.randn((vocab, dim), device=DEV, generator=gen(dim)) * 0.02).to(kind)
+    ids = words((tokens,), vocab, tokens, skew=False, dtype=torch.int32 if tokens % 2 else torch.int64)
+    h = binding.Embedding(vocab, dim)
+    for scale in (1.0, dim ** 0.5):
+        got = h.lookup(table, ids, scale=scale, dtype=out)
+        assert torch.equal(got, (table[ids.long()].float() * scale).to(out))
+    assert h.last_error() == 0
+
+
+def test_lookup_shapes_strides_and_alignment(binding):
+    vocab, dim = 97, 24
+    wide = torch.randn((vocab, dim + 9), device=DEV, generator=gen(1))
+    h = binding.Embedding(vocab, dim)
+    data = words((6, 31), vocab, 2, skew=False)
+    for table in (wide[:, :dim], wide[:, 8:8 + dim], wide[:, 3:3 + dim]):
+        for ids in (data, data[:, :-1], data[:, 1:], data.t(), data[::2, 3:9], data[0, 0], data[:0]):
+            got = h.lookup(table, ids)
+            assert got.shape == (*ids.shape, dim) and torch.equal(got, table[ids])
+            buf = torch.full((*ids.shape, dim + 5), 7.0, device=DEV)
+            h.lookup(table, ids, scale=-2.0, out=buf[..., 2:2 + dim])
+            assert torch.equal(buf[..., 2:2 + dim], table[ids] * -2.0)
+            assert bool((buf[..., :2] == 7).all()) and bool((buf[..., 2 + dim:] == 7).all())
+    out = torch.empty((31, 6, dim), device=DEV).transpose(0, 1)             # rows in another order
+    assert torch.equal(h.lookup(table, data, out=out), table[data])
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_lookup_of_tokens_outside_the_vocabulary(binding, dtype):
+    vocab, dim = 50, 40
+    table = torch.randn((vocab, dim), device=DEV, generator=gen(1))
+    ids = torch.tensor([0, -1, 49, 50, 7, 2 ** 31 - 1, -2 ** 31] + ([2 ** 32, 2 ** 32 + 3, -2 ** 63] if dtype == torch.int64 else []), device=DEV).to(dtype)
+    h = binding.Embedding(vocab, dim)
+    got = h.lookup(table, ids)
+    ok = (ids >= 0) & (ids < vocab)
+    assert torch.equal(got[ok], table[ids[ok].long()]) and bool((got[~ok] == 0).all())
+    assert h.last_error() == binding.ERR_INVALID and h.last_error() == 0
+
+
+def test_lookup_beyond_32_bits(binding):
+    vocab, dim = 1_100_000, 4096                                            # 4.5e9 entries
+    table = torch.empty((vocab, dim), device=DEV, dtype=torch.bfloat16)
+    ids = torch.tensor([0, 1_048_575, 1_048_576, 1_048_577, vocab - 1], device=DEV)
+    table[ids] = torch.randn((5, dim), device=DEV, generator=gen(1)).bfloat16()
+    h = binding.Embedding(vocab, dim)
+    assert torch.equal(h.lookup(table, ids), table[ids])
+
+
+def test_lookup_keeps_infinities_and_nan(binding):
+    table = torch.tensor([[1.0, float("inf"), float("nan"), -0.0], [float("-inf"), 2.0, 3.0, 4.0]], device=DEV)
+    h = binding.Embedding(2, 4)
+    got = h.lookup(table, torch.tensor([1, 0], device=DEV), scale=2.0, dtype=torch.float16)
+    assert torch.equal(torch.nan_to_num(got, nan=-9.0), torch.nan_to_num((table[[1, 0]] * 2).half(), nan=-9.0))
+
+
+# --------------------------------------------------------------------------------------------- gradient
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 257, 1024, 1025, 2048, 2049, 8192, 8193, 20_000, 70_000])
+@pytest.mark.parametrize("vocab", [1, 2, 300, 70_000])
+def test_numbers_of_tokens_and_vocabularies(binding, n, vocab):
+    tokens = words((n,), vocab, n + vocab)
+    grad = torch.randn((n, 16), device=DEV, generator=gen(n))
+    check_grad(binding, tokens, grad, vocab)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("out", TYPES)
+@pytest.mark.parametrize("dim", [1, 6, 8, 64, 129, 1000, 1024, 2050])
+def test_types_and_widths(binding, kind, out, dim):
+    n, vocab = 1_500, 333
+    tokens = words((n,), vocab, dim, dtype=torch.int32)
+    grad = torch.randn((n, dim), device=DEV, generator=gen(dim)).to(kind)
+    check_grad(binding, tokens, grad, vocab, scale=0.25, pad=5, out_type=out)
+
+
+@pytest.mark.parametrize("spread", ["one", "two", "all different", "long runs", "falling"])
+@pytest.mark.parametrize("n", [40, 3_000, 30_000])
+def test_spreads(binding, spread, n):
+    vocab, dim = max(n, 64), 64
+    i = torch.arange(n, device=DEV)
+    tokens = {"one": i * 0 + 17, "two": (i % 2) * 40 + 3, "all different": torch.randperm(n, device=DEV, generator=gen(n)),
+              "long runs": i // 700, "falling": n - 1 - i}[spread]
+    grad = torch.randn((n, dim), device=DEV, generator=gen(n)).bfloat16()
+    check_grad(binding, tokens, grad, vocab, scale=3.0)
+
+
+@pytest.mark.parametrize("workers,n,vocab", [(2, 1, 5), (3, 700, 100), (8, 2_048, 3_000), (50, 100, 11), (4, 9_000, 33)])
+def test_workers(binding, workers, n, vocab):
+    tokens = words((workers, n), vocab, n)
+    tokens[workers // 2] = 3                                                # a worker with nothing but padding
+    grad = torch.randn((workers, n, 40), device=DEV, generator=gen(n)).half()
+    check_grad(binding, tokens, grad, vocab, workers=workers, scale=0.5, pad=3)
+
+
+def test_only_padding_no_tokens_and_tokens_outside(binding):
+    grad = torch.randn((300, 24), device=DEV, generator=gen(1))
+    check_grad(binding, torch.full((300,), 4, device=DEV), grad, 9, pad=4)
+    check_grad(binding, torch.empty((0,), dtype=torch.int64, device=DEV), grad[:0], 9, workers=1)
+    tokens = words((300,), 9, 7)
+    tokens[::3] = -1
+    tokens[1::7] = 9
+    tokens[5] = 2 ** 40
+    check_grad(binding, tokens, grad, 9, bad=True)
+    check_grad(binding, tokens * 0 - 1, grad, 9, bad=True)
+    h = binding.Embedding(9, 24, max_tokens=300, padding_idx=4)
+    h.grad_rows(words((300,), 9, 7), grad)                                  # a handle that has seen errors and others goes on
+    check_grad(binding, words((200,), 9, 8), grad[:200], 9, pad=4, handle=h)
+
+
+def test_strided_tokens_and_gradients(binding):
+    data = words((7, 65), 50, 1)
+    wide = torch.randn((7, 65, 48), device=DEV, generator=gen(2))
+    for tokens, grad in ((data[:, :-1], wide[:, :-1]), (data[:, 1:], wide[:, 1:, :32]), (data[:, 1:], wide[:, 1:, 3:40]),
+                         (data.t(), wide.transpose(0, 1)), (data[::2], wide[::2, :, 16:]), (data[3], wide[3]),
+                         (data, wide[:1, :1].expand(7, 65, 48))):
+        check_grad(binding, tokens, grad, 50)
+
+
+def test_masked_rows_of_infinities_do_not_leak(binding):
+    """The gradient of a padding token is not read into any sum, whatever it holds; an infinity reaches its own row alone."""
+    n, vocab, dim = 2_000, 40, 32
+    tokens = words((n,), vocab, 1)
+    grad = torch.randn((n, dim), device=DEV, generator=gen(1))
+    grad[tokens == 6] = float("nan")
+    check_grad(binding, tokens, grad, vocab, pad=6)
+    grad = torch.randn((n, dim), device=DEV, generator=gen(1))
+    at = int((tokens == 9).nonzero()[0])
+    grad[at, 5], grad[at, 6] = float("inf"), torch.finfo(torch.float32).min
+    h = binding.Embedding(vocab, dim, max_tokens=n)
+    out = h.grad_dense(tokens, grad, torch.empty((vocab, dim), device=DEV))
+    assert bool(torch.isinf(out[9, 5]))
+    out[9, 5] = 0
+    assert bool(torch.isfinite(out).all())
+
+
+def test_gradient_against_differences(binding):
+    """sum(lookup(E) R) is linear in E: its difference quotient along any direction is <dE, direction>."""
+    vocab, dim, n, scale = 60, 33, 500, 4.0
+    g = gen(5)
+    table = torch.randn((vocab, dim), device=DEV, generator=g)
+    way = torch.randn((vocab, dim), device=DEV, generator=g)
+    R = torch.randn((n, dim), device=DEV, generator=g)
+    tokens = words((n,), vocab, 3)
+    h = binding.Embedding(vocab, dim, max_tokens=n)
+    dE = h.grad_dense(tokens, R, torch.empty((vocab, dim), device=DEV), scale=scale)
+    step = 0.5
+    up, down = (h.lookup(table + s * step * way, tokens, scale=scale).double() for s in (1, -1))
+    quotient = ((up - down) * R.double()).sum() / (2 * step)
+    exact = (dE.double() * way.double()).sum()
+    # every looked-up entry is rounded three times (the moved table, the product; twice over), the sums as above
+    size = (h.lookup(table.abs() + step * way.abs(), tokens, scale=scale).double() * R.double().abs()).sum()
+    assert abs(float(quotient - exact)) <= float(4 * U * size / step + n * U * (plain(tokens, R, vocab, 1, scale, None)[1] * way.double().abs()).sum())
+
+
+def test_update_is_what_the_server_applies(binding):
+    """Lookup gradient -> update -> server, next to the oracle's server on the same pairs."""
+    vocab, dim, workers, n, offset = 500, 48, 3, 400, 777
+    P = offset + vocab * dim + 55
+    theta = torch.randn(P, device=DEV, generator=gen(1))
+    ref = oracle.Server(theta.cpu().numpy())
+    srv = binding.Server(theta, history_pairs=10 * workers * n * dim, max_window_updates=16)
+    srv.set_validation(True)
+    h = binding.Embedding(vocab, dim, max_tokens=workers * n, max_workers=workers, padding_idx=0)
+    for step in range(2):
+        tokens = words((workers, n), vocab, step)
+        grad = torch.randn((workers, n, dim), device=DEV, generator=gen(step))
+        idx, val, begin = h.grad_update(tokens, grad, workers=workers, offset=offset)
+        b = np.array(begin.tolist(), dtype=np.uint64) * np.uint64(dim)
+        pulls = np.full(workers, step, dtype=np.uint64)
+        srv.apply(idx.view(-1), val.view(-1), b[:-1], np.diff(b).astype(np.uint32), pulls, 0.1)
+        h_idx, h_val = idx.cpu().numpy().view(np.uint32).reshape(-1), val.cpu().numpy().reshape(-1)
+        for w in range(workers):
+            lo, hi = int(b[w]), int(b[w + 1])
+            ref.apply(h_idx[lo:hi], h_val[lo:hi], step, 0.1)
+    assert srv.last_error() == 0 and h.last_error() == 0
+    assert np.array_equal(theta.cpu().numpy().view(np.uint32), ref.theta().view(np.uint32))
+
+
+def test_large_batch_with_frequent_tokens(binding):
+    n, vocab, dim = 200_000, 32_000, 256
+    tokens = words((n,), vocab, 1)
+    tokens[torch.rand(n, device=DEV, generator=gen(2)) < 0.3] = 11          # one token is a third of the batch
+    grad = torch.randn((n, dim), device=DEV, generator=gen(1)).bfloat16()
+    check_grad(binding, tokens, grad, vocab, scale=0.125)
+
+
+def test_vocabularies_of_many_bits(binding):
+    for vocab, workers in ((2 ** 31 - 1, 2), (2 ** 32 - 2, 1), (2 ** 20, 4095)):
+        h = binding.Embedding(vocab, 2, max_tokens=workers * 300, max_workers=workers)
+        tokens = torch.randint(vocab, (workers, 300), device=DEV, generator=gen(1))
+        tokens[:, ::4] = tokens[:, :1]
+        tokens[-1, 7] = vocab - 1
+        grad = torch.randn((workers, 300, 2), device=DEV, generator=gen(1))
+        rows, values, begin = h.grad_rows(tokens, grad, workers=workers)
+        keys, inverse = torch.unique(tokens + torch.arange(workers, device=DEV).view(-1, 1) * vocab, return_inverse=True)
+        assert int(begin[-1]) == len(keys)
+        assert torch.equal(rows[:len(keys)].long() & 0xFFFFFFFF, keys % vocab)
+        want = torch.zeros((len(keys), 2), dtype=torch.float64, device=DEV).index_add_(0, inverse.view(-1), grad.view(-1, 2).double())
+        assert float((values[:len(keys)] - want).abs().max()) <= 76 * U * 76 * 6
+
+
+def test_another_stream(binding):
+    side = torch.cuda.Stream()
+    n, vocab, dim = 5_000, 900, 128
+    tokens, grad = words((n,), vocab, 1), torch.randn((n, dim), device=DEV, generator=gen(1))
+    h = binding.Embedding(vocab, dim, max_tokens=n)
+    side.wait_stream(torch.cuda.current_stream())
+    got = [h.grad_rows(tokens, grad, stream=side) for _ in range(3)]
+    looked = h.lookup(grad[:vocab], tokens, stream=side)
+    assert h.last_error(stream=side) == 0
+    rows, values, begin = h.grad_rows(tokens, grad)
+    U_ = int(begin[1])
+    for r, v, b in got:
+        assert torch.equal(r[:U_], rows[:U_]) and torch.equal(v[:U_], values[:U_]) and torch.equal(b, begin)
+    assert torch.equal(looked, grad[tokens])
+
+
+def test_refusals(binding):
+    lib = binding.raw()
+    vocab, dim = 20, 16
+    h = binding.Embedding(vocab, dim, max_tokens=100, max_workers=2)
+    tokens = torch.zeros(50, dtype=torch.int64, device=DEV)
+    grad, table = torch.zeros((50, dim), device=DEV), torch.zeros((vocab, dim), device=DEV)
+    out, begin = torch.zeros((50, dim), device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV)
+
+    def rows(t, kind, **fields):
+        r = binding.Rows()
+        r.d_data, r.type, r.row_stride = t.data_ptr(), kind, dim if t.dim() > 1 else 1
+        for k, v in fields.items():
+            setattr(r, k, v)
+        return ctypes.byref(r)
+
+    def lookup(t={}, k={}, o={}, n=50, scale=1.0):
+        return lib.adacomp_embed_lookup(h._h, rows(table, 0, **t), rows(tokens, 1, **k), n, scale, rows(out, 0, **o), None)
+
+    def sums(k={}, g={}, n=50, workers=1, scale=1.0, b=begin.data_ptr(), v=out.data_ptr(), kind=0, idx=None, offset=0):
+        return lib.adacomp_embed_grad_rows(h._h, rows(tokens, 1, **k), n, workers, rows(grad, 0, **g), scale, None, b, v, kind, idx, offset, None)
+
+    def dense(k={}, g={}, o={}, n=50, workers=1):
+        return lib.adacomp_embed_grad_dense(h._h, rows(tokens, 1, **k), n, workers, rows(grad, 0, **g), 1.0, rows(table, 0, **o), 0, None)
+
+    inf = float("inf")
+    for bad in (dict(t=dict(type=3)), dict(k=dict(type=2)), dict(o=dict(type=-1)), dict(t=dict(d_data=None)), dict(k=dict(d_data=None)),
+                dict(o=dict(d_data=None)), dict(t=dict(d_data=table.data_ptr() + 2)), dict(k=dict(d_data=tokens.data_ptr() + 4)),
+                dict(o=dict(row_stride=dim - 1)), dict(o=dict(group=5, group_stride=0)), dict(t=dict(group=4, group_stride=7)),
+                dict(scale=inf), dict(scale=float("nan")), dict(n=2 ** 31)):
+        assert lookup(**bad) == binding.ERR_INVALID, bad
+    for bad in (dict(k=dict(type=5)), dict(g=dict(type=7)), dict(workers=0), dict(workers=3), dict(scale=inf), dict(b=None), dict(v=None),
+                dict(v=out.data_ptr() + 2), dict(kind=9), dict(idx=out.data_ptr(), offset=2 ** 32 - 100), dict(g=dict(d_data=None))):
+        assert sums(**bad) == binding.ERR_INVALID, bad
+    assert sums(n=101) == binding.ERR_CAPACITY and sums(n=51, workers=2) == binding.ERR_CAPACITY
+    for bad in (dict(o=dict(type=4)), dict(o=dict(row_stride=3)), dict(o=dict(d_data=None))):
+        assert dense(**bad) == binding.ERR_INVALID, bad
+    assert lookup() == 0 and sums() == 0 and dense() == 0 and h.last_error() == 0
+    for bad in (lambda: h.lookup(table[:5], tokens), lambda: h.lookup(table, tokens.float()), lambda: h.lookup(table.double(), tokens),
+                lambda: h.lookup(table, tokens.cpu()), lambda: h.lookup(table.cpu(), tokens), lambda: h.lookup(table[:, :4], tokens),
+                lambda: h.lookup(table, tokens, out=out[:9]), lambda: h.lookup(table.t().contiguous().t(), tokens),
+                lambda: h.grad_rows(tokens, grad, workers=3), lambda: h.grad_rows(tokens, grad[:9]), lambda: h.grad_rows(tokens, grad, values_out=out[:9]),
+                lambda: h.grad_update(tokens, grad, val_out=out.half()), lambda: h.grad_dense(tokens, grad, table[:7]),
+                lambda: h.grad_dense(tokens[:vocab], table, table), lambda: binding.Embedding(5, 5, padding_idx=5)):
+        with pytest.raises((TypeError, ValueError)):
+            bad()
+    for bad in (lambda: binding.Embedding(0, 5), lambda: binding.Embedding(5, -1), lambda: binding.Embedding(2 ** 31, 5, max_workers=2)):
+        with pytest.raises(binding.AdacompError):
+            bad()
