@@ -18,20 +18,30 @@ struct adacomp_embed {
     uint32_t vocab, dim, max_tokens, max_workers, padding;
     int n_sms;
     int* d_status;
-    uint32_t* d_key[2];             // [max_tokens] worker * vocab + token, before and after a pass of the sort
+    uint32_t* d_barrier;            // arrivals, and blocks that are through
+    uint32_t* d_key[2];             // [max_tokens] worker * vocab + token, between the passes of the sort
     uint32_t* d_pos[2];             // [max_tokens] which token it is
-    uint32_t* d_table;              // [tiles][256] digit counts per tile, then their places
-    uint32_t* d_seg_begin;          // [max_tokens + 1] first sorted token of every distinct one
+    uint32_t* d_table;              // [kSortBlocks][kMaxBins] digit counts per block
+    uint32_t* d_seg_begin;          // [max_tokens + 1] first sorted token of every distinct one, and their end
     uint32_t* d_seg_key;            // [max_tokens]
+    uint32_t* d_chunk_seg;          // [chunks + 1] how many segments begin before the chunk
     uint32_t* d_n_segs;
+    uint32_t* d_long;               // how many segments are longer than a chunk, then the chunks they begin in
+    float* d_partial;               // [chunks][2][dim] sums of pieces of those
 };
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSortItems = 8;
-constexpr uint32_t kTile = kThreads * kSortItems;           // tokens per block of the sort
-constexpr int kBins = 256;
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kItems = 8;                                   // tokens per thread and step of the sort
+constexpr uint32_t kStep = kSortThreads * kItems;
+constexpr uint32_t kOneBlock = 8192;                        // up to here one block sorts alone
+constexpr uint32_t kSortBlocks = 64;
+constexpr int kDigitBits = 9;
+constexpr int kMaxBins = 1 << kDigitBits;
+constexpr uint32_t kSpinLimit = 1u << 22;                   // polls of a barrier, some seconds
 
 // Device view of adacomp_rows_t.
 struct Rows {
@@ -92,156 +102,272 @@ __global__ void __launch_bounds__(kThreads) k_embed_lookup(Rows table, Rows toke
 
 // ---------------------------------------------------------------------------------------------- sort
 
-__global__ void __launch_bounds__(kThreads) k_embed_keys(Rows tokens, uint32_t n, uint32_t n_tokens, uint32_t vocab, uint32_t padding,
-                                                          uint32_t none, uint32_t* key, uint32_t* pos, int* status) {
-    const uint32_t t = blockIdx.x * kThreads + threadIdx.x;
-    if (t >= n) return;
-    const uint32_t v = load_token(tokens, t, vocab);
-    if (v == 0xFFFFFFFFu) record_error(status, ADACOMP_ERR_INVALID);
-    key[t] = v == 0xFFFFFFFFu || v == padding ? none : (t / n_tokens) * vocab + v;
-    pos[t] = t;
-}
+struct SortJob {
+    Rows tokens;
+    uint32_t n, n_tokens, n_workers, vocab, padding, none;  // none = n_workers * vocab: the key of tokens without a gradient
+    uint32_t n_blocks, per_block;                           // blocks that sort, tokens of each (a multiple of kSortThreads)
+    int passes, bits;
+    uint32_t* key[2];
+    uint32_t* pos[2];
+    uint32_t* table;
+    uint32_t *seg_begin, *seg_key, *n_segs, *chunk_seg, *n_long;
+    uint32_t chunk_shift;
+    uint64_t* row_begin;                                    // or null
+    uint32_t* barrier;
+    int* status;
+    // rows that become zeros before the sums are written (the blocks that do not sort)
+    Rows zero;
+    uint64_t zero_rows;
+    uint32_t dim;
+    int zero_vec;
+};
 
-__global__ void __launch_bounds__(kThreads) k_radix_count(const uint32_t* key, uint32_t n, int shift, uint32_t* table) {
-    __shared__ uint32_t s_count[kBins];
-    s_count[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = 0; i < kSortItems; ++i) {
-        const uint32_t t = blockIdx.x * kTile + i * kThreads + threadIdx.x;
-        if (t < n) atomicAdd(&s_count[(key[t] >> shift) & (kBins - 1)], 1u);
+// Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
+// does not, the block says so and the caller gives up.
+__device__ __forceinline__ bool meet(const SortJob& j) {
+    __shared__ int s_ok;
+    if (j.n_blocks == 1) {
+        __syncthreads();
+        return true;
     }
     __syncthreads();
-    table[threadIdx.x * gridDim.x + blockIdx.x] = s_count[threadIdx.x];     // digit-major: one running total over it gives the places
+    if (threadIdx.x == 0) {
+        __threadfence();
+        const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
+        uint32_t seen = 0, polls = 0;
+        do {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
+        } while (seen < target && ++polls < kSpinLimit);
+        s_ok = seen >= target;
+        if (seen < target) record_error(j.status, ADACOMP_ERR_TIMEOUT);
+    }
+    __syncthreads();
+    return s_ok != 0;
 }
 
-// Inclusive sum over the block's 1024 threads.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* s_warp) {
+// Sum over the block's threads before this one, and over all of them.
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s_warp, uint32_t* total) {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t upto = v;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, v, d);
-        if (lane >= static_cast<uint32_t>(d)) v += y;
+        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+        if (lane >= static_cast<uint32_t>(d)) upto += y;
     }
     __syncthreads();
-    if (lane == 31) s_warp[warp] = v;
+    if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    uint32_t before = 0;
-    for (uint32_t k = 0; k < warp; ++k) before += s_warp[k];
-    return v + before;
+    const uint32_t w = s_warp[lane];
+    *total = __reduce_add_sync(0xFFFFFFFFu, w);
+    return __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u) + upto - v;
 }
 
-// In place: counts become the totals before them; *total (if any) their sum.
-__global__ void __launch_bounds__(1024) k_running_total(uint32_t* a, uint32_t n, uint32_t* total) {
+template <typename B> __device__ __forceinline__ void zero_row(B* dst, uint32_t dim, bool vec) {
+    if (vec) {
+        const uint32_t n = dim * static_cast<uint32_t>(sizeof(B)) / 16;
+        for (uint32_t c = threadIdx.x; c < n; c += blockDim.x) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        for (uint32_t c = threadIdx.x; c < dim; c += blockDim.x) dst[c] = from_float<B>(0.f);
+    }
+}
+__device__ __forceinline__ void zero_row(const Rows& out, uint64_t row, uint32_t dim, bool vec) {
+    const uint64_t at = out.offset(static_cast<uint32_t>(row));
+    if (out.type == ADACOMP_F32) zero_row(reinterpret_cast<float*>(out.data) + at, dim, vec);
+    else zero_row(reinterpret_cast<__half*>(out.data) + at, dim, vec);      // the zeros of both 16-bit types are the same bits
+}
+
+// Stable sort of the tokens by worker and token, and what the sums need to know about the sorted list.  Least significant
+// digit first; a block ranks its tokens with ballots (a warp's rows of 32 in turn, one counter per warp and digit),
+// the blocks tell each other their counts through a table in global memory.
+__global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j) {
+    __shared__ uint16_t s_count[kSortWarps][kMaxBins];      // of a digit in the warps before
+    __shared__ uint32_t s_base[kMaxBins];
     __shared__ uint32_t s_warp[32];
-    __shared__ uint32_t s_carry;
-    if (threadIdx.x == 0) s_carry = 0;
-    __syncthreads();
-    for (uint32_t base = 0; base < n; base += 1024) {
-        const uint32_t i = base + threadIdx.x;
-        const uint32_t v = i < n ? a[i] : 0;
-        const uint32_t upto = block_scan(v, s_warp) + s_carry;
-        if (i < n) a[i] = upto - v;
-        __syncthreads();
-        if (threadIdx.x == 1023) s_carry = upto;
-        __syncthreads();
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (blockIdx.x >= j.n_blocks) {
+        for (uint64_t r = blockIdx.x - j.n_blocks; r < j.zero_rows; r += gridDim.x - j.n_blocks) zero_row(j.zero, r, j.dim, j.zero_vec != 0);
+        return;
     }
-    if (total && threadIdx.x == 0) *total = s_carry;
-}
-
-__global__ void __launch_bounds__(kThreads) k_radix_scatter(const uint32_t* key, const uint32_t* pos, uint32_t n, int shift,
-                                                             const uint32_t* table, uint32_t* key_out, uint32_t* pos_out) {
-    __shared__ uint32_t s_place[kThreads / 32][kBins];      // how many of a digit the warps before have, then places
-    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (uint32_t d = lane; d < kBins; d += 32) s_place[warp][d] = 0;
-    __syncwarp();
-    uint32_t k[kSortItems], rank[kSortItems];
-    const uint32_t base = blockIdx.x * kTile + warp * (32 * kSortItems) + lane;
+    const uint64_t from = static_cast<uint64_t>(blockIdx.x) * j.per_block;
+    const uint64_t to = from + j.per_block < j.n ? from + j.per_block : j.n;
+    const uint32_t bins = 1u << j.bits, mask = bins - 1;
+    const uint32_t items = j.per_block < kStep ? j.per_block / kSortThreads : kItems;     // rows of 32 per warp and step
+    const bool one_step = j.per_block <= kStep;
+    uint32_t key[kItems], pos[kItems], rank[kItems];
+    for (int pass = 0; pass < j.passes; ++pass) {
+        const uint32_t* key_in = j.key[(pass & 1) ^ 1];
+        const uint32_t* pos_in = j.pos[(pass & 1) ^ 1];
+        const int shift = pass * j.bits;
+        // Loads step `at`, ranks it and leaves s_count as places within the step; returns the step's count of digit tid.
+        auto rank_step = [&](uint64_t at, bool report) -> uint32_t {
+            for (uint32_t d = lane; d < bins; d += 32) s_count[warp][d] = 0;
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-        const uint32_t t = base + i * 32;
-        k[i] = t < n ? key[t] : 0xFFFFFFFFu;
-        const uint32_t d = (k[i] >> shift) & (kBins - 1);
-        uint32_t same = __ballot_sync(0xFFFFFFFFu, t < n);
-        if (t >= n) same = ~same;
+            for (int i = 0; i < kItems; ++i) {
+                const uint64_t t = at + (warp * items + i) * 32 + lane;
+                key[i] = j.none;
+                pos[i] = 0;
+                if (i >= items || t >= to) continue;
+                if (pass == 0) {
+                    const uint32_t v = load_token(j.tokens, static_cast<uint32_t>(t), j.vocab);
+                    if (v == 0xFFFFFFFFu && report) record_error(j.status, ADACOMP_ERR_INVALID);
+                    if (v != 0xFFFFFFFFu && v != j.padding) key[i] = (j.n_workers == 1 ? 0u : static_cast<uint32_t>(t) / j.n_tokens * j.vocab) + v;
+                    pos[i] = static_cast<uint32_t>(t);
+                } else {
+                    key[i] = __ldcg(key_in + t);
+                    pos[i] = __ldcg(pos_in + t);
+                }
+            }
+            __syncwarp();
 #pragma unroll
-        for (int b = 0; b < 8; ++b) {
-            const uint32_t vote = __ballot_sync(0xFFFFFFFFu, (d >> b) & 1);
-            same &= (d >> b) & 1 ? vote : ~vote;
+            for (int i = 0; i < kItems; ++i) {
+                if (i >= items) break;
+                const bool real = at + (warp * items + i) * 32 + lane < to;
+                const uint32_t d = (key[i] >> shift) & mask;
+                uint32_t same = __ballot_sync(0xFFFFFFFFu, real);
+                if (!real) same = ~same;
+                for (int b = 0; b < j.bits; ++b) {
+                    const uint32_t vote = __ballot_sync(0xFFFFFFFFu, (d >> b) & 1);
+                    same &= (d >> b) & 1 ? vote : ~vote;
+                }
+                const uint32_t before = __popc(same & ((1u << lane) - 1));
+                rank[i] = s_count[warp][d] + before;
+                __syncwarp();
+                if (real && before == 0) s_count[warp][d] += static_cast<uint16_t>(__popc(same));
+                __syncwarp();
+            }
+            __syncthreads();
+            uint32_t sum = 0;
+            if (tid < bins) {
+#pragma unroll 8
+                for (int w = 0; w < kSortWarps; ++w) {
+                    const uint32_t c = s_count[w][tid];
+                    s_count[w][tid] = static_cast<uint16_t>(sum);
+                    sum += c;
+                }
+            }
+            return sum;
+        };
+        uint32_t count = 0;
+        for (uint64_t at = from; at < to || at == from; at += kStep) {
+            if (at != from) __syncthreads();
+            count += rank_step(at, true);
         }
-        const uint32_t before = __popc(same & ((1u << lane) - 1));
-        rank[i] = s_place[warp][d] + before;
-        __syncwarp();
-        if (t < n && before == 0) s_place[warp][d] += __popc(same);
-        __syncwarp();
-    }
-    __syncthreads();
-    uint32_t at = table[threadIdx.x * gridDim.x + blockIdx.x];
-    for (int w = 0; w < kThreads / 32; ++w) {
-        const uint32_t c = s_place[w][threadIdx.x];
-        s_place[w][threadIdx.x] = at;
-        at += c;
-    }
-    __syncthreads();
+        uint32_t all = count, before = 0;
+        if (j.n_blocks > 1) {
+            if (tid < bins) __stcg(j.table + blockIdx.x * bins + tid, count);
+            if (!meet(j)) return;
+            if (tid < bins) {
+                all = 0;
+#pragma unroll 8
+                for (uint32_t b = 0; b < j.n_blocks; ++b) {
+                    const uint32_t c = __ldcg(j.table + b * bins + tid);
+                    all += c;
+                    if (b < blockIdx.x) before += c;
+                }
+            }
+        }
+        uint32_t total;
+        const uint32_t base = block_before(tid < bins ? all : 0u, s_warp, &total) + before;
+        if (tid < bins) s_base[tid] = base;
+        for (uint64_t at = from; at < to; at += kStep) {
+            uint32_t step_count = 0;
+            if (!one_step) {
+                __syncthreads();
+                step_count = rank_step(at, false);
+            }
+            __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kSortItems; ++i) {
-        const uint32_t t = base + i * 32;
-        if (t >= n) continue;
-        const uint32_t to = s_place[warp][(k[i] >> shift) & (kBins - 1)] + rank[i];
-        key_out[to] = k[i];
-        pos_out[to] = pos[t];
+            for (int i = 0; i < kItems; ++i) {
+                if (i >= items || at + (warp * items + i) * 32 + lane >= to) continue;
+                const uint32_t d = (key[i] >> shift) & mask;
+                const uint32_t place = s_base[d] + s_count[warp][d] + rank[i];
+                __stcg(j.key[pass & 1] + place, key[i]);
+                __stcg(j.pos[pass & 1] + place, pos[i]);
+            }
+            if (!one_step) {
+                __syncthreads();
+                if (tid < bins) s_base[tid] += step_count;
+            }
+        }
+        if (!meet(j)) return;
     }
-}
 
-// ---------------------------------------------------------------------------------------------- segments
-
-__device__ __forceinline__ bool is_head(const uint32_t* key, uint32_t i, uint32_t none) {
-    return key[i] != none && (i == 0 || key[i - 1] != key[i]);
-}
-
-__global__ void __launch_bounds__(kThreads) k_heads_count(const uint32_t* key, uint32_t n, uint32_t none, uint32_t* count) {
-    int c = 0;
-    for (int i = 0; i < kSortItems; ++i) {
-        const uint32_t t = blockIdx.x * kTile + i * kThreads + threadIdx.x;
-        c += __syncthreads_count(t < n && is_head(key, t, none));
+    // Segments: where each begins, how many begin before every chunk, where each worker's begin.
+    const uint32_t* sorted = j.key[(j.passes - 1) & 1];
+    uint32_t segs = 0, total;
+    if (j.n_blocks > 1) {
+        for (uint64_t at = from; at < to; at += kSortThreads) {
+            const uint64_t i = at + tid;
+            bool head = false;
+            if (i < to) {
+                const uint32_t k = __ldcg(sorted + i);
+                head = k != j.none && (i == 0 || __ldcg(sorted + i - 1) != k);
+            }
+            segs += __syncthreads_count(head);
+        }
+        if (tid == 0) __stcg(j.table + blockIdx.x, segs);
+        if (!meet(j)) return;
+        const uint32_t c = tid < j.n_blocks ? __ldcg(j.table + tid) : 0u;
+        block_before(tid < blockIdx.x ? c : 0u, s_warp, &total);
+        segs = total;
     }
-    if (threadIdx.x == 0) count[blockIdx.x] = c;
-}
-
-__global__ void __launch_bounds__(1024) k_heads_emit(const uint32_t* key, uint32_t n, uint32_t none, const uint32_t* place, uint32_t* seg_begin,
-                                                      uint32_t* seg_key, uint32_t* n_segs) {
-    __shared__ uint32_t s_warp[32];
-    uint32_t carry = place[blockIdx.x];
-    for (uint32_t base = blockIdx.x * kTile; base < n && base < (blockIdx.x + 1) * kTile; base += 1024) {
-        const uint32_t t = base + threadIdx.x;
-        const bool head = t < n && is_head(key, t, none);
-        const uint32_t upto = carry + block_scan(head, s_warp);
+    for (uint64_t at = from; at < to; at += kSortThreads) {
+        const uint64_t i = at + tid;
+        uint32_t k = j.none, last = j.none, next = j.none;
+        if (i < to) {
+            k = __ldcg(sorted + i);
+            if (i > 0) last = __ldcg(sorted + i - 1);
+            if (i + 1 < j.n) next = __ldcg(sorted + i + 1);
+        }
+        const bool head = k != j.none && (i == 0 || last != k);
+        const uint32_t u = segs + block_before(head, s_warp, &total);      // segments that begin before i
+        segs += total;
+        if (i >= to) continue;
+        if ((i & ((1u << j.chunk_shift) - 1)) == 0) j.chunk_seg[i >> j.chunk_shift] = u;
         if (head) {
-            seg_begin[upto - 1] = t;
-            seg_key[upto - 1] = key[t];
+            j.seg_begin[u] = static_cast<uint32_t>(i);
+            j.seg_key[u] = k;
         }
-        // the last segment ends where the tokens without a gradient begin, or with the list
-        if (t < n && key[t] != none && (t + 1 == n || key[t + 1] == none)) seg_begin[upto] = t + 1;
-        carry += __syncthreads_count(head);
+        const bool end = k != j.none && next == j.none;                    // the last token with a gradient
+        const uint32_t n_segs = u + head;
+        if (end) {
+            j.seg_begin[n_segs] = static_cast<uint32_t>(i) + 1;
+            *j.n_segs = n_segs;
+        }
+        if (j.row_begin && (head || end)) {
+            const uint32_t w = j.n_workers == 1 ? 0u : k / j.vocab;
+            if (head)
+                for (uint32_t v = i == 0 ? 0u : (j.n_workers == 1 ? 0u : last / j.vocab) + 1; v <= w; ++v) j.row_begin[v] = u;
+            if (end)
+                for (uint32_t v = w + 1; v <= j.n_workers; ++v) j.row_begin[v] = n_segs;
+        }
     }
-    (void)n_segs;
-}
-
-__global__ void k_row_begin(const uint32_t* seg_key, const uint32_t* n_segs, uint32_t n_workers, uint32_t vocab, uint64_t* row_begin) {
-    const uint32_t w = blockIdx.x * blockDim.x + threadIdx.x;
-    if (w > n_workers) return;
-    const uint64_t bound = static_cast<uint64_t>(w) * vocab;
-    uint32_t lo = 0, hi = *n_segs;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (seg_key[mid] < bound) lo = mid + 1; else hi = mid;
+    const bool nothing = j.n == 0 || (blockIdx.x == 0 && __ldcg(sorted) == j.none);     // not one token with a gradient
+    if (blockIdx.x == 0) {
+        if (nothing) {
+            if (tid == 0) *j.n_segs = 0;
+            if (j.row_begin)
+                for (uint32_t v = tid; v <= j.n_workers; v += kSortThreads) j.row_begin[v] = 0;
+        }
+        if (tid == 0) *j.n_long = 0;
     }
-    row_begin[w] = lo;
+    // the last block through leaves the barrier as it was
+    if (j.n_blocks > 1 && tid == 0 && atomicAdd(j.barrier + 1, 1u) == j.n_blocks - 1) {
+        j.barrier[0] = 0;
+        j.barrier[1] = 0;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- sums
 
 struct Sums {
-    const uint32_t *pos, *seg_begin, *seg_key, *n_segs;
+    const uint32_t *key, *pos, *seg_begin, *seg_key, *chunk_seg, *n_segs;
+    uint32_t n, n_chunks, chunk_shift;
+    uint32_t tiles;                 // blocks along a row
+    uint32_t sum_blocks;            // the blocks behind them write zeros
+    uint32_t* n_long;
+    float* partial;
+    const int* status;
     Rows grad;
     uint32_t dim, vocab;
     float scale;
@@ -253,73 +379,276 @@ struct Sums {
     // dense form
     int dense, accumulate;
     Rows out;
+    uint64_t zero_rows;             // rows to look at for zeros, zero_run of them per block
+    uint32_t zero_run;
+    int zero_vec;
 };
 
-template <typename A, typename B, int N>
-__global__ void __launch_bounds__(kThreads) k_embed_sums(const Sums p) {
-    const uint32_t n_segs = *p.n_segs;
-    for (uint32_t u = blockIdx.x * blockDim.y + threadIdx.y; u < n_segs; u += gridDim.x * blockDim.y) {
-        const uint32_t from = p.seg_begin[u], to = p.seg_begin[u + 1], key = p.seg_key[u];
-        if (p.rows_out && threadIdx.x == 0) p.rows_out[u] = key % p.vocab;
-        B* dst = p.dense ? reinterpret_cast<B*>(p.out.data) + p.out.offset(key)
-                         : reinterpret_cast<B*>(p.values) + static_cast<uint64_t>(u) * p.dim;
-        for (uint32_t c = threadIdx.x * N; c < p.dim; c += blockDim.x * N) {
-            float sum[N];
+constexpr int kUnroll = 4;
+constexpr uint32_t kMaxChunk = 64;
+constexpr uint64_t kEnds = 1ull << 63;          // flag of a token that is its segment's last
+
+// A finished sum goes to its row: `slot` counts segments, `at` is where the row starts in the dense table.
+template <typename B, int N>
+__device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t at, uint32_t row, uint32_t c, float (&sum)[N]) {
+    B* dst = p.dense ? reinterpret_cast<B*>(p.out.data) + at + c : reinterpret_cast<B*>(p.values) + static_cast<uint64_t>(slot) * p.dim + c;
 #pragma unroll
-            for (int j = 0; j < N; ++j) sum[j] = 0.f;
-            for (uint32_t i = from; i < to; ++i) {
-                const A* src = reinterpret_cast<const A*>(p.grad.data) + p.grad.offset(p.pos[i]) + c;
-                float f[N];
-                if constexpr (N > 1) {
-                    Packed<A, N> v;
-                    v.load(src);
-                    v.unpack(f);
-                } else {
-                    f[0] = to_float(*src);
-                }
+    for (int k = 0; k < N; ++k) sum[k] = __fmul_rn(sum[k], p.scale);
+    if constexpr (N > 1) {
+        Packed<B, N> q;
+        if (p.accumulate) {
+            float old[N];
 #pragma unroll
-                for (int j = 0; j < N; ++j) sum[j] = __fadd_rn(sum[j], f[j]);
-            }
+            for (int i = 0; i < Packed<B, N>::kVecs; ++i) q.v[i] = reinterpret_cast<const uint4*>(dst)[i];
+            q.unpack(old);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                sum[j] = __fmul_rn(sum[j], p.scale);
-                if (p.accumulate) sum[j] = __fadd_rn(sum[j], to_float(dst[c + j]));
-                dst[c + j] = from_float<B>(sum[j]);
-                if (p.idx_out) p.idx_out[static_cast<uint64_t>(u) * p.dim + c + j] = p.idx_offset + (key % p.vocab) * p.dim + c + j;
-            }
+            for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], old[k]);
+        }
+        q.pack(sum);
+        q.store(dst);
+    } else {
+        if (p.accumulate) sum[0] = __fadd_rn(sum[0], to_float(*dst));
+        *dst = from_float<B>(sum[0]);
+    }
+    if (p.idx_out) {
+        uint32_t* idx = p.idx_out + static_cast<uint64_t>(slot) * p.dim + c;
+        const uint32_t first = p.idx_offset + row * p.dim + c;
+        if constexpr (N > 1) {
+#pragma unroll
+            for (int k = 0; k < N; k += 4) *reinterpret_cast<uint4*>(idx + k) = make_uint4(first + k, first + k + 1, first + k + 2, first + k + 3);
+        } else {
+            *idx = first;
         }
     }
 }
 
-template <typename B>
-__global__ void __launch_bounds__(kThreads) k_embed_zero(Rows out, uint32_t n_rows, uint32_t dim) {
-    for (uint32_t r = blockIdx.x; r < n_rows; r += gridDim.x)
-        for (uint32_t c = threadIdx.x; c < dim; c += kThreads)
-            reinterpret_cast<B*>(out.data)[out.offset(r) + c] = from_float<B>(0.f);
+// Rows without a token, a run of them per block: which of them have one is looked up in the sorted list.
+__device__ void zero_gaps(const Sums& p, uint32_t block) {
+    __shared__ uint32_t s_has[kMaxChunk / 32];
+    const uint32_t n_segs = *p.n_segs;
+    const uint64_t from = static_cast<uint64_t>(block) * p.zero_run;
+    const uint64_t to = from + p.zero_run < p.zero_rows ? from + p.zero_run : p.zero_rows;
+    const uint32_t tid = threadIdx.y * blockDim.x + threadIdx.x, n_threads = blockDim.x * blockDim.y;
+    if (tid < kMaxChunk / 32) s_has[tid] = 0;
+    uint32_t lo = 0, hi = n_segs;               // first segment whose key is not below `from`
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (p.seg_key[mid] < from) lo = mid + 1; else hi = mid;
+    }
+    __syncthreads();
+    for (uint32_t k = tid; k < p.zero_run && lo + k < n_segs; k += n_threads) {
+        const uint64_t r = p.seg_key[lo + k];
+        if (r < to) atomicOr(&s_has[(r - from) / 32], 1u << ((r - from) & 31));
+    }
+    __syncthreads();
+    for (uint64_t r = from; r < to; ++r) {
+        if (s_has[(r - from) / 32] >> ((r - from) & 31) & 1) continue;
+        const uint64_t at = p.out.offset(static_cast<uint32_t>(r));
+        const uint32_t size = p.out.type == ADACOMP_F32 ? 4u : 2u;
+        char* dst = p.out.data + at * size;
+        if (p.zero_vec) {
+            for (uint32_t c = tid; c < p.dim * size / 16; c += n_threads) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+        } else if (size == 4) {
+            for (uint32_t c = tid; c < p.dim; c += n_threads) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
+        } else {
+            for (uint32_t c = tid; c < p.dim; c += n_threads) reinterpret_cast<uint16_t*>(dst)[c] = 0;
+        }
+    }
+}
+
+// Sums over the sorted list, cut into chunks of 2^chunk_shift tokens.  A chunk owns the segments that begin in it, to their
+// end even if that lies in the next chunk; a segment longer than a chunk is cut at the chunks' borders, its pieces are
+// added up by k_embed_join.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
+// depends on the tokens alone.  A thread keeps N columns; x runs along the row, y over chunks.
+template <typename A, typename B, int N>
+__global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
+    extern __shared__ uint64_t s_mem[];
+    if (*p.status == ADACOMP_ERR_TIMEOUT) return;           // the sort gave up: its lists are not to be followed
+    if (blockIdx.x >= p.sum_blocks) {
+        zero_gaps(p, blockIdx.x - p.sum_blocks);
+        return;
+    }
+    const uint32_t size = 1u << p.chunk_shift;
+    uint64_t* s_src = s_mem + static_cast<size_t>(threadIdx.y) * (3 * size);    // [2 size] where the rows of the chunk's tokens start
+    uint64_t* s_dst = s_src + 2 * size;                                         // [size] where its segments' rows start
+    const uint32_t chunk = blockIdx.x / p.tiles * blockDim.y + threadIdx.y, tile = blockIdx.x % p.tiles;
+    const uint32_t n_segs = *p.n_segs;
+    const uint32_t live = n_segs ? p.seg_begin[n_segs] : 0;
+    const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
+    uint32_t a = 0, b = 0, u0 = 0, u1 = 0;
+    bool lead = false, trail = false;
+    const uint64_t i0 = static_cast<uint64_t>(chunk) << p.chunk_shift;
+    if (i0 < live) {
+        const uint32_t i1 = static_cast<uint32_t>(i0 + size < live ? i0 + size : live);
+        u0 = p.chunk_seg[chunk];
+        u1 = i0 + size < live ? p.chunk_seg[chunk + 1] : n_segs;
+        const uint32_t first = p.seg_begin[u0];             // of the segments that begin here (or the end of the list)
+        if (first > i0) lead = first - p.seg_begin[u0 - 1] > size;
+        a = lead ? static_cast<uint32_t>(i0) : first;
+        if (u1 > u0) {
+            const uint32_t end = p.seg_begin[u1];
+            trail = end - p.seg_begin[u1 - 1] > size;
+            b = trail ? i1 : end;
+        } else {
+            b = lead ? i1 : a;
+        }
+        if (lead && u1 == u0 && first < i1) b = first;
+    }
+    for (uint32_t k = threadIdx.x; k < b - a; k += blockDim.x) {
+        const uint32_t i = a + k;
+        const bool ends = i + 1 >= live || p.key[i] != p.key[i + 1];
+        s_src[k] = p.grad.offset(p.pos[i]) | (ends ? kEnds : 0ull);
+    }
+    for (uint32_t k = threadIdx.x; k < u1 - u0; k += blockDim.x) {
+        const uint32_t key = p.seg_key[u0 + k];
+        s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
+        if (p.rows_out && tile == 0) p.rows_out[u0 + k] = key % p.vocab;
+    }
+    if (trail && tile == 0 && threadIdx.x == 0) p.n_long[1 + atomicAdd(p.n_long, 1u)] = chunk;
+    __syncthreads();
+    if (c >= p.dim) return;
+    float sum[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    uint32_t slot = lead ? u0 - 1 : u0;
+    const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
+    const uint32_t len = b - a;
+    bool open = false;
+    for (uint32_t i = 0; i < len; i += kUnroll) {
+        float f[kUnroll][N];
+        uint64_t src[kUnroll];
+        if constexpr (N > 1) {
+            Packed<A, N> v[kUnroll];
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                src[k] = i + k < len ? s_src[i + k] : 0ull;
+                if (i + k < len) v[k].load(grad + (src[k] & ~kEnds));
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) v[k].unpack(f[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                src[k] = i + k < len ? s_src[i + k] : 0ull;
+                if (i + k < len) f[k][0] = to_float(grad[src[k] & ~kEnds]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+            if (i + k >= len) break;
+#pragma unroll
+            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[k][q]);
+            open = true;
+            if (src[k] & kEnds) {
+                if (slot + 1 == u0) {           // the last piece of a long segment
+#pragma unroll
+                    for (int q = 0; q < N; ++q) p.partial[static_cast<uint64_t>(chunk) * 2 * p.dim + c + q] = sum[q];
+                } else {
+                    const uint64_t at = s_dst[slot - u0];
+                    put_row<B, N>(p, slot, at, static_cast<uint32_t>(at), c, sum);
+                }
+#pragma unroll
+                for (int q = 0; q < N; ++q) sum[q] = 0.f;
+                ++slot;
+                open = false;
+            }
+        }
+    }
+    if (open) {                                 // a piece that goes on in the next chunk
+        float* dst = p.partial + (static_cast<uint64_t>(chunk) * 2 + (slot + 1 == u0 ? 0 : 1)) * p.dim + c;
+#pragma unroll
+        for (int q = 0; q < N; ++q) dst[q] = sum[q];
+    }
+}
+
+// The long segments: their pieces, in order.  Eight lanes of the block (y) take every eighth piece each.
+constexpr int kJoinLanes = 8;
+template <typename B, int N>
+__global__ void __launch_bounds__(32 * kJoinLanes) k_embed_join(const Sums p) {
+    __shared__ float s_sum[kJoinLanes][32 * N];
+    if (*p.status == ADACOMP_ERR_TIMEOUT) return;
+    const uint32_t n_long = p.n_long[0], n_segs = *p.n_segs;
+    const uint32_t tiles = (p.dim + 32 * N - 1) / (32 * N);
+    const uint32_t live = n_segs ? p.seg_begin[n_segs] : 0;
+    for (uint64_t job = blockIdx.x; job < static_cast<uint64_t>(n_long) * tiles; job += gridDim.x) {
+        const uint32_t chunk = p.n_long[1 + job / tiles], c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N;
+        const uint64_t next = static_cast<uint64_t>(chunk + 1) << p.chunk_shift;
+        const uint32_t u = (next < live ? p.chunk_seg[chunk + 1] : n_segs) - 1;
+        const uint32_t pieces = ((p.seg_begin[u + 1] - 1) >> p.chunk_shift) - chunk + 1, key = p.seg_key[u];
+        float sum[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum[k] = 0.f;
+        if (c < p.dim) {
+            for (uint32_t q = threadIdx.y; q < pieces; q += kJoinLanes) {
+                const float* src = p.partial + (static_cast<uint64_t>(chunk + q) * 2 + (q == 0 ? 1 : 0)) * p.dim + c;
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], src[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < N; ++k) s_sum[threadIdx.y][threadIdx.x * N + k] = sum[k];
+        __syncthreads();
+        if (threadIdx.y == 0 && c < p.dim) {
+            for (int y = 1; y < kJoinLanes; ++y)
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], s_sum[y][threadIdx.x * N + k]);
+            put_row<B, N>(p, u, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
+        }
+        __syncthreads();
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- host
 
-size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens) {
-    Carver c(ws);
-    const size_t n = max_tokens, tiles = (n + kTile - 1) / kTile;
-    int* status = c.take<int>(1);
-    uint32_t* n_segs = c.take<uint32_t>(1);
-    uint32_t* list[6] = {};
-    if (n) {
-        for (int i = 0; i < 4; ++i) list[i] = c.take<uint32_t>(n);
-        list[4] = c.take<uint32_t>(n + 1);
-        list[5] = c.take<uint32_t>(n);
+// Tokens per chunk: long enough to keep the pieces of long segments rare, short enough that all SMs have work.
+uint32_t chunk_shift_of(uint64_t n, uint32_t dim) {
+    uint32_t shift = 3;
+    while (shift < 6 && (n * dim >> (21 + shift)) > 0) ++shift;
+    return shift;
+}
+
+// Chunks of the largest call: calls of fewer tokens may have shorter, and so more, chunks.
+uint64_t max_chunks(uint64_t max_tokens, uint32_t dim) {
+    uint64_t most = 0;
+    for (uint32_t shift = 3; shift <= 6; ++shift) {
+        uint64_t n = shift < 6 ? ((1ull << (21 + shift)) - 1) / dim : max_tokens;      // the most tokens with such chunks
+        if (n > max_tokens) n = max_tokens;
+        if (chunk_shift_of(n, dim) == shift && (n >> shift) + 1 > most) most = (n >> shift) + 1;
     }
-    uint32_t* table = n ? c.take<uint32_t>(tiles * kBins) : nullptr;
+    return most;
+}
+
+size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
+    Carver c(ws);
+    const size_t n = max_tokens ? max_tokens : 1, chunks = max_chunks(n, dim);
+    adacomp_embed_t e = {};
+    e.d_status = c.take<int>(1);
+    e.d_n_segs = c.take<uint32_t>(1);
+    e.d_barrier = c.take<uint32_t>(2);
+    for (int i = 0; i < 2; ++i) {
+        e.d_key[i] = c.take<uint32_t>(n);
+        e.d_pos[i] = c.take<uint32_t>(n);
+    }
+    e.d_table = c.take<uint32_t>(static_cast<size_t>(kSortBlocks) * kMaxBins);
+    e.d_seg_begin = c.take<uint32_t>(n + 1);
+    e.d_seg_key = c.take<uint32_t>(n);
+    e.d_chunk_seg = c.take<uint32_t>(chunks + 1);
+    e.d_long = c.take<uint32_t>(chunks + 1);
+    e.d_partial = c.take<float>(chunks * 2 * dim);
     if (h) {
-        h->d_status = status;
-        h->d_n_segs = n_segs;
-        h->d_key[0] = list[0]; h->d_key[1] = list[1];
-        h->d_pos[0] = list[2]; h->d_pos[1] = list[3];
-        h->d_seg_begin = list[4];
-        h->d_seg_key = list[5];
-        h->d_table = table;
+        h->d_status = e.d_status;
+        h->d_n_segs = e.d_n_segs;
+        h->d_barrier = e.d_barrier;
+        for (int i = 0; i < 2; ++i) {
+            h->d_key[i] = e.d_key[i];
+            h->d_pos[i] = e.d_pos[i];
+        }
+        h->d_table = e.d_table;
+        h->d_seg_begin = e.d_seg_begin;
+        h->d_seg_key = e.d_seg_key;
+        h->d_chunk_seg = e.d_chunk_seg;
+        h->d_long = e.d_long;
+        h->d_partial = e.d_partial;
     }
     return c.used;
 }
@@ -381,19 +710,47 @@ int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32
     return ADACOMP_OK;
 }
 
-template <typename A, typename B>
-int launch_sums(const Sums& p, uint32_t n, bool out_vec, uint32_t n_out_rows, cudaStream_t stream) {
-    constexpr int N = kItemElems<A, B>;
-    if (p.dense && !p.accumulate) {
-        k_embed_zero<B><<<n_out_rows < 2048 ? n_out_rows : 2048, kThreads, 0, stream>>>(p.out, n_out_rows, p.dim);
-        ADACOMP_LAUNCH_CHECK();
+// Threads of a sum's block along a row of `cols` threads' worth of work, chunks of a block, and blocks along the row.
+void along_row(uint32_t cols, uint32_t chunk_bytes, uint32_t* x, uint32_t* y, uint32_t* tiles) {
+    if (cols <= 16) {
+        *x = 1;
+        while (*x < cols) *x *= 2;
+        *tiles = 1;
+    } else {
+        *tiles = (cols + 511) / 512;
+        *x = ((cols + *tiles - 1) / *tiles + 31) / 32 * 32;
     }
-    if (n == 0) return ADACOMP_OK;
+    *y = *x >= 256 ? 1 : 256 / *x;
+    while (*y > 1 && *y * chunk_bytes > 32 * 1024) *y /= 2;
+}
+
+template <typename A, typename B>
+int launch_sums(Sums p, bool out_vec, bool gaps, const adacomp_embed_t* h, cudaStream_t stream) {
+    constexpr int N = kItemElems<A, B>;
     const bool vec = p.dim % N == 0 && on_grid(p.grad) && out_vec;
-    const uint32_t x = threads_along(p.dim, vec ? N : 1), y = kThreads / x;
-    const dim3 grid((n + y - 1) / y), block(x, y);
-    if (vec) k_embed_sums<A, B, N><<<grid, block, 0, stream>>>(p);
-    else k_embed_sums<A, B, 1><<<grid, block, 0, stream>>>(p);
+    const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
+    uint32_t x, y;
+    along_row((p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), chunk_bytes, &x, &y, &p.tiles);
+    p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
+    uint32_t zero_blocks = 0;
+    if (gaps) {
+        const uint32_t size = type_size(p.out.type);
+        p.zero_run = 1;
+        while (p.zero_run < kMaxChunk && static_cast<uint64_t>(p.zero_run) * p.dim * size < 32768) p.zero_run *= 2;
+        p.zero_vec = on_grid(p.out) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
+        zero_blocks = static_cast<uint32_t>((p.zero_rows + p.zero_run - 1) / p.zero_run);
+    }
+    if (p.sum_blocks + zero_blocks == 0) return ADACOMP_OK;
+    const dim3 block(x, y);
+    if (vec) k_embed_sums<A, B, N><<<p.sum_blocks + zero_blocks, block, y * chunk_bytes, stream>>>(p);
+    else k_embed_sums<A, B, 1><<<p.sum_blocks + zero_blocks, block, y * chunk_bytes, stream>>>(p);
+    ADACOMP_LAUNCH_CHECK();
+    if (p.n_chunks < 2) return ADACOMP_OK;              // no segment is longer than a chunk
+    const dim3 lanes(32, kJoinLanes);
+    const uint32_t grid = 4 * static_cast<uint32_t>(h->n_sms);
+    constexpr int kWide = 16 / sizeof(B);
+    if (out_vec && p.dim % kWide == 0) k_embed_join<B, kWide><<<grid, lanes, 0, stream>>>(p);
+    else k_embed_join<B, 1><<<grid, lanes, 0, stream>>>(p);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
@@ -414,33 +771,78 @@ int launch_sums(const Sums& p, uint32_t n, bool out_vec, uint32_t n_out_rows, cu
         }                                                                                                       \
     }()
 
-// Sorts the call's tokens and finds the segments; returns which of the two buffers holds the sorted list.
-int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens, uint32_t n_workers, cudaStream_t stream, int* in) {
-    const uint32_t n = n_tokens * n_workers, none = n_workers * h->vocab, tiles = (n + kTile - 1) / kTile;
-    *in = 0;
-    if (n == 0) {
-        ADACOMP_CUDA(cudaMemsetAsync(h->d_n_segs, 0, sizeof(uint32_t), stream));
-        return ADACOMP_OK;
+// Sorts the call's tokens and finds the segments; fills in what the sums read.  zero: rows to clear on the side, or null.
+int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens, uint32_t n_workers, uint64_t* d_row_begin,
+                const Rows* zero, uint64_t zero_rows, cudaStream_t stream, Sums* p) {
+    SortJob j = {};
+    j.tokens = tokens;
+    j.n = n_tokens * n_workers;
+    j.n_tokens = n_tokens;
+    j.n_workers = n_workers;
+    j.vocab = h->vocab;
+    j.padding = h->padding;
+    j.none = n_workers * h->vocab;
+    j.n_blocks = 1;
+    if (j.n > kOneBlock) {
+        j.n_blocks = (j.n + 2047) / 2048;
+        if (j.n_blocks > kSortBlocks) j.n_blocks = kSortBlocks;
     }
-    k_embed_keys<<<(n + kThreads - 1) / kThreads, kThreads, 0, stream>>>(tokens, n, n_tokens, h->vocab, h->padding, none, h->d_key[0],
-                                                                         h->d_pos[0], h->d_status);
-    ADACOMP_LAUNCH_CHECK();
-    for (int shift = 0; shift < 32 && (none >> shift) != 0; shift += 8) {
-        k_radix_count<<<tiles, kThreads, 0, stream>>>(h->d_key[*in], n, shift, h->d_table);
-        ADACOMP_LAUNCH_CHECK();
-        k_running_total<<<1, 1024, 0, stream>>>(h->d_table, tiles * kBins, nullptr);
-        ADACOMP_LAUNCH_CHECK();
-        k_radix_scatter<<<tiles, kThreads, 0, stream>>>(h->d_key[*in], h->d_pos[*in], n, shift, h->d_table, h->d_key[*in ^ 1],
-                                                        h->d_pos[*in ^ 1]);
-        ADACOMP_LAUNCH_CHECK();
-        *in ^= 1;
+    const uint32_t unit = (j.n + j.n_blocks - 1) / j.n_blocks > kStep ? kStep : kSortThreads;
+    j.per_block = ((j.n + j.n_blocks - 1) / j.n_blocks + unit - 1) / unit * unit;
+    if (j.per_block == 0) j.per_block = kSortThreads;
+    int bits = 0;
+    while (bits < 32 && (j.none >> bits) != 0) ++bits;
+    j.passes = (bits + kDigitBits - 1) / kDigitBits;
+    j.bits = (bits + j.passes - 1) / j.passes;
+    for (int i = 0; i < 2; ++i) {
+        j.key[i] = h->d_key[i];
+        j.pos[i] = h->d_pos[i];
     }
-    k_heads_count<<<tiles, kThreads, 0, stream>>>(h->d_key[*in], n, none, h->d_table);
+    j.table = h->d_table;
+    j.seg_begin = h->d_seg_begin;
+    j.seg_key = h->d_seg_key;
+    j.n_segs = h->d_n_segs;
+    j.chunk_seg = h->d_chunk_seg;
+    j.n_long = h->d_long;
+    j.chunk_shift = chunk_shift_of(j.n, h->dim);
+    j.row_begin = d_row_begin;
+    j.barrier = h->d_barrier;
+    j.status = h->d_status;
+    uint32_t grid = j.n_blocks;
+    if (zero) {
+        j.zero = *zero;
+        j.zero_rows = zero_rows;
+        j.dim = h->dim;
+        j.zero_vec = on_grid(*zero) && static_cast<uint64_t>(h->dim) * type_size(zero->type) % 16 == 0;
+        const uint64_t spare = static_cast<uint32_t>(h->n_sms) > grid ? static_cast<uint32_t>(h->n_sms) - grid : 1;
+        grid += static_cast<uint32_t>(zero_rows < spare ? zero_rows : spare);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = j.n_blocks > 1 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_embed_sort, j);
+    if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
-    k_running_total<<<1, 1024, 0, stream>>>(h->d_table, tiles, h->d_n_segs);
-    ADACOMP_LAUNCH_CHECK();
-    k_heads_emit<<<tiles, 1024, 0, stream>>>(h->d_key[*in], n, none, h->d_table, h->d_seg_begin, h->d_seg_key, h->d_n_segs);
-    ADACOMP_LAUNCH_CHECK();
+    p->key = j.key[(j.passes - 1) & 1];
+    p->pos = j.pos[(j.passes - 1) & 1];
+    p->seg_begin = j.seg_begin;
+    p->seg_key = j.seg_key;
+    p->chunk_seg = j.chunk_seg;
+    p->n_segs = j.n_segs;
+    p->n = j.n;
+    p->chunk_shift = j.chunk_shift;
+    p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
+    p->n_long = h->d_long;
+    p->partial = h->d_partial;
+    p->status = h->d_status;
+    p->dim = h->dim;
+    p->vocab = h->vocab;
     return ADACOMP_OK;
 }
 
@@ -458,7 +860,7 @@ int adacomp_embed_workspace_bytes(uint32_t vocab, uint32_t dim, uint32_t max_tok
     if (!bytes_out) return ADACOMP_ERR_INVALID;
     const int rc = check_limits(vocab, dim, max_tokens, max_workers);
     if (rc != ADACOMP_OK) return rc;
-    *bytes_out = carve(nullptr, nullptr, max_tokens);
+    *bytes_out = carve(nullptr, nullptr, max_tokens, dim);
     return ADACOMP_OK;
 }
 
@@ -479,11 +881,12 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     e->max_tokens = max_tokens;
     e->max_workers = max_workers;
     e->padding = padding_token;
-    carve(e, d_workspace, max_tokens);
+    carve(e, d_workspace, max_tokens, dim);
     DeviceGuard guard(device);
     cudaError_t err = guard.err;
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&e->n_sms, cudaDevAttrMultiProcessorCount, device);
     if (err == cudaSuccess) err = cudaMemset(e->d_status, 0, sizeof(int));
+    if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 2 * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaStreamSynchronize(nullptr);
     if (err != cudaSuccess) {
         delete e;
@@ -525,17 +928,8 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    int in = 0;
-    rc = sort_tokens(h, k, n_tokens, n_workers, stream, &in);
+    rc = sort_tokens(h, k, n_tokens, n_workers, d_row_begin_out, nullptr, 0, stream, &p);
     if (rc != ADACOMP_OK) return rc;
-    k_row_begin<<<(n_workers + 128) / 128, 128, 0, stream>>>(h->d_seg_key, h->d_n_segs, n_workers, h->vocab, d_row_begin_out);
-    ADACOMP_LAUNCH_CHECK();
-    p.pos = h->d_pos[in];
-    p.seg_begin = h->d_seg_begin;
-    p.seg_key = h->d_seg_key;
-    p.n_segs = h->d_n_segs;
-    p.dim = h->dim;
-    p.vocab = h->vocab;
     p.scale = scale;
     p.rows_out = d_rows_out;
     p.values = static_cast<char*>(d_values_out);
@@ -543,7 +937,7 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     p.idx_offset = static_cast<uint32_t>(idx_offset);
     const bool vec = reinterpret_cast<uintptr_t>(d_values_out) % 16 == 0 && static_cast<uint64_t>(h->dim) * type_size(values_type) % 16 == 0 &&
                      (!d_idx_out || (reinterpret_cast<uintptr_t>(d_idx_out) % 16 == 0 && h->dim % 4 == 0));
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, p, n, vec, 0, stream);
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, p, vec, false, h, stream);
 }
 
 int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens, uint32_t n_workers,
@@ -561,19 +955,17 @@ int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, u
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    int in = 0;
-    rc = sort_tokens(h, k, n_tokens, n_workers, stream, &in);
+    // Rows without a token become zeros.  Few tokens: everything is cleared by the SMs that do not sort, and some rows are
+    // written twice; many: the rows that need it are cleared next to the sums.
+    const uint64_t n_rows = static_cast<uint64_t>(n_workers) * h->vocab;
+    const bool early = !accumulate && n <= n_rows / 4;
+    rc = sort_tokens(h, k, n_tokens, n_workers, nullptr, early ? &p.out : nullptr, n_rows, stream, &p);
     if (rc != ADACOMP_OK) return rc;
-    p.pos = h->d_pos[in];
-    p.seg_begin = h->d_seg_begin;
-    p.seg_key = h->d_seg_key;
-    p.n_segs = h->d_n_segs;
-    p.dim = h->dim;
-    p.vocab = h->vocab;
     p.scale = scale;
     p.dense = 1;
     p.accumulate = accumulate != 0;
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, p, n, on_grid(p.out), n_workers * h->vocab, stream);
+    p.zero_rows = n_rows;
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, p, on_grid(p.out), !accumulate && !early, h, stream);
 }
 
 int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {
@@ -585,6 +977,10 @@ int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {
     ADACOMP_CUDA(cudaMemcpyAsync(&status, h->d_status, sizeof(int), cudaMemcpyDeviceToHost, stream));
     ADACOMP_CUDA(cudaMemsetAsync(h->d_status, 0, sizeof(int), stream));
     ADACOMP_CUDA(cudaStreamSynchronize(stream));
+    if (status == ADACOMP_ERR_TIMEOUT) {                            // blocks that gave up left the barrier anywhere
+        ADACOMP_CUDA(cudaMemsetAsync(h->d_barrier, 0, 2 * sizeof(uint32_t), stream));
+        ADACOMP_CUDA(cudaStreamSynchronize(stream));
+    }
     return status;
 }
 
