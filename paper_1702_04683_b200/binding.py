@@ -494,11 +494,16 @@ def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.T
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _element_type(t: torch.Tensor, device: torch.device, name: str) -> int:
+def _element_type(t: torch.Tensor, device: int, name: str) -> int:
     kind = ELEMENT_TYPES.get(t.dtype)
-    if kind is None or t.device != device:
-        raise TypeError(f"{name}: need a float32, bfloat16 or float16 tensor on {device}")
+    if kind is None or t.get_device() != device:
+        raise TypeError(f"{name}: need a float32, bfloat16 or float16 tensor on cuda:{device}")
     return kind
+
+
+def _stream_on(stream: Optional[torch.cuda.Stream], device: int) -> int:
+    """The given stream, or the device's current one (asked for without building a stream object, which costs as much as a launch)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def _is_dense(t: torch.Tensor) -> bool:
@@ -525,8 +530,8 @@ class GradList:
             raise ValueError("grads: need at least one tensor")
         if len(self.out) != len(self.grads):
             raise ValueError("out: need one tensor for each gradient")
-        self.device = self.grads[0].device
-        if self.device.type != "cuda":
+        self.device = self.grads[0].get_device()
+        if self.device < 0:
             raise TypeError("grads: need CUDA tensors")
         self.table = (GradTensor * len(self.grads))()
         spans = []                              # (begin, end, written)
@@ -561,6 +566,7 @@ class Clipper:
         self.device = torch.device(device if device is not None else "cuda")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.max_workers = int(max_workers)
         nbytes = ctypes.c_size_t(0)
         _check(_lib.adacomp_clip_workspace_bytes(self.max_workers, ctypes.byref(nbytes)), "adacomp_clip_workspace_bytes")
@@ -577,12 +583,12 @@ class Clipper:
         elif out is not None and isinstance(grads, GradList):
             raise ValueError("out: the list already says where its outputs go")
         if isinstance(grads, GradList):
-            if grads.device != self.device:
+            if grads.device != self._index:
                 raise TypeError(f"grads: need tensors on {self.device}")
             return grads.table, len(grads.grads), 1, 0, 0, grads.out
         out = grads if out is None else out
         e = GradTensor()
-        e.grad_type, e.out_type = _element_type(grads, self.device, "grads"), _element_type(out, self.device, "out")
+        e.grad_type, e.out_type = _element_type(grads, self._index, "grads"), _element_type(out, self._index, "out")
         if grads.dim() != 2 or out.shape != grads.shape:
             raise ValueError("grads: need a matrix [workers, entries], and out of the same shape")
         W, n = grads.shape
@@ -606,7 +612,7 @@ class Clipper:
         elif norm_out.numel() != W:
             raise ValueError("norm_out: need one entry per worker")
         _check(_lib.adacomp_grad_norm(self._h, table, count, stride, W, float(scale), _dev(norm_out, torch.float32, "norm_out"),
-                                      _stream_ptr(stream)), "adacomp_grad_norm")
+                                      _stream_on(stream, self._index)), "adacomp_grad_norm")
         return norm_out
 
     def clip(self, grads, max_norm: float, scale: float = 1.0, out=None, norm_out: Optional[torch.Tensor] = None,
@@ -622,7 +628,7 @@ class Clipper:
         _check(_lib.adacomp_clip(self._h, table, count, stride, out_stride, W, float(scale), float(max_norm),
                                  _dev(norm_out, torch.float32, "norm_out"),
                                  _dev(coef_out, torch.float32, "coef_out") if coef_out is not None else None,
-                                 _stream_ptr(stream)), "adacomp_clip")
+                                 _stream_on(stream, self._index)), "adacomp_clip")
         return out, norm_out
 
     def close(self):
@@ -641,15 +647,14 @@ class Clipper:
 
 def _rows(t: torch.Tensor, dims: int, kind: int, name: str) -> Rows:
     """The first `dims` dimensions of a tensor as the numbering of its rows."""
-    r = Rows()
-    r.d_data, r.type = t.data_ptr(), kind
-    shape, strides = t.shape, t.stride()
+    shape = t.shape
     if t.is_contiguous():
         row = 1
         for n in shape[dims:]:
             row *= n
-        r.row_stride = row
-        return r
+        return Rows(t.data_ptr(), kind, 0, row, 0)
+    r = Rows(t.data_ptr(), kind)
+    strides = t.stride()
     merged = []                                 # [rows, distance], outermost first; neighbours that make one run are joined
     for n, st in zip(shape[:dims], strides[:dims]):
         if n == 1:
@@ -676,6 +681,7 @@ class Embedding:
         self.device = torch.device(device if device is not None else "cuda")
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
         self.vocab, self.dim, self.max_tokens, self.max_workers = int(vocab), int(dim), int(max_tokens), int(max_workers)
         if padding_idx is not None and not 0 <= padding_idx < self.vocab:
             raise ValueError("padding_idx: need a token of the vocabulary")
@@ -695,17 +701,22 @@ class Embedding:
 
     def _tokens(self, tokens: torch.Tensor) -> Rows:
         kind = TOKEN_TYPES.get(tokens.dtype)
-        if kind is None or tokens.device != self.device:
+        if kind is None or tokens.get_device() != self._index:
             raise TypeError(f"tokens: need an int32 or int64 tensor on {self.device}")
         if tokens.numel() >= 1 << 31:
             raise ValueError("tokens: too many")
         return _rows(tokens, tokens.dim(), kind, "tokens")
 
     def _wide(self, t: torch.Tensor, name: str) -> Rows:
-        kind = _element_type(t, self.device, name)
-        if t.dim() == 0 or t.shape[-1] != self.dim or (self.dim > 1 and t.stride(-1) != 1):
-            raise TypeError(f"{name}: need contiguous rows of {self.dim} entries")
-        return _rows(t, t.dim() - 1, kind, name)
+        kind = _element_type(t, self._index, name)
+        shape = t.shape
+        if not shape or shape[-1] != self.dim:
+            raise TypeError(f"{name}: need rows of {self.dim} entries")
+        if t.is_contiguous():
+            return Rows(t.data_ptr(), kind, 0, self.dim, 0)
+        if self.dim > 1 and t.stride(-1) != 1:
+            raise TypeError(f"{name}: need contiguous rows")
+        return _rows(t, len(shape) - 1, kind, name)
 
     def lookup(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
@@ -720,7 +731,7 @@ class Embedding:
         elif out.shape != shape or (dtype is not None and out.dtype != dtype):
             raise ValueError("out: need a row for every token, and the type asked for")
         _check(_lib.adacomp_embed_lookup(self._h, ctypes.byref(self._wide(table, "table")), ctypes.byref(ids), tokens.numel(),
-                                         float(scale), ctypes.byref(self._wide(out, "out")), _stream_ptr(stream)),
+                                         float(scale), ctypes.byref(self._wide(out, "out")), _stream_on(stream, self._index)),
                "adacomp_embed_lookup")
         return out
 
@@ -738,12 +749,12 @@ class Embedding:
             if t is not None and t.numel() < need:
                 raise ValueError(f"{name}: too small")
         begin = _empty((workers + 1,), torch.int64, self.device, stream)
-        kind = _element_type(values_out, self.device, "values_out")
+        kind = _element_type(values_out, self._index, "values_out")
         _check(_lib.adacomp_embed_grad_rows(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
                                             _dev(rows_out, torch.int32, "rows_out") if rows_out is not None else None,
                                             begin.data_ptr(), _dev(values_out, values_out.dtype, "values_out"), kind,
                                             _dev(idx_out, torch.int32, "idx_out") if idx_out is not None else None, int(offset),
-                                            _stream_ptr(stream)), "adacomp_embed_grad_rows")
+                                            _stream_on(stream, self._index)), "adacomp_embed_grad_rows")
         return begin
 
     def grad_rows(self, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, workers: int = 1,
@@ -787,13 +798,13 @@ class Embedding:
         if out.data_ptr() == grad.data_ptr() and grad.numel():
             raise ValueError("out: overlaps the gradient")
         _check(_lib.adacomp_embed_grad_dense(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
-                                             ctypes.byref(self._wide(out, "out")), int(accumulate), _stream_ptr(stream)),
+                                             ctypes.byref(self._wide(out, "out")), int(accumulate), _stream_on(stream, self._index)),
                "adacomp_embed_grad_dense")
         return out
 
     def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Waits for the stream; the first error the device recorded since the last call (a token outside the vocabulary)."""
-        return int(_lib.adacomp_embed_last_error(self._h, _stream_ptr(stream)))
+        return int(_lib.adacomp_embed_last_error(self._h, _stream_on(stream, self._index)))
 
     def close(self):
         if getattr(self, "_h", None):

@@ -3,8 +3,8 @@
 //   norm_w = |s| sqrt(sum_i g_i^2),   c_w = s min(1, max_norm / (norm_w + 1e-6)),   out_i = round(g_i c_w)
 //
 // Both kernels are one pass over the data (2 and 1 operations an entry): HBM bounds them.  The tensors of a call are cut
-// into units of 1024 vectors of 16 bytes; a block takes a run of consecutive units, so it looks a tensor up once and then walks on.
-// The second pass walks the same runs from the back: what the first pass read last is still in L2.
+// into units of some 16 KB; blocks take units in turn, so short tensors next to each other in the list go to different
+// blocks.  The second pass walks the units from the back: what the first pass read last is still in L2.
 #include <math.h>
 #include <new>
 #include <vector>
@@ -26,8 +26,16 @@ struct adacomp_clip {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVecsPerThread = 4;
+constexpr int kVecsPerThread = 8;
 constexpr uint32_t kUnit = kThreads * kVecsPerThread;       // vectors of 16 bytes (norm) or items (write) per unit
+// Blocks resident per SM.  Loads in flight count: 8 vectors a thread and 3 blocks read 6.4 GB in 866 us (7.4 TB/s), 4 and 6 in
+// 884, 4 and 8 in 937.
+constexpr int kNormBlocks = 3, kWriteBlocks = 4;
+constexpr uint32_t kMaxBlocks = 1024;                       // partial sums per worker the workspace has room for
+// Gradients up to this many bytes: what the second pass reads and writes is given up first by L2, so that what the first pass
+// read stays until it is read again.  Measured, both passes: 102 MB of fp32 57.2 -> 53.3 us, 52 MB of fp16 44.5 -> 40.2 us;
+// but 683 MB of bf16 464 -> 471 us, where little of it can stay anyway.
+constexpr uint64_t kKeepInL2 = 160ull << 20;
 constexpr double kEps = 1e-6;
 
 struct Tensor {
@@ -51,6 +59,7 @@ struct Job {
     float scale;
     float max_norm;
     int first, last;                // of the call's launches
+    int give_up_first;              // the second pass's lines in L2
     uint32_t n_blocks;
     double* partial;
     uint32_t* done;
@@ -59,15 +68,29 @@ struct Job {
     float* coef_out;
 };
 
-// Position of a unit: the last tensor whose first unit is not behind it.
-template <int MAX> __device__ __forceinline__ uint32_t find_tensor(const Table<MAX>& tab, uint32_t n, uint32_t unit) {
-    uint32_t lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (tab.t[mid].first_unit <= unit) lo = mid; else hi = mid;
+// The table's copy in shared memory, and the tensor of a unit: the last one whose first unit is not behind it.  A warp looks
+// it up in two steps of 32 entries each (a list has at most 960).
+struct Lookup {
+    const Tensor* t;
+    uint32_t n, stride;
+    template <int MAX> __device__ __forceinline__ Lookup(const Table<MAX>& tab, uint32_t count, Tensor* s_tab)
+        : t(s_tab), n(count), stride((count + 31) / 32) {
+        const uint4* src = reinterpret_cast<const uint4*>(tab.t);
+        // read through a generic address, a thread an entry: as constant loads with an index they would go one by one (161
+        // tensors: 25.4 -> 20.4 us for 102 MB)
+        asm volatile("" : "+l"(src));
+        for (uint32_t k = threadIdx.x; k < 2 * n; k += kThreads) reinterpret_cast<uint4*>(s_tab)[k] = src[k];
+        __syncthreads();
     }
-    return lo;
-}
+    __device__ __forceinline__ const Tensor& of(uint32_t unit) const {
+        const uint32_t lane = threadIdx.x & 31;
+        const uint32_t a = lane * stride;
+        const uint32_t run = __popc(__ballot_sync(0xFFFFFFFFu, a < n && t[a].first_unit <= unit)) - 1;
+        const uint32_t b = run * stride + lane;
+        const uint32_t in = __popc(__ballot_sync(0xFFFFFFFFu, lane < stride && b < n && t[b].first_unit <= unit)) - 1;
+        return t[run * stride + in];
+    }
+};
 
 __device__ __forceinline__ uint32_t or4(const uint4& v) { return v.x | v.y | v.z | v.w; }
 
@@ -122,10 +145,16 @@ template <typename T> __device__ __forceinline__ uint4 load_clamped(uintptr_t a,
 template <typename T>
 __device__ __forceinline__ double unit_squares(const char* base, uint64_t n, uint32_t unit) {
     const uintptr_t p = reinterpret_cast<uintptr_t>(base), end = p + n * sizeof(T);
-    const uintptr_t a = (p & ~static_cast<uintptr_t>(15)) + (static_cast<uint64_t>(unit) * kUnit + threadIdx.x) * 16;
+    const uintptr_t first = (p & ~static_cast<uintptr_t>(15)) + static_cast<uint64_t>(unit) * kUnit * 16;
+    const uintptr_t a = first + threadIdx.x * 16;
     uint4 v[kVecsPerThread];
+    if (first >= p && first + kUnit * 16 <= end) {
 #pragma unroll
-    for (int k = 0; k < kVecsPerThread; ++k) v[k] = load_clamped<T>(a + static_cast<uintptr_t>(k) * kThreads * 16, p, end);
+        for (int k = 0; k < kVecsPerThread; ++k) v[k] = load16(reinterpret_cast<const void*>(a + k * kThreads * 16));
+    } else {
+#pragma unroll
+        for (int k = 0; k < kVecsPerThread; ++k) v[k] = load_clamped<T>(a + k * kThreads * 16, p, end);
+    }
     return sum_squares<T>(v);
 }
 
@@ -142,17 +171,15 @@ __device__ __forceinline__ double block_sum(double x, double* s_warp) {
 }
 
 template <int MAX>
-__global__ void __launch_bounds__(kThreads) k_grad_norm(const __grid_constant__ Table<MAX> tab, const Job job) {
+__global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __grid_constant__ Table<MAX> tab, const Job job) {
     __shared__ double s_warp[kThreads / 32];
     __shared__ bool s_last;
+    extern __shared__ Tensor s_tab[];
     const uint32_t w = blockIdx.y, b = blockIdx.x;
-    const uint32_t from = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * b / job.n_blocks);
-    const uint32_t to = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * (b + 1) / job.n_blocks);
+    const Lookup tensors(tab, job.n_tensors, s_tab);
     double sum = 0.0;
-    uint32_t i = from < to ? find_tensor(tab, job.n_tensors, from) : 0;
-    for (uint32_t u = from; u < to; ++u) {
-        while (i + 1 < job.n_tensors && tab.t[i + 1].first_unit <= u) ++i;
-        const Tensor& t = tab.t[i];
+    for (uint32_t u = b; u < job.n_units; u += job.n_blocks) {
+        const Tensor& t = tensors.of(u);
         const char* base = t.in + w * job.in_stride * type_size(t.in_type);
         const uint32_t at = u - t.first_unit;
         if (t.in_type == ADACOMP_F32) sum += unit_squares<float>(base, t.n, at);
@@ -227,42 +254,47 @@ __device__ __forceinline__ Packed<A, N> load_shifted(const A* in, int64_t e, uin
 }
 
 template <typename A, typename B, int N>
-__device__ __forceinline__ void scale_store(const Packed<A, N>& p, B* out, float c) {
+__device__ __forceinline__ void scale_store(const Packed<A, N>& p, B* out, float c, uint64_t policy) {
     float f[N];
     p.unpack(f);
 #pragma unroll
     for (int j = 0; j < N; ++j) f[j] = __fmul_rn(f[j], c);
     Packed<B, N> q;
     q.pack(f);
-    q.store(out);
+    q.store_whole(out, policy);
 }
 
+// Entries per item of the second pass: 16 bytes of a 16-bit type, 32 of fp32.
+constexpr int kItem = 8;
+constexpr int kItemsPerThread = 4;
+constexpr uint32_t kWriteUnit = kThreads * kItemsPerThread;
+
 template <typename A, typename B>
-__device__ __forceinline__ void write_unit(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c) {
-    constexpr int N = kItemElems<A, B>;
+__device__ __forceinline__ void write_unit(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c, uint64_t policy) {
+    constexpr int N = kItem;
     const A* in = reinterpret_cast<const A*>(t.in) + w * job.in_stride;
     B* out = reinterpret_cast<B*>(t.out) + w * job.out_stride;
     const int64_t n = static_cast<int64_t>(t.n);
-    // items start on the output's 16-byte grid: item j holds entries [j N - skew, j N - skew + N)
-    const int64_t skew = static_cast<int64_t>((reinterpret_cast<uintptr_t>(out) & 15) / sizeof(B));
-    const int64_t unit_at = static_cast<int64_t>(unit) * kUnit * N - skew, e0 = unit_at + threadIdx.x * N;
-    const bool on_grid = (reinterpret_cast<uintptr_t>(in + e0) & 15) == 0;
-    if (on_grid && unit_at >= 0 && unit_at + static_cast<int64_t>(kUnit) * N <= n) {
-        Packed<A, N> p[kVecsPerThread];
+    // items start on the output's own grid: item j holds entries [j N - skew, j N - skew + N)
+    const int64_t skew = static_cast<int64_t>((reinterpret_cast<uintptr_t>(out) & (N * sizeof(B) - 1)) / sizeof(B));
+    const int64_t unit_at = static_cast<int64_t>(unit) * kWriteUnit * N - skew, e0 = unit_at + threadIdx.x * N;
+    const bool on_grid = (reinterpret_cast<uintptr_t>(in + e0) & (N * sizeof(A) - 1)) == 0;
+    if (on_grid && unit_at >= 0 && unit_at + static_cast<int64_t>(kWriteUnit) * N <= n) {
+        Packed<A, N> p[kItemsPerThread];
 #pragma unroll
-        for (int k = 0; k < kVecsPerThread; ++k) p[k].load(in + e0 + k * (kThreads * N));
+        for (int k = 0; k < kItemsPerThread; ++k) p[k].load_whole(in + e0 + k * (kThreads * N), policy);
 #pragma unroll
-        for (int k = 0; k < kVecsPerThread; ++k) scale_store<A, B, N>(p[k], out + e0 + k * (kThreads * N), c);
+        for (int k = 0; k < kItemsPerThread; ++k) scale_store<A, B, N>(p[k], out + e0 + k * (kThreads * N), c, policy);
         return;
     }
 #pragma unroll 1
-    for (int k = 0; k < kVecsPerThread; ++k) {
+    for (int k = 0; k < kItemsPerThread; ++k) {
         const int64_t e = e0 + k * (kThreads * N);
         if (e >= 0 && e + N <= n) {
             Packed<A, N> p;
-            if (on_grid) p.load(in + e);
+            if (on_grid) p.load_whole(in + e, policy);
             else p = load_shifted<A, N>(in, e, t.n);
-            scale_store<A, B, N>(p, out + e, c);
+            scale_store<A, B, N>(p, out + e, c, policy);
         } else {
 #pragma unroll 1
             for (int j = 0; j < N; ++j)
@@ -272,49 +304,53 @@ __device__ __forceinline__ void write_unit(const Tensor& t, uint32_t w, const Jo
 }
 
 template <typename A>
-__device__ __forceinline__ void write_unit_from(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c) {
-    if (t.out_type == ADACOMP_F32) write_unit<A, float>(t, w, job, unit, c);
-    else if (t.out_type == ADACOMP_BF16) write_unit<A, __nv_bfloat16>(t, w, job, unit, c);
-    else write_unit<A, __half>(t, w, job, unit, c);
+__device__ __forceinline__ void write_unit_from(const Tensor& t, uint32_t w, const Job& job, uint32_t unit, float c, uint64_t policy) {
+    if (t.out_type == ADACOMP_F32) write_unit<A, float>(t, w, job, unit, c, policy);
+    else if (t.out_type == ADACOMP_BF16) write_unit<A, __nv_bfloat16>(t, w, job, unit, c, policy);
+    else write_unit<A, __half>(t, w, job, unit, c, policy);
 }
 
 template <int MAX>
-__global__ void __launch_bounds__(kThreads) k_clip_write(const __grid_constant__ Table<MAX> tab, const Job job) {
+__global__ void __launch_bounds__(kThreads, kWriteBlocks) k_clip_write(const __grid_constant__ Table<MAX> tab, const Job job) {
+    extern __shared__ Tensor s_tab[];
     const uint32_t w = blockIdx.y, b = blockIdx.x;
-    const uint32_t from = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * b / job.n_blocks);
-    const uint32_t to = static_cast<uint32_t>(static_cast<uint64_t>(job.n_units) * (b + 1) / job.n_blocks);
-    if (from >= to) return;
+    const Lookup tensors(tab, job.n_tensors, s_tab);
+    const uint64_t policy = l2_policy(job.give_up_first != 0);
+    cudaGridDependencySynchronize();
     const float c = job.coef[w];
-    uint32_t i = find_tensor(tab, job.n_tensors, to - 1);
-    for (uint32_t u = to; u-- > from;) {
-        while (tab.t[i].first_unit > u) --i;
-        const Tensor& t = tab.t[i];
+    for (uint32_t k = b; k < job.n_units; k += job.n_blocks) {
+        const uint32_t u = job.n_units - 1 - k;
+        const Tensor& t = tensors.of(u);
         if (c == 1.0f && t.out == t.in) continue;           // in place, nothing to change
         const uint32_t at = u - t.first_unit;
-        if (t.in_type == ADACOMP_F32) write_unit_from<float>(t, w, job, at, c);
-        else if (t.in_type == ADACOMP_BF16) write_unit_from<__nv_bfloat16>(t, w, job, at, c);
-        else write_unit_from<__half>(t, w, job, at, c);
+        if (t.in_type == ADACOMP_F32) write_unit_from<float>(t, w, job, at, c, policy);
+        else if (t.in_type == ADACOMP_BF16) write_unit_from<__nv_bfloat16>(t, w, job, at, c, policy);
+        else write_unit_from<__half>(t, w, job, at, c, policy);
     }
 }
 
 // Units of a tensor: by its input's vectors (norm) or by its items on the output's grid (write), counted so that they
 // suffice wherever a worker's copy sits on the 16-byte grid.
 uint64_t units_of(const adacomp_grad_tensor_t& t, bool write) {
-    uint64_t vecs;
-    if (write) {
-        const uint64_t n_item = type_size(t.grad_type) == 4 && type_size(t.out_type) == 4 ? 4 : 8;
-        vecs = (t.n + 7 + n_item - 1) / n_item;
-    } else {
-        vecs = (t.n * type_size(t.grad_type) + 14 + 15) / 16;
-    }
-    return (vecs + kUnit - 1) / kUnit;
+    if (write) return (t.n + kItem - 1 + static_cast<uint64_t>(kWriteUnit) * kItem - 1) / (static_cast<uint64_t>(kWriteUnit) * kItem);
+    return (t.n * type_size(t.grad_type) + 14 + kUnit * 16 - 1) / (kUnit * 16);
 }
 
 template <int MAX>
 int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, bool write, cudaStream_t stream) {
-    const dim3 grid(job.n_blocks, n_workers);
-    if (write) k_clip_write<MAX><<<grid, kThreads, 0, stream>>>(tab, job);
-    else k_grad_norm<MAX><<<grid, kThreads, 0, stream>>>(tab, job);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(job.n_blocks, n_workers);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = job.n_tensors * sizeof(Tensor);
+    cfg.stream = stream;
+    // a write launch may start while the norm's last blocks finish: it waits for them itself
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = write ? 1 : 0;
+    const cudaError_t e = write ? cudaLaunchKernelEx(&cfg, k_clip_write<MAX>, tab, job) : cudaLaunchKernelEx(&cfg, k_grad_norm<MAX>, tab, job);
+    if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
@@ -379,7 +415,17 @@ int run_pass(const adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t 
     return ADACOMP_OK;
 }
 
-uint32_t blocks_per_worker(int n_sms) { return 6u * static_cast<uint32_t>(n_sms); }
+// Blocks of one worker: all of a call's are resident at once where there are not more workers than that, and none is
+// without work.
+uint32_t blocks_per_worker(const adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint32_t n_workers, bool write) {
+    uint64_t units = 0;
+    for (uint32_t i = 0; i < n_tensors; ++i)
+        if (ts[i].n) units += units_of(ts[i], write);
+    uint64_t blocks = static_cast<uint64_t>(write ? kWriteBlocks : kNormBlocks) * h->n_sms / n_workers;
+    if (blocks > units) blocks = units;
+    if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    return blocks < 1 ? 1 : static_cast<uint32_t>(blocks);
+}
 
 size_t carve(adacomp_clip_t* h, void* ws, uint32_t max_workers, uint32_t n_blocks) {
     Carver c(ws);
@@ -393,8 +439,6 @@ size_t carve(adacomp_clip_t* h, void* ws, uint32_t max_workers, uint32_t n_block
     }
     return c.used;
 }
-
-constexpr uint32_t kMaxBlocks = 1024;       // partial sums per worker the workspace has room for
 
 int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t in_stride, uint64_t out_stride,
         uint32_t n_workers, float scale, float max_norm, float* d_norm, float* d_coef_out, bool write, void* cuda_stream) {
@@ -410,10 +454,7 @@ int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, 
     job.out_stride = out_stride;
     job.scale = scale;
     job.max_norm = max_norm;
-    // all blocks of a call are resident at once where there are fewer workers than that
-    job.n_blocks = blocks_per_worker(h->n_sms) / n_workers;
-    if (job.n_blocks < 1) job.n_blocks = 1;
-    if (job.n_blocks > kMaxBlocks) job.n_blocks = kMaxBlocks;
+    job.n_blocks = blocks_per_worker(h, ts, n_tensors, n_workers, false);
     job.partial = h->d_partial;
     job.done = h->d_done;
     job.norm_out = d_norm;
@@ -421,6 +462,10 @@ int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, 
     job.coef_out = d_coef_out;
     rc = run_pass(h, ts, n_tensors, n_workers, job, false, stream);
     if (rc != ADACOMP_OK || !write) return rc;
+    job.n_blocks = blocks_per_worker(h, ts, n_tensors, n_workers, true);
+    uint64_t bytes = 0;
+    for (uint32_t i = 0; i < n_tensors; ++i) bytes += ts[i].n * type_size(ts[i].grad_type);
+    job.give_up_first = bytes * n_workers <= kKeepInL2;
     return run_pass(h, ts, n_tensors, n_workers, job, true, stream);
 }
 

@@ -52,6 +52,34 @@ __device__ __forceinline__ uint4 load16(const void* p) {
     return v;
 }
 
+// How a kernel's loads and stores want to be kept in L2: as usual, or given up first.
+__device__ __forceinline__ uint64_t l2_policy(bool give_up_first) {
+    uint64_t p;
+    if (give_up_first) asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    else asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+
+__device__ __forceinline__ uint4 load16(const void* p, uint64_t policy) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p), "l"(policy));
+    return v;
+}
+__device__ __forceinline__ void store16(void* p, const uint4& v, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;"
+                 :: "l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy) : "memory");
+}
+// 32-byte vectors, one instruction each (32-byte aligned).
+__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b, uint64_t policy) {
+    asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], %9;"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p), "l"(policy));
+}
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b, uint64_t policy) {
+    asm volatile("st.global.L2::cache_hint.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8}, %9;"
+                 :: "l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w), "l"(policy) : "memory");
+}
+
 // N elements (N * size a multiple of 16 bytes) between their packed form and fp32.
 template <typename T, int N> struct Packed {
     static constexpr int kVecs = N * static_cast<int>(sizeof(T)) / 16;
@@ -61,6 +89,15 @@ template <typename T, int N> struct Packed {
     __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) v[i] = load16(reinterpret_cast<const char*>(p) + 16 * i);
+    }
+    // The same for items on their own grid: 32-byte ones in one instruction.
+    __device__ __forceinline__ void load_whole(const T* p, uint64_t policy) {
+        if constexpr (kVecs == 2) load32(p, v[0], v[1], policy);
+        else v[0] = load16(p, policy);
+    }
+    __device__ __forceinline__ void store_whole(T* p, uint64_t policy) const {
+        if constexpr (kVecs == 2) store32(p, v[0], v[1], policy);
+        else store16(p, v[0], policy);
     }
     __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
