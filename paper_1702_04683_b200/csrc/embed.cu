@@ -6,6 +6,7 @@
 // The gradient sorts the pairs (worker * vocab + token, position), stable, so a row's summands stand together and in
 // order; every row is then summed by whoever owns it, without atomics.  All of it is bound by HBM (one fp32 addition per
 // entry read).
+#include <cooperative_groups.h>
 #include <math.h>
 #include <new>
 
@@ -25,8 +26,11 @@ struct adacomp_embed {
     uint32_t* d_seg_begin;          // [max_tokens + 1] first sorted token of every distinct one, and their end
     uint32_t* d_seg_key;            // [max_tokens]
     uint32_t* d_chunk_seg;          // [chunks + 1] how many segments begin before the chunk
-    uint32_t* d_n_segs;
-    uint32_t* d_long;               // how many segments are longer than a chunk, then the chunks they begin in
+    uint32_t* d_n_segs;             // [2] distinct tokens, and how many tokens of the sorted list have a gradient
+    uint32_t* d_n_long;             // [2] how many segments are longer than a chunk
+    uint4* d_long;                  // [chunks] those
+    uint32_t* d_order;              // [max_tokens] positions in the order of the sort
+    uint32_t cluster;               // blocks of the largest cluster that the device takes
     float* d_partial;               // [chunks][2][dim] sums of pieces of those
 };
 
@@ -37,10 +41,10 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kItems = 8;                                   // tokens per thread and step of the sort
 constexpr uint32_t kStep = kSortThreads * kItems;
-constexpr uint32_t kOneBlock = 8192;                        // up to here one block sorts alone
 constexpr uint32_t kSortBlocks = 64;
 constexpr int kDigitBits = 9;
 constexpr int kMaxBins = 1 << kDigitBits;
+constexpr uint32_t kClusterSmem = 2 * kStep * 4 + 16 * kMaxBins * 4 + kSortWarps * kMaxBins * 2;
 constexpr uint32_t kSpinLimit = 1u << 22;                   // polls of a barrier, some seconds
 
 // Device view of adacomp_rows_t.
@@ -110,17 +114,15 @@ struct SortJob {
     uint32_t* key[2];
     uint32_t* pos[2];
     uint32_t* table;
+    uint32_t *order;                                        // the sorted tokens' positions, kLast set where a segment ends
     uint32_t *seg_begin, *seg_key, *n_segs, *chunk_seg, *n_long;
     uint32_t chunk_shift;
+    uint32_t share_shift;                                   // cluster form: log2 of the tokens of a block
     uint64_t* row_begin;                                    // or null
     uint32_t* barrier;
     int* status;
-    // rows that become zeros before the sums are written (the blocks that do not sort)
-    Rows zero;
-    uint64_t zero_rows;
-    uint32_t dim;
-    int zero_vec;
 };
+constexpr uint32_t kLast = 1u << 31;
 
 // Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
 // does not, the block says so and the caller gives up.
@@ -162,35 +164,103 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s_warp, u
     return __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u) + upto - v;
 }
 
-template <typename B> __device__ __forceinline__ void zero_row(B* dst, uint32_t dim, bool vec) {
+__device__ __forceinline__ void zero_row(const Rows& out, uint64_t row, uint32_t dim, bool vec, uint32_t tid, uint32_t n_threads) {
+    const uint32_t size = type_size(out.type);
+    char* dst = out.data + out.offset(static_cast<uint32_t>(row)) * size;
     if (vec) {
-        const uint32_t n = dim * static_cast<uint32_t>(sizeof(B)) / 16;
-        for (uint32_t c = threadIdx.x; c < n; c += blockDim.x) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+        for (uint32_t c = tid; c < dim * size / 16; c += n_threads) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+    } else if (size == 4) {
+        for (uint32_t c = tid; c < dim; c += n_threads) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
     } else {
-        for (uint32_t c = threadIdx.x; c < dim; c += blockDim.x) dst[c] = from_float<B>(0.f);
+        for (uint32_t c = tid; c < dim; c += n_threads) reinterpret_cast<uint16_t*>(dst)[c] = 0;
     }
 }
-__device__ __forceinline__ void zero_row(const Rows& out, uint64_t row, uint32_t dim, bool vec) {
-    const uint64_t at = out.offset(static_cast<uint32_t>(row));
-    if (out.type == ADACOMP_F32) zero_row(reinterpret_cast<float*>(out.data) + at, dim, vec);
-    else zero_row(reinterpret_cast<__half*>(out.data) + at, dim, vec);      // the zeros of both 16-bit types are the same bits
+
+// Clears a table while the tokens are being sorted on other SMs.  It needs nothing of the sort, but the sums wait for this
+// kernel alone, so it ends after the sort.
+__global__ void __launch_bounds__(kThreads) k_embed_clear(Rows out, uint64_t n_rows, uint32_t dim, int vec) {
+    for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) zero_row(out, r, dim, vec != 0, threadIdx.x, kThreads);
+    cudaGridDependencySynchronize();
+}
+
+// Lanes of the warp that hold the same digit (of at most kDigitBits bits), among the real ones or among the others.
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool real) {
+    const uint32_t all = __ballot_sync(0xFFFFFFFFu, real);
+    uint32_t same = real ? all : ~all;
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
+        const uint32_t vote = __ballot_sync(0xFFFFFFFFu, (d >> b) & 1);
+        same &= (d >> b) & 1 ? vote : ~vote;
+    }
+    return same;
+}
+
+// Counts of digit `d` in the block's warps become the counts before each warp; returns their sum.
+__device__ __forceinline__ uint32_t counts_to_places(uint16_t* s_count, uint32_t bins, uint32_t d) {
+    uint32_t c[kSortWarps];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) c[w] = s_count[w * bins + d];
+    uint32_t sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        s_count[w * bins + d] = static_cast<uint16_t>(sum);
+        sum += c[w];
+    }
+    return sum;
+}
+
+// Sorted token i with key k between `last` and `next`, and its place in the lists that the sums read; `u` segments begin
+// before it.
+__device__ __forceinline__ void put_segment(const SortJob& j, uint64_t i, uint32_t k, uint32_t last, uint32_t next, uint32_t pos, bool head, uint32_t u) {
+    if ((i & ((1u << j.chunk_shift) - 1)) == 0) j.chunk_seg[i >> j.chunk_shift] = u;
+    j.order[i] = pos | (next != k ? kLast : 0u);
+    if (head) {
+        j.seg_begin[u] = static_cast<uint32_t>(i);
+        j.seg_key[u] = k;
+    }
+    const bool end = k != j.none && next == j.none;                        // the last token with a gradient
+    const uint32_t n_segs = u + head;
+    if (end) {
+        j.seg_begin[n_segs] = static_cast<uint32_t>(i) + 1;
+        j.n_segs[0] = n_segs;
+        j.n_segs[1] = static_cast<uint32_t>(i) + 1;
+    }
+    if (!j.row_begin || !(head || end)) return;
+    if (j.n_workers == 1) {
+        if (i == 0) j.row_begin[0] = 0;
+        if (end) j.row_begin[1] = n_segs;
+        return;
+    }
+    // only a worker's first token finds a worker before it that is not its own
+    const uint32_t w = k / j.vocab;
+    if (head && (i == 0 || last < w * j.vocab))
+        for (uint32_t v = i == 0 ? 0u : last / j.vocab + 1; v <= w; ++v) j.row_begin[v] = u;
+    if (end)
+        for (uint32_t v = w + 1; v <= j.n_workers; ++v) j.row_begin[v] = n_segs;
+}
+
+// Block 0: the lists of a call without a token that has a gradient, and what the sums count up from zero.
+__device__ __forceinline__ void put_empty(const SortJob& j, bool nothing) {
+    if (threadIdx.x < 2) j.n_long[threadIdx.x] = 0;
+    if (!nothing) return;
+    if (threadIdx.x < 2) j.n_segs[threadIdx.x] = 0;
+    if (j.row_begin)
+        for (uint32_t v = threadIdx.x; v <= j.n_workers; v += kSortThreads) j.row_begin[v] = 0;
 }
 
 // Stable sort of the tokens by worker and token, and what the sums need to know about the sorted list.  Least significant
 // digit first; a block ranks its tokens with ballots (a warp's rows of 32 in turn, one counter per warp and digit),
 // the blocks tell each other their counts through a table in global memory.
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j) {
-    __shared__ uint16_t s_count[kSortWarps][kMaxBins];      // of a digit in the warps before
+    cudaTriggerProgrammaticLaunchCompletion();              // the sums' blocks may line up: they wait for this kernel's end
+    __shared__ uint16_t s_count[kSortWarps * kMaxBins];     // [warps][bins] of a digit in the warps before
     __shared__ uint32_t s_base[kMaxBins];
     __shared__ uint32_t s_warp[32];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (blockIdx.x >= j.n_blocks) {
-        for (uint64_t r = blockIdx.x - j.n_blocks; r < j.zero_rows; r += gridDim.x - j.n_blocks) zero_row(j.zero, r, j.dim, j.zero_vec != 0);
-        return;
-    }
     const uint64_t from = static_cast<uint64_t>(blockIdx.x) * j.per_block;
     const uint64_t to = from + j.per_block < j.n ? from + j.per_block : j.n;
     const uint32_t bins = 1u << j.bits, mask = bins - 1;
+    uint16_t* mine = s_count + warp * bins;
     const uint32_t items = j.per_block < kStep ? j.per_block / kSortThreads : kItems;     // rows of 32 per warp and step
     const bool one_step = j.per_block <= kStep;
     uint32_t key[kItems], pos[kItems], rank[kItems];
@@ -200,7 +270,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
         const int shift = pass * j.bits;
         // Loads step `at`, ranks it and leaves s_count as places within the step; returns the step's count of digit tid.
         auto rank_step = [&](uint64_t at, bool report) -> uint32_t {
-            for (uint32_t d = lane; d < bins; d += 32) s_count[warp][d] = 0;
+            for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 const uint64_t t = at + (warp * items + i) * 32 + lane;
@@ -223,29 +293,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
                 if (i >= items) break;
                 const bool real = at + (warp * items + i) * 32 + lane < to;
                 const uint32_t d = (key[i] >> shift) & mask;
-                uint32_t same = __ballot_sync(0xFFFFFFFFu, real);
-                if (!real) same = ~same;
-                for (int b = 0; b < j.bits; ++b) {
-                    const uint32_t vote = __ballot_sync(0xFFFFFFFFu, (d >> b) & 1);
-                    same &= (d >> b) & 1 ? vote : ~vote;
-                }
+                const uint32_t same = same_digit(d, real);
                 const uint32_t before = __popc(same & ((1u << lane) - 1));
-                rank[i] = s_count[warp][d] + before;
+                rank[i] = mine[d] + before;
                 __syncwarp();
-                if (real && before == 0) s_count[warp][d] += static_cast<uint16_t>(__popc(same));
+                if (real && before == 0) mine[d] += static_cast<uint16_t>(__popc(same));
                 __syncwarp();
             }
             __syncthreads();
-            uint32_t sum = 0;
-            if (tid < bins) {
-#pragma unroll 8
-                for (int w = 0; w < kSortWarps; ++w) {
-                    const uint32_t c = s_count[w][tid];
-                    s_count[w][tid] = static_cast<uint16_t>(sum);
-                    sum += c;
-                }
-            }
-            return sum;
+            return tid < bins ? counts_to_places(s_count, bins, tid) : 0u;
         };
         uint32_t count = 0;
         for (uint64_t at = from; at < to || at == from; at += kStep) {
@@ -280,7 +336,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
             for (int i = 0; i < kItems; ++i) {
                 if (i >= items || at + (warp * items + i) * 32 + lane >= to) continue;
                 const uint32_t d = (key[i] >> shift) & mask;
-                const uint32_t place = s_base[d] + s_count[warp][d] + rank[i];
+                const uint32_t place = s_base[d] + mine[d] + rank[i];
                 __stcg(j.key[pass & 1] + place, key[i]);
                 __stcg(j.pos[pass & 1] + place, pos[i]);
             }
@@ -294,6 +350,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
 
     // Segments: where each begins, how many begin before every chunk, where each worker's begin.
     const uint32_t* sorted = j.key[(j.passes - 1) & 1];
+    const uint32_t* sorted_pos = j.pos[(j.passes - 1) & 1];
     uint32_t segs = 0, total;
     if (j.n_blocks > 1) {
         for (uint64_t at = from; at < to; at += kSortThreads) {
@@ -313,44 +370,19 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     }
     for (uint64_t at = from; at < to; at += kSortThreads) {
         const uint64_t i = at + tid;
-        uint32_t k = j.none, last = j.none, next = j.none;
+        uint32_t k = j.none, last = j.none, next = j.none, pos_i = 0;
         if (i < to) {
             k = __ldcg(sorted + i);
+            pos_i = __ldcg(sorted_pos + i);
             if (i > 0) last = __ldcg(sorted + i - 1);
             if (i + 1 < j.n) next = __ldcg(sorted + i + 1);
         }
         const bool head = k != j.none && (i == 0 || last != k);
-        const uint32_t u = segs + block_before(head, s_warp, &total);      // segments that begin before i
+        const uint32_t u = segs + block_before(head, s_warp, &total);
         segs += total;
-        if (i >= to) continue;
-        if ((i & ((1u << j.chunk_shift) - 1)) == 0) j.chunk_seg[i >> j.chunk_shift] = u;
-        if (head) {
-            j.seg_begin[u] = static_cast<uint32_t>(i);
-            j.seg_key[u] = k;
-        }
-        const bool end = k != j.none && next == j.none;                    // the last token with a gradient
-        const uint32_t n_segs = u + head;
-        if (end) {
-            j.seg_begin[n_segs] = static_cast<uint32_t>(i) + 1;
-            *j.n_segs = n_segs;
-        }
-        if (j.row_begin && (head || end)) {
-            const uint32_t w = j.n_workers == 1 ? 0u : k / j.vocab;
-            if (head)
-                for (uint32_t v = i == 0 ? 0u : (j.n_workers == 1 ? 0u : last / j.vocab) + 1; v <= w; ++v) j.row_begin[v] = u;
-            if (end)
-                for (uint32_t v = w + 1; v <= j.n_workers; ++v) j.row_begin[v] = n_segs;
-        }
+        if (i < to) put_segment(j, i, k, last, next, pos_i, head, u);
     }
-    const bool nothing = j.n == 0 || (blockIdx.x == 0 && __ldcg(sorted) == j.none);     // not one token with a gradient
-    if (blockIdx.x == 0) {
-        if (nothing) {
-            if (tid == 0) *j.n_segs = 0;
-            if (j.row_begin)
-                for (uint32_t v = tid; v <= j.n_workers; v += kSortThreads) j.row_begin[v] = 0;
-        }
-        if (tid == 0) *j.n_long = 0;
-    }
+    if (blockIdx.x == 0) put_empty(j, j.n == 0 || __ldcg(sorted) == j.none);
     // the last block through leaves the barrier as it was
     if (j.n_blocks > 1 && tid == 0 && atomicAdd(j.barrier + 1, 1u) == j.n_blocks - 1) {
         j.barrier[0] = 0;
@@ -358,14 +390,149 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     }
 }
 
+// The same sort for up to kStep tokens per block in one thread-block cluster (ONE: a single block): the tokens stay in
+// registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
+// belong to, and the cluster's barrier takes the place of the one in global memory.
+template <bool ONE>
+__global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const SortJob j) {
+    extern __shared__ uint64_t s_mem64[];
+    __shared__ uint32_t s_base[kMaxBins];
+    __shared__ uint32_t s_warp[32];
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    auto meet_all = [&] {
+        if constexpr (ONE) __syncthreads();
+        else cluster.sync();
+    };
+    cudaTriggerProgrammaticLaunchCompletion();
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t n_ranks = ONE ? 1 : gridDim.x, me = ONE ? 0 : blockIdx.x;    // one cluster
+    const uint32_t share = 1u << j.share_shift, items = share / kSortThreads;
+    uint64_t* s_tok = s_mem64;                                                  // [share] key and position
+    const uint32_t bins = 1u << j.bits, mask = bins - 1;
+    uint32_t* s_all = reinterpret_cast<uint32_t*>(s_tok + share);               // [n_ranks][bins] the blocks' counts
+    uint16_t* s_count = reinterpret_cast<uint16_t*>(s_all + n_ranks * bins);    // [kSortWarps][bins]
+    uint16_t* mine = s_count + warp * bins;
+    const uint32_t from = me << j.share_shift;
+    const uint32_t n_here = j.n > from ? (j.n - from < share ? j.n - from : share) : 0;
+    const uint32_t span = warp * items * 32 + lane;                             // the warp's tokens: rows of 32, one after the other
+    uint64_t tok[kItems];
+    uint32_t rank[kItems];
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const uint32_t t = span + i * 32;
+        tok[i] = static_cast<uint64_t>(j.none) << 32;
+        if (i >= items || t >= n_here) continue;
+        const uint32_t v = load_token(j.tokens, from + t, j.vocab);
+        if (v == 0xFFFFFFFFu) record_error(j.status, ADACOMP_ERR_INVALID);
+        const uint32_t k = v == 0xFFFFFFFFu || v == j.padding ? j.none : (j.n_workers == 1 ? 0u : (from + t) / j.n_tokens * j.vocab) + v;
+        tok[i] = static_cast<uint64_t>(k) << 32 | (from + t);
+    }
+    if constexpr (!ONE) cluster.sync();         // every block has started: its shared memory may be written from here on
+    for (int pass = 0; pass < j.passes; ++pass) {
+        const int shift = 32 + pass * j.bits;
+        for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
+        if (pass > 0) {
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+                if (i < items && span + i * 32 < n_here) tok[i] = s_tok[span + i * 32];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            if (i >= items) break;
+            const bool real = span + i * 32 < n_here;
+            const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
+            const uint32_t same = same_digit(d, real);
+            const uint32_t before = __popc(same & ((1u << lane) - 1));
+            const uint32_t had = mine[d];
+            rank[i] = had + before;
+            __syncwarp();
+            if (real && before == 0) mine[d] = static_cast<uint16_t>(had + __popc(same));
+            __syncwarp();
+        }
+        __syncthreads();
+        uint32_t all = 0, before = 0, total;
+        if (tid < bins) {
+            all = counts_to_places(s_count, bins, tid);
+            if constexpr (!ONE)
+                for (uint32_t r = 0; r < n_ranks; ++r) cluster.map_shared_rank(s_all, r)[me * bins + tid] = all;
+        }
+        if constexpr (!ONE) {
+            cluster.sync();                     // the counts have arrived, and every block has its tokens in registers
+            if (tid < bins) {
+                all = 0;
+                for (uint32_t r = 0; r < n_ranks; ++r) {
+                    const uint32_t c = s_all[r * bins + tid];
+                    all += c;
+                    if (r < me) before += c;
+                }
+            }
+        }
+        const uint32_t base = block_before(all, s_warp, &total) + before;
+        if (tid < bins) s_base[tid] = base;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            if (i >= items) break;
+            if (span + i * 32 >= n_here) continue;
+            const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
+            const uint32_t place = s_base[d] + mine[d] + rank[i];
+            if constexpr (ONE) s_tok[place] = tok[i];
+            else cluster.map_shared_rank(s_tok, place >> j.share_shift)[place & (share - 1)] = tok[i];
+        }
+        meet_all();
+    }
+    // Segments.  A warp's tokens are consecutive: its heads are counted by ballots, the warps' counts by one scan.
+    const uint32_t* s_key = reinterpret_cast<const uint32_t*>(s_tok) + 1;       // [2 t] is token t's key
+    uint32_t before_me = j.none, behind_me = j.none;
+    if constexpr (!ONE) {
+        if (me > 0) before_me = cluster.map_shared_rank(s_key, me - 1)[2 * (share - 1)];
+        if (n_here == share && from + share < j.n) behind_me = cluster.map_shared_rank(s_key, me + 1)[0];
+    }
+    uint32_t heads[kItems], in_warp = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        heads[i] = 0;
+        if (i >= items) break;
+        const uint32_t t = span + i * 32;
+        bool head = false;
+        if (t < n_here && s_key[2 * t] != j.none) head = t == 0 ? me == 0 || before_me != s_key[0] : s_key[2 * t - 2] != s_key[2 * t];
+        heads[i] = __ballot_sync(0xFFFFFFFFu, head);
+        in_warp += __popc(heads[i]);
+    }
+    uint32_t segs_here;
+    uint32_t u = __shfl_sync(0xFFFFFFFFu, block_before(lane == 0 ? in_warp : 0u, s_warp, &segs_here), 0);
+    if constexpr (!ONE) {
+        if (tid < n_ranks) cluster.map_shared_rank(s_all, tid)[me] = segs_here;
+        cluster.sync();
+        for (uint32_t r = 0; r < me; ++r) u += s_all[r];
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        if (i >= items) break;
+        const uint32_t t = span + i * 32;
+        if (t < n_here) {
+            const uint64_t x = s_tok[t];
+            const uint32_t last = t == 0 ? before_me : s_key[2 * t - 2];
+            const uint32_t next = t + 1 < n_here ? s_key[2 * t + 2] : t + 1 == share ? behind_me : j.none;
+            put_segment(j, from + t, static_cast<uint32_t>(x >> 32), last, next, static_cast<uint32_t>(x), heads[i] >> lane & 1,
+                        u + __popc(heads[i] & ((1u << lane) - 1)));
+        }
+        u += __popc(heads[i]);
+    }
+    if (me == 0) put_empty(j, j.n == 0 || s_key[0] == j.none);
+    if constexpr (!ONE) cluster.sync();         // nobody leaves while a neighbour may still read here
+}
+
 // ---------------------------------------------------------------------------------------------- sums
 
 struct Sums {
-    const uint32_t *key, *pos, *seg_begin, *seg_key, *chunk_seg, *n_segs;
+    const uint32_t *order, *seg_begin, *seg_key, *chunk_seg, *n_segs;
     uint32_t n, n_chunks, chunk_shift;
     uint32_t tiles;                 // blocks along a row
     uint32_t sum_blocks;            // the blocks behind them write zeros
-    uint32_t* n_long;
+    uint32_t* n_long;               // [2] segments of a few pieces, and of many
+    uint4* long_list;               // first chunk, segment, pieces
     float* partial;
     const int* status;
     Rows grad;
@@ -382,10 +549,11 @@ struct Sums {
     uint64_t zero_rows;             // rows to look at for zeros, zero_run of them per block
     uint32_t zero_run;
     int zero_vec;
+    int wide;                       // rows of the results start on 32-byte boundaries
 };
 
-constexpr int kUnroll = 4;
 constexpr uint32_t kMaxChunk = 64;
+constexpr uint32_t kFewPieces = 16;             // a warp adds them alone
 constexpr uint64_t kEnds = 1ull << 63;          // flag of a token that is its segment's last
 
 // A finished sum goes to its row: `slot` counts segments, `at` is where the row starts in the dense table.
@@ -405,7 +573,8 @@ __device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t a
             for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], old[k]);
         }
         q.pack(sum);
-        q.store(dst);
+        if (Packed<B, N>::kVecs == 2 && p.wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
+        else q.store(dst);
     } else {
         if (p.accumulate) sum[0] = __fadd_rn(sum[0], to_float(*dst));
         *dst = from_float<B>(sum[0]);
@@ -413,9 +582,16 @@ __device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t a
     if (p.idx_out) {
         uint32_t* idx = p.idx_out + static_cast<uint64_t>(slot) * p.dim + c;
         const uint32_t first = p.idx_offset + row * p.dim + c;
-        if constexpr (N > 1) {
-#pragma unroll
-            for (int k = 0; k < N; k += 4) *reinterpret_cast<uint4*>(idx + k) = make_uint4(first + k, first + k + 1, first + k + 2, first + k + 3);
+        if constexpr (N == 8) {
+            const uint4 a = make_uint4(first, first + 1, first + 2, first + 3), b = make_uint4(first + 4, first + 5, first + 6, first + 7);
+            if (p.wide) {
+                store32(idx, a, b);
+            } else {
+                reinterpret_cast<uint4*>(idx)[0] = a;
+                reinterpret_cast<uint4*>(idx)[1] = b;
+            }
+        } else if constexpr (N == 4) {
+            *reinterpret_cast<uint4*>(idx) = make_uint4(first, first + 1, first + 2, first + 3);
         } else {
             *idx = first;
         }
@@ -441,19 +617,8 @@ __device__ void zero_gaps(const Sums& p, uint32_t block) {
         if (r < to) atomicOr(&s_has[(r - from) / 32], 1u << ((r - from) & 31));
     }
     __syncthreads();
-    for (uint64_t r = from; r < to; ++r) {
-        if (s_has[(r - from) / 32] >> ((r - from) & 31) & 1) continue;
-        const uint64_t at = p.out.offset(static_cast<uint32_t>(r));
-        const uint32_t size = p.out.type == ADACOMP_F32 ? 4u : 2u;
-        char* dst = p.out.data + at * size;
-        if (p.zero_vec) {
-            for (uint32_t c = tid; c < p.dim * size / 16; c += n_threads) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
-        } else if (size == 4) {
-            for (uint32_t c = tid; c < p.dim; c += n_threads) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
-        } else {
-            for (uint32_t c = tid; c < p.dim; c += n_threads) reinterpret_cast<uint16_t*>(dst)[c] = 0;
-        }
-    }
+    for (uint64_t r = from; r < to; ++r)
+        if (!(s_has[(r - from) / 32] >> ((r - from) & 31) & 1)) zero_row(p.out, r, p.dim, p.zero_vec != 0, tid, n_threads);
 }
 
 // Sums over the sorted list, cut into chunks of 2^chunk_shift tokens.  A chunk owns the segments that begin in it, to their
@@ -463,6 +628,7 @@ __device__ void zero_gaps(const Sums& p, uint32_t block) {
 template <typename A, typename B, int N>
 __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
     extern __shared__ uint64_t s_mem[];
+    cudaGridDependencySynchronize();
     if (*p.status == ADACOMP_ERR_TIMEOUT) return;           // the sort gave up: its lists are not to be followed
     if (blockIdx.x >= p.sum_blocks) {
         zero_gaps(p, blockIdx.x - p.sum_blocks);
@@ -472,8 +638,7 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
     uint64_t* s_src = s_mem + static_cast<size_t>(threadIdx.y) * (3 * size);    // [2 size] where the rows of the chunk's tokens start
     uint64_t* s_dst = s_src + 2 * size;                                         // [size] where its segments' rows start
     const uint32_t chunk = blockIdx.x / p.tiles * blockDim.y + threadIdx.y, tile = blockIdx.x % p.tiles;
-    const uint32_t n_segs = *p.n_segs;
-    const uint32_t live = n_segs ? p.seg_begin[n_segs] : 0;
+    const uint32_t n_segs = p.n_segs[0], live = p.n_segs[1];
     const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
     uint32_t a = 0, b = 0, u0 = 0, u1 = 0;
     bool lead = false, trail = false;
@@ -495,16 +660,20 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
         if (lead && u1 == u0 && first < i1) b = first;
     }
     for (uint32_t k = threadIdx.x; k < b - a; k += blockDim.x) {
-        const uint32_t i = a + k;
-        const bool ends = i + 1 >= live || p.key[i] != p.key[i + 1];
-        s_src[k] = p.grad.offset(p.pos[i]) | (ends ? kEnds : 0ull);
+        const uint32_t at = p.order[a + k];
+        s_src[k] = p.grad.offset(at & ~kLast) | (at & kLast ? kEnds : 0ull);
     }
     for (uint32_t k = threadIdx.x; k < u1 - u0; k += blockDim.x) {
         const uint32_t key = p.seg_key[u0 + k];
         s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
         if (p.rows_out && tile == 0) p.rows_out[u0 + k] = key % p.vocab;
     }
-    if (trail && tile == 0 && threadIdx.x == 0) p.n_long[1 + atomicAdd(p.n_long, 1u)] = chunk;
+    if (trail && tile == 0 && threadIdx.x == 0) {          // for k_embed_join: short lists from the front, long ones from the back
+        const uint32_t pieces = ((p.seg_begin[u1] - 1) >> p.chunk_shift) - chunk + 1;
+        const bool many = pieces > kFewPieces;
+        const uint32_t e = atomicAdd(p.n_long + many, 1u);
+        p.long_list[many ? p.n_chunks - 1 - e : e] = make_uint4(chunk, u1 - 1, pieces, 0u);
+    }
     __syncthreads();
     if (c >= p.dim) return;
     float sum[N];
@@ -514,32 +683,27 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
     const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
     const uint32_t len = b - a;
     bool open = false;
-    for (uint32_t i = 0; i < len; i += kUnroll) {
-        float f[kUnroll][N];
-        uint64_t src[kUnroll];
-        if constexpr (N > 1) {
-            Packed<A, N> v[kUnroll];
+    // kBatch rows in flight per thread.  Fetching the next batch before the last is added costs the registers of a block per SM
+    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
+    constexpr int kBatch = N * sizeof(A) == 32 ? 2 : 4;
+    struct Batch {
+        Packed<A, N> v[kBatch];
+    };
+    auto fetch = [&](Batch& t, uint32_t i) {
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                src[k] = i + k < len ? s_src[i + k] : 0ull;
-                if (i + k < len) v[k].load(grad + (src[k] & ~kEnds));
-            }
+        for (int k = 0; k < kBatch; ++k)
+            if (i + k < len) t.v[k].load(grad + (s_src[i + k] & ~kEnds));
+    };
+    auto add = [&](const Batch& t, uint32_t i) {
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) v[k].unpack(f[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
-                src[k] = i + k < len ? s_src[i + k] : 0ull;
-                if (i + k < len) f[k][0] = to_float(grad[src[k] & ~kEnds]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
+        for (int k = 0; k < kBatch; ++k) {
             if (i + k >= len) break;
+            float f[N];
+            t.v[k].unpack(f);
 #pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[k][q]);
+            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[q]);
             open = true;
-            if (src[k] & kEnds) {
+            if (s_src[i + k] & kEnds) {
                 if (slot + 1 == u0) {           // the last piece of a long segment
 #pragma unroll
                     for (int q = 0; q < N; ++q) p.partial[static_cast<uint64_t>(chunk) * 2 * p.dim + c + q] = sum[q];
@@ -553,6 +717,11 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
                 open = false;
             }
         }
+    };
+    Batch rows;
+    for (uint32_t i = 0; i < len; i += kBatch) {
+        fetch(rows, i);
+        add(rows, i);
     }
     if (open) {                                 // a piece that goes on in the next chunk
         float* dst = p.partial + (static_cast<uint64_t>(chunk) * 2 + (slot + 1 == u0 ? 0 : 1)) * p.dim + c;
@@ -561,30 +730,51 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
     }
 }
 
-// The long segments: their pieces, in order.  Eight lanes of the block (y) take every eighth piece each.
+// The long segments: their pieces, in order.  32 N columns of a segment are one job; with few pieces a warp does it, with many
+// the block's eight warps take every eighth piece each.  Four pieces are in flight either way.
 constexpr int kJoinLanes = 8;
+template <int N>
+__device__ __forceinline__ void add_pieces(const Sums& p, uint32_t chunk, uint32_t pieces, uint32_t first, uint32_t step, uint32_t c, float (&sum)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    if (c >= p.dim) return;
+    for (uint32_t q0 = first; q0 < pieces; q0 += 4 * step) {
+        float f[4][N];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const uint32_t q = q0 + r * step;
+            const float* src = p.partial + (static_cast<uint64_t>(chunk + q) * 2 + (q == 0 ? 1 : 0)) * p.dim + c;
+            if constexpr (N % 4 == 0) {
+#pragma unroll
+                for (int k = 0; k < N; k += 4) {
+                    const float4 v = q < pieces ? *reinterpret_cast<const float4*>(src + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    f[r][k] = v.x; f[r][k + 1] = v.y; f[r][k + 2] = v.z; f[r][k + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) f[r][k] = q < pieces ? src[k] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (q0 + r * step < pieces)
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], f[r][k]);
+    }
+}
+
 template <typename B, int N>
 __global__ void __launch_bounds__(32 * kJoinLanes) k_embed_join(const Sums p) {
     __shared__ float s_sum[kJoinLanes][32 * N];
+    cudaGridDependencySynchronize();
     if (*p.status == ADACOMP_ERR_TIMEOUT) return;
-    const uint32_t n_long = p.n_long[0], n_segs = *p.n_segs;
+    const uint32_t few = p.n_long[0], many = p.n_long[1];
     const uint32_t tiles = (p.dim + 32 * N - 1) / (32 * N);
-    const uint32_t live = n_segs ? p.seg_begin[n_segs] : 0;
-    for (uint64_t job = blockIdx.x; job < static_cast<uint64_t>(n_long) * tiles; job += gridDim.x) {
-        const uint32_t chunk = p.n_long[1 + job / tiles], c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N;
-        const uint64_t next = static_cast<uint64_t>(chunk + 1) << p.chunk_shift;
-        const uint32_t u = (next < live ? p.chunk_seg[chunk + 1] : n_segs) - 1;
-        const uint32_t pieces = ((p.seg_begin[u + 1] - 1) >> p.chunk_shift) - chunk + 1, key = p.seg_key[u];
-        float sum[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k) sum[k] = 0.f;
-        if (c < p.dim) {
-            for (uint32_t q = threadIdx.y; q < pieces; q += kJoinLanes) {
-                const float* src = p.partial + (static_cast<uint64_t>(chunk + q) * 2 + (q == 0 ? 1 : 0)) * p.dim + c;
-#pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], src[k]);
-            }
-        }
+    float sum[N];
+    for (uint64_t job = blockIdx.x; job < static_cast<uint64_t>(many) * tiles; job += gridDim.x) {
+        const uint4 seg = p.long_list[p.n_chunks - 1 - job / tiles];
+        const uint32_t c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N, key = p.seg_key[seg.y];
+        add_pieces<N>(p, seg.x, seg.z, threadIdx.y, kJoinLanes, c, sum);
 #pragma unroll
         for (int k = 0; k < N; ++k) s_sum[threadIdx.y][threadIdx.x * N + k] = sum[k];
         __syncthreads();
@@ -592,26 +782,35 @@ __global__ void __launch_bounds__(32 * kJoinLanes) k_embed_join(const Sums p) {
             for (int y = 1; y < kJoinLanes; ++y)
 #pragma unroll
                 for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], s_sum[y][threadIdx.x * N + k]);
-            put_row<B, N>(p, u, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
+            put_row<B, N>(p, seg.y, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
         }
         __syncthreads();
+    }
+    for (uint64_t job = static_cast<uint64_t>(blockIdx.x) * kJoinLanes + threadIdx.y; job < static_cast<uint64_t>(few) * tiles;
+         job += static_cast<uint64_t>(gridDim.x) * kJoinLanes) {
+        const uint4 seg = p.long_list[job / tiles];
+        const uint32_t c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N, key = p.seg_key[seg.y];
+        add_pieces<N>(p, seg.x, seg.z, 0, 1, c, sum);
+        if (c < p.dim) put_row<B, N>(p, seg.y, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
     }
 }
 
 // ---------------------------------------------------------------------------------------------- host
 
 // Tokens per chunk: long enough to keep the pieces of long segments rare, short enough that all SMs have work.
+constexpr uint32_t kMinShift = 3, kMaxShift = 6;
+constexpr uint32_t kChunkBits = 22;
 uint32_t chunk_shift_of(uint64_t n, uint32_t dim) {
-    uint32_t shift = 3;
-    while (shift < 6 && (n * dim >> (21 + shift)) > 0) ++shift;
+    uint32_t shift = kMinShift;
+    while (shift < kMaxShift && (n * dim >> (kChunkBits + shift)) > 0) ++shift;
     return shift;
 }
 
 // Chunks of the largest call: calls of fewer tokens may have shorter, and so more, chunks.
 uint64_t max_chunks(uint64_t max_tokens, uint32_t dim) {
     uint64_t most = 0;
-    for (uint32_t shift = 3; shift <= 6; ++shift) {
-        uint64_t n = shift < 6 ? ((1ull << (21 + shift)) - 1) / dim : max_tokens;      // the most tokens with such chunks
+    for (uint32_t shift = kMinShift; shift <= kMaxShift; ++shift) {
+        uint64_t n = shift < kMaxShift ? ((1ull << (kChunkBits + shift)) - 1) / dim : max_tokens;  // the most tokens with such chunks
         if (n > max_tokens) n = max_tokens;
         if (chunk_shift_of(n, dim) == shift && (n >> shift) + 1 > most) most = (n >> shift) + 1;
     }
@@ -623,7 +822,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     const size_t n = max_tokens ? max_tokens : 1, chunks = max_chunks(n, dim);
     adacomp_embed_t e = {};
     e.d_status = c.take<int>(1);
-    e.d_n_segs = c.take<uint32_t>(1);
+    e.d_n_segs = c.take<uint32_t>(2);
     e.d_barrier = c.take<uint32_t>(2);
     for (int i = 0; i < 2; ++i) {
         e.d_key[i] = c.take<uint32_t>(n);
@@ -633,7 +832,9 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     e.d_seg_begin = c.take<uint32_t>(n + 1);
     e.d_seg_key = c.take<uint32_t>(n);
     e.d_chunk_seg = c.take<uint32_t>(chunks + 1);
-    e.d_long = c.take<uint32_t>(chunks + 1);
+    e.d_n_long = c.take<uint32_t>(2);
+    e.d_long = c.take<uint4>(chunks);
+    e.d_order = c.take<uint32_t>(n);
     e.d_partial = c.take<float>(chunks * 2 * dim);
     if (h) {
         h->d_status = e.d_status;
@@ -647,7 +848,9 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
         h->d_seg_begin = e.d_seg_begin;
         h->d_seg_key = e.d_seg_key;
         h->d_chunk_seg = e.d_chunk_seg;
+        h->d_n_long = e.d_n_long;
         h->d_long = e.d_long;
+        h->d_order = e.d_order;
         h->d_partial = e.d_partial;
     }
     return c.used;
@@ -684,11 +887,11 @@ bool rows_apart(const Rows& r, uint64_t n_rows, uint64_t dim) {
     return r.group_stride >= dim && r.row_stride >= (groups - 1) * r.group_stride + dim;
 }
 
-// Whether every row starts on a 16-byte boundary.
-bool on_grid(const Rows& r) {
+// Whether every row starts on a boundary of so many bytes.
+bool on_grid(const Rows& r, uint32_t bytes) {
     const uint32_t size = type_size(r.type);
-    return reinterpret_cast<uintptr_t>(r.data) % 16 == 0 && r.row_stride * size % 16 == 0 &&
-           (r.group == 0 || r.group_stride * size % 16 == 0);
+    return reinterpret_cast<uintptr_t>(r.data) % bytes == 0 && r.row_stride * size % bytes == 0 &&
+           (r.group == 0 || r.group_stride * size % bytes == 0);
 }
 
 uint32_t threads_along(uint32_t dim, uint32_t n) {
@@ -701,7 +904,7 @@ template <typename A, typename B>
 int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h,
                   float scale, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
-    const bool vec = h->dim % N == 0 && on_grid(table) && on_grid(out);
+    const bool vec = h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16);
     const uint32_t x = threads_along(h->dim, vec ? N : 1), y = kThreads / x;
     const dim3 grid((n_tokens + y - 1) / y), block(x, y);
     if (vec) k_embed_lookup<A, B, N><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, scale, h->d_status);
@@ -724,10 +927,30 @@ void along_row(uint32_t cols, uint32_t chunk_bytes, uint32_t* x, uint32_t* y, ui
     while (*y > 1 && *y * chunk_bytes > 32 * 1024) *y /= 2;
 }
 
+// A launch whose blocks may line up while the kernel before it ends; they wait for it themselves.
+template <typename... Args>
+int launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (e != cudaSuccess) return cuda_fail(e);
+    ADACOMP_LAUNCH_CHECK();
+    return ADACOMP_OK;
+}
+
 template <typename A, typename B>
-int launch_sums(Sums p, bool out_vec, bool gaps, const adacomp_embed_t* h, cudaStream_t stream) {
+int launch_sums(Sums p, uint32_t out_grid, bool gaps, const adacomp_embed_t* h, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
-    const bool vec = p.dim % N == 0 && on_grid(p.grad) && out_vec;
+    const bool vec = p.dim % N == 0 && on_grid(p.grad, 16) && out_grid >= 16;
+    p.wide = out_grid >= 32;
     const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
     uint32_t x, y;
     along_row((p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), chunk_bytes, &x, &y, &p.tiles);
@@ -737,22 +960,16 @@ int launch_sums(Sums p, bool out_vec, bool gaps, const adacomp_embed_t* h, cudaS
         const uint32_t size = type_size(p.out.type);
         p.zero_run = 1;
         while (p.zero_run < kMaxChunk && static_cast<uint64_t>(p.zero_run) * p.dim * size < 32768) p.zero_run *= 2;
-        p.zero_vec = on_grid(p.out) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
+        p.zero_vec = on_grid(p.out, 16) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
         zero_blocks = static_cast<uint32_t>((p.zero_rows + p.zero_run - 1) / p.zero_run);
     }
     if (p.sum_blocks + zero_blocks == 0) return ADACOMP_OK;
     const dim3 block(x, y);
-    if (vec) k_embed_sums<A, B, N><<<p.sum_blocks + zero_blocks, block, y * chunk_bytes, stream>>>(p);
-    else k_embed_sums<A, B, 1><<<p.sum_blocks + zero_blocks, block, y * chunk_bytes, stream>>>(p);
-    ADACOMP_LAUNCH_CHECK();
-    if (p.n_chunks < 2) return ADACOMP_OK;              // no segment is longer than a chunk
-    const dim3 lanes(32, kJoinLanes);
-    const uint32_t grid = 4 * static_cast<uint32_t>(h->n_sms);
+    int rc = launch_after(vec ? k_embed_sums<A, B, N> : k_embed_sums<A, B, 1>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
+    if (rc != ADACOMP_OK || p.n_chunks < 2) return rc;              // one chunk: no segment is longer
     constexpr int kWide = 16 / sizeof(B);
-    if (out_vec && p.dim % kWide == 0) k_embed_join<B, kWide><<<grid, lanes, 0, stream>>>(p);
-    else k_embed_join<B, 1><<<grid, lanes, 0, stream>>>(p);
-    ADACOMP_LAUNCH_CHECK();
-    return ADACOMP_OK;
+    const bool join_vec = out_grid >= 16 && p.dim % kWide == 0;
+    return launch_after(join_vec ? k_embed_join<B, kWide> : k_embed_join<B, 1>, dim3(4 * static_cast<uint32_t>(h->n_sms)), dim3(32, kJoinLanes), 0, stream, p);
 }
 
 // Calls f<A, B>() for the types' numbers.
@@ -782,14 +999,6 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
     j.vocab = h->vocab;
     j.padding = h->padding;
     j.none = n_workers * h->vocab;
-    j.n_blocks = 1;
-    if (j.n > kOneBlock) {
-        j.n_blocks = (j.n + 2047) / 2048;
-        if (j.n_blocks > kSortBlocks) j.n_blocks = kSortBlocks;
-    }
-    const uint32_t unit = (j.n + j.n_blocks - 1) / j.n_blocks > kStep ? kStep : kSortThreads;
-    j.per_block = ((j.n + j.n_blocks - 1) / j.n_blocks + unit - 1) / unit * unit;
-    if (j.per_block == 0) j.per_block = kSortThreads;
     int bits = 0;
     while (bits < 32 && (j.none >> bits) != 0) ++bits;
     j.passes = (bits + kDigitBits - 1) / kDigitBits;
@@ -803,34 +1012,53 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
     j.seg_key = h->d_seg_key;
     j.n_segs = h->d_n_segs;
     j.chunk_seg = h->d_chunk_seg;
-    j.n_long = h->d_long;
+    j.n_long = h->d_n_long;
+    j.order = h->d_order;
     j.chunk_shift = chunk_shift_of(j.n, h->dim);
     j.row_begin = d_row_begin;
     j.barrier = h->d_barrier;
     j.status = h->d_status;
-    uint32_t grid = j.n_blocks;
-    if (zero) {
-        j.zero = *zero;
-        j.zero_rows = zero_rows;
-        j.dim = h->dim;
-        j.zero_vec = on_grid(*zero) && static_cast<uint64_t>(h->dim) * type_size(zero->type) % 16 == 0;
-        const uint64_t spare = static_cast<uint32_t>(h->n_sms) > grid ? static_cast<uint32_t>(h->n_sms) - grid : 1;
-        grid += static_cast<uint32_t>(zero_rows < spare ? zero_rows : spare);
-    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(kSortThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeCooperative;
-    attr[0].val.cooperative = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = j.n_blocks > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_embed_sort, j);
+    cfg.numAttrs = 1;
+    cudaError_t e;
+    if (j.n <= h->cluster * kStep) {
+        // as many blocks as have a token per thread, then more tokens per thread
+        uint32_t blocks = 1;
+        while (blocks < h->cluster && blocks * kSortThreads < j.n) blocks *= 2;
+        j.share_shift = 10;
+        while ((blocks << j.share_shift) < j.n) ++j.share_shift;
+        cfg.gridDim = dim3(blocks);
+        cfg.dynamicSmemBytes = (2u << j.share_shift) * 4 + (blocks << j.bits) * 4 + (kSortWarps << j.bits) * 2;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = blocks;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.numAttrs = blocks > 1 ? 1 : 0;
+        e = cudaLaunchKernelEx(&cfg, blocks > 1 ? k_embed_sort_cluster<false> : k_embed_sort_cluster<true>, j);
+    } else {
+        j.n_blocks = (j.n + 2047) / 2048;
+        if (j.n_blocks > kSortBlocks) j.n_blocks = kSortBlocks;
+        const uint32_t unit = (j.n + j.n_blocks - 1) / j.n_blocks > kStep ? kStep : kSortThreads;
+        j.per_block = ((j.n + j.n_blocks - 1) / j.n_blocks + unit - 1) / unit * unit;
+        cfg.gridDim = dim3(j.n_blocks);
+        attr[0].id = cudaLaunchAttributeCooperative;
+        attr[0].val.cooperative = 1;
+        e = cudaLaunchKernelEx(&cfg, k_embed_sort, j);
+    }
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
-    p->key = j.key[(j.passes - 1) & 1];
-    p->pos = j.pos[(j.passes - 1) & 1];
+    if (zero) {
+        const int vec = on_grid(*zero, 16) && static_cast<uint64_t>(h->dim) * type_size(zero->type) % 16 == 0;
+        const uint32_t most = 8 * static_cast<uint32_t>(h->n_sms);
+        const int rc = launch_after(k_embed_clear, dim3(zero_rows < most ? static_cast<uint32_t>(zero_rows) : most), dim3(kThreads), 0, stream,
+                                    *zero, zero_rows, h->dim, vec);
+        if (rc != ADACOMP_OK) return rc;
+    }
+    p->order = j.order;
     p->seg_begin = j.seg_begin;
     p->seg_key = j.seg_key;
     p->chunk_seg = j.chunk_seg;
@@ -838,12 +1066,38 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
     p->n = j.n;
     p->chunk_shift = j.chunk_shift;
     p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
-    p->n_long = h->d_long;
+    p->n_long = h->d_n_long;
+    p->long_list = h->d_long;
     p->partial = h->d_partial;
     p->status = h->d_status;
     p->dim = h->dim;
     p->vocab = h->vocab;
     return ADACOMP_OK;
+}
+
+// The largest cluster that fits the device, with the shared memory that the sort's blocks may need.
+cudaError_t prepare_cluster(uint32_t* blocks_out) {
+    cudaError_t e = cudaFuncSetAttribute(k_embed_sort_cluster<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort_cluster<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort_cluster<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    for (uint32_t blocks = 16; e == cudaSuccess; blocks /= 2) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(blocks);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = kClusterSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = blocks;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        e = cudaOccupancyMaxActiveClusters(&n, k_embed_sort_cluster<false>, &cfg);
+        *blocks_out = blocks;
+        if (n > 0 || blocks == 1) break;
+    }
+    return e;
 }
 
 int check_grad(const adacomp_embed_t* h, uint32_t n_tokens, uint32_t n_workers, float scale) {
@@ -885,6 +1139,7 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     DeviceGuard guard(device);
     cudaError_t err = guard.err;
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&e->n_sms, cudaDevAttrMultiProcessorCount, device);
+    if (err == cudaSuccess) err = prepare_cluster(&e->cluster);
     if (err == cudaSuccess) err = cudaMemset(e->d_status, 0, sizeof(int));
     if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 2 * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaStreamSynchronize(nullptr);
@@ -935,9 +1190,10 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     p.values = static_cast<char*>(d_values_out);
     p.idx_out = d_idx_out;
     p.idx_offset = static_cast<uint32_t>(idx_offset);
-    const bool vec = reinterpret_cast<uintptr_t>(d_values_out) % 16 == 0 && static_cast<uint64_t>(h->dim) * type_size(values_type) % 16 == 0 &&
-                     (!d_idx_out || (reinterpret_cast<uintptr_t>(d_idx_out) % 16 == 0 && h->dim % 4 == 0));
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, p, vec, false, h, stream);
+    uint64_t grid = reinterpret_cast<uintptr_t>(d_values_out) | static_cast<uint64_t>(h->dim) * type_size(values_type);
+    if (d_idx_out) grid |= reinterpret_cast<uintptr_t>(d_idx_out) | static_cast<uint64_t>(h->dim) * 4;
+    const uint32_t out_grid = grid % 32 == 0 ? 32 : grid % 16 == 0 ? 16 : 1;
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, p, out_grid, false, h, stream);
 }
 
 int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens, uint32_t n_workers,
@@ -965,7 +1221,8 @@ int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, u
     p.dense = 1;
     p.accumulate = accumulate != 0;
     p.zero_rows = n_rows;
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, p, on_grid(p.out), !accumulate && !early, h, stream);
+    const uint32_t out_grid = on_grid(p.out, 32) ? 32 : on_grid(p.out, 16) ? 16 : 1;
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, p, out_grid, !accumulate && !early, h, stream);
 }
 
 int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {

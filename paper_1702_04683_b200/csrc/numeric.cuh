@@ -70,6 +70,10 @@ __device__ __forceinline__ void store16(void* p, const uint4& v, uint64_t policy
     asm volatile("st.global.L2::cache_hint.v4.b32 [%0], {%1, %2, %3, %4}, %5;"
                  :: "l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w), "l"(policy) : "memory");
 }
+__device__ __forceinline__ void store32(void* p, const uint4& a, const uint4& b) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 :: "l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
 // 32-byte vectors, one instruction each (32-byte aligned).
 __device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b, uint64_t policy) {
     asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], %9;"
@@ -131,6 +135,17 @@ template <typename T, int N> struct Packed {
             v[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
+};
+
+// A single entry, with the same interface.
+template <typename T> struct Packed<T, 1> {
+    static constexpr int kVecs = 1;
+    uint4 v[1];                     // unused
+    T x;
+    __device__ __forceinline__ void load(const T* p) { x = __ldg(p); }
+    __device__ __forceinline__ void store(T* p) const { *p = x; }
+    __device__ __forceinline__ void unpack(float (&f)[1]) const { f[0] = to_float(x); }
+    __device__ __forceinline__ void pack(const float (&f)[1]) { x = from_float<T>(f[0]); }
 };
 
 // Entries per vectorised item: 16 bytes of the narrower of the two types.
