@@ -31,6 +31,7 @@ struct adacomp_embed {
     uint4* d_long;                  // [chunks] those
     uint32_t* d_order;              // [max_tokens] positions in the order of the sort
     uint32_t cluster;               // blocks of the largest cluster that the device takes
+    uint32_t* d_tickets;            // [kSmallChunks][blocks along a row]
     float* d_partial;               // [chunks][2][dim] sums of pieces of those
 };
 
@@ -124,6 +125,13 @@ struct SortJob {
 };
 constexpr uint32_t kLast = 1u << 31;
 
+// Token t's key.
+__device__ __forceinline__ uint32_t load_key(const SortJob& j, uint32_t t, bool report) {
+    const uint32_t v = load_token(j.tokens, t, j.vocab);
+    if (v == 0xFFFFFFFFu && report) record_error(j.status, ADACOMP_ERR_INVALID);
+    return v == 0xFFFFFFFFu || v == j.padding ? j.none : (j.n_workers == 1 ? 0u : t / j.n_tokens * j.vocab) + v;
+}
+
 // Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
 // does not, the block says so and the caller gives up.
 __device__ __forceinline__ bool meet(const SortJob& j) {
@@ -148,6 +156,7 @@ __device__ __forceinline__ bool meet(const SortJob& j) {
 }
 
 // Sum over the block's threads before this one, and over all of them.
+template <int WARPS = kSortWarps>
 __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s_warp, uint32_t* total) {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     uint32_t upto = v;
@@ -159,7 +168,7 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s_warp, u
     __syncthreads();
     if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    const uint32_t w = s_warp[lane];
+    const uint32_t w = WARPS == 32 || lane < WARPS ? s_warp[lane] : 0u;
     *total = __reduce_add_sync(0xFFFFFFFFu, w);
     return __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u) + upto - v;
 }
@@ -196,13 +205,14 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d, bool real) {
 }
 
 // Counts of digit `d` in the block's warps become the counts before each warp; returns their sum.
+template <int WARPS = kSortWarps>
 __device__ __forceinline__ uint32_t counts_to_places(uint16_t* s_count, uint32_t bins, uint32_t d) {
-    uint32_t c[kSortWarps];
+    uint32_t c[WARPS];
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) c[w] = s_count[w * bins + d];
+    for (int w = 0; w < WARPS; ++w) c[w] = s_count[w * bins + d];
     uint32_t sum = 0;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) {
+    for (int w = 0; w < WARPS; ++w) {
         s_count[w * bins + d] = static_cast<uint16_t>(sum);
         sum += c[w];
     }
@@ -278,9 +288,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
                 pos[i] = 0;
                 if (i >= items || t >= to) continue;
                 if (pass == 0) {
-                    const uint32_t v = load_token(j.tokens, static_cast<uint32_t>(t), j.vocab);
-                    if (v == 0xFFFFFFFFu && report) record_error(j.status, ADACOMP_ERR_INVALID);
-                    if (v != 0xFFFFFFFFu && v != j.padding) key[i] = (j.n_workers == 1 ? 0u : static_cast<uint32_t>(t) / j.n_tokens * j.vocab) + v;
+                    key[i] = load_key(j, static_cast<uint32_t>(t), report);
                     pos[i] = static_cast<uint32_t>(t);
                 } else {
                     key[i] = __ldcg(key_in + t);
@@ -390,22 +398,16 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     }
 }
 
-// The same sort for up to kStep tokens per block in one thread-block cluster (ONE: a single block): the tokens stay in
-// registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
+// The same sort for up to kStep tokens per block in one thread-block cluster: the tokens stay in registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
 // belong to, and the cluster's barrier takes the place of the one in global memory.
-template <bool ONE>
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const SortJob j) {
     extern __shared__ uint64_t s_mem64[];
     __shared__ uint32_t s_base[kMaxBins];
     __shared__ uint32_t s_warp[32];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
-    auto meet_all = [&] {
-        if constexpr (ONE) __syncthreads();
-        else cluster.sync();
-    };
     cudaTriggerProgrammaticLaunchCompletion();
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t n_ranks = ONE ? 1 : gridDim.x, me = ONE ? 0 : blockIdx.x;    // one cluster
+    const uint32_t n_ranks = gridDim.x, me = blockIdx.x;    // one cluster
     const uint32_t share = 1u << j.share_shift, items = share / kSortThreads;
     uint64_t* s_tok = s_mem64;                                                  // [share] key and position
     const uint32_t bins = 1u << j.bits, mask = bins - 1;
@@ -422,12 +424,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         const uint32_t t = span + i * 32;
         tok[i] = static_cast<uint64_t>(j.none) << 32;
         if (i >= items || t >= n_here) continue;
-        const uint32_t v = load_token(j.tokens, from + t, j.vocab);
-        if (v == 0xFFFFFFFFu) record_error(j.status, ADACOMP_ERR_INVALID);
-        const uint32_t k = v == 0xFFFFFFFFu || v == j.padding ? j.none : (j.n_workers == 1 ? 0u : (from + t) / j.n_tokens * j.vocab) + v;
-        tok[i] = static_cast<uint64_t>(k) << 32 | (from + t);
+        tok[i] = static_cast<uint64_t>(load_key(j, from + t, true)) << 32 | (from + t);
     }
-    if constexpr (!ONE) cluster.sync();         // every block has started: its shared memory may be written from here on
+    cluster.sync();                             // every block has started: its shared memory may be written from here on
     for (int pass = 0; pass < j.passes; ++pass) {
         const int shift = 32 + pass * j.bits;
         for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
@@ -454,18 +453,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         uint32_t all = 0, before = 0, total;
         if (tid < bins) {
             all = counts_to_places(s_count, bins, tid);
-            if constexpr (!ONE)
-                for (uint32_t r = 0; r < n_ranks; ++r) cluster.map_shared_rank(s_all, r)[me * bins + tid] = all;
+            for (uint32_t r = 0; r < n_ranks; ++r) cluster.map_shared_rank(s_all, r)[me * bins + tid] = all;
         }
-        if constexpr (!ONE) {
-            cluster.sync();                     // the counts have arrived, and every block has its tokens in registers
-            if (tid < bins) {
-                all = 0;
-                for (uint32_t r = 0; r < n_ranks; ++r) {
-                    const uint32_t c = s_all[r * bins + tid];
-                    all += c;
-                    if (r < me) before += c;
-                }
+        cluster.sync();                         // the counts have arrived, and every block has its tokens in registers
+        if (tid < bins) {
+            all = 0;
+            for (uint32_t r = 0; r < n_ranks; ++r) {
+                const uint32_t c = s_all[r * bins + tid];
+                all += c;
+                if (r < me) before += c;
             }
         }
         const uint32_t base = block_before(all, s_warp, &total) + before;
@@ -477,18 +473,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
             if (span + i * 32 >= n_here) continue;
             const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
             const uint32_t place = s_base[d] + mine[d] + rank[i];
-            if constexpr (ONE) s_tok[place] = tok[i];
-            else cluster.map_shared_rank(s_tok, place >> j.share_shift)[place & (share - 1)] = tok[i];
+            cluster.map_shared_rank(s_tok, place >> j.share_shift)[place & (share - 1)] = tok[i];
         }
-        meet_all();
+        cluster.sync();
     }
     // Segments.  A warp's tokens are consecutive: its heads are counted by ballots, the warps' counts by one scan.
     const uint32_t* s_key = reinterpret_cast<const uint32_t*>(s_tok) + 1;       // [2 t] is token t's key
     uint32_t before_me = j.none, behind_me = j.none;
-    if constexpr (!ONE) {
-        if (me > 0) before_me = cluster.map_shared_rank(s_key, me - 1)[2 * (share - 1)];
-        if (n_here == share && from + share < j.n) behind_me = cluster.map_shared_rank(s_key, me + 1)[0];
-    }
+    if (me > 0) before_me = cluster.map_shared_rank(s_key, me - 1)[2 * (share - 1)];
+    if (n_here == share && from + share < j.n) behind_me = cluster.map_shared_rank(s_key, me + 1)[0];
     uint32_t heads[kItems], in_warp = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
@@ -502,11 +495,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     }
     uint32_t segs_here;
     uint32_t u = __shfl_sync(0xFFFFFFFFu, block_before(lane == 0 ? in_warp : 0u, s_warp, &segs_here), 0);
-    if constexpr (!ONE) {
-        if (tid < n_ranks) cluster.map_shared_rank(s_all, tid)[me] = segs_here;
-        cluster.sync();
-        for (uint32_t r = 0; r < me; ++r) u += s_all[r];
-    }
+    if (tid < n_ranks) cluster.map_shared_rank(s_all, tid)[me] = segs_here;
+    cluster.sync();
+    for (uint32_t r = 0; r < me; ++r) u += s_all[r];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
         if (i >= items) break;
@@ -521,7 +512,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         u += __popc(heads[i]);
     }
     if (me == 0) put_empty(j, j.n == 0 || s_key[0] == j.none);
-    if constexpr (!ONE) cluster.sync();         // nobody leaves while a neighbour may still read here
+    cluster.sync();                             // nobody leaves while a neighbour may still read here
 }
 
 // ---------------------------------------------------------------------------------------------- sums
@@ -534,6 +525,7 @@ struct Sums {
     uint32_t* n_long;               // [2] segments of a few pieces, and of many
     uint4* long_list;               // first chunk, segment, pieces
     float* partial;
+    uint32_t* tickets;              // [kSmallChunks][tiles], all zero between calls
     const int* status;
     Rows grad;
     uint32_t dim, vocab;
@@ -621,6 +613,86 @@ __device__ void zero_gaps(const Sums& p, uint32_t block) {
         if (!(s_has[(r - from) / 32] >> ((r - from) & 31) & 1)) zero_row(p.out, r, p.dim, p.zero_vec != 0, tid, n_threads);
 }
 
+// Piece of a long segment that chunk `chunk` has summed: the one that begins in front of the chunk (0), or in it (1).
+__device__ __forceinline__ float* piece_at(const Sums& p, uint32_t chunk, uint32_t which, uint32_t c) {
+    return p.partial + (static_cast<uint64_t>(chunk) * 2 + which) * p.dim + c;
+}
+template <int N> __device__ __forceinline__ void put_piece(float* dst, const float (&sum)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int q = 0; q < N; q += 4) *reinterpret_cast<float4*>(dst + q) = make_float4(sum[q], sum[q + 1], sum[q + 2], sum[q + 3]);
+    } else {
+#pragma unroll
+        for (int q = 0; q < N; ++q) dst[q] = sum[q];
+    }
+}
+
+// Sums of one chunk's tokens: s_src says where their rows start and which of them end a segment, s_dst where the segments'
+// results go.  `slot` is the first token's segment, u0 the first one that begins in the chunk.
+template <typename A, typename B, int N>
+__device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, const uint64_t* s_dst, uint32_t len, uint32_t slot, uint32_t u0,
+                                          uint32_t chunk, uint32_t c) {
+    float sum[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
+    bool open = false;
+    // kBatch rows in flight per thread.  Fetching the next batch before the last is added costs the registers of a block per SM
+    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
+    constexpr int kBatch = N * sizeof(A) == 32 ? 2 : 4;
+    for (uint32_t i = 0; i < len; i += kBatch) {
+        Packed<A, N> v[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+            if (i + k < len) v[k].load(grad + (s_src[i + k] & ~kEnds));
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (i + k >= len) break;
+            float f[N];
+            v[k].unpack(f);
+#pragma unroll
+            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[q]);
+            open = true;
+            if (s_src[i + k] & kEnds) {
+                if (slot + 1 == u0) {           // the last piece of a long segment
+                    put_piece<N>(piece_at(p, chunk, 0, c), sum);
+                } else {
+                    const uint64_t at = s_dst[slot - u0];
+                    put_row<B, N>(p, slot, at, static_cast<uint32_t>(at), c, sum);
+                }
+#pragma unroll
+                for (int q = 0; q < N; ++q) sum[q] = 0.f;
+                ++slot;
+                open = false;
+            }
+        }
+    }
+    if (open) put_piece<N>(piece_at(p, chunk, slot + 1 == u0 ? 0 : 1, c), sum);     // a piece that goes on in the next chunk
+}
+
+// What a chunk has to do.
+struct Share {
+    uint32_t a, b;                  // its tokens
+    uint32_t u0, u1;                // the segments that begin in it
+    bool lead, trail;               // whether it begins, ends with a piece of a long segment
+};
+template <typename Begin>
+__device__ __forceinline__ Share share_of(uint64_t i0, uint32_t size, uint32_t live, uint32_t u0, uint32_t u1, const Begin& seg_begin) {
+    Share s = {0, 0, u0, u1, false, false};
+    const uint32_t i1 = static_cast<uint32_t>(i0 + size < live ? i0 + size : live);
+    const uint32_t first = seg_begin[u0];                   // of the segments that begin here (or the end of the list)
+    if (first > i0) s.lead = first - seg_begin[u0 - 1] > size;
+    s.a = s.lead ? static_cast<uint32_t>(i0) : first;
+    if (u1 > u0) {
+        const uint32_t end = seg_begin[u1];
+        s.trail = end - seg_begin[u1 - 1] > size;
+        s.b = s.trail ? i1 : end;
+    } else {
+        s.b = !s.lead ? s.a : first < i1 ? first : i1;
+    }
+    return s;
+}
+
 // Sums over the sorted list, cut into chunks of 2^chunk_shift tokens.  A chunk owns the segments that begin in it, to their
 // end even if that lies in the next chunk; a segment longer than a chunk is cut at the chunks' borders, its pieces are
 // added up by k_embed_join.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
@@ -640,94 +712,26 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
     const uint32_t chunk = blockIdx.x / p.tiles * blockDim.y + threadIdx.y, tile = blockIdx.x % p.tiles;
     const uint32_t n_segs = p.n_segs[0], live = p.n_segs[1];
     const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
-    uint32_t a = 0, b = 0, u0 = 0, u1 = 0;
-    bool lead = false, trail = false;
     const uint64_t i0 = static_cast<uint64_t>(chunk) << p.chunk_shift;
-    if (i0 < live) {
-        const uint32_t i1 = static_cast<uint32_t>(i0 + size < live ? i0 + size : live);
-        u0 = p.chunk_seg[chunk];
-        u1 = i0 + size < live ? p.chunk_seg[chunk + 1] : n_segs;
-        const uint32_t first = p.seg_begin[u0];             // of the segments that begin here (or the end of the list)
-        if (first > i0) lead = first - p.seg_begin[u0 - 1] > size;
-        a = lead ? static_cast<uint32_t>(i0) : first;
-        if (u1 > u0) {
-            const uint32_t end = p.seg_begin[u1];
-            trail = end - p.seg_begin[u1 - 1] > size;
-            b = trail ? i1 : end;
-        } else {
-            b = lead ? i1 : a;
-        }
-        if (lead && u1 == u0 && first < i1) b = first;
-    }
-    for (uint32_t k = threadIdx.x; k < b - a; k += blockDim.x) {
-        const uint32_t at = p.order[a + k];
+    Share s = {};
+    if (i0 < live) s = share_of(i0, size, live, p.chunk_seg[chunk], i0 + size < live ? p.chunk_seg[chunk + 1] : n_segs, p.seg_begin);
+    for (uint32_t k = threadIdx.x; k < s.b - s.a; k += blockDim.x) {
+        const uint32_t at = p.order[s.a + k];
         s_src[k] = p.grad.offset(at & ~kLast) | (at & kLast ? kEnds : 0ull);
     }
-    for (uint32_t k = threadIdx.x; k < u1 - u0; k += blockDim.x) {
-        const uint32_t key = p.seg_key[u0 + k];
+    for (uint32_t k = threadIdx.x; k < s.u1 - s.u0; k += blockDim.x) {
+        const uint32_t key = p.seg_key[s.u0 + k];
         s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
-        if (p.rows_out && tile == 0) p.rows_out[u0 + k] = key % p.vocab;
+        if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
     }
-    if (trail && tile == 0 && threadIdx.x == 0) {          // for k_embed_join: short lists from the front, long ones from the back
-        const uint32_t pieces = ((p.seg_begin[u1] - 1) >> p.chunk_shift) - chunk + 1;
+    if (s.trail && tile == 0 && threadIdx.x == 0) {        // for k_embed_join: short lists from the front, long ones from the back
+        const uint32_t pieces = ((p.seg_begin[s.u1] - 1) >> p.chunk_shift) - chunk + 1;
         const bool many = pieces > kFewPieces;
         const uint32_t e = atomicAdd(p.n_long + many, 1u);
-        p.long_list[many ? p.n_chunks - 1 - e : e] = make_uint4(chunk, u1 - 1, pieces, 0u);
+        p.long_list[many ? p.n_chunks - 1 - e : e] = make_uint4(chunk, s.u1 - 1, pieces, 0u);
     }
     __syncthreads();
-    if (c >= p.dim) return;
-    float sum[N];
-#pragma unroll
-    for (int k = 0; k < N; ++k) sum[k] = 0.f;
-    uint32_t slot = lead ? u0 - 1 : u0;
-    const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
-    const uint32_t len = b - a;
-    bool open = false;
-    // kBatch rows in flight per thread.  Fetching the next batch before the last is added costs the registers of a block per SM
-    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
-    constexpr int kBatch = N * sizeof(A) == 32 ? 2 : 4;
-    struct Batch {
-        Packed<A, N> v[kBatch];
-    };
-    auto fetch = [&](Batch& t, uint32_t i) {
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            if (i + k < len) t.v[k].load(grad + (s_src[i + k] & ~kEnds));
-    };
-    auto add = [&](const Batch& t, uint32_t i) {
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            if (i + k >= len) break;
-            float f[N];
-            t.v[k].unpack(f);
-#pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[q]);
-            open = true;
-            if (s_src[i + k] & kEnds) {
-                if (slot + 1 == u0) {           // the last piece of a long segment
-#pragma unroll
-                    for (int q = 0; q < N; ++q) p.partial[static_cast<uint64_t>(chunk) * 2 * p.dim + c + q] = sum[q];
-                } else {
-                    const uint64_t at = s_dst[slot - u0];
-                    put_row<B, N>(p, slot, at, static_cast<uint32_t>(at), c, sum);
-                }
-#pragma unroll
-                for (int q = 0; q < N; ++q) sum[q] = 0.f;
-                ++slot;
-                open = false;
-            }
-        }
-    };
-    Batch rows;
-    for (uint32_t i = 0; i < len; i += kBatch) {
-        fetch(rows, i);
-        add(rows, i);
-    }
-    if (open) {                                 // a piece that goes on in the next chunk
-        float* dst = p.partial + (static_cast<uint64_t>(chunk) * 2 + (slot + 1 == u0 ? 0 : 1)) * p.dim + c;
-#pragma unroll
-        for (int q = 0; q < N; ++q) dst[q] = sum[q];
-    }
+    if (c < p.dim) sum_chunk<A, B, N>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
 }
 
 // The long segments: their pieces, in order.  32 N columns of a segment are one job; with few pieces a warp does it, with many
@@ -743,16 +747,16 @@ __device__ __forceinline__ void add_pieces(const Sums& p, uint32_t chunk, uint32
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const uint32_t q = q0 + r * step;
-            const float* src = p.partial + (static_cast<uint64_t>(chunk + q) * 2 + (q == 0 ? 1 : 0)) * p.dim + c;
+            const float* src = piece_at(p, chunk + q, q == 0 ? 1 : 0, c);
             if constexpr (N % 4 == 0) {
 #pragma unroll
                 for (int k = 0; k < N; k += 4) {
-                    const float4 v = q < pieces ? *reinterpret_cast<const float4*>(src + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float4 v = q < pieces ? __ldcg(reinterpret_cast<const float4*>(src + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
                     f[r][k] = v.x; f[r][k + 1] = v.y; f[r][k + 2] = v.z; f[r][k + 3] = v.w;
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < N; ++k) f[r][k] = q < pieces ? src[k] : 0.f;
+                for (int k = 0; k < N; ++k) f[r][k] = q < pieces ? __ldcg(src + k) : 0.f;
             }
         }
 #pragma unroll
@@ -795,6 +799,224 @@ __global__ void __launch_bounds__(32 * kJoinLanes) k_embed_join(const Sums p) {
     }
 }
 
+// ---------------------------------------------------------------------------------------------- few tokens
+
+// Up to kSmallTokens tokens: one launch does everything.  Every block sorts all tokens for itself in shared memory, which
+// takes less than a second kernel's start, and then sums its chunks; the block that delivers the last piece of a long segment
+// adds the pieces up.
+constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32, kSmallItems = 2;
+constexpr uint32_t kSmallTokens = kSmallThreads * kSmallItems;
+constexpr uint32_t kSmallShift = 3, kSmallChunk = 1u << kSmallShift, kSmallChunks = kSmallTokens / kSmallChunk;
+constexpr uint32_t kSmallLanes = 64;                        // chunks a block takes at a time, at most
+
+struct SmallMem {
+    uint64_t tok[kSmallTokens];                             // key and position
+    union {
+        uint16_t count[kSmallWarps * kMaxBins];
+        uint64_t rows[kSmallLanes][3 * kSmallChunk];        // s_src and s_dst of sum_chunk
+    };
+    uint32_t base[kMaxBins];
+    uint32_t warp[32];
+    uint32_t seg_begin[kSmallTokens + 1], seg_key[kSmallTokens];
+    uint32_t chunk_seg[kSmallChunks + 1];
+    uint32_t n_segs, live, any_long;
+    uint32_t done[2 * kSmallLanes];                         // whether a chunk's piece was the last one
+};
+
+__device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
+    const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bins = 1u << j.bits, mask = bins - 1;
+    const uint32_t items = j.n <= kSmallThreads ? 1 : kSmallItems;
+    const uint32_t span = warp * items * 32 + lane;
+    uint16_t* mine = m.count + warp * bins;
+    uint64_t tok[kSmallItems];
+    uint32_t rank[kSmallItems], total;
+    if (tid == 0) m.n_segs = m.live = m.any_long = 0;
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+        const uint32_t t = span + i * 32;
+        tok[i] = static_cast<uint64_t>(j.none) << 32;
+        if (i < items && t < j.n) tok[i] = static_cast<uint64_t>(load_key(j, t, blockIdx.x == 0)) << 32 | t;
+    }
+    for (int pass = 0; pass < j.passes; ++pass) {
+        const int shift = 32 + pass * j.bits;
+        for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
+        if (pass > 0) {
+#pragma unroll
+            for (int i = 0; i < kSmallItems; ++i)
+                if (i < items && span + i * 32 < j.n) tok[i] = m.tok[span + i * 32];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kSmallItems; ++i) {
+            if (i >= items || span - lane + i * 32 >= j.n) break;
+            const bool real = span + i * 32 < j.n;
+            const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
+            const uint32_t same = same_digit(d, real);
+            const uint32_t before = __popc(same & ((1u << lane) - 1));
+            const uint32_t had = mine[d];
+            rank[i] = had + before;
+            __syncwarp();
+            if (real && before == 0) mine[d] = static_cast<uint16_t>(had + __popc(same));
+            __syncwarp();
+        }
+        __syncthreads();
+        const uint32_t all = tid < bins ? counts_to_places<kSmallWarps>(m.count, bins, tid) : 0u;
+        const uint32_t base = block_before<kSmallWarps>(all, m.warp, &total);
+        if (tid < bins) m.base[tid] = base;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kSmallItems; ++i) {
+            if (i >= items || span + i * 32 >= j.n) continue;
+            const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
+            m.tok[m.base[d] + mine[d] + rank[i]] = tok[i];
+        }
+        __syncthreads();
+    }
+    uint32_t heads[kSmallItems], in_warp = 0;
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+        const uint32_t t = span + i * 32;
+        bool head = false;
+        if (i < items && t < j.n) {
+            const uint32_t k = static_cast<uint32_t>(m.tok[t] >> 32);
+            head = k != j.none && (t == 0 || static_cast<uint32_t>(m.tok[t - 1] >> 32) != k);
+        }
+        heads[i] = __ballot_sync(0xFFFFFFFFu, head);
+        in_warp += __popc(heads[i]);
+    }
+    uint32_t u = __shfl_sync(0xFFFFFFFFu, block_before<kSmallWarps>(lane == 0 ? in_warp : 0u, m.warp, &total), 0);
+#pragma unroll
+    for (int i = 0; i < kSmallItems; ++i) {
+        const uint32_t t = span + i * 32;
+        if (i < items && t < j.n) {
+            const uint32_t k = static_cast<uint32_t>(m.tok[t] >> 32);
+            const uint32_t at = u + __popc(heads[i] & ((1u << lane) - 1));
+            const bool head = heads[i] >> lane & 1;
+            if (t % kSmallChunk == 0) m.chunk_seg[t / kSmallChunk] = at;
+            if (head) {
+                m.seg_begin[at] = t;
+                m.seg_key[at] = k;
+            }
+            if (k != j.none) {
+                if (t + kSmallChunk < j.n && static_cast<uint32_t>(m.tok[t + kSmallChunk] >> 32) == k) m.any_long = 1;
+                if (t + 1 == j.n || static_cast<uint32_t>(m.tok[t + 1] >> 32) == j.none) {
+                    m.n_segs = at + head;
+                    m.live = t + 1;
+                    m.seg_begin[at + head] = t + 1;
+                }
+            }
+        }
+        u += __popc(heads[i]);
+    }
+    __syncthreads();
+}
+
+// Rows without a token in this block's share of the table: the stretches between two rows that have one.
+__device__ __forceinline__ void clear_small(const Sums& p, const SmallMem& m) {
+    const uint64_t from = p.zero_rows * blockIdx.x / gridDim.x, to = p.zero_rows * (blockIdx.x + 1) / gridDim.x;
+    const uint32_t size = type_size(p.out.type);
+    const bool flat = p.out.row_stride == p.dim;
+    uint32_t lo = 0, hi = m.n_segs;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (m.seg_key[mid] < from) lo = mid + 1; else hi = mid;
+    }
+    for (uint64_t r = from; r < to;) {
+        uint64_t stop = lo < m.n_segs && m.seg_key[lo] < to ? m.seg_key[lo] : to;
+        if (stop == r) {
+            ++lo;
+            ++r;
+            continue;
+        }
+        if (!flat) stop = r + 1;
+        else if (p.out.group && (r / p.out.group + 1) * p.out.group < stop) stop = (r / p.out.group + 1) * p.out.group;
+        char* dst = p.out.data + p.out.offset(static_cast<uint32_t>(r)) * size;
+        const uint64_t bytes = (stop - r) * p.dim * size;
+        if (p.zero_vec) {
+            for (uint64_t c = threadIdx.x * 16; c < bytes; c += kSmallThreads * 16) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0u, 0u, 0u, 0u);
+        } else if (size == 4) {
+            for (uint64_t c = threadIdx.x * 4; c < bytes; c += kSmallThreads * 4) *reinterpret_cast<uint32_t*>(dst + c) = 0u;
+        } else {
+            for (uint64_t c = threadIdx.x * 2; c < bytes; c += kSmallThreads * 2) *reinterpret_cast<uint16_t*>(dst + c) = 0;
+        }
+        r = stop;
+    }
+}
+
+template <typename A, typename B, int N>
+__global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
+    __shared__ SmallMem m;
+    sort_small(j, m);
+    if (blockIdx.x == 0 && j.row_begin) {
+        for (uint32_t w = threadIdx.x; w <= j.n_workers; w += kSmallThreads) {
+            uint32_t lo = 0, hi = m.n_segs;
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (m.seg_key[mid] < static_cast<uint64_t>(w) * j.vocab) lo = mid + 1; else hi = mid;
+            }
+            j.row_begin[w] = lo;
+        }
+    }
+    const uint32_t tx = threadIdx.x % x, ty = threadIdx.x / x;
+    const uint32_t jobs = (p.n_chunks + y - 1) / y * p.tiles;
+    for (uint32_t job = blockIdx.x; job < jobs; job += gridDim.x) {
+        const uint32_t chunk = job / p.tiles * y + ty, tile = job % p.tiles, c = (tile * x + tx) * N;
+        const uint32_t i0 = chunk * kSmallChunk;
+        uint64_t* s_src = m.rows[ty < y ? ty : 0];
+        uint64_t* s_dst = s_src + 2 * kSmallChunk;
+        Share s = {};
+        if (ty < y && i0 < m.live) {
+            s = share_of(i0, kSmallChunk, m.live, m.chunk_seg[chunk], i0 + kSmallChunk < m.live ? m.chunk_seg[chunk + 1] : m.n_segs, m.seg_begin);
+            for (uint32_t k = tx; k < s.b - s.a; k += x) {
+                const uint32_t t = s.a + k, key = static_cast<uint32_t>(m.tok[t] >> 32);
+                const bool ends = t + 1 == m.live || static_cast<uint32_t>(m.tok[t + 1] >> 32) != key;
+                s_src[k] = p.grad.offset(static_cast<uint32_t>(m.tok[t])) | (ends ? kEnds : 0ull);
+            }
+            for (uint32_t k = tx; k < s.u1 - s.u0; k += x) {
+                const uint32_t key = m.seg_key[s.u0 + k];
+                s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
+                if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
+            }
+        }
+        __syncthreads();
+        if (c < p.dim) sum_chunk<A, B, N>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
+        __syncthreads();
+        if (!m.any_long) continue;
+        // whose piece was the last of its segment
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x < 2 * kSmallLanes) m.done[threadIdx.x] = 0;
+        __syncthreads();
+        uint32_t head[2] = {0, chunk}, pieces[2] = {0, 0};
+        if (s.lead) head[0] = m.seg_begin[s.u0 - 1] / kSmallChunk, pieces[0] = (m.seg_begin[s.u0] - 1) / kSmallChunk - head[0] + 1;
+        if (s.trail) pieces[1] = (m.seg_begin[s.u1] - 1) / kSmallChunk - chunk + 1;
+        if (tx == 0) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (pieces[q] == 0) continue;
+                uint32_t* ticket = p.tickets + head[q] * p.tiles + tile;
+                if (atomicAdd(ticket, 1u) == pieces[q] - 1) {
+                    *ticket = 0;
+                    m.done[2 * ty + q] = 1;
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (pieces[q] == 0 || !m.done[2 * ty + q] || c >= p.dim) continue;
+            __threadfence();
+            const uint32_t u = q == 0 ? s.u0 - 1 : s.u1 - 1, key = m.seg_key[u];
+            float sum[N];
+            add_pieces<N>(p, head[q], pieces[q], 0, 1, c, sum);
+            put_row<B, N>(p, u, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
+        }
+        __syncthreads();
+    }
+    if (p.zero_rows) clear_small(p, m);
+}
+
 // ---------------------------------------------------------------------------------------------- host
 
 // Tokens per chunk: long enough to keep the pieces of long segments rare, short enough that all SMs have work.
@@ -808,7 +1030,7 @@ uint32_t chunk_shift_of(uint64_t n, uint32_t dim) {
 
 // Chunks of the largest call: calls of fewer tokens may have shorter, and so more, chunks.
 uint64_t max_chunks(uint64_t max_tokens, uint32_t dim) {
-    uint64_t most = 0;
+    uint64_t most = max_tokens < kSmallTokens ? (max_tokens >> kSmallShift) + 1 : kSmallChunks;
     for (uint32_t shift = kMinShift; shift <= kMaxShift; ++shift) {
         uint64_t n = shift < kMaxShift ? ((1ull << (kChunkBits + shift)) - 1) / dim : max_tokens;  // the most tokens with such chunks
         if (n > max_tokens) n = max_tokens;
@@ -816,6 +1038,8 @@ uint64_t max_chunks(uint64_t max_tokens, uint32_t dim) {
     }
     return most;
 }
+
+size_t ticket_count(uint32_t dim) { return static_cast<size_t>(kSmallChunks) * ((dim + 511) / 512); }
 
 size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     Carver c(ws);
@@ -835,6 +1059,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     e.d_n_long = c.take<uint32_t>(2);
     e.d_long = c.take<uint4>(chunks);
     e.d_order = c.take<uint32_t>(n);
+    e.d_tickets = c.take<uint32_t>(ticket_count(dim));
     e.d_partial = c.take<float>(chunks * 2 * dim);
     if (h) {
         h->d_status = e.d_status;
@@ -851,6 +1076,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
         h->d_n_long = e.d_n_long;
         h->d_long = e.d_long;
         h->d_order = e.d_order;
+        h->d_tickets = e.d_tickets;
         h->d_partial = e.d_partial;
     }
     return c.used;
@@ -946,51 +1172,8 @@ int launch_after(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cu
     return ADACOMP_OK;
 }
 
-template <typename A, typename B>
-int launch_sums(Sums p, uint32_t out_grid, bool gaps, const adacomp_embed_t* h, cudaStream_t stream) {
-    constexpr int N = kItemElems<A, B>;
-    const bool vec = p.dim % N == 0 && on_grid(p.grad, 16) && out_grid >= 16;
-    p.wide = out_grid >= 32;
-    const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
-    uint32_t x, y;
-    along_row((p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), chunk_bytes, &x, &y, &p.tiles);
-    p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
-    uint32_t zero_blocks = 0;
-    if (gaps) {
-        const uint32_t size = type_size(p.out.type);
-        p.zero_run = 1;
-        while (p.zero_run < kMaxChunk && static_cast<uint64_t>(p.zero_run) * p.dim * size < 32768) p.zero_run *= 2;
-        p.zero_vec = on_grid(p.out, 16) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
-        zero_blocks = static_cast<uint32_t>((p.zero_rows + p.zero_run - 1) / p.zero_run);
-    }
-    if (p.sum_blocks + zero_blocks == 0) return ADACOMP_OK;
-    const dim3 block(x, y);
-    int rc = launch_after(vec ? k_embed_sums<A, B, N> : k_embed_sums<A, B, 1>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
-    if (rc != ADACOMP_OK || p.n_chunks < 2) return rc;              // one chunk: no segment is longer
-    constexpr int kWide = 16 / sizeof(B);
-    const bool join_vec = out_grid >= 16 && p.dim % kWide == 0;
-    return launch_after(join_vec ? k_embed_join<B, kWide> : k_embed_join<B, 1>, dim3(4 * static_cast<uint32_t>(h->n_sms)), dim3(32, kJoinLanes), 0, stream, p);
-}
-
-// Calls f<A, B>() for the types' numbers.
-#define ADACOMP_BY_TYPE(fn, ta, tb, ...)                                                                        \
-    [&]() -> int {                                                                                              \
-        switch ((ta) * 3 + (tb)) {                                                                              \
-            case 0: return fn<float, float>(__VA_ARGS__);                                                       \
-            case 1: return fn<float, __nv_bfloat16>(__VA_ARGS__);                                               \
-            case 2: return fn<float, __half>(__VA_ARGS__);                                                      \
-            case 3: return fn<__nv_bfloat16, float>(__VA_ARGS__);                                               \
-            case 4: return fn<__nv_bfloat16, __nv_bfloat16>(__VA_ARGS__);                                       \
-            case 5: return fn<__nv_bfloat16, __half>(__VA_ARGS__);                                              \
-            case 6: return fn<__half, float>(__VA_ARGS__);                                                      \
-            case 7: return fn<__half, __nv_bfloat16>(__VA_ARGS__);                                              \
-            default: return fn<__half, __half>(__VA_ARGS__);                                                    \
-        }                                                                                                       \
-    }()
-
-// Sorts the call's tokens and finds the segments; fills in what the sums read.  zero: rows to clear on the side, or null.
-int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens, uint32_t n_workers, uint64_t* d_row_begin,
-                const Rows* zero, uint64_t zero_rows, cudaStream_t stream, Sums* p) {
+// What the sort has to do, and what the sums read of it.
+SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens, uint32_t n_workers, uint64_t* d_row_begin, float scale, Sums* p) {
     SortJob j = {};
     j.tokens = tokens;
     j.n = n_tokens * n_workers;
@@ -1018,6 +1201,27 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
     j.row_begin = d_row_begin;
     j.barrier = h->d_barrier;
     j.status = h->d_status;
+    p->order = j.order;
+    p->seg_begin = j.seg_begin;
+    p->seg_key = j.seg_key;
+    p->chunk_seg = j.chunk_seg;
+    p->n_segs = j.n_segs;
+    p->n = j.n;
+    p->chunk_shift = j.chunk_shift;
+    p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
+    p->n_long = h->d_n_long;
+    p->long_list = h->d_long;
+    p->partial = h->d_partial;
+    p->status = h->d_status;
+    p->dim = h->dim;
+    p->vocab = h->vocab;
+    p->tickets = h->d_tickets;
+    p->scale = scale;
+    return j;
+}
+
+// Sorts the call's tokens and finds the segments.  zero: rows to clear on the side, or null.
+int sort_tokens(const adacomp_embed_t* h, SortJob j, const Rows* zero, uint64_t zero_rows, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kSortThreads);
     cfg.stream = stream;
@@ -1037,8 +1241,7 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
         attr[0].val.clusterDim.x = blocks;
         attr[0].val.clusterDim.y = 1;
         attr[0].val.clusterDim.z = 1;
-        cfg.numAttrs = blocks > 1 ? 1 : 0;
-        e = cudaLaunchKernelEx(&cfg, blocks > 1 ? k_embed_sort_cluster<false> : k_embed_sort_cluster<true>, j);
+        e = cudaLaunchKernelEx(&cfg, k_embed_sort_cluster, j);
     } else {
         j.n_blocks = (j.n + 2047) / 2048;
         if (j.n_blocks > kSortBlocks) j.n_blocks = kSortBlocks;
@@ -1058,28 +1261,74 @@ int sort_tokens(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens,
                                     *zero, zero_rows, h->dim, vec);
         if (rc != ADACOMP_OK) return rc;
     }
-    p->order = j.order;
-    p->seg_begin = j.seg_begin;
-    p->seg_key = j.seg_key;
-    p->chunk_seg = j.chunk_seg;
-    p->n_segs = j.n_segs;
-    p->n = j.n;
-    p->chunk_shift = j.chunk_shift;
-    p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
-    p->n_long = h->d_n_long;
-    p->long_list = h->d_long;
-    p->partial = h->d_partial;
-    p->status = h->d_status;
-    p->dim = h->dim;
-    p->vocab = h->vocab;
     return ADACOMP_OK;
 }
 
+template <typename A, typename B>
+int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const adacomp_embed_t* h, cudaStream_t stream) {
+    constexpr int N = kItemElems<A, B>;
+    const bool vec = p.dim % N == 0 && on_grid(p.grad, 16) && out_grid >= 16;
+    p.wide = out_grid >= 32;
+    const uint32_t cols = (p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), size = type_size(p.out.type);
+    p.zero_vec = clear && on_grid(p.out, 16) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
+    if (!clear) p.zero_rows = 0;
+    uint32_t x, y;
+    if (j.n <= kSmallTokens) {
+        along_row(cols, 1, &x, &y, &p.tiles);
+        y = kSmallThreads / x < kSmallLanes ? kSmallThreads / x : kSmallLanes;
+        p.chunk_shift = kSmallShift;
+        p.n_chunks = (j.n + kSmallChunk - 1) / kSmallChunk;
+        uint64_t blocks = static_cast<uint64_t>((p.n_chunks + y - 1) / y) * p.tiles;
+        const uint64_t most = 2 * static_cast<uint64_t>(h->n_sms);
+        if (blocks < 1) blocks = 1;
+        if (blocks > most || (clear && p.zero_rows * p.dim >= most * 4096)) blocks = most;
+        if (vec) k_embed_small<A, B, N><<<static_cast<uint32_t>(blocks), kSmallThreads, 0, stream>>>(j, p, x, y);
+        else k_embed_small<A, B, 1><<<static_cast<uint32_t>(blocks), kSmallThreads, 0, stream>>>(j, p, x, y);
+        ADACOMP_LAUNCH_CHECK();
+        return ADACOMP_OK;
+    }
+    // Rows without a token become zeros.  Few tokens: everything is cleared while they are sorted, and some rows are written
+    // twice; many: the rows that need it are cleared next to the sums.
+    const bool early = clear && j.n <= p.zero_rows / 4, gaps = clear && !early;
+    int rc = sort_tokens(h, j, early ? &p.out : nullptr, p.zero_rows, stream);
+    if (rc != ADACOMP_OK) return rc;
+    const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
+    along_row(cols, chunk_bytes, &x, &y, &p.tiles);
+    p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
+    uint32_t zero_blocks = 0;
+    if (gaps) {
+        p.zero_run = 1;
+        while (p.zero_run < kMaxChunk && static_cast<uint64_t>(p.zero_run) * p.dim * size < 32768) p.zero_run *= 2;
+        zero_blocks = static_cast<uint32_t>((p.zero_rows + p.zero_run - 1) / p.zero_run);
+    }
+    const dim3 block(x, y);
+    rc = launch_after(vec ? k_embed_sums<A, B, N> : k_embed_sums<A, B, 1>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
+    if (rc != ADACOMP_OK || p.n_chunks < 2) return rc;              // one chunk: no segment is longer
+    constexpr int kWide = 16 / sizeof(B);
+    const bool join_vec = out_grid >= 16 && p.dim % kWide == 0;
+    return launch_after(join_vec ? k_embed_join<B, kWide> : k_embed_join<B, 1>, dim3(4 * static_cast<uint32_t>(h->n_sms)), dim3(32, kJoinLanes), 0, stream, p);
+}
+
+// Calls f<A, B>() for the types' numbers.
+#define ADACOMP_BY_TYPE(fn, ta, tb, ...)                                                                        \
+    [&]() -> int {                                                                                              \
+        switch ((ta) * 3 + (tb)) {                                                                              \
+            case 0: return fn<float, float>(__VA_ARGS__);                                                       \
+            case 1: return fn<float, __nv_bfloat16>(__VA_ARGS__);                                               \
+            case 2: return fn<float, __half>(__VA_ARGS__);                                                      \
+            case 3: return fn<__nv_bfloat16, float>(__VA_ARGS__);                                               \
+            case 4: return fn<__nv_bfloat16, __nv_bfloat16>(__VA_ARGS__);                                       \
+            case 5: return fn<__nv_bfloat16, __half>(__VA_ARGS__);                                              \
+            case 6: return fn<__half, float>(__VA_ARGS__);                                                      \
+            case 7: return fn<__half, __nv_bfloat16>(__VA_ARGS__);                                              \
+            default: return fn<__half, __half>(__VA_ARGS__);                                                    \
+        }                                                                                                       \
+    }()
+
 // The largest cluster that fits the device, with the shared memory that the sort's blocks may need.
 cudaError_t prepare_cluster(uint32_t* blocks_out) {
-    cudaError_t e = cudaFuncSetAttribute(k_embed_sort_cluster<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort_cluster<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort_cluster<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaError_t e = cudaFuncSetAttribute(k_embed_sort_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_embed_sort_cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     for (uint32_t blocks = 16; e == cudaSuccess; blocks /= 2) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(blocks);
@@ -1093,7 +1342,7 @@ cudaError_t prepare_cluster(uint32_t* blocks_out) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, k_embed_sort_cluster<false>, &cfg);
+        e = cudaOccupancyMaxActiveClusters(&n, k_embed_sort_cluster, &cfg);
         *blocks_out = blocks;
         if (n > 0 || blocks == 1) break;
     }
@@ -1142,6 +1391,7 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     if (err == cudaSuccess) err = prepare_cluster(&e->cluster);
     if (err == cudaSuccess) err = cudaMemset(e->d_status, 0, sizeof(int));
     if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 2 * sizeof(uint32_t));
+    if (err == cudaSuccess) err = cudaMemset(e->d_tickets, 0, ticket_count(dim) * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaStreamSynchronize(nullptr);
     if (err != cudaSuccess) {
         delete e;
@@ -1183,9 +1433,7 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    rc = sort_tokens(h, k, n_tokens, n_workers, d_row_begin_out, nullptr, 0, stream, &p);
-    if (rc != ADACOMP_OK) return rc;
-    p.scale = scale;
+    const SortJob j = describe(h, k, n_tokens, n_workers, d_row_begin_out, scale, &p);
     p.rows_out = d_rows_out;
     p.values = static_cast<char*>(d_values_out);
     p.idx_out = d_idx_out;
@@ -1193,7 +1441,7 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     uint64_t grid = reinterpret_cast<uintptr_t>(d_values_out) | static_cast<uint64_t>(h->dim) * type_size(values_type);
     if (d_idx_out) grid |= reinterpret_cast<uintptr_t>(d_idx_out) | static_cast<uint64_t>(h->dim) * 4;
     const uint32_t out_grid = grid % 32 == 0 ? 32 : grid % 16 == 0 ? 16 : 1;
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, p, out_grid, false, h, stream);
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, values_type, j, p, out_grid, false, h, stream);
 }
 
 int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens, uint32_t n_workers,
@@ -1211,18 +1459,12 @@ int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, u
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    // Rows without a token become zeros.  Few tokens: everything is cleared by the SMs that do not sort, and some rows are
-    // written twice; many: the rows that need it are cleared next to the sums.
-    const uint64_t n_rows = static_cast<uint64_t>(n_workers) * h->vocab;
-    const bool early = !accumulate && n <= n_rows / 4;
-    rc = sort_tokens(h, k, n_tokens, n_workers, nullptr, early ? &p.out : nullptr, n_rows, stream, &p);
-    if (rc != ADACOMP_OK) return rc;
-    p.scale = scale;
+    const SortJob j = describe(h, k, n_tokens, n_workers, nullptr, scale, &p);
     p.dense = 1;
     p.accumulate = accumulate != 0;
-    p.zero_rows = n_rows;
+    p.zero_rows = static_cast<uint64_t>(n_workers) * h->vocab;
     const uint32_t out_grid = on_grid(p.out, 32) ? 32 : on_grid(p.out, 16) ? 16 : 1;
-    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, p, out_grid, !accumulate && !early, h, stream);
+    return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, j, p, out_grid, !accumulate, h, stream);
 }
 
 int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {
