@@ -70,38 +70,42 @@ __device__ __forceinline__ uint32_t load_token(const Rows& tokens, uint32_t t, u
 
 // ---------------------------------------------------------------------------------------------- lookup
 
-// Threads of a block: x along a row, y over rows.
-template <typename A, typename B, int N>
-__global__ void __launch_bounds__(kThreads) k_embed_lookup(Rows table, Rows tokens, Rows out, uint32_t n_tokens, uint32_t vocab,
-                                                            uint32_t dim, float scale, int* status) {
-    const uint32_t t = blockIdx.x * blockDim.y + threadIdx.y;
-    if (t >= n_tokens) return;
-    const uint32_t v = load_token(tokens, t, vocab);
-    B* dst = reinterpret_cast<B*>(out.data) + out.offset(t);
-    const A* src = reinterpret_cast<const A*>(table.data) + static_cast<uint64_t>(v) * table.row_stride;
-    if (v == 0xFFFFFFFFu && threadIdx.x == 0) record_error(status, ADACOMP_ERR_INVALID);
-    for (uint32_t c = (blockIdx.y * blockDim.x + threadIdx.x) * N; c < dim; c += gridDim.y * blockDim.x * N) {
+// Threads of a block: x along a row (in `tiles` blocks), y over rows; a thread copies the same columns of R tokens, all of them
+// on their way before the first is stored.
+template <typename A, typename B, int N, int R>
+__global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, Rows out, uint32_t n_tokens, uint32_t vocab, uint32_t dim,
+                                                       uint32_t tiles, int wide, float scale, int* status) {
+    const uint32_t t0 = blockIdx.x / tiles * (blockDim.y * R) + threadIdx.y, tile = blockIdx.x % tiles;
+    const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
+    uint32_t v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t t = t0 + r * blockDim.y;
+        v[r] = t < n_tokens ? load_token(tokens, t, vocab) : 0xFFFFFFFFu;
+    }
+    Packed<A, N> row[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (v[r] != 0xFFFFFFFFu && c < dim) row[r].load(reinterpret_cast<const A*>(table.data) + v[r] * table.row_stride + c);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t t = t0 + r * blockDim.y;
+        if (t >= n_tokens || c >= dim) continue;
         float f[N];
+        if (v[r] != 0xFFFFFFFFu) {
+            row[r].unpack(f);
 #pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = 0.f;
-        if (v != 0xFFFFFFFFu) {
-            if constexpr (N > 1) {
-                Packed<A, N> p;
-                p.load(src + c);
-                p.unpack(f);
-            } else {
-                f[0] = to_float(src[c]);
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) f[j] = __fmul_rn(f[j], scale);
-        }
-        if constexpr (N > 1) {
-            Packed<B, N> q;
-            q.pack(f);
-            q.store(dst + c);
+            for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
         } else {
-            dst[c] = from_float<B>(f[0]);
+            if (c == 0) record_error(status, ADACOMP_ERR_INVALID);
+#pragma unroll
+            for (int k = 0; k < N; ++k) f[k] = 0.f;
         }
+        Packed<B, N> q;
+        q.pack(f);
+        B* dst = reinterpret_cast<B*>(out.data) + out.offset(t) + c;
+        if (Packed<B, N>::kVecs == 2 && wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
+        else q.store(dst);
     }
 }
 
@@ -629,7 +633,7 @@ template <int N> __device__ __forceinline__ void put_piece(float* dst, const flo
 
 // Sums of one chunk's tokens: s_src says where their rows start and which of them end a segment, s_dst where the segments'
 // results go.  `slot` is the first token's segment, u0 the first one that begins in the chunk.
-template <typename A, typename B, int N>
+template <typename A, typename B, int N, int BATCH>
 __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, const uint64_t* s_dst, uint32_t len, uint32_t slot, uint32_t u0,
                                           uint32_t chunk, uint32_t c) {
     float sum[N];
@@ -637,9 +641,7 @@ __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, 
     for (int k = 0; k < N; ++k) sum[k] = 0.f;
     const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
     bool open = false;
-    // kBatch rows in flight per thread.  Fetching the next batch before the last is added costs the registers of a block per SM
-    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
-    constexpr int kBatch = N * sizeof(A) == 32 ? 2 : 4;
+    constexpr int kBatch = N * sizeof(A) == 32 ? BATCH / 2 : BATCH;         // rows in flight
     for (uint32_t i = 0; i < len; i += kBatch) {
         Packed<A, N> v[kBatch];
 #pragma unroll
@@ -698,7 +700,12 @@ __device__ __forceinline__ Share share_of(uint64_t i0, uint32_t size, uint32_t l
 // added up by k_embed_join.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
 // depends on the tokens alone.  A thread keeps N columns; x runs along the row, y over chunks.
 template <typename A, typename B, int N>
-__global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
+#ifdef V_MR
+__global__ void __maxnreg__(V_MR) k_embed_sums
+#else
+__global__ void __launch_bounds__(512) k_embed_sums
+#endif
+(const Sums p) {
     extern __shared__ uint64_t s_mem[];
     cudaGridDependencySynchronize();
     if (*p.status == ADACOMP_ERR_TIMEOUT) return;           // the sort gave up: its lists are not to be followed
@@ -731,7 +738,9 @@ __global__ void __launch_bounds__(512) k_embed_sums(const Sums p) {
         p.long_list[many ? p.n_chunks - 1 - e : e] = make_uint4(chunk, s.u1 - 1, pieces, 0u);
     }
     __syncthreads();
-    if (c < p.dim) sum_chunk<A, B, N>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
+    // Four rows in flight per thread.  Fetching the next four before the last are added costs the registers of a block per SM
+    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
+    if (c < p.dim) sum_chunk<A, B, N, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
 }
 
 // The long segments: their pieces, in order.  32 N columns of a segment are one job; with few pieces a warp does it, with many
@@ -948,7 +957,9 @@ template <typename A, typename B, int N>
 __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
     __shared__ SmallMem m;
     sort_small(j, m);
-    if (blockIdx.x == 0 && j.row_begin) {
+    if (blockIdx.x == 0 && j.row_begin && j.n_workers == 1) {
+        if (threadIdx.x < 2) j.row_begin[threadIdx.x] = threadIdx.x ? m.n_segs : 0;
+    } else if (blockIdx.x == 0 && j.row_begin) {
         for (uint32_t w = threadIdx.x; w <= j.n_workers; w += kSmallThreads) {
             uint32_t lo = 0, hi = m.n_segs;
             while (lo < hi) {
@@ -980,7 +991,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, 
             }
         }
         __syncthreads();
-        if (c < p.dim) sum_chunk<A, B, N>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
+        if (c < p.dim) sum_chunk<A, B, N, 8>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
         __syncthreads();
         if (!m.any_long) continue;
         // whose piece was the last of its segment
@@ -1120,25 +1131,6 @@ bool on_grid(const Rows& r, uint32_t bytes) {
            (r.group == 0 || r.group_stride * size % bytes == 0);
 }
 
-uint32_t threads_along(uint32_t dim, uint32_t n) {
-    uint32_t x = 32;
-    while (x < kThreads && x * n < dim) x *= 2;
-    return x;
-}
-
-template <typename A, typename B>
-int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h,
-                  float scale, cudaStream_t stream) {
-    constexpr int N = kItemElems<A, B>;
-    const bool vec = h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16);
-    const uint32_t x = threads_along(h->dim, vec ? N : 1), y = kThreads / x;
-    const dim3 grid((n_tokens + y - 1) / y), block(x, y);
-    if (vec) k_embed_lookup<A, B, N><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, scale, h->d_status);
-    else k_embed_lookup<A, B, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, scale, h->d_status);
-    ADACOMP_LAUNCH_CHECK();
-    return ADACOMP_OK;
-}
-
 // Threads of a sum's block along a row of `cols` threads' worth of work, chunks of a block, and blocks along the row.
 void along_row(uint32_t cols, uint32_t chunk_bytes, uint32_t* x, uint32_t* y, uint32_t* tiles) {
     if (cols <= 16) {
@@ -1151,6 +1143,35 @@ void along_row(uint32_t cols, uint32_t chunk_bytes, uint32_t* x, uint32_t* y, ui
     }
     *y = *x >= 256 ? 1 : 256 / *x;
     while (*y > 1 && *y * chunk_bytes > 32 * 1024) *y /= 2;
+}
+
+template <typename A, typename B, int N>
+int launch_lookup_vec(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h, float scale,
+                      cudaStream_t stream) {
+    uint32_t x, y, tiles;
+    const uint32_t cols = (h->dim + N - 1) / N;
+    along_row(cols, 1, &x, &y, &tiles);
+    const dim3 block(x, y);
+    const int wide = on_grid(out, 32);
+    // four tokens per thread once that still leaves every SM two thousand threads
+    if (static_cast<uint64_t>(n_tokens) * cols >= 4ull * 2048 * h->n_sms) {
+        const uint64_t grid = (static_cast<uint64_t>(n_tokens) + 4 * y - 1) / (4 * y) * tiles;
+        if (grid > 0x7FFFFFFFull) return ADACOMP_ERR_INVALID;
+        k_embed_lookup<A, B, N, 4><<<static_cast<uint32_t>(grid), block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
+    } else {
+        const uint32_t grid = (n_tokens + y - 1) / y * tiles;
+        k_embed_lookup<A, B, N, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
+    }
+    ADACOMP_LAUNCH_CHECK();
+    return ADACOMP_OK;
+}
+
+template <typename A, typename B>
+int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h,
+                  float scale, cudaStream_t stream) {
+    constexpr int N = kItemElems<A, B>;
+    if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16)) return launch_lookup_vec<A, B, N>(table, tokens, out, n_tokens, h, scale, stream);
+    return launch_lookup_vec<A, B, 1>(table, tokens, out, n_tokens, h, scale, stream);
 }
 
 // A launch whose blocks may line up while the kernel before it ends; they wait for it themselves.
