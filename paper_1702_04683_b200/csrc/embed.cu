@@ -27,11 +27,10 @@ struct adacomp_embed {
     uint32_t* d_seg_key;            // [max_tokens]
     uint32_t* d_chunk_seg;          // [chunks + 1] how many segments begin before the chunk
     uint32_t* d_n_segs;             // [2] distinct tokens, and how many tokens of the sorted list have a gradient
-    uint32_t* d_n_long;             // [2] how many segments are longer than a chunk
-    uint4* d_long;                  // [chunks] those
     uint32_t* d_order;              // [max_tokens] positions in the order of the sort
     uint32_t cluster;               // blocks of the largest cluster that the device takes
-    uint32_t* d_tickets;            // [kSmallChunks][blocks along a row]
+    uint32_t* d_tickets;            // [levels][chunks][2][blocks along a row], all zero between calls
+    uint32_t chunks;                // the most that a call has
     float* d_partial;               // [chunks][2][dim] sums of pieces of those
 };
 
@@ -45,7 +44,7 @@ constexpr uint32_t kStep = kSortThreads * kItems;
 constexpr uint32_t kSortBlocks = 64;
 constexpr int kDigitBits = 9;
 constexpr int kMaxBins = 1 << kDigitBits;
-constexpr uint32_t kClusterSmem = 2 * kStep * 4 + 16 * kMaxBins * 4 + kSortWarps * kMaxBins * 2;
+constexpr uint32_t kClusterSmem = 2 * kStep * 4 + 16 * kMaxBins * 2 + kSortWarps * kMaxBins * 2;
 constexpr uint32_t kSpinLimit = 1u << 22;                   // polls of a barrier, some seconds
 
 // Device view of adacomp_rows_t.
@@ -70,42 +69,49 @@ __device__ __forceinline__ uint32_t load_token(const Rows& tokens, uint32_t t, u
 
 // ---------------------------------------------------------------------------------------------- lookup
 
-// Threads of a block: x along a row (in `tiles` blocks), y over rows; a thread copies the same columns of R tokens, all of them
-// on their way before the first is stored.
-template <typename A, typename B, int N, int R>
+// Threads of a block: x along a row (in `tiles` blocks), y over rows.  A thread copies the same columns of R tokens (K groups
+// of N columns, as the sums below), all of them on their way before the first is stored.
+template <typename A, typename B, int N, int K, int R>
 __global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, Rows out, uint32_t n_tokens, uint32_t vocab, uint32_t dim,
                                                        uint32_t tiles, int wide, float scale, int* status) {
     const uint32_t t0 = blockIdx.x / tiles * (blockDim.y * R) + threadIdx.y, tile = blockIdx.x % tiles;
-    const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
+    const uint32_t step = blockDim.x * N, c = tile * K * step + threadIdx.x * N;
     uint32_t v[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const uint32_t t = t0 + r * blockDim.y;
         v[r] = t < n_tokens ? load_token(tokens, t, vocab) : 0xFFFFFFFFu;
     }
-    Packed<A, N> row[R];
+    Packed<A, N> row[R][K];
 #pragma unroll
     for (int r = 0; r < R; ++r)
-        if (v[r] != 0xFFFFFFFFu && c < dim) row[r].load(reinterpret_cast<const A*>(table.data) + v[r] * table.row_stride + c);
+#pragma unroll
+        for (int g = 0; g < K; ++g)
+            if (v[r] != 0xFFFFFFFFu && c + g * step < dim)
+                row[r][g].load(reinterpret_cast<const A*>(table.data) + v[r] * table.row_stride + c + g * step);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const uint32_t t = t0 + r * blockDim.y;
-        if (t >= n_tokens || c >= dim) continue;
-        float f[N];
-        if (v[r] != 0xFFFFFFFFu) {
-            row[r].unpack(f);
-#pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
-        } else {
-            if (c == 0) record_error(status, ADACOMP_ERR_INVALID);
-#pragma unroll
-            for (int k = 0; k < N; ++k) f[k] = 0.f;
-        }
-        Packed<B, N> q;
-        q.pack(f);
+        if (t >= n_tokens) continue;
+        if (v[r] == 0xFFFFFFFFu && c == 0) record_error(status, ADACOMP_ERR_INVALID);
         B* dst = reinterpret_cast<B*>(out.data) + out.offset(t) + c;
-        if (Packed<B, N>::kVecs == 2 && wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
-        else q.store(dst);
+#pragma unroll
+        for (int g = 0; g < K; ++g) {
+            if (c + g * step >= dim) continue;
+            float f[N];
+            if (v[r] != 0xFFFFFFFFu) {
+                row[r][g].unpack(f);
+#pragma unroll
+                for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) f[k] = 0.f;
+            }
+            Packed<B, N> q;
+            q.pack(f);
+            if (Packed<B, N>::kVecs == 2 && wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
+            else q.store(dst + g * step);
+        }
     }
 }
 
@@ -120,7 +126,7 @@ struct SortJob {
     uint32_t* pos[2];
     uint32_t* table;
     uint32_t *order;                                        // the sorted tokens' positions, kLast set where a segment ends
-    uint32_t *seg_begin, *seg_key, *n_segs, *chunk_seg, *n_long;
+    uint32_t *seg_begin, *seg_key, *n_segs, *chunk_seg;
     uint32_t chunk_shift;
     uint32_t share_shift;                                   // cluster form: log2 of the tokens of a block
     uint64_t* row_begin;                                    // or null
@@ -177,26 +183,37 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s_warp, u
     return __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u) + upto - v;
 }
 
-__device__ __forceinline__ void zero_row(const Rows& out, uint64_t row, uint32_t dim, bool vec, uint32_t tid, uint32_t n_threads) {
+// Rows [r, stop) become zeros; where the table's rows follow each other without gaps, as one stretch of memory.
+__device__ __forceinline__ void clear_rows(const Rows& out, uint64_t r, uint64_t stop, uint32_t dim, bool vec, uint32_t tid, uint32_t n_threads) {
     const uint32_t size = type_size(out.type);
-    char* dst = out.data + out.offset(static_cast<uint32_t>(row)) * size;
-    if (vec) {
-        for (uint32_t c = tid; c < dim * size / 16; c += n_threads) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
-    } else if (size == 4) {
-        for (uint32_t c = tid; c < dim; c += n_threads) reinterpret_cast<uint32_t*>(dst)[c] = 0u;
-    } else {
-        for (uint32_t c = tid; c < dim; c += n_threads) reinterpret_cast<uint16_t*>(dst)[c] = 0;
+    while (r < stop) {
+        uint64_t end = r + 1;
+        if (out.row_stride == dim) {
+            end = stop;
+            if (out.group && (r / out.group + 1) * out.group < end) end = (r / out.group + 1) * out.group;
+        }
+        char* dst = out.data + out.offset(static_cast<uint32_t>(r)) * size;
+        const uint64_t bytes = (end - r) * dim * size;
+        if (vec) {
+            for (uint64_t c = tid * 16; c < bytes; c += n_threads * 16) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0u, 0u, 0u, 0u);
+        } else if (size == 4) {
+            for (uint64_t c = tid * 4; c < bytes; c += n_threads * 4) *reinterpret_cast<uint32_t*>(dst + c) = 0u;
+        } else {
+            for (uint64_t c = tid * 2; c < bytes; c += n_threads * 2) *reinterpret_cast<uint16_t*>(dst + c) = 0;
+        }
+        r = end;
     }
 }
 
-// Clears a table while the tokens are being sorted on other SMs.  It needs nothing of the sort, but the sums wait for this
+// Clears rows while the tokens are being sorted on other SMs.  It needs nothing of the sort, but the sums wait for this
 // kernel alone, so it ends after the sort.
 __global__ void __launch_bounds__(kThreads) k_embed_clear(Rows out, uint64_t n_rows, uint32_t dim, int vec) {
-    for (uint64_t r = blockIdx.x; r < n_rows; r += gridDim.x) zero_row(out, r, dim, vec != 0, threadIdx.x, kThreads);
+    clear_rows(out, n_rows * blockIdx.x / gridDim.x, n_rows * (blockIdx.x + 1) / gridDim.x, dim, vec != 0, threadIdx.x, kThreads);
     cudaGridDependencySynchronize();
 }
 
-// Lanes of the warp that hold the same digit (of at most kDigitBits bits), among the real ones or among the others.
+// Lanes of the warp that hold the same digit (of at most kDigitBits bits), among the real ones or among the others.  (The
+// hardware's match instruction is no faster: 19.5 against 19.1 us for the sort of 32768 tokens.)
 __device__ __forceinline__ uint32_t same_digit(uint32_t d, bool real) {
     const uint32_t all = __ballot_sync(0xFFFFFFFFu, real);
     uint32_t same = real ? all : ~all;
@@ -222,6 +239,23 @@ __device__ __forceinline__ uint32_t counts_to_places(uint16_t* s_count, uint32_t
     }
     return sum;
 }
+
+// The same for digits 2 d and 2 d + 1 at once, in the halves of a word.
+__device__ __forceinline__ uint32_t pair_counts_to_places(uint32_t* s_count, uint32_t pairs, uint32_t d) {
+    uint32_t c[kSortWarps];
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) c[w] = s_count[w * pairs + d];
+    uint32_t sum = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) {
+        s_count[w * pairs + d] = sum;
+        sum += c[w];
+    }
+    return sum;
+}
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // Sorted token i with key k between `last` and `next`, and its place in the lists that the sums read; `u` segments begin
 // before it.
@@ -253,9 +287,8 @@ __device__ __forceinline__ void put_segment(const SortJob& j, uint64_t i, uint32
         for (uint32_t v = w + 1; v <= j.n_workers; ++v) j.row_begin[v] = n_segs;
 }
 
-// Block 0: the lists of a call without a token that has a gradient, and what the sums count up from zero.
+// Block 0: the lists of a call without a token that has a gradient.
 __device__ __forceinline__ void put_empty(const SortJob& j, bool nothing) {
-    if (threadIdx.x < 2) j.n_long[threadIdx.x] = 0;
     if (!nothing) return;
     if (threadIdx.x < 2) j.n_segs[threadIdx.x] = 0;
     if (j.row_begin)
@@ -410,13 +443,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     __shared__ uint32_t s_warp[32];
     cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
     cudaTriggerProgrammaticLaunchCompletion();
+    cluster_arrive();
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t n_ranks = gridDim.x, me = blockIdx.x;    // one cluster
     const uint32_t share = 1u << j.share_shift, items = share / kSortThreads;
     uint64_t* s_tok = s_mem64;                                                  // [share] key and position
     const uint32_t bins = 1u << j.bits, mask = bins - 1;
-    uint32_t* s_all = reinterpret_cast<uint32_t*>(s_tok + share);               // [n_ranks][bins] the blocks' counts
-    uint16_t* s_count = reinterpret_cast<uint16_t*>(s_all + n_ranks * bins);    // [kSortWarps][bins]
+    const uint32_t pairs = bins / 2;                                            // digits are counted in 16 bits, two to a word
+    uint32_t* s_all = reinterpret_cast<uint32_t*>(s_tok + share);               // [n_ranks][pairs] the blocks' counts
+    uint16_t* s_count = reinterpret_cast<uint16_t*>(s_all + n_ranks * pairs);   // [kSortWarps][bins]
     uint16_t* mine = s_count + warp * bins;
     const uint32_t from = me << j.share_shift;
     const uint32_t n_here = j.n > from ? (j.n - from < share ? j.n - from : share) : 0;
@@ -430,10 +465,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         if (i >= items || t >= n_here) continue;
         tok[i] = static_cast<uint64_t>(load_key(j, from + t, true)) << 32 | (from + t);
     }
-    cluster.sync();                             // every block has started: its shared memory may be written from here on
+    cluster_wait();                             // every block has started: its shared memory may be written from here on
     for (int pass = 0; pass < j.passes; ++pass) {
         const int shift = 32 + pass * j.bits;
-        for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
+        for (uint32_t d = lane; d < pairs; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
         if (pass > 0) {
 #pragma unroll
             for (int i = 0; i < kItems; ++i)
@@ -454,22 +489,28 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
             __syncwarp();
         }
         __syncthreads();
-        uint32_t all = 0, before = 0, total;
-        if (tid < bins) {
-            all = counts_to_places(s_count, bins, tid);
-            for (uint32_t r = 0; r < n_ranks; ++r) cluster.map_shared_rank(s_all, r)[me * bins + tid] = all;
+        if (tid < pairs) {
+            const uint32_t both = pair_counts_to_places(reinterpret_cast<uint32_t*>(s_count), pairs, tid);
+            for (uint32_t r = 0; r < n_ranks; ++r) cluster.map_shared_rank(s_all, r)[me * pairs + tid] = both;
         }
         cluster.sync();                         // the counts have arrived, and every block has its tokens in registers
-        if (tid < bins) {
-            all = 0;
+        uint32_t all[2] = {0, 0}, before[2] = {0, 0}, total;
+        if (tid < pairs) {
             for (uint32_t r = 0; r < n_ranks; ++r) {
-                const uint32_t c = s_all[r * bins + tid];
-                all += c;
-                if (r < me) before += c;
+                const uint32_t c = s_all[r * pairs + tid];
+                all[0] += c & 0xFFFFu;
+                all[1] += c >> 16;
+                if (r < me) {
+                    before[0] += c & 0xFFFFu;
+                    before[1] += c >> 16;
+                }
             }
         }
-        const uint32_t base = block_before(all, s_warp, &total) + before;
-        if (tid < bins) s_base[tid] = base;
+        const uint32_t base = block_before(all[0] + all[1], s_warp, &total);
+        if (tid < pairs) {
+            s_base[2 * tid] = base + before[0];
+            s_base[2 * tid + 1] = base + all[0] + before[1];
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
@@ -501,6 +542,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     uint32_t u = __shfl_sync(0xFFFFFFFFu, block_before(lane == 0 ? in_warp : 0u, s_warp, &segs_here), 0);
     if (tid < n_ranks) cluster.map_shared_rank(s_all, tid)[me] = segs_here;
     cluster.sync();
+    cluster_arrive();                           // no more reads of the neighbours' shared memory
     for (uint32_t r = 0; r < me; ++r) u += s_all[r];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
@@ -516,7 +558,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         u += __popc(heads[i]);
     }
     if (me == 0) put_empty(j, j.n == 0 || s_key[0] == j.none);
-    cluster.sync();                             // nobody leaves while a neighbour may still read here
+    cluster_wait();                             // nobody leaves while a neighbour may still read here
 }
 
 // ---------------------------------------------------------------------------------------------- sums
@@ -526,10 +568,9 @@ struct Sums {
     uint32_t n, n_chunks, chunk_shift;
     uint32_t tiles;                 // blocks along a row
     uint32_t sum_blocks;            // the blocks behind them write zeros
-    uint32_t* n_long;               // [2] segments of a few pieces, and of many
-    uint4* long_list;               // first chunk, segment, pieces
     float* partial;
-    uint32_t* tickets;              // [kSmallChunks][tiles], all zero between calls
+    uint32_t* tickets;              // [levels][max_chunks][2][tiles]
+    uint32_t max_chunks;
     const int* status;
     Rows grad;
     uint32_t dim, vocab;
@@ -542,14 +583,13 @@ struct Sums {
     // dense form
     int dense, accumulate;
     Rows out;
-    uint64_t zero_rows;             // rows to look at for zeros, zero_run of them per block
-    uint32_t zero_run;
+    uint64_t zero_first, zero_rows; // rows that become zeros where they have no token: zero_first .. zero_rows - 1
     int zero_vec;
     int wide;                       // rows of the results start on 32-byte boundaries
 };
 
-constexpr uint32_t kMaxChunk = 64;
-constexpr uint32_t kFewPieces = 16;             // a warp adds them alone
+constexpr int kSumThreads = 288;               // a warp more than 256: rows of 257 .. 288 threads' width stay in one block
+constexpr uint32_t kFanBits = 4, kFan = 1u << kFanBits;      // pieces that one block adds up
 constexpr uint64_t kEnds = 1ull << 63;          // flag of a token that is its segment's last
 
 // A finished sum goes to its row: `slot` counts segments, `at` is where the row starts in the dense table.
@@ -594,27 +634,41 @@ __device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t a
     }
 }
 
-// Rows without a token, a run of them per block: which of them have one is looked up in the sorted list.
-__device__ void zero_gaps(const Sums& p, uint32_t block) {
-    __shared__ uint32_t s_has[kMaxChunk / 32];
-    const uint32_t n_segs = *p.n_segs;
-    const uint64_t from = static_cast<uint64_t>(block) * p.zero_run;
-    const uint64_t to = from + p.zero_run < p.zero_rows ? from + p.zero_run : p.zero_rows;
-    const uint32_t tid = threadIdx.y * blockDim.x + threadIdx.x, n_threads = blockDim.x * blockDim.y;
-    if (tid < kMaxChunk / 32) s_has[tid] = 0;
-    uint32_t lo = 0, hi = n_segs;               // first segment whose key is not below `from`
+// First of the n ascending keys that is not below `bound`, by a whole warp: 32 probes a step (one at a time, 17 steps to the L2
+// and back took longer than the clearing they were for).
+__device__ __forceinline__ uint32_t warp_lower_bound(const uint32_t* keys, uint32_t n, uint64_t bound) {
+    const uint32_t lane = threadIdx.x + threadIdx.y * blockDim.x & 31;
+    uint32_t lo = 0, hi = n;
     while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (p.seg_key[mid] < from) lo = mid + 1; else hi = mid;
+        const uint32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+        const uint32_t below = __popc(__ballot_sync(0xFFFFFFFFu, at < hi && keys[at] < bound));
+        if (below == 0) return lo;
+        lo += (below - 1) * step + 1;
+        if (lo + step - 1 < hi) hi = lo + step - 1;
     }
-    __syncthreads();
-    for (uint32_t k = tid; k < p.zero_run && lo + k < n_segs; k += n_threads) {
-        const uint64_t r = p.seg_key[lo + k];
-        if (r < to) atomicOr(&s_has[(r - from) / 32], 1u << ((r - from) & 31));
+    return lo;
+}
+
+// A block's share of the rows without a token: the stretches between the keys of the sorted list.
+__device__ void zero_gaps(const Sums& p, uint32_t block, uint32_t n_blocks) {
+    constexpr uint32_t kKeys = 64;
+    __shared__ uint32_t s_key[kKeys];
+    const uint32_t n_segs = p.n_segs[0], tid = threadIdx.y * blockDim.x + threadIdx.x, n_threads = blockDim.x * blockDim.y;
+    const uint64_t rows = p.zero_rows - p.zero_first, from = p.zero_first + rows * block / n_blocks, to = p.zero_first + rows * (block + 1) / n_blocks;
+    uint32_t base = warp_lower_bound(p.seg_key, n_segs, from), k = kKeys;
+    for (uint64_t r = from; r < to;) {
+        if (k == kKeys) {
+            __syncthreads();
+            if (tid < kKeys) s_key[tid] = base + tid < n_segs ? p.seg_key[base + tid] : 0xFFFFFFFFu;
+            __syncthreads();
+            base += kKeys;
+            k = 0;
+        }
+        const uint64_t next = s_key[k] < to ? s_key[k] : to;
+        clear_rows(p.out, r, next, p.dim, p.zero_vec != 0, tid, n_threads);
+        r = next + 1;
+        ++k;
     }
-    __syncthreads();
-    for (uint64_t r = from; r < to; ++r)
-        if (!(s_has[(r - from) / 32] >> ((r - from) & 31) & 1)) zero_row(p.out, r, p.dim, p.zero_vec != 0, tid, n_threads);
 }
 
 // Piece of a long segment that chunk `chunk` has summed: the one that begins in front of the chunk (0), or in it (1).
@@ -632,44 +686,61 @@ template <int N> __device__ __forceinline__ void put_piece(float* dst, const flo
 }
 
 // Sums of one chunk's tokens: s_src says where their rows start and which of them end a segment, s_dst where the segments'
-// results go.  `slot` is the first token's segment, u0 the first one that begins in the chunk.
-template <typename A, typename B, int N, int BATCH>
+// results go.  `slot` is the first token's segment, u0 the first one that begins in the chunk.  A thread keeps K groups of N
+// columns, `step` apart: N > 1 and K = 1 where rows sit on the 16-byte grid, N = 1 and K > 1 where they do not (one column at
+// a time would leave too little in flight: rows of 1001 bf16 entries, 32768 tokens, 105 us).
+template <typename A, typename B, int N, int K, int BATCH>
 __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, const uint64_t* s_dst, uint32_t len, uint32_t slot, uint32_t u0,
-                                          uint32_t chunk, uint32_t c) {
-    float sum[N];
+                                          uint32_t chunk, uint32_t c, uint32_t step) {
+    float sum[K][N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) sum[k] = 0.f;
+    for (int g = 0; g < K; ++g)
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[g][q] = 0.f;
     const A* grad = reinterpret_cast<const A*>(p.grad.data) + c;
     bool open = false;
     constexpr int kBatch = N * sizeof(A) == 32 ? BATCH / 2 : BATCH;         // rows in flight
     for (uint32_t i = 0; i < len; i += kBatch) {
-        Packed<A, N> v[kBatch];
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            if (i + k < len) v[k].load(grad + (s_src[i + k] & ~kEnds));
+        Packed<A, N> v[kBatch][K];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             if (i + k >= len) break;
-            float f[N];
-            v[k].unpack(f);
+            const A* src = grad + (s_src[i + k] & ~kEnds);
 #pragma unroll
-            for (int q = 0; q < N; ++q) sum[q] = __fadd_rn(sum[q], f[q]);
+            for (int g = 0; g < K; ++g)
+                if (g == 0 || c + g * step < p.dim) v[k][g].load(src + g * step);
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (i + k >= len) break;
+#pragma unroll
+            for (int g = 0; g < K; ++g) {
+                float f[N];
+                v[k][g].unpack(f);
+#pragma unroll
+                for (int q = 0; q < N; ++q) sum[g][q] = __fadd_rn(sum[g][q], f[q]);
+            }
             open = true;
-            if (s_src[i + k] & kEnds) {
-                if (slot + 1 == u0) {           // the last piece of a long segment
-                    put_piece<N>(piece_at(p, chunk, 0, c), sum);
-                } else {
-                    const uint64_t at = s_dst[slot - u0];
-                    put_row<B, N>(p, slot, at, static_cast<uint32_t>(at), c, sum);
+            if (!(s_src[i + k] & kEnds)) continue;
+            const bool piece = slot + 1 == u0;          // the last piece of a long segment
+            const uint64_t at = piece ? 0 : s_dst[slot - u0];
+#pragma unroll
+            for (int g = 0; g < K; ++g) {
+                if (g == 0 || c + g * step < p.dim) {
+                    if (piece) put_piece<N>(piece_at(p, chunk, 0, c + g * step), sum[g]);
+                    else put_row<B, N>(p, slot, at, static_cast<uint32_t>(at), c + g * step, sum[g]);
                 }
 #pragma unroll
-                for (int q = 0; q < N; ++q) sum[q] = 0.f;
-                ++slot;
-                open = false;
+                for (int q = 0; q < N; ++q) sum[g][q] = 0.f;
             }
+            ++slot;
+            open = false;
         }
     }
-    if (open) put_piece<N>(piece_at(p, chunk, slot + 1 == u0 ? 0 : 1, c), sum);     // a piece that goes on in the next chunk
+    if (!open) return;
+#pragma unroll
+    for (int g = 0; g < K; ++g)                         // a piece that goes on in the next chunk
+        if (g == 0 || c + g * step < p.dim) put_piece<N>(piece_at(p, chunk, slot + 1 == u0 ? 0 : 1, c + g * step), sum[g]);
 }
 
 // What a chunk has to do.
@@ -695,22 +766,105 @@ __device__ __forceinline__ Share share_of(uint64_t i0, uint32_t size, uint32_t l
     return s;
 }
 
+// The pieces of long segments that a chunk has just delivered: the one it begins with (0) and the one it ends with (1).  The block
+// that delivers the last of kFan consecutive pieces adds them up, in order, in the place of the first, and delivers that sum
+// as a piece of the next level, until the segment is one.  So nobody waits, the tree of additions is fixed, and a segment of
+// any length costs a few turns.  The whole block takes part.
+struct Pieces {
+    uint32_t head[2], count[2], seg[2];     // chunk in which the segment begins, its chunks (0: no piece), its number
+};
+template <typename Begin>
+__device__ __forceinline__ Pieces pieces_of(const Share& s, uint32_t chunk, uint32_t shift, const Begin& seg_begin) {
+    Pieces x = {{0, chunk}, {0, 0}, {s.u0 - 1, s.u1 - 1}};
+    if (s.lead) {
+        x.head[0] = seg_begin[s.u0 - 1] >> shift;
+        x.count[0] = ((seg_begin[s.u0] - 1) >> shift) - x.head[0] + 1;
+    }
+    if (s.trail) x.count[1] = ((seg_begin[s.u1] - 1) >> shift) - chunk + 1;
+    return x;
+}
+template <typename B, int N, int K>
+__device__ __forceinline__ void finish_long(const Sums& p, const Pieces& x, uint32_t chunk, uint32_t tile, uint32_t c, uint32_t step, bool leader,
+                                            const uint32_t* seg_key, uint32_t* s_last) {
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const uint32_t head = x.head[which];
+        uint32_t count = x.count[which], node = chunk - head, level = 0;
+        bool active = count > 0;
+        while (__syncthreads_or(active)) {
+            const uint32_t parent = node >> kFanBits, width = kFanBits * level;
+            const uint32_t first = head + (parent << (width + kFanBits));                   // chunk of the group's first piece
+            const uint32_t n = active ? (count - parent * kFan < kFan ? count - parent * kFan : kFan) : 0;
+            if (active) __threadfence();
+            __syncthreads();
+            if (leader) {
+                *s_last = 0;
+                if (active) {
+                    uint32_t* ticket = p.tickets + ((static_cast<uint64_t>(level) * p.max_chunks + first) * 2 + (first == head)) * p.tiles + tile;
+                    if (atomicAdd(ticket, 1u) == n - 1) {
+                        *ticket = 0;
+                        *s_last = 1;
+                    }
+                }
+            }
+            __syncthreads();
+            active = active && *s_last;
+            if (!active) continue;
+            __threadfence();
+            const bool whole = count <= kFan;
+#pragma unroll 1
+            for (uint32_t g = 0, col = c; g < K && col < p.dim; ++g, col += step) {
+                float sum[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = 0.f;
+                for (uint32_t q = 0; q < n; q += 4) {
+                    float f[4][N];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t at = first + ((q + r) << width);
+                        const float* src = piece_at(p, at, at == head ? 1 : 0, col);
+                        if constexpr (N % 4 == 0) {
+#pragma unroll
+                            for (int k = 0; k < N; k += 4) {
+                                const float4 v = q + r < n ? __ldcg(reinterpret_cast<const float4*>(src + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                                f[r][k] = v.x; f[r][k + 1] = v.y; f[r][k + 2] = v.z; f[r][k + 3] = v.w;
+                            }
+                        } else {
+                            f[r][0] = q + r < n ? __ldcg(src) : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (q + r < n)
+#pragma unroll
+                            for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], f[r][k]);
+                }
+                if (whole) {
+                    const uint32_t key = seg_key[x.seg[which]];
+                    put_row<B, N>(p, x.seg[which], p.dense ? p.out.offset(key) : 0, key % p.vocab, col, sum);
+                } else {
+                    put_piece<N>(piece_at(p, first, first == head ? 1 : 0, col), sum);
+                }
+            }
+            if (whole) active = false;
+            node = parent;
+            count = (count + kFan - 1) >> kFanBits;
+            ++level;
+        }
+    }
+}
+
 // Sums over the sorted list, cut into chunks of 2^chunk_shift tokens.  A chunk owns the segments that begin in it, to their
 // end even if that lies in the next chunk; a segment longer than a chunk is cut at the chunks' borders, its pieces are
-// added up by k_embed_join.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
+// added up by finish_long.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
 // depends on the tokens alone.  A thread keeps N columns; x runs along the row, y over chunks.
-template <typename A, typename B, int N>
-#ifdef V_MR
-__global__ void __maxnreg__(V_MR) k_embed_sums
-#else
-__global__ void __launch_bounds__(512) k_embed_sums
-#endif
-(const Sums p) {
+template <typename A, typename B, int N, int K>
+__global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(const Sums p) {
     extern __shared__ uint64_t s_mem[];
     cudaGridDependencySynchronize();
     if (*p.status == ADACOMP_ERR_TIMEOUT) return;           // the sort gave up: its lists are not to be followed
     if (blockIdx.x >= p.sum_blocks) {
-        zero_gaps(p, blockIdx.x - p.sum_blocks);
+        zero_gaps(p, blockIdx.x - p.sum_blocks, gridDim.x - p.sum_blocks);
         return;
     }
     const uint32_t size = 1u << p.chunk_shift;
@@ -718,7 +872,7 @@ __global__ void __launch_bounds__(512) k_embed_sums
     uint64_t* s_dst = s_src + 2 * size;                                         // [size] where its segments' rows start
     const uint32_t chunk = blockIdx.x / p.tiles * blockDim.y + threadIdx.y, tile = blockIdx.x % p.tiles;
     const uint32_t n_segs = p.n_segs[0], live = p.n_segs[1];
-    const uint32_t c = (tile * blockDim.x + threadIdx.x) * N;
+    const uint32_t c = (tile * K * blockDim.x + threadIdx.x) * N;
     const uint64_t i0 = static_cast<uint64_t>(chunk) << p.chunk_shift;
     Share s = {};
     if (i0 < live) s = share_of(i0, size, live, p.chunk_seg[chunk], i0 + size < live ? p.chunk_seg[chunk + 1] : n_segs, p.seg_begin);
@@ -731,81 +885,14 @@ __global__ void __launch_bounds__(512) k_embed_sums
         s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
         if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
     }
-    if (s.trail && tile == 0 && threadIdx.x == 0) {        // for k_embed_join: short lists from the front, long ones from the back
-        const uint32_t pieces = ((p.seg_begin[s.u1] - 1) >> p.chunk_shift) - chunk + 1;
-        const bool many = pieces > kFewPieces;
-        const uint32_t e = atomicAdd(p.n_long + many, 1u);
-        p.long_list[many ? p.n_chunks - 1 - e : e] = make_uint4(chunk, s.u1 - 1, pieces, 0u);
-    }
     __syncthreads();
-    // Four rows in flight per thread.  Fetching the next four before the last are added costs the registers of a block per SM
-    // and gains nothing (524288 tokens: 512 -> 529 us for the whole call).
-    if (c < p.dim) sum_chunk<A, B, N, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
-}
-
-// The long segments: their pieces, in order.  32 N columns of a segment are one job; with few pieces a warp does it, with many
-// the block's eight warps take every eighth piece each.  Four pieces are in flight either way.
-constexpr int kJoinLanes = 8;
-template <int N>
-__device__ __forceinline__ void add_pieces(const Sums& p, uint32_t chunk, uint32_t pieces, uint32_t first, uint32_t step, uint32_t c, float (&sum)[N]) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) sum[k] = 0.f;
-    if (c >= p.dim) return;
-    for (uint32_t q0 = first; q0 < pieces; q0 += 4 * step) {
-        float f[4][N];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint32_t q = q0 + r * step;
-            const float* src = piece_at(p, chunk + q, q == 0 ? 1 : 0, c);
-            if constexpr (N % 4 == 0) {
-#pragma unroll
-                for (int k = 0; k < N; k += 4) {
-                    const float4 v = q < pieces ? __ldcg(reinterpret_cast<const float4*>(src + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    f[r][k] = v.x; f[r][k + 1] = v.y; f[r][k + 2] = v.z; f[r][k + 3] = v.w;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < N; ++k) f[r][k] = q < pieces ? __ldcg(src + k) : 0.f;
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (q0 + r * step < pieces)
-#pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], f[r][k]);
-    }
-}
-
-template <typename B, int N>
-__global__ void __launch_bounds__(32 * kJoinLanes) k_embed_join(const Sums p) {
-    __shared__ float s_sum[kJoinLanes][32 * N];
-    cudaGridDependencySynchronize();
-    if (*p.status == ADACOMP_ERR_TIMEOUT) return;
-    const uint32_t few = p.n_long[0], many = p.n_long[1];
-    const uint32_t tiles = (p.dim + 32 * N - 1) / (32 * N);
-    float sum[N];
-    for (uint64_t job = blockIdx.x; job < static_cast<uint64_t>(many) * tiles; job += gridDim.x) {
-        const uint4 seg = p.long_list[p.n_chunks - 1 - job / tiles];
-        const uint32_t c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N, key = p.seg_key[seg.y];
-        add_pieces<N>(p, seg.x, seg.z, threadIdx.y, kJoinLanes, c, sum);
-#pragma unroll
-        for (int k = 0; k < N; ++k) s_sum[threadIdx.y][threadIdx.x * N + k] = sum[k];
-        __syncthreads();
-        if (threadIdx.y == 0 && c < p.dim) {
-            for (int y = 1; y < kJoinLanes; ++y)
-#pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], s_sum[y][threadIdx.x * N + k]);
-            put_row<B, N>(p, seg.y, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
-        }
-        __syncthreads();
-    }
-    for (uint64_t job = static_cast<uint64_t>(blockIdx.x) * kJoinLanes + threadIdx.y; job < static_cast<uint64_t>(few) * tiles;
-         job += static_cast<uint64_t>(gridDim.x) * kJoinLanes) {
-        const uint4 seg = p.long_list[job / tiles];
-        const uint32_t c = (static_cast<uint32_t>(job % tiles) * 32 + threadIdx.x) * N, key = p.seg_key[seg.y];
-        add_pieces<N>(p, seg.x, seg.z, 0, 1, c, sum);
-        if (c < p.dim) put_row<B, N>(p, seg.y, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
-    }
+    // Four rows in flight per thread, 48 registers (five blocks of 256 per SM): 524288 tokens x 2048 in 410 us, 6.2 TB/s with the
+    // pieces of long segments counted.  The next four fetched before the last are added (80 registers): 430; rings of
+    // asynchronous copies to shared memory, eight rows deep: 410.
+    if (c < p.dim) sum_chunk<A, B, N, K, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, blockDim.x * N);
+    if (!__syncthreads_or(s.lead || s.trail)) return;
+    finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0, p.seg_key,
+                         reinterpret_cast<uint32_t*>(s_src));
 }
 
 // ---------------------------------------------------------------------------------------------- few tokens
@@ -829,7 +916,7 @@ struct SmallMem {
     uint32_t seg_begin[kSmallTokens + 1], seg_key[kSmallTokens];
     uint32_t chunk_seg[kSmallChunks + 1];
     uint32_t n_segs, live, any_long;
-    uint32_t done[2 * kSmallLanes];                         // whether a chunk's piece was the last one
+    uint32_t last[kSmallLanes + 1];                         // whether a chunk's piece was the last one of its group
 };
 
 __device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
@@ -924,32 +1011,15 @@ __device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
 // Rows without a token in this block's share of the table: the stretches between two rows that have one.
 __device__ __forceinline__ void clear_small(const Sums& p, const SmallMem& m) {
     const uint64_t from = p.zero_rows * blockIdx.x / gridDim.x, to = p.zero_rows * (blockIdx.x + 1) / gridDim.x;
-    const uint32_t size = type_size(p.out.type);
-    const bool flat = p.out.row_stride == p.dim;
     uint32_t lo = 0, hi = m.n_segs;
     while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
         if (m.seg_key[mid] < from) lo = mid + 1; else hi = mid;
     }
-    for (uint64_t r = from; r < to;) {
-        uint64_t stop = lo < m.n_segs && m.seg_key[lo] < to ? m.seg_key[lo] : to;
-        if (stop == r) {
-            ++lo;
-            ++r;
-            continue;
-        }
-        if (!flat) stop = r + 1;
-        else if (p.out.group && (r / p.out.group + 1) * p.out.group < stop) stop = (r / p.out.group + 1) * p.out.group;
-        char* dst = p.out.data + p.out.offset(static_cast<uint32_t>(r)) * size;
-        const uint64_t bytes = (stop - r) * p.dim * size;
-        if (p.zero_vec) {
-            for (uint64_t c = threadIdx.x * 16; c < bytes; c += kSmallThreads * 16) *reinterpret_cast<uint4*>(dst + c) = make_uint4(0u, 0u, 0u, 0u);
-        } else if (size == 4) {
-            for (uint64_t c = threadIdx.x * 4; c < bytes; c += kSmallThreads * 4) *reinterpret_cast<uint32_t*>(dst + c) = 0u;
-        } else {
-            for (uint64_t c = threadIdx.x * 2; c < bytes; c += kSmallThreads * 2) *reinterpret_cast<uint16_t*>(dst + c) = 0;
-        }
-        r = stop;
+    for (uint64_t r = from; r < to; ++lo) {
+        const uint64_t next = lo < m.n_segs && m.seg_key[lo] < to ? m.seg_key[lo] : to;
+        clear_rows(p.out, r, next, p.dim, p.zero_vec != 0, threadIdx.x, kSmallThreads);
+        r = next + 1;
     }
 }
 
@@ -991,38 +1061,10 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, 
             }
         }
         __syncthreads();
-        if (c < p.dim) sum_chunk<A, B, N, 8>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c);
+        if (c < p.dim) sum_chunk<A, B, N, 1, 8>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, x * N);
         __syncthreads();
         if (!m.any_long) continue;
-        // whose piece was the last of its segment
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x < 2 * kSmallLanes) m.done[threadIdx.x] = 0;
-        __syncthreads();
-        uint32_t head[2] = {0, chunk}, pieces[2] = {0, 0};
-        if (s.lead) head[0] = m.seg_begin[s.u0 - 1] / kSmallChunk, pieces[0] = (m.seg_begin[s.u0] - 1) / kSmallChunk - head[0] + 1;
-        if (s.trail) pieces[1] = (m.seg_begin[s.u1] - 1) / kSmallChunk - chunk + 1;
-        if (tx == 0) {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                if (pieces[q] == 0) continue;
-                uint32_t* ticket = p.tickets + head[q] * p.tiles + tile;
-                if (atomicAdd(ticket, 1u) == pieces[q] - 1) {
-                    *ticket = 0;
-                    m.done[2 * ty + q] = 1;
-                }
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            if (pieces[q] == 0 || !m.done[2 * ty + q] || c >= p.dim) continue;
-            __threadfence();
-            const uint32_t u = q == 0 ? s.u0 - 1 : s.u1 - 1, key = m.seg_key[u];
-            float sum[N];
-            add_pieces<N>(p, head[q], pieces[q], 0, 1, c, sum);
-            put_row<B, N>(p, u, p.dense ? p.out.offset(key) : 0, key % p.vocab, c, sum);
-        }
+        finish_long<B, N, 1>(p, pieces_of(s, chunk, kSmallShift, m.seg_begin), chunk, tile, c, 0, tx == 0 && ty < y, m.seg_key, &m.last[ty < y ? ty : kSmallLanes]);
         __syncthreads();
     }
     if (p.zero_rows) clear_small(p, m);
@@ -1050,7 +1092,11 @@ uint64_t max_chunks(uint64_t max_tokens, uint32_t dim) {
     return most;
 }
 
-size_t ticket_count(uint32_t dim) { return static_cast<size_t>(kSmallChunks) * ((dim + 511) / 512); }
+size_t ticket_count(uint64_t chunks, uint32_t dim) {
+    uint32_t levels = 1;
+    while ((chunks >> (kFanBits * levels)) > 0) ++levels;
+    return static_cast<size_t>(levels) * chunks * 2 * ((dim + 511) / 512);
+}
 
 size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     Carver c(ws);
@@ -1067,10 +1113,8 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     e.d_seg_begin = c.take<uint32_t>(n + 1);
     e.d_seg_key = c.take<uint32_t>(n);
     e.d_chunk_seg = c.take<uint32_t>(chunks + 1);
-    e.d_n_long = c.take<uint32_t>(2);
-    e.d_long = c.take<uint4>(chunks);
     e.d_order = c.take<uint32_t>(n);
-    e.d_tickets = c.take<uint32_t>(ticket_count(dim));
+    e.d_tickets = c.take<uint32_t>(ticket_count(chunks, dim));
     e.d_partial = c.take<float>(chunks * 2 * dim);
     if (h) {
         h->d_status = e.d_status;
@@ -1084,10 +1128,9 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
         h->d_seg_begin = e.d_seg_begin;
         h->d_seg_key = e.d_seg_key;
         h->d_chunk_seg = e.d_chunk_seg;
-        h->d_n_long = e.d_n_long;
-        h->d_long = e.d_long;
         h->d_order = e.d_order;
         h->d_tickets = e.d_tickets;
+        h->chunks = static_cast<uint32_t>(chunks);
         h->d_partial = e.d_partial;
     }
     return c.used;
@@ -1131,36 +1174,35 @@ bool on_grid(const Rows& r, uint32_t bytes) {
            (r.group == 0 || r.group_stride * size % bytes == 0);
 }
 
-// Threads of a sum's block along a row of `cols` threads' worth of work, chunks of a block, and blocks along the row.
-void along_row(uint32_t cols, uint32_t chunk_bytes, uint32_t* x, uint32_t* y, uint32_t* tiles) {
+// Threads of a block along a row of `cols` threads' worth of work (at most `most`), rows of a block, and blocks along the row.
+void along_row(uint32_t cols, uint32_t most, uint32_t* x, uint32_t* y, uint32_t* tiles) {
     if (cols <= 16) {
         *x = 1;
         while (*x < cols) *x *= 2;
         *tiles = 1;
     } else {
-        *tiles = (cols + 511) / 512;
+        *tiles = (cols + most - 1) / most;
         *x = ((cols + *tiles - 1) / *tiles + 31) / 32 * 32;
     }
     *y = *x >= 256 ? 1 : 256 / *x;
-    while (*y > 1 && *y * chunk_bytes > 32 * 1024) *y /= 2;
 }
 
-template <typename A, typename B, int N>
+template <typename A, typename B, int N, int K>
 int launch_lookup_vec(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h, float scale,
                       cudaStream_t stream) {
     uint32_t x, y, tiles;
-    const uint32_t cols = (h->dim + N - 1) / N;
-    along_row(cols, 1, &x, &y, &tiles);
+    const uint32_t cols = (h->dim + N * K - 1) / (N * K);
+    along_row(cols, 512, &x, &y, &tiles);
     const dim3 block(x, y);
     const int wide = on_grid(out, 32);
     // four tokens per thread once that still leaves every SM two thousand threads
     if (static_cast<uint64_t>(n_tokens) * cols >= 4ull * 2048 * h->n_sms) {
         const uint64_t grid = (static_cast<uint64_t>(n_tokens) + 4 * y - 1) / (4 * y) * tiles;
         if (grid > 0x7FFFFFFFull) return ADACOMP_ERR_INVALID;
-        k_embed_lookup<A, B, N, 4><<<static_cast<uint32_t>(grid), block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
+        k_embed_lookup<A, B, N, K, 4><<<static_cast<uint32_t>(grid), block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
     } else {
         const uint32_t grid = (n_tokens + y - 1) / y * tiles;
-        k_embed_lookup<A, B, N, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
+        k_embed_lookup<A, B, N, K, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, scale, h->d_status);
     }
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
@@ -1170,8 +1212,8 @@ template <typename A, typename B>
 int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h,
                   float scale, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
-    if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16)) return launch_lookup_vec<A, B, N>(table, tokens, out, n_tokens, h, scale, stream);
-    return launch_lookup_vec<A, B, 1>(table, tokens, out, n_tokens, h, scale, stream);
+    if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16)) return launch_lookup_vec<A, B, N, 1>(table, tokens, out, n_tokens, h, scale, stream);
+    return launch_lookup_vec<A, B, 1, 4>(table, tokens, out, n_tokens, h, scale, stream);
 }
 
 // A launch whose blocks may line up while the kernel before it ends; they wait for it themselves.
@@ -1216,7 +1258,6 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     j.seg_key = h->d_seg_key;
     j.n_segs = h->d_n_segs;
     j.chunk_seg = h->d_chunk_seg;
-    j.n_long = h->d_n_long;
     j.order = h->d_order;
     j.chunk_shift = chunk_shift_of(j.n, h->dim);
     j.row_begin = d_row_begin;
@@ -1230,13 +1271,12 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     p->n = j.n;
     p->chunk_shift = j.chunk_shift;
     p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
-    p->n_long = h->d_n_long;
-    p->long_list = h->d_long;
     p->partial = h->d_partial;
     p->status = h->d_status;
     p->dim = h->dim;
     p->vocab = h->vocab;
     p->tickets = h->d_tickets;
+    p->max_chunks = h->chunks;
     p->scale = scale;
     return j;
 }
@@ -1257,7 +1297,7 @@ int sort_tokens(const adacomp_embed_t* h, SortJob j, const Rows* zero, uint64_t 
         j.share_shift = 10;
         while ((blocks << j.share_shift) < j.n) ++j.share_shift;
         cfg.gridDim = dim3(blocks);
-        cfg.dynamicSmemBytes = (2u << j.share_shift) * 4 + (blocks << j.bits) * 4 + (kSortWarps << j.bits) * 2;
+        cfg.dynamicSmemBytes = (2u << j.share_shift) * 4 + (blocks << j.bits) * 2 + (kSortWarps << j.bits) * 2;
         attr[0].id = cudaLaunchAttributeClusterDimension;
         attr[0].val.clusterDim.x = blocks;
         attr[0].val.clusterDim.y = 1;
@@ -1285,17 +1325,21 @@ int sort_tokens(const adacomp_embed_t* h, SortJob j, const Rows* zero, uint64_t 
     return ADACOMP_OK;
 }
 
+constexpr uint64_t kSortMicros = 16, kTokensPerMicro = 8192, kClearPerMicro = 5 << 20;     // what sorting takes, and clearing meanwhile
+
 template <typename A, typename B>
 int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const adacomp_embed_t* h, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
     const bool vec = p.dim % N == 0 && on_grid(p.grad, 16) && out_grid >= 16;
     p.wide = out_grid >= 32;
-    const uint32_t cols = (p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), size = type_size(p.out.type);
+    constexpr int K = sizeof(A) == 4 ? 4 : 8;               // columns per thread off the grid, where there is work enough
+    const bool small = j.n <= kSmallTokens;
+    const uint32_t per_thread = vec ? N : small ? 1 : K, cols = (p.dim + per_thread - 1) / per_thread, size = type_size(p.out.type);
     p.zero_vec = clear && on_grid(p.out, 16) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
     if (!clear) p.zero_rows = 0;
     uint32_t x, y;
-    if (j.n <= kSmallTokens) {
-        along_row(cols, 1, &x, &y, &p.tiles);
+    if (small) {
+        along_row(cols, 512, &x, &y, &p.tiles);
         y = kSmallThreads / x < kSmallLanes ? kSmallThreads / x : kSmallLanes;
         p.chunk_shift = kSmallShift;
         p.n_chunks = (j.n + kSmallChunk - 1) / kSmallChunk;
@@ -1308,26 +1352,27 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
         ADACOMP_LAUNCH_CHECK();
         return ADACOMP_OK;
     }
-    // Rows without a token become zeros.  Few tokens: everything is cleared while they are sorted, and some rows are written
-    // twice; many: the rows that need it are cleared next to the sums.
-    const bool early = clear && j.n <= p.zero_rows / 4, gaps = clear && !early;
-    int rc = sort_tokens(h, j, early ? &p.out : nullptr, p.zero_rows, stream);
+    // Rows without a token become zeros.  Where most have none, as many rows are cleared while the tokens are sorted as the
+    // other SMs manage in that time (the sums write some of them once more); the others next to the sums, as they need it.
+    p.zero_first = 0;
+    if (clear && j.n <= p.zero_rows / 4) {
+        const uint64_t row = static_cast<uint64_t>(p.dim) * size, in_time = (kSortMicros + j.n / kTokensPerMicro) * kClearPerMicro / row;
+        if (in_time < p.zero_rows / 2) p.zero_first = in_time;      // for less the launch is not worth it
+    }
+    int rc = sort_tokens(h, j, p.zero_first ? &p.out : nullptr, p.zero_first, stream);
     if (rc != ADACOMP_OK) return rc;
     const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
-    along_row(cols, chunk_bytes, &x, &y, &p.tiles);
+    along_row(cols, kSumThreads, &x, &y, &p.tiles);
+    while (y > 1 && y * chunk_bytes > 32 * 1024) y /= 2;
     p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
     uint32_t zero_blocks = 0;
-    if (gaps) {
-        p.zero_run = 1;
-        while (p.zero_run < kMaxChunk && static_cast<uint64_t>(p.zero_run) * p.dim * size < 32768) p.zero_run *= 2;
-        zero_blocks = static_cast<uint32_t>((p.zero_rows + p.zero_run - 1) / p.zero_run);
+    if (clear && p.zero_first < p.zero_rows) {
+        // some 64 KB per block: with 512 KB the last blocks run alone (131072 x 1024 fp32, 16384 tokens: 110 -> 129 us)
+        const uint64_t left = p.zero_rows - p.zero_first, blocks = left * p.dim * size / 65536 + 1;
+        zero_blocks = static_cast<uint32_t>(left < blocks ? left : blocks);
     }
     const dim3 block(x, y);
-    rc = launch_after(vec ? k_embed_sums<A, B, N> : k_embed_sums<A, B, 1>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
-    if (rc != ADACOMP_OK || p.n_chunks < 2) return rc;              // one chunk: no segment is longer
-    constexpr int kWide = 16 / sizeof(B);
-    const bool join_vec = out_grid >= 16 && p.dim % kWide == 0;
-    return launch_after(join_vec ? k_embed_join<B, kWide> : k_embed_join<B, 1>, dim3(4 * static_cast<uint32_t>(h->n_sms)), dim3(32, kJoinLanes), 0, stream, p);
+    return launch_after(vec ? k_embed_sums<A, B, N, 1> : k_embed_sums<A, B, 1, K>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
 }
 
 // Calls f<A, B>() for the types' numbers.
@@ -1412,7 +1457,7 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     if (err == cudaSuccess) err = prepare_cluster(&e->cluster);
     if (err == cudaSuccess) err = cudaMemset(e->d_status, 0, sizeof(int));
     if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 2 * sizeof(uint32_t));
-    if (err == cudaSuccess) err = cudaMemset(e->d_tickets, 0, ticket_count(dim) * sizeof(uint32_t));
+    if (err == cudaSuccess) err = cudaMemset(e->d_tickets, 0, ticket_count(e->chunks, dim) * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaStreamSynchronize(nullptr);
     if (err != cudaSuccess) {
         delete e;
