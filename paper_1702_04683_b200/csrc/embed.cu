@@ -20,8 +20,7 @@ struct adacomp_embed {
     int n_sms;
     int* d_status;
     uint32_t* d_barrier;            // arrivals, and blocks that are through
-    uint32_t* d_key[2];             // [max_tokens] worker * vocab + token, between the passes of the sort
-    uint32_t* d_pos[2];             // [max_tokens] which token it is
+    uint64_t* d_tok[2];             // [max_tokens] worker * vocab + token and which token it is, between the passes of a large sort
     uint32_t* d_table;              // [kSortBlocks][kMaxBins] digit counts per block
     uint32_t* d_seg_begin;          // [max_tokens + 1] first sorted token of every distinct one, and their end
     uint32_t* d_seg_key;            // [max_tokens]
@@ -41,7 +40,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kItems = 8;                                   // tokens per thread and step of the sort
 constexpr uint32_t kStep = kSortThreads * kItems;
-constexpr uint32_t kSortBlocks = 64;
+constexpr uint32_t kSortBlocks = 128;
 constexpr int kDigitBits = 9;
 constexpr int kMaxBins = 1 << kDigitBits;
 constexpr uint32_t kClusterSmem = 2 * kStep * 4 + 16 * kMaxBins * 2 + kSortWarps * kMaxBins * 2;
@@ -122,8 +121,7 @@ struct SortJob {
     uint32_t n, n_tokens, n_workers, vocab, padding, none;  // none = n_workers * vocab: the key of tokens without a gradient
     uint32_t n_blocks, per_block;                           // blocks that sort, tokens of each (a multiple of kSortThreads)
     int passes, bits;
-    uint32_t* key[2];
-    uint32_t* pos[2];
+    uint64_t* tok[2];                                       // key and position, between the passes (the form without a cluster)
     uint32_t* table;
     uint32_t *order;                                        // the sorted tokens' positions, kLast set where a segment ends
     uint32_t *seg_begin, *seg_key, *n_segs, *chunk_seg;
@@ -146,10 +144,6 @@ __device__ __forceinline__ uint32_t load_key(const SortJob& j, uint32_t t, bool 
 // does not, the block says so and the caller gives up.
 __device__ __forceinline__ bool meet(const SortJob& j) {
     __shared__ int s_ok;
-    if (j.n_blocks == 1) {
-        __syncthreads();
-        return true;
-    }
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
@@ -302,6 +296,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     cudaTriggerProgrammaticLaunchCompletion();              // the sums' blocks may line up: they wait for this kernel's end
     __shared__ uint16_t s_count[kSortWarps * kMaxBins];     // [warps][bins] of a digit in the warps before
     __shared__ uint32_t s_base[kMaxBins];
+    __shared__ uint32_t s_all[kSortThreads], s_before[kSortThreads];
     __shared__ uint32_t s_warp[32];
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint64_t from = static_cast<uint64_t>(blockIdx.x) * j.per_block;
@@ -310,39 +305,33 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     uint16_t* mine = s_count + warp * bins;
     const uint32_t items = j.per_block < kStep ? j.per_block / kSortThreads : kItems;     // rows of 32 per warp and step
     const bool one_step = j.per_block <= kStep;
-    uint32_t key[kItems], pos[kItems], rank[kItems];
+    uint64_t tok[kItems];
+    uint32_t rank[kItems];
     for (int pass = 0; pass < j.passes; ++pass) {
-        const uint32_t* key_in = j.key[(pass & 1) ^ 1];
-        const uint32_t* pos_in = j.pos[(pass & 1) ^ 1];
-        const int shift = pass * j.bits;
+        const uint64_t* in = j.tok[(pass & 1) ^ 1];
+        const int shift = 32 + pass * j.bits;
         // Loads step `at`, ranks it and leaves s_count as places within the step; returns the step's count of digit tid.
         auto rank_step = [&](uint64_t at, bool report) -> uint32_t {
             for (uint32_t d = lane; d < bins / 2; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 const uint64_t t = at + (warp * items + i) * 32 + lane;
-                key[i] = j.none;
-                pos[i] = 0;
                 if (i >= items || t >= to) continue;
-                if (pass == 0) {
-                    key[i] = load_key(j, static_cast<uint32_t>(t), report);
-                    pos[i] = static_cast<uint32_t>(t);
-                } else {
-                    key[i] = __ldcg(key_in + t);
-                    pos[i] = __ldcg(pos_in + t);
-                }
+                if (pass == 0) tok[i] = static_cast<uint64_t>(load_key(j, static_cast<uint32_t>(t), report)) << 32 | t;
+                else tok[i] = __ldcg(in + t);
             }
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 if (i >= items) break;
                 const bool real = at + (warp * items + i) * 32 + lane < to;
-                const uint32_t d = (key[i] >> shift) & mask;
+                const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
                 const uint32_t same = same_digit(d, real);
                 const uint32_t before = __popc(same & ((1u << lane) - 1));
-                rank[i] = mine[d] + before;
+                const uint32_t had = mine[d];
+                rank[i] = had + before;
                 __syncwarp();
-                if (real && before == 0) mine[d] += static_cast<uint16_t>(__popc(same));
+                if (real && before == 0) mine[d] = static_cast<uint16_t>(had + __popc(same));
                 __syncwarp();
             }
             __syncthreads();
@@ -353,21 +342,25 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
             if (at != from) __syncthreads();
             count += rank_step(at, true);
         }
-        uint32_t all = count, before = 0;
-        if (j.n_blocks > 1) {
-            if (tid < bins) __stcg(j.table + blockIdx.x * bins + tid, count);
-            if (!meet(j)) return;
-            if (tid < bins) {
-                all = 0;
-#pragma unroll 8
-                for (uint32_t b = 0; b < j.n_blocks; ++b) {
-                    const uint32_t c = __ldcg(j.table + b * bins + tid);
-                    all += c;
-                    if (b < blockIdx.x) before += c;
-                }
+        if (tid < bins) __stcg(j.table + blockIdx.x * bins + tid, count);
+        if (!meet(j)) return;
+        // the blocks' counts of a digit: kSortThreads / bins threads share them
+        uint32_t all = 0, before = 0, total;
+#pragma unroll 16
+        for (uint32_t b = tid >> j.bits; b < j.n_blocks; b += kSortThreads >> j.bits) {
+            const uint32_t c = __ldcg(j.table + b * bins + (tid & mask));
+            all += c;
+            if (b < blockIdx.x) before += c;
+        }
+        s_all[tid] = all;
+        s_before[tid] = before;
+        __syncthreads();
+        if (tid < bins) {
+            for (uint32_t k = tid + bins; k < kSortThreads; k += bins) {
+                all += s_all[k];
+                before += s_before[k];
             }
         }
-        uint32_t total;
         const uint32_t base = block_before(tid < bins ? all : 0u, s_warp, &total) + before;
         if (tid < bins) s_base[tid] = base;
         for (uint64_t at = from; at < to; at += kStep) {
@@ -380,10 +373,8 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 if (i >= items || at + (warp * items + i) * 32 + lane >= to) continue;
-                const uint32_t d = (key[i] >> shift) & mask;
-                const uint32_t place = s_base[d] + mine[d] + rank[i];
-                __stcg(j.key[pass & 1] + place, key[i]);
-                __stcg(j.pos[pass & 1] + place, pos[i]);
+                const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
+                __stcg(j.tok[pass & 1] + s_base[d] + mine[d] + rank[i], tok[i]);
             }
             if (!one_step) {
                 __syncthreads();
@@ -393,43 +384,65 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
         if (!meet(j)) return;
     }
 
-    // Segments: where each begins, how many begin before every chunk, where each worker's begin.
-    const uint32_t* sorted = j.key[(j.passes - 1) & 1];
-    const uint32_t* sorted_pos = j.pos[(j.passes - 1) & 1];
-    uint32_t segs = 0, total;
-    if (j.n_blocks > 1) {
-        for (uint64_t at = from; at < to; at += kSortThreads) {
-            const uint64_t i = at + tid;
-            bool head = false;
-            if (i < to) {
-                const uint32_t k = __ldcg(sorted + i);
-                head = k != j.none && (i == 0 || __ldcg(sorted + i - 1) != k);
-            }
-            segs += __syncthreads_count(head);
+    // Segments: where each begins, how many begin before every chunk, where each worker's begin.  A warp's tokens are
+    // consecutive: neighbours come by shuffle, heads are counted by ballots, the warps' counts by one scan per step.
+    const uint64_t* sorted = j.tok[(j.passes - 1) & 1];
+    const uint64_t none = static_cast<uint64_t>(j.none) << 32;
+    uint32_t heads[kItems], segs = 0, total;
+    auto head_step = [&](uint64_t at) -> uint32_t {
+        const uint64_t span = at + warp * items * 32 + lane;
+        uint32_t before = j.none, in_warp = 0;                          // key in front of a row
+#pragma unroll
+        for (int i = 0; i < kItems; ++i)
+            tok[i] = i < items && span + i * 32 < to ? __ldcg(sorted + span + i * 32) : none;
+        if (span - lane > 0 && span - lane < j.n) before = static_cast<uint32_t>(__ldcg(sorted + (span - lane) - 1) >> 32);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const uint32_t k = static_cast<uint32_t>(tok[i] >> 32);
+            uint32_t last = __shfl_up_sync(0xFFFFFFFFu, k, 1);
+            if (lane == 0) last = before;
+            heads[i] = i < items ? __ballot_sync(0xFFFFFFFFu, k != j.none && (last != k || span + i * 32 == 0)) : 0u;
+            in_warp += __popc(heads[i]);
+            before = __shfl_sync(0xFFFFFFFFu, k, 31);
         }
-        if (tid == 0) __stcg(j.table + blockIdx.x, segs);
-        if (!meet(j)) return;
-        const uint32_t c = tid < j.n_blocks ? __ldcg(j.table + tid) : 0u;
-        block_before(tid < blockIdx.x ? c : 0u, s_warp, &total);
-        segs = total;
-    }
-    for (uint64_t at = from; at < to; at += kSortThreads) {
-        const uint64_t i = at + tid;
-        uint32_t k = j.none, last = j.none, next = j.none, pos_i = 0;
-        if (i < to) {
-            k = __ldcg(sorted + i);
-            pos_i = __ldcg(sorted_pos + i);
-            if (i > 0) last = __ldcg(sorted + i - 1);
-            if (i + 1 < j.n) next = __ldcg(sorted + i + 1);
-        }
-        const bool head = k != j.none && (i == 0 || last != k);
-        const uint32_t u = segs + block_before(head, s_warp, &total);
+        return in_warp;
+    };
+    uint32_t in_warp = 0;
+    for (uint64_t at = from; at < to; at += kStep) {
+        in_warp = head_step(at);
+        block_before(lane == 0 ? in_warp : 0u, s_warp, &total);
         segs += total;
-        if (i < to) put_segment(j, i, k, last, next, pos_i, head, u);
     }
-    if (blockIdx.x == 0) put_empty(j, j.n == 0 || __ldcg(sorted) == j.none);
+    if (tid == 0) __stcg(j.table + blockIdx.x, segs);
+    if (!meet(j)) return;
+    block_before(tid < blockIdx.x ? __ldcg(j.table + tid) : 0u, s_warp, &total);
+    segs = total;
+    for (uint64_t at = from; at < to; at += kStep) {
+        const uint64_t span = at + warp * items * 32 + lane;
+        if (!one_step) in_warp = head_step(at);
+        uint32_t u = segs + __shfl_sync(0xFFFFFFFFu, block_before(lane == 0 ? in_warp : 0u, s_warp, &total), 0);
+        segs += total;
+        uint32_t before = j.none, behind = j.none;
+        const uint64_t first = span - lane, end = first + items * 32;
+        if (first > 0 && first < j.n) before = static_cast<uint32_t>(__ldcg(sorted + first - 1) >> 32);
+        if (end < j.n) behind = static_cast<uint32_t>(__ldcg(sorted + end) >> 32);
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            if (i >= items) break;
+            const uint64_t t = span + i * 32;
+            const uint32_t k = static_cast<uint32_t>(tok[i] >> 32);
+            uint32_t last = __shfl_up_sync(0xFFFFFFFFu, k, 1), next = __shfl_down_sync(0xFFFFFFFFu, k, 1);
+            const uint32_t after = i + 1 < items ? __shfl_sync(0xFFFFFFFFu, static_cast<uint32_t>(tok[i + 1 < kItems ? i + 1 : i] >> 32), 0) : behind;
+            if (lane == 0) last = before;
+            if (lane == 31) next = after;
+            if (t < to) put_segment(j, t, k, last, t + 1 < j.n ? next : j.none, static_cast<uint32_t>(tok[i]), heads[i] >> lane & 1, u + __popc(heads[i] & ((1u << lane) - 1)));
+            u += __popc(heads[i]);
+            before = __shfl_sync(0xFFFFFFFFu, k, 31);
+        }
+    }
+    if (blockIdx.x == 0) put_empty(j, __ldcg(sorted) >> 32 == j.none);
     // the last block through leaves the barrier as it was
-    if (j.n_blocks > 1 && tid == 0 && atomicAdd(j.barrier + 1, 1u) == j.n_blocks - 1) {
+    if (tid == 0 && atomicAdd(j.barrier + 1, 1u) == j.n_blocks - 1) {
         j.barrier[0] = 0;
         j.barrier[1] = 0;
     }
@@ -1105,10 +1118,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     e.d_status = c.take<int>(1);
     e.d_n_segs = c.take<uint32_t>(2);
     e.d_barrier = c.take<uint32_t>(2);
-    for (int i = 0; i < 2; ++i) {
-        e.d_key[i] = c.take<uint32_t>(n);
-        e.d_pos[i] = c.take<uint32_t>(n);
-    }
+    for (int i = 0; i < 2; ++i) e.d_tok[i] = c.take<uint64_t>(n);
     e.d_table = c.take<uint32_t>(static_cast<size_t>(kSortBlocks) * kMaxBins);
     e.d_seg_begin = c.take<uint32_t>(n + 1);
     e.d_seg_key = c.take<uint32_t>(n);
@@ -1120,10 +1130,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
         h->d_status = e.d_status;
         h->d_n_segs = e.d_n_segs;
         h->d_barrier = e.d_barrier;
-        for (int i = 0; i < 2; ++i) {
-            h->d_key[i] = e.d_key[i];
-            h->d_pos[i] = e.d_pos[i];
-        }
+        for (int i = 0; i < 2; ++i) h->d_tok[i] = e.d_tok[i];
         h->d_table = e.d_table;
         h->d_seg_begin = e.d_seg_begin;
         h->d_seg_key = e.d_seg_key;
@@ -1249,10 +1256,7 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     while (bits < 32 && (j.none >> bits) != 0) ++bits;
     j.passes = (bits + kDigitBits - 1) / kDigitBits;
     j.bits = (bits + j.passes - 1) / j.passes;
-    for (int i = 0; i < 2; ++i) {
-        j.key[i] = h->d_key[i];
-        j.pos[i] = h->d_pos[i];
-    }
+    for (int i = 0; i < 2; ++i) j.tok[i] = h->d_tok[i];
     j.table = h->d_table;
     j.seg_begin = h->d_seg_begin;
     j.seg_key = h->d_seg_key;
@@ -1290,7 +1294,10 @@ int sort_tokens(const adacomp_embed_t* h, SortJob j, const Rows* zero, uint64_t 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e;
-    if (j.n <= h->cluster * kStep) {
+#ifndef V_CL
+#define V_CL 131072
+#endif
+    if (j.n <= h->cluster * kStep && j.n <= V_CL) {
         // as many blocks as have a token per thread, then more tokens per thread
         uint32_t blocks = 1;
         while (blocks < h->cluster && blocks * kSortThreads < j.n) blocks *= 2;

@@ -297,6 +297,15 @@ def test_large_batch_with_frequent_tokens(binding):
     check_grad(binding, tokens, grad, vocab, scale=0.125)
 
 
+@pytest.mark.parametrize("n,vocab,workers", [(131_072, 50_000, 1), (131_073, 400, 1), (300_001, 100_000, 3), (1_048_577, 9_000, 1), (2_500_000, 70_000, 2)])
+def test_sorts_of_every_size(binding, n, vocab, workers):
+    """One cluster's most tokens and one more, many blocks, several steps per block; frequent tokens of several levels of pieces."""
+    tokens = words((workers, n // workers), vocab, n)
+    tokens[torch.rand(tokens.shape, device=DEV, generator=gen(2)) < 0.2] = 17
+    grad = torch.randn((*tokens.shape, 4), device=DEV, generator=gen(1))
+    check_grad(binding, tokens, grad, vocab, workers=workers, pad=3)
+
+
 def test_vocabularies_of_many_bits(binding):
     for vocab, workers in ((2 ** 31 - 1, 2), (2 ** 32 - 2, 1), (2 ** 20, 4095)):
         h = binding.Embedding(vocab, 2, max_tokens=workers * 300, max_workers=workers)
