@@ -5,6 +5,7 @@
 // Both kernels are one pass over the data (2 and 1 operations an entry): HBM bounds them.  The tensors of a call are cut
 // into units of some 16 KB; blocks take units in turn, so short tensors next to each other in the list go to different
 // blocks.  The second pass walks the units from the back: what the first pass read last is still in L2.
+#include <cooperative_groups.h>
 #include <math.h>
 #include <new>
 #include <vector>
@@ -36,15 +37,17 @@ constexpr uint32_t kMaxBlocks = 1024;                       // partial sums per 
 // read stays until it is read again.  Measured, both passes: 102 MB of fp32 57.2 -> 53.3 us, 52 MB of fp16 44.5 -> 40.2 us;
 // but 683 MB of bf16 464 -> 471 us, where little of it can stay anyway.
 constexpr uint64_t kKeepInL2 = 160ull << 20;
+// Gradients of so many bytes a worker, and all workers together, are clipped in one launch.  The call with two launches and with
+// one: 64 KB 10.3 and 8.8 us, 16 workers of 256 KB 11.2 and 9.1, of 512 KB 11.2 and 11.4; 64 workers of 64 KB 11.4 and
+// 10.5, of 256 KB 12.4 and 14.6.
+constexpr uint64_t kSmallBytes = 256 << 10, kSmallTotal = 4 << 20;
 constexpr double kEps = 1e-6;
 
 struct Tensor {
     const char* in;
     char* out;
-    uint64_t n;
-    uint32_t first_unit;            // of this tensor among the call's units
-    uint8_t in_type, out_type;
-    uint16_t unused;
+    uint64_t n : 48, in_type : 8, out_type : 8;
+    uint32_t first[2];              // its first unit among the launch's, of the first and of the second pass
 };
 static_assert(sizeof(Tensor) == 32, "table entries are packed");
 
@@ -54,7 +57,7 @@ template <int MAX> struct Table { Tensor t[MAX]; };
 constexpr int kFew = 64, kMany = 960;
 
 struct Job {
-    uint32_t n_tensors, n_units;
+    uint32_t n_tensors, n_units[2];
     uint64_t in_stride, out_stride;
     float scale;
     float max_norm;
@@ -82,12 +85,12 @@ struct Lookup {
         for (uint32_t k = threadIdx.x; k < 2 * n; k += kThreads) reinterpret_cast<uint4*>(s_tab)[k] = src[k];
         __syncthreads();
     }
-    __device__ __forceinline__ const Tensor& of(uint32_t unit) const {
+    __device__ __forceinline__ const Tensor& of(uint32_t unit, int pass) const {
         const uint32_t lane = threadIdx.x & 31;
         const uint32_t a = lane * stride;
-        const uint32_t run = __popc(__ballot_sync(0xFFFFFFFFu, a < n && t[a].first_unit <= unit)) - 1;
+        const uint32_t run = __popc(__ballot_sync(0xFFFFFFFFu, a < n && t[a].first[pass] <= unit)) - 1;
         const uint32_t b = run * stride + lane;
-        const uint32_t in = __popc(__ballot_sync(0xFFFFFFFFu, lane < stride && b < n && t[b].first_unit <= unit)) - 1;
+        const uint32_t in = __popc(__ballot_sync(0xFFFFFFFFu, lane < stride && b < n && t[b].first[pass] <= unit)) - 1;
         return t[run * stride + in];
     }
 };
@@ -170,6 +173,29 @@ __device__ __forceinline__ double block_sum(double x, double* s_warp) {
     return total;                   // of thread 0
 }
 
+// This thread's share of the squares of worker w: units b, b + n_blocks, ...
+__device__ __forceinline__ double worker_squares(const Lookup& tensors, const Job& job, uint32_t w, uint32_t b, uint32_t n_blocks) {
+    double sum = 0.0;
+    for (uint32_t u = b; u < job.n_units[0]; u += n_blocks) {
+        const Tensor& t = tensors.of(u, 0);
+        const char* base = t.in + w * job.in_stride * type_size(t.in_type);
+        const uint32_t at = u - t.first[0];
+        if (t.in_type == ADACOMP_F32) sum += unit_squares<float>(base, t.n, at);
+        else if (t.in_type == ADACOMP_BF16) sum += unit_squares<__nv_bfloat16>(base, t.n, at);
+        else sum += unit_squares<__half>(base, t.n, at);
+    }
+    return sum;
+}
+
+// A worker's norm from its sum of squares, and the factor for its entries.
+__device__ __forceinline__ float norm_and_factor(const Job& job, double total, float* norm_out) {
+    const double norm = fabs(static_cast<double>(job.scale)) * sqrt(total);
+    *norm_out = static_cast<float>(norm);
+    double c = static_cast<double>(job.max_norm) / (norm + kEps);
+    if (c > 1.0 || isinf(job.max_norm)) c = 1.0;                // a NaN stays one
+    return static_cast<float>(c * static_cast<double>(job.scale));
+}
+
 template <int MAX>
 __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __grid_constant__ Table<MAX> tab, const Job job) {
     __shared__ double s_warp[kThreads / 32];
@@ -177,16 +203,7 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __gri
     extern __shared__ Tensor s_tab[];
     const uint32_t w = blockIdx.y, b = blockIdx.x;
     const Lookup tensors(tab, job.n_tensors, s_tab);
-    double sum = 0.0;
-    for (uint32_t u = b; u < job.n_units; u += job.n_blocks) {
-        const Tensor& t = tensors.of(u);
-        const char* base = t.in + w * job.in_stride * type_size(t.in_type);
-        const uint32_t at = u - t.first_unit;
-        if (t.in_type == ADACOMP_F32) sum += unit_squares<float>(base, t.n, at);
-        else if (t.in_type == ADACOMP_BF16) sum += unit_squares<__nv_bfloat16>(base, t.n, at);
-        else sum += unit_squares<__half>(base, t.n, at);
-    }
-    sum = block_sum(sum, s_warp);
+    const double sum = block_sum(worker_squares(tensors, job, w, b, job.n_blocks), s_warp);
     if (threadIdx.x == 0) {
         double* slot = job.partial + static_cast<uint64_t>(w) * job.n_blocks + b;
         *slot = job.first ? sum : *slot + sum;
@@ -206,15 +223,9 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __gri
     total = block_sum(total, s_warp);
     if (threadIdx.x == 0) {
         job.done[w] = 0;
-        const double norm = fabs(static_cast<double>(job.scale)) * sqrt(total);
-        job.norm_out[w] = static_cast<float>(norm);
-        if (job.coef) {
-            double c = static_cast<double>(job.max_norm) / (norm + kEps);
-            if (c > 1.0 || isinf(job.max_norm)) c = 1.0;        // a NaN stays one
-            const float f = static_cast<float>(c * static_cast<double>(job.scale));
-            job.coef[w] = f;
-            if (job.coef_out) job.coef_out[w] = f;
-        }
+        const float f = norm_and_factor(job, total, job.norm_out + w);
+        if (job.coef) job.coef[w] = f;
+        if (job.coef_out) job.coef_out[w] = f;
     }
 }
 
@@ -310,23 +321,59 @@ __device__ __forceinline__ void write_unit_from(const Tensor& t, uint32_t w, con
     else write_unit<A, __half>(t, w, job, unit, c, policy);
 }
 
-template <int MAX>
-__global__ void __launch_bounds__(kThreads, kWriteBlocks) k_clip_write(const __grid_constant__ Table<MAX> tab, const Job job) {
-    extern __shared__ Tensor s_tab[];
-    const uint32_t w = blockIdx.y, b = blockIdx.x;
-    const Lookup tensors(tab, job.n_tensors, s_tab);
+// The second pass of worker w: units from the back.
+__device__ __forceinline__ void worker_write(const Lookup& tensors, const Job& job, uint32_t w, uint32_t b, uint32_t n_blocks, float c) {
     const uint64_t policy = l2_policy(job.give_up_first != 0);
-    cudaGridDependencySynchronize();
-    const float c = job.coef[w];
-    for (uint32_t k = b; k < job.n_units; k += job.n_blocks) {
-        const uint32_t u = job.n_units - 1 - k;
-        const Tensor& t = tensors.of(u);
+    for (uint32_t k = b; k < job.n_units[1]; k += n_blocks) {
+        const uint32_t u = job.n_units[1] - 1 - k;
+        const Tensor& t = tensors.of(u, 1);
         if (c == 1.0f && t.out == t.in) continue;           // in place, nothing to change
-        const uint32_t at = u - t.first_unit;
+        const uint32_t at = u - t.first[1];
         if (t.in_type == ADACOMP_F32) write_unit_from<float>(t, w, job, at, c, policy);
         else if (t.in_type == ADACOMP_BF16) write_unit_from<__nv_bfloat16>(t, w, job, at, c, policy);
         else write_unit_from<__half>(t, w, job, at, c, policy);
     }
+}
+
+template <int MAX>
+__global__ void __launch_bounds__(kThreads, kWriteBlocks) k_clip_write(const __grid_constant__ Table<MAX> tab, const Job job) {
+    extern __shared__ Tensor s_tab[];
+    const Lookup tensors(tab, job.n_tensors, s_tab);
+    cudaGridDependencySynchronize();
+    worker_write(tensors, job, blockIdx.y, blockIdx.x, job.n_blocks, job.coef[blockIdx.y]);
+}
+
+// Both passes of a small gradient in one launch: a cluster of kCluster blocks per worker, which tell each other their sums through
+// shared memory.  The second read comes from L2.
+constexpr uint32_t kCluster = 8;
+template <int MAX>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, kNormBlocks) k_clip_small(const __grid_constant__ Table<MAX> tab, const Job job) {
+    __shared__ double s_warp[kThreads / 32];
+    __shared__ double s_sums[kCluster];
+    __shared__ float s_factor;
+    extern __shared__ Tensor s_tab[];
+    cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+    const uint32_t w = blockIdx.y, b = blockIdx.x;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const Lookup tensors(tab, job.n_tensors, s_tab);
+    const double sum = block_sum(worker_squares(tensors, job, w, b, kCluster), s_warp);
+    if (threadIdx.x == 0) s_warp[0] = sum;
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // every block has started: its shared memory may be written
+    __syncthreads();
+    if (threadIdx.x < kCluster) *cluster.map_shared_rank(s_sums + b, threadIdx.x) = s_warp[0];
+    cluster.sync();
+    if (threadIdx.x == 0) {
+        double total = 0.0;
+        for (uint32_t k = 0; k < kCluster; ++k) total += s_sums[k];
+        float norm;
+        s_factor = norm_and_factor(job, total, &norm);
+        if (b == 0) {
+            job.norm_out[w] = norm;
+            if (job.coef_out) job.coef_out[w] = s_factor;
+        }
+    }
+    __syncthreads();
+    worker_write(tensors, job, w, b, kCluster, s_factor);
 }
 
 // Units of a tensor: by its input's vectors (norm) or by its items on the output's grid (write), counted so that they
@@ -336,10 +383,12 @@ uint64_t units_of(const adacomp_grad_tensor_t& t, bool write) {
     return (t.n * type_size(t.grad_type) + 14 + kUnit * 16 - 1) / (kUnit * 16);
 }
 
+enum Pass { kNorm = 0, kWrite = 1, kBoth = 2 };
+
 template <int MAX>
-int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, bool write, cudaStream_t stream) {
+int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, Pass pass, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(job.n_blocks, n_workers);
+    cfg.gridDim = dim3(pass == kBoth ? kCluster : job.n_blocks, n_workers);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = job.n_tensors * sizeof(Tensor);
     cfg.stream = stream;
@@ -348,8 +397,9 @@ int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, bool write
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = write ? 1 : 0;
-    const cudaError_t e = write ? cudaLaunchKernelEx(&cfg, k_clip_write<MAX>, tab, job) : cudaLaunchKernelEx(&cfg, k_grad_norm<MAX>, tab, job);
+    cfg.numAttrs = pass == kWrite ? 1 : 0;
+    const cudaError_t e = pass == kWrite ? cudaLaunchKernelEx(&cfg, k_clip_write<MAX>, tab, job)
+                        : pass == kNorm ? cudaLaunchKernelEx(&cfg, k_grad_norm<MAX>, tab, job) : cudaLaunchKernelEx(&cfg, k_clip_small<MAX>, tab, job);
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
@@ -369,58 +419,45 @@ int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, bool writ
     return ADACOMP_OK;
 }
 
-// One pass over all tensors, in as many launches as the parameter space needs.
-int run_pass(const adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint32_t n_workers, Job job,
-             bool write, cudaStream_t stream) {
-    static thread_local Table<kMany> tab;
-    uint32_t at = 0;
-    bool first = true;
-    do {
-        uint32_t n = 0;
-        uint64_t units = 0;
-        for (; at < n_tensors && n < kMany; ++at) {
-            const adacomp_grad_tensor_t& t = ts[at];
-            if (t.n == 0) continue;
-            const uint64_t u = units_of(t, write);
-            if (units + u >= (1ull << 32)) {
-                if (n) break;
-                return ADACOMP_ERR_INVALID;
-            }
-            Tensor& e = tab.t[n++];
-            e.in = static_cast<const char*>(t.d_grad);
-            e.out = static_cast<char*>(t.d_out);
-            e.n = t.n;
-            e.first_unit = static_cast<uint32_t>(units);
-            e.in_type = static_cast<uint8_t>(t.grad_type);
-            e.out_type = static_cast<uint8_t>(t.out_type);
-            e.unused = 0;
-            units += u;
+// Fills the table from tensor *at on; false if a tensor alone has too many units.
+bool fill_table(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint32_t* at, bool write, Table<kMany>* tab, Job* job) {
+    uint32_t n = 0;
+    uint64_t units[2] = {0, 0};
+    for (; *at < n_tensors && n < kMany; ++*at) {
+        const adacomp_grad_tensor_t& t = ts[*at];
+        if (t.n == 0) continue;
+        const uint64_t u[2] = {units_of(t, false), write ? units_of(t, true) : 0};
+        if (units[0] + u[0] >= (1ull << 32) || units[1] + u[1] >= (1ull << 32)) {
+            if (n == 0) return false;
+            break;
         }
-        job.n_tensors = n;
-        job.n_units = static_cast<uint32_t>(units);
-        job.first = first;
-        job.last = at == n_tensors;
-        first = false;
-        if (write && n == 0) continue;
-        int rc;
-        if (n <= kFew) {
-            Table<kFew> few;
-            for (uint32_t k = 0; k < n; ++k) few.t[k] = tab.t[k];
-            rc = launch(few, job, n_workers, write, stream);
-        } else {
-            rc = launch(tab, job, n_workers, write, stream);
+        Tensor& e = tab->t[n++];
+        e.in = static_cast<const char*>(t.d_grad);
+        e.out = static_cast<char*>(t.d_out);
+        e.n = t.n;
+        e.in_type = static_cast<uint8_t>(t.grad_type);
+        e.out_type = static_cast<uint8_t>(t.out_type);
+        for (int p = 0; p < 2; ++p) {
+            e.first[p] = static_cast<uint32_t>(units[p]);
+            units[p] += u[p];
         }
-        if (rc != ADACOMP_OK) return rc;
-    } while (at < n_tensors);
-    return ADACOMP_OK;
+    }
+    job->n_tensors = n;
+    job->n_units[0] = static_cast<uint32_t>(units[0]);
+    job->n_units[1] = static_cast<uint32_t>(units[1]);
+    return true;
+}
+
+int launch_table(const Table<kMany>& tab, const Job& job, uint32_t n_workers, Pass pass, cudaStream_t stream) {
+    if (job.n_tensors > kFew) return launch(tab, job, n_workers, pass, stream);
+    Table<kFew> few;
+    for (uint32_t k = 0; k < job.n_tensors; ++k) few.t[k] = tab.t[k];
+    return launch(few, job, n_workers, pass, stream);
 }
 
 // Blocks of one worker: all of a call's are resident at once where there are not more workers than that, and none is
 // without work.
-uint32_t blocks_per_worker(const adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint32_t n_workers, bool write) {
-    uint64_t units = 0;
-    for (uint32_t i = 0; i < n_tensors; ++i)
-        if (ts[i].n) units += units_of(ts[i], write);
+uint32_t blocks_per_worker(const adacomp_clip_t* h, uint64_t units, uint32_t n_workers, bool write) {
     uint64_t blocks = static_cast<uint64_t>(write ? kWriteBlocks : kNormBlocks) * h->n_sms / n_workers;
     if (blocks > units) blocks = units;
     if (blocks > kMaxBlocks) blocks = kMaxBlocks;
@@ -454,19 +491,40 @@ int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, 
     job.out_stride = out_stride;
     job.scale = scale;
     job.max_norm = max_norm;
-    job.n_blocks = blocks_per_worker(h, ts, n_tensors, n_workers, false);
     job.partial = h->d_partial;
     job.done = h->d_done;
     job.norm_out = d_norm;
     job.coef = write ? h->d_coef : nullptr;
     job.coef_out = d_coef_out;
-    rc = run_pass(h, ts, n_tensors, n_workers, job, false, stream);
-    if (rc != ADACOMP_OK || !write) return rc;
-    job.n_blocks = blocks_per_worker(h, ts, n_tensors, n_workers, true);
-    uint64_t bytes = 0;
-    for (uint32_t i = 0; i < n_tensors; ++i) bytes += ts[i].n * type_size(ts[i].grad_type);
+    uint64_t bytes = 0, units[2] = {0, 0};
+    for (uint32_t i = 0; i < n_tensors; ++i) {
+        if (ts[i].n == 0) continue;
+        bytes += ts[i].n * type_size(ts[i].grad_type);
+        units[0] += units_of(ts[i], false);
+        if (write) units[1] += units_of(ts[i], true);
+    }
     job.give_up_first = bytes * n_workers <= kKeepInL2;
-    return run_pass(h, ts, n_tensors, n_workers, job, true, stream);
+    static thread_local Table<kMany> tab;
+    bool whole = false;                                     // whether one table holds the call
+    for (int pass = 0; pass < (write ? 2 : 1); ++pass) {
+        job.n_blocks = blocks_per_worker(h, units[pass], n_workers, pass == 1);
+        uint32_t at = 0;
+        job.first = 1;
+        do {
+            if (!whole) {
+                if (!fill_table(ts, n_tensors, &at, write, &tab, &job)) return ADACOMP_ERR_INVALID;
+                whole = job.first && at == n_tensors;
+            } else {
+                at = n_tensors;
+            }
+            job.last = at == n_tensors;
+            if (write && whole && bytes <= kSmallBytes && bytes * n_workers <= kSmallTotal) return launch_table(tab, job, n_workers, kBoth, stream);
+            if (pass == 0 || job.n_tensors) rc = launch_table(tab, job, n_workers, pass == 0 ? kNorm : kWrite, stream);
+            if (rc != ADACOMP_OK) return rc;
+            job.first = 0;
+        } while (at < n_tensors);
+    }
+    return ADACOMP_OK;
 }
 
 }  // namespace

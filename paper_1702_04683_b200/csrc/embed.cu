@@ -40,10 +40,14 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kItems = 8;                                   // tokens per thread and step of the sort
 constexpr uint32_t kStep = kSortThreads * kItems;
+// Tokens per block of a cluster.  The whole call at 32768, 65536 and 131072 tokens of 64 columns: 25, 33 and 53 us with a
+// cluster, 33, 35 and 43 without.
+constexpr int kClusterItems = 4;
+constexpr uint32_t kClusterStep = kSortThreads * kClusterItems;
 constexpr uint32_t kSortBlocks = 128;
 constexpr int kDigitBits = 9;
 constexpr int kMaxBins = 1 << kDigitBits;
-constexpr uint32_t kClusterSmem = 2 * kStep * 4 + 16 * kMaxBins * 2 + kSortWarps * kMaxBins * 2;
+constexpr uint32_t kClusterSmem = kClusterStep * 8 + 16 * kMaxBins * 2 + kSortWarps * kMaxBins * 2;
 constexpr uint32_t kSpinLimit = 1u << 22;                   // polls of a barrier, some seconds
 
 // Device view of adacomp_rows_t.
@@ -448,7 +452,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     }
 }
 
-// The same sort for up to kStep tokens per block in one thread-block cluster: the tokens stay in registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
+// The same sort for up to kClusterStep tokens per block in one thread-block cluster: the tokens stay in registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
 // belong to, and the cluster's barrier takes the place of the one in global memory.
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const SortJob j) {
     extern __shared__ uint64_t s_mem64[];
@@ -469,10 +473,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     const uint32_t from = me << j.share_shift;
     const uint32_t n_here = j.n > from ? (j.n - from < share ? j.n - from : share) : 0;
     const uint32_t span = warp * items * 32 + lane;                             // the warp's tokens: rows of 32, one after the other
-    uint64_t tok[kItems];
-    uint32_t rank[kItems];
+    uint64_t tok[kClusterItems];
+    uint32_t rank[kClusterItems];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < kClusterItems; ++i) {
         const uint32_t t = span + i * 32;
         tok[i] = static_cast<uint64_t>(j.none) << 32;
         if (i >= items || t >= n_here) continue;
@@ -484,12 +488,12 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         for (uint32_t d = lane; d < pairs; d += 32) reinterpret_cast<uint32_t*>(mine)[d] = 0;
         if (pass > 0) {
 #pragma unroll
-            for (int i = 0; i < kItems; ++i)
+            for (int i = 0; i < kClusterItems; ++i)
                 if (i < items && span + i * 32 < n_here) tok[i] = s_tok[span + i * 32];
         }
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < kClusterItems; ++i) {
             if (i >= items) break;
             const bool real = span + i * 32 < n_here;
             const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
@@ -526,7 +530,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
+        for (int i = 0; i < kClusterItems; ++i) {
             if (i >= items) break;
             if (span + i * 32 >= n_here) continue;
             const uint32_t d = static_cast<uint32_t>(tok[i] >> shift) & mask;
@@ -540,9 +544,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     uint32_t before_me = j.none, behind_me = j.none;
     if (me > 0) before_me = cluster.map_shared_rank(s_key, me - 1)[2 * (share - 1)];
     if (n_here == share && from + share < j.n) behind_me = cluster.map_shared_rank(s_key, me + 1)[0];
-    uint32_t heads[kItems], in_warp = 0;
+    uint32_t heads[kClusterItems], in_warp = 0;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < kClusterItems; ++i) {
         heads[i] = 0;
         if (i >= items) break;
         const uint32_t t = span + i * 32;
@@ -558,7 +562,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
     cluster_arrive();                           // no more reads of the neighbours' shared memory
     for (uint32_t r = 0; r < me; ++r) u += s_all[r];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < kClusterItems; ++i) {
         if (i >= items) break;
         const uint32_t t = span + i * 32;
         if (t < n_here) {
@@ -796,9 +800,9 @@ __device__ __forceinline__ Pieces pieces_of(const Share& s, uint32_t chunk, uint
     if (s.trail) x.count[1] = ((seg_begin[s.u1] - 1) >> shift) - chunk + 1;
     return x;
 }
-template <typename B, int N, int K>
+template <typename B, int N, int K, typename KeyOf>
 __device__ __forceinline__ void finish_long(const Sums& p, const Pieces& x, uint32_t chunk, uint32_t tile, uint32_t c, uint32_t step, bool leader,
-                                            const uint32_t* seg_key, uint32_t* s_last) {
+                                            const KeyOf& key_of, uint32_t* s_last) {
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         const uint32_t head = x.head[which];
@@ -853,7 +857,7 @@ __device__ __forceinline__ void finish_long(const Sums& p, const Pieces& x, uint
                             for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], f[r][k]);
                 }
                 if (whole) {
-                    const uint32_t key = seg_key[x.seg[which]];
+                    const uint32_t key = key_of(x.seg[which]);
                     put_row<B, N>(p, x.seg[which], p.dense ? p.out.offset(key) : 0, key % p.vocab, col, sum);
                 } else {
                     put_piece<N>(piece_at(p, first, first == head ? 1 : 0, col), sum);
@@ -904,21 +908,23 @@ __global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(cons
     // asynchronous copies to shared memory, eight rows deep: 410.
     if (c < p.dim) sum_chunk<A, B, N, K, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, blockDim.x * N);
     if (!__syncthreads_or(s.lead || s.trail)) return;
-    finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0, p.seg_key,
+    finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0, [&](uint32_t u) { return p.seg_key[u]; },
                          reinterpret_cast<uint32_t*>(s_src));
 }
 
 // ---------------------------------------------------------------------------------------------- few tokens
 
-// Up to kSmallTokens tokens: one launch does everything.  Every block sorts all tokens for itself in shared memory, which
+// Few tokens: one launch does everything.  Every block sorts all tokens for itself in shared memory, which
 // takes less than a second kernel's start, and then sums its chunks; the block that delivers the last piece of a long segment
 // adds the pieces up.
-constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32, kSmallItems = 2;
+constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32, kSmallItems = 4;
 constexpr uint32_t kSmallTokens = kSmallThreads * kSmallItems;
 constexpr uint32_t kSmallShift = 3, kSmallChunk = 1u << kSmallShift, kSmallChunks = kSmallTokens / kSmallChunk;
 constexpr uint32_t kSmallLanes = 64;                        // chunks a block takes at a time, at most
 
 struct SmallMem {
+    __device__ __forceinline__ uint32_t key(uint32_t t) const { return static_cast<uint32_t>(tok[t] >> 32); }
+    __device__ __forceinline__ uint32_t seg_key(uint32_t u) const { return key(seg_begin[u]); }
     uint64_t tok[kSmallTokens];                             // key and position
     union {
         uint16_t count[kSmallWarps * kMaxBins];
@@ -926,8 +932,8 @@ struct SmallMem {
     };
     uint32_t base[kMaxBins];
     uint32_t warp[32];
-    uint32_t seg_begin[kSmallTokens + 1], seg_key[kSmallTokens];
-    uint32_t chunk_seg[kSmallChunks + 1];
+    uint16_t seg_begin[kSmallTokens + 1];
+    uint16_t chunk_seg[kSmallChunks + 1];
     uint32_t n_segs, live, any_long;
     uint32_t last[kSmallLanes + 1];                         // whether a chunk's piece was the last one of its group
 };
@@ -935,7 +941,7 @@ struct SmallMem {
 __device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bins = 1u << j.bits, mask = bins - 1;
-    const uint32_t items = j.n <= kSmallThreads ? 1 : kSmallItems;
+    const uint32_t items = (j.n + kSmallThreads - 1) / kSmallThreads;
     const uint32_t span = warp * items * 32 + lane;
     uint16_t* mine = m.count + warp * bins;
     uint64_t tok[kSmallItems];
@@ -988,8 +994,8 @@ __device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
         const uint32_t t = span + i * 32;
         bool head = false;
         if (i < items && t < j.n) {
-            const uint32_t k = static_cast<uint32_t>(m.tok[t] >> 32);
-            head = k != j.none && (t == 0 || static_cast<uint32_t>(m.tok[t - 1] >> 32) != k);
+            const uint32_t k = m.key(t);
+            head = k != j.none && (t == 0 || m.key(t - 1) != k);
         }
         heads[i] = __ballot_sync(0xFFFFFFFFu, head);
         in_warp += __popc(heads[i]);
@@ -999,20 +1005,17 @@ __device__ __forceinline__ void sort_small(const SortJob& j, SmallMem& m) {
     for (int i = 0; i < kSmallItems; ++i) {
         const uint32_t t = span + i * 32;
         if (i < items && t < j.n) {
-            const uint32_t k = static_cast<uint32_t>(m.tok[t] >> 32);
+            const uint32_t k = m.key(t);
             const uint32_t at = u + __popc(heads[i] & ((1u << lane) - 1));
             const bool head = heads[i] >> lane & 1;
-            if (t % kSmallChunk == 0) m.chunk_seg[t / kSmallChunk] = at;
-            if (head) {
-                m.seg_begin[at] = t;
-                m.seg_key[at] = k;
-            }
+            if (t % kSmallChunk == 0) m.chunk_seg[t / kSmallChunk] = static_cast<uint16_t>(at);
+            if (head) m.seg_begin[at] = static_cast<uint16_t>(t);
             if (k != j.none) {
-                if (t + kSmallChunk < j.n && static_cast<uint32_t>(m.tok[t + kSmallChunk] >> 32) == k) m.any_long = 1;
-                if (t + 1 == j.n || static_cast<uint32_t>(m.tok[t + 1] >> 32) == j.none) {
+                if (t + kSmallChunk < j.n && m.key(t + kSmallChunk) == k) m.any_long = 1;
+                if (t + 1 == j.n || m.key(t + 1) == j.none) {
                     m.n_segs = at + head;
                     m.live = t + 1;
-                    m.seg_begin[at + head] = t + 1;
+                    m.seg_begin[at + head] = static_cast<uint16_t>(t + 1);
                 }
             }
         }
@@ -1027,17 +1030,17 @@ __device__ __forceinline__ void clear_small(const Sums& p, const SmallMem& m) {
     uint32_t lo = 0, hi = m.n_segs;
     while (lo < hi) {
         const uint32_t mid = (lo + hi) / 2;
-        if (m.seg_key[mid] < from) lo = mid + 1; else hi = mid;
+        if (m.seg_key(mid) < from) lo = mid + 1; else hi = mid;
     }
     for (uint64_t r = from; r < to; ++lo) {
-        const uint64_t next = lo < m.n_segs && m.seg_key[lo] < to ? m.seg_key[lo] : to;
+        const uint64_t next = lo < m.n_segs && m.seg_key(lo) < to ? m.seg_key(lo) : to;
         clear_rows(p.out, r, next, p.dim, p.zero_vec != 0, threadIdx.x, kSmallThreads);
         r = next + 1;
     }
 }
 
 template <typename A, typename B, int N>
-__global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
+__global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
     __shared__ SmallMem m;
     sort_small(j, m);
     if (blockIdx.x == 0 && j.row_begin && j.n_workers == 1) {
@@ -1047,7 +1050,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, 
             uint32_t lo = 0, hi = m.n_segs;
             while (lo < hi) {
                 const uint32_t mid = (lo + hi) / 2;
-                if (m.seg_key[mid] < static_cast<uint64_t>(w) * j.vocab) lo = mid + 1; else hi = mid;
+                if (m.seg_key(mid) < static_cast<uint64_t>(w) * j.vocab) lo = mid + 1; else hi = mid;
             }
             j.row_begin[w] = lo;
         }
@@ -1063,12 +1066,12 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, 
         if (ty < y && i0 < m.live) {
             s = share_of(i0, kSmallChunk, m.live, m.chunk_seg[chunk], i0 + kSmallChunk < m.live ? m.chunk_seg[chunk + 1] : m.n_segs, m.seg_begin);
             for (uint32_t k = tx; k < s.b - s.a; k += x) {
-                const uint32_t t = s.a + k, key = static_cast<uint32_t>(m.tok[t] >> 32);
-                const bool ends = t + 1 == m.live || static_cast<uint32_t>(m.tok[t + 1] >> 32) != key;
+                const uint32_t t = s.a + k;
+                const bool ends = t + 1 == m.live || m.key(t + 1) != m.key(t);
                 s_src[k] = p.grad.offset(static_cast<uint32_t>(m.tok[t])) | (ends ? kEnds : 0ull);
             }
             for (uint32_t k = tx; k < s.u1 - s.u0; k += x) {
-                const uint32_t key = m.seg_key[s.u0 + k];
+                const uint32_t key = m.seg_key(s.u0 + k);
                 s_dst[k] = p.dense ? p.out.offset(key) : key % p.vocab;
                 if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
             }
@@ -1077,7 +1080,7 @@ __global__ void __launch_bounds__(kSmallThreads) k_embed_small(const SortJob j, 
         if (c < p.dim) sum_chunk<A, B, N, 1, 8>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, x * N);
         __syncthreads();
         if (!m.any_long) continue;
-        finish_long<B, N, 1>(p, pieces_of(s, chunk, kSmallShift, m.seg_begin), chunk, tile, c, 0, tx == 0 && ty < y, m.seg_key, &m.last[ty < y ? ty : kSmallLanes]);
+        finish_long<B, N, 1>(p, pieces_of(s, chunk, kSmallShift, m.seg_begin), chunk, tile, c, 0, tx == 0 && ty < y, [&](uint32_t u) { return m.seg_key(u); }, &m.last[ty < y ? ty : kSmallLanes]);
         __syncthreads();
     }
     if (p.zero_rows) clear_small(p, m);
@@ -1294,10 +1297,7 @@ int sort_tokens(const adacomp_embed_t* h, SortJob j, const Rows* zero, uint64_t 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e;
-#ifndef V_CL
-#define V_CL 131072
-#endif
-    if (j.n <= h->cluster * kStep && j.n <= V_CL) {
+    if (j.n <= h->cluster * kClusterStep) {
         // as many blocks as have a token per thread, then more tokens per thread
         uint32_t blocks = 1;
         while (blocks < h->cluster && blocks * kSortThreads < j.n) blocks *= 2;
@@ -1340,17 +1340,20 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
     const bool vec = p.dim % N == 0 && on_grid(p.grad, 16) && out_grid >= 16;
     p.wide = out_grid >= 32;
     constexpr int K = sizeof(A) == 4 ? 4 : 8;               // columns per thread off the grid, where there is work enough
-    const bool small = j.n <= kSmallTokens;
-    const uint32_t per_thread = vec ? N : small ? 1 : K, cols = (p.dim + per_thread - 1) / per_thread, size = type_size(p.out.type);
+    const uint32_t size = type_size(p.out.type);
+    uint32_t x, y;
+    along_row((p.dim + (vec ? N : 1) - 1) / (vec ? N : 1), 512, &x, &y, &p.tiles);
+    y = kSmallThreads / x < kSmallLanes ? kSmallThreads / x : kSmallLanes;
+    // One launch as long as its blocks run at once: with more of them every SM sorts more than once (2048 tokens: 15 us for the
+    // call at 1024 columns, where two launches take 19, but 25 at 4096, where they take 21).
+    const uint64_t small_blocks = static_cast<uint64_t>((j.n + kSmallChunk * y - 1) / (kSmallChunk * y)) * p.tiles;
+    const bool small = j.n <= kSmallTokens / 2 || (j.n <= kSmallTokens && small_blocks <= static_cast<uint64_t>(h->n_sms));
     p.zero_vec = clear && on_grid(p.out, 16) && static_cast<uint64_t>(p.dim) * size % 16 == 0;
     if (!clear) p.zero_rows = 0;
-    uint32_t x, y;
     if (small) {
-        along_row(cols, 512, &x, &y, &p.tiles);
-        y = kSmallThreads / x < kSmallLanes ? kSmallThreads / x : kSmallLanes;
         p.chunk_shift = kSmallShift;
         p.n_chunks = (j.n + kSmallChunk - 1) / kSmallChunk;
-        uint64_t blocks = static_cast<uint64_t>((p.n_chunks + y - 1) / y) * p.tiles;
+        uint64_t blocks = small_blocks;
         const uint64_t most = 2 * static_cast<uint64_t>(h->n_sms);
         if (blocks < 1) blocks = 1;
         if (blocks > most || (clear && p.zero_rows * p.dim >= most * 4096)) blocks = most;
@@ -1369,7 +1372,8 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
     int rc = sort_tokens(h, j, p.zero_first ? &p.out : nullptr, p.zero_first, stream);
     if (rc != ADACOMP_OK) return rc;
     const uint32_t chunk_bytes = (3u << p.chunk_shift) * sizeof(uint64_t);
-    along_row(cols, kSumThreads, &x, &y, &p.tiles);
+    const uint32_t per_thread = vec ? N : K;
+    along_row((p.dim + per_thread - 1) / per_thread, kSumThreads, &x, &y, &p.tiles);
     while (y > 1 && y * chunk_bytes > 32 * 1024) y /= 2;
     p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
     uint32_t zero_blocks = 0;
