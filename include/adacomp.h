@@ -422,7 +422,7 @@ ADACOMP_API int adacomp_clip_create(adacomp_clip_t** h, uint32_t max_workers, vo
  * scale being what the stored entries still have to be multiplied by (1 / the loss scale of half-precision
  * training; 1 otherwise).  Worker w's entries of tensor t start grad_stride * w elements behind h_tensors[t].d_grad
  * (grad_stride is in elements of each tensor's own type; 0 is legal with one worker).  Squares are summed in fp32 inside
- * groups of at most 64 entries and in 64 bits above that; groups whose sum would leave fp32's safe range are summed in 64
+ * groups of at most 64 entries (two chains of 32) and in 64 bits above that; groups whose sum would leave fp32's safe range are summed in 64
  * bits altogether, so neither large nor tiny entries overflow or vanish.  The order of summation is fixed: the same
  * call on the same device gives the same bits.  An infinity gives +Inf, a NaN gives NaN, no entries at all give 0.
  * h_tensors is read before the call returns.  Errors: ADACOMP_ERR_INVALID (null pointer, unknown type, misaligned pointer,
@@ -484,7 +484,8 @@ ADACOMP_API int adacomp_embed_lookup(adacomp_embed_t* h, const adacomp_rows_t* t
  *     sum[w][v] = scale * (sum over w's tokens equal to v of their gradient rows).
  * Summands are added in fp32 along the order of the tokens in a fixed tree (the same call gives the same bits) and rounded
  * once to the result's type.  Padding tokens and tokens outside 0 .. vocab - 1 contribute nothing; the latter are
- * reported by adacomp_embed_last_error as ADACOMP_ERR_INVALID.  n_workers * n_tokens <= max_tokens.
+ * reported by adacomp_embed_last_error as ADACOMP_ERR_INVALID.  Results must not overlap the gradients or the tokens.
+ * n_workers * n_tokens <= max_tokens (ADACOMP_ERR_CAPACITY otherwise).
  *
  * rows form: the distinct tokens, worker after worker, ascending within a worker:
  *   d_row_begin_out  [n_workers + 1]: worker w's rows are entries d_row_begin_out[w] .. d_row_begin_out[w + 1] - 1 of the
@@ -506,7 +507,9 @@ ADACOMP_API int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t
 ADACOMP_API int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens,
                                          uint32_t n_workers, const adacomp_rows_t* grad, float scale,
                                          const adacomp_rows_t* out, int accumulate, void* cuda_stream);
-/* Waits for cuda_stream, returns and clears the first error recorded on the device. */
+/* Waits for cuda_stream, returns and clears the first error recorded on the device.  ADACOMP_ERR_TIMEOUT: the blocks of a large
+ * sort waited for each other in vain (they run together, so this is not expected); gradients of that and later calls up to
+ * this one were not written. */
 ADACOMP_API int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream);
 ADACOMP_API int adacomp_embed_destroy(adacomp_embed_t* h);
 

@@ -19,7 +19,7 @@ struct adacomp_embed {
     uint32_t vocab, dim, max_tokens, max_workers, padding;
     int n_sms;
     int* d_status;
-    uint32_t* d_barrier;            // arrivals, and blocks that are through
+    uint32_t* d_barrier;            // [3] arrivals, blocks that are through, and whether a wait ever ran out
     uint64_t* d_tok[2];             // [max_tokens] worker * vocab + token and which token it is, between the passes of a large sort
     uint32_t* d_table;              // [kSortBlocks][kMaxBins] digit counts per block
     uint32_t* d_seg_begin;          // [max_tokens + 1] first sorted token of every distinct one, and their end
@@ -146,19 +146,19 @@ __device__ __forceinline__ uint32_t load_key(const SortJob& j, uint32_t t, bool 
 }
 
 // Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
-// does not, the block says so and the caller gives up.
+// does not, the block says so and the caller gives up: the sums then leave its lists alone.
 __device__ __forceinline__ bool meet(const SortJob& j) {
     __shared__ int s_ok;
     __syncthreads();
     if (threadIdx.x == 0) {
         __threadfence();
         const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
-        uint32_t seen = 0, polls = 0;
+        uint32_t seen = 0, polls = __ldcg(j.barrier + 2) ? kSpinLimit : 0;      // nobody waits for a block that gave up
         do {
             asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
         } while (seen < target && ++polls < kSpinLimit);
         s_ok = seen >= target;
-        if (seen < target) record_error(j.status, ADACOMP_ERR_TIMEOUT);
+        if (seen < target) j.barrier[2] = 1;
     }
     __syncthreads();
     return s_ok != 0;
@@ -589,7 +589,7 @@ struct Sums {
     float* partial;
     uint32_t* tickets;              // [levels][max_chunks][2][tiles]
     uint32_t max_chunks;
-    const int* status;
+    const uint32_t* gave_up;
     Rows grad;
     uint32_t dim, vocab;
     float scale;
@@ -880,7 +880,7 @@ template <typename A, typename B, int N, int K>
 __global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(const Sums p) {
     extern __shared__ uint64_t s_mem[];
     cudaGridDependencySynchronize();
-    if (*p.status == ADACOMP_ERR_TIMEOUT) return;           // the sort gave up: its lists are not to be followed
+    if (*p.gave_up) return;                                 // the sort did not get through: its lists are not to be followed
     if (blockIdx.x >= p.sum_blocks) {
         zero_gaps(p, blockIdx.x - p.sum_blocks, gridDim.x - p.sum_blocks);
         return;
@@ -1121,7 +1121,7 @@ size_t carve(adacomp_embed_t* h, void* ws, uint32_t max_tokens, uint32_t dim) {
     adacomp_embed_t e = {};
     e.d_status = c.take<int>(1);
     e.d_n_segs = c.take<uint32_t>(2);
-    e.d_barrier = c.take<uint32_t>(2);
+    e.d_barrier = c.take<uint32_t>(3);
     for (int i = 0; i < 2; ++i) e.d_tok[i] = c.take<uint64_t>(n);
     e.d_table = c.take<uint32_t>(static_cast<size_t>(kSortBlocks) * kMaxBins);
     e.d_seg_begin = c.take<uint32_t>(n + 1);
@@ -1282,7 +1282,7 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     p->chunk_shift = j.chunk_shift;
     p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
     p->partial = h->d_partial;
-    p->status = h->d_status;
+    p->gave_up = h->d_barrier + 2;
     p->dim = h->dim;
     p->vocab = h->vocab;
     p->tickets = h->d_tickets;
@@ -1358,8 +1358,9 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
         p.n_chunks = (j.n + kSmallChunk - 1) / kSmallChunk;
         uint64_t blocks = small_blocks;
         const uint64_t most = 2 * static_cast<uint64_t>(h->n_sms);
+        if (clear && blocks < p.zero_rows * p.dim * size / 32768) blocks = p.zero_rows * p.dim * size / 32768;     // 32 KB each
         if (blocks < 1) blocks = 1;
-        if (blocks > most || (clear && p.zero_rows * p.dim >= most * 4096)) blocks = most;
+        if (blocks > most) blocks = most;
         if (vec) k_embed_small<A, B, N><<<static_cast<uint32_t>(blocks), kSmallThreads, 0, stream>>>(j, p, x, y);
         else k_embed_small<A, B, 1><<<static_cast<uint32_t>(blocks), kSmallThreads, 0, stream>>>(j, p, x, y);
         ADACOMP_LAUNCH_CHECK();
@@ -1470,7 +1471,7 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     if (err == cudaSuccess) err = cudaDeviceGetAttribute(&e->n_sms, cudaDevAttrMultiProcessorCount, device);
     if (err == cudaSuccess) err = prepare_cluster(&e->cluster);
     if (err == cudaSuccess) err = cudaMemset(e->d_status, 0, sizeof(int));
-    if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 2 * sizeof(uint32_t));
+    if (err == cudaSuccess) err = cudaMemset(e->d_barrier, 0, 3 * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaMemset(e->d_tickets, 0, ticket_count(e->chunks, dim) * sizeof(uint32_t));
     if (err == cudaSuccess) err = cudaStreamSynchronize(nullptr);
     if (err != cudaSuccess) {
@@ -1553,12 +1554,15 @@ int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     int status = 0;
+    uint32_t gave_up = 0;
     ADACOMP_CUDA(cudaMemcpyAsync(&status, h->d_status, sizeof(int), cudaMemcpyDeviceToHost, stream));
+    ADACOMP_CUDA(cudaMemcpyAsync(&gave_up, h->d_barrier + 2, sizeof(uint32_t), cudaMemcpyDeviceToHost, stream));
     ADACOMP_CUDA(cudaMemsetAsync(h->d_status, 0, sizeof(int), stream));
     ADACOMP_CUDA(cudaStreamSynchronize(stream));
-    if (status == ADACOMP_ERR_TIMEOUT) {                            // blocks that gave up left the barrier anywhere
-        ADACOMP_CUDA(cudaMemsetAsync(h->d_barrier, 0, 2 * sizeof(uint32_t), stream));
+    if (gave_up) {                                                  // blocks that gave up left the barrier anywhere
+        ADACOMP_CUDA(cudaMemsetAsync(h->d_barrier, 0, 3 * sizeof(uint32_t), stream));
         ADACOMP_CUDA(cudaStreamSynchronize(stream));
+        return ADACOMP_ERR_TIMEOUT;
     }
     return status;
 }
