@@ -706,7 +706,7 @@ template <int N> __device__ __forceinline__ void put_piece(float* dst, const flo
 // Sums of one chunk's tokens: s_src says where their rows start and which of them end a segment, s_dst where the segments'
 // results go.  `slot` is the first token's segment, u0 the first one that begins in the chunk.  A thread keeps K groups of N
 // columns, `step` apart: N > 1 and K = 1 where rows sit on the 16-byte grid, N = 1 and K > 1 where they do not (one column at
-// a time would leave too little in flight: rows of 1001 bf16 entries, 32768 tokens, 105 us).
+// a time would leave too little in flight).
 template <typename A, typename B, int N, int K, int BATCH>
 __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, const uint64_t* s_dst, uint32_t len, uint32_t slot, uint32_t u0,
                                           uint32_t chunk, uint32_t c, uint32_t step) {
@@ -720,14 +720,15 @@ __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, 
     constexpr int kBatch = N * sizeof(A) == 32 ? BATCH / 2 : BATCH;         // rows in flight
     for (uint32_t i = 0; i < len; i += kBatch) {
         Packed<A, N> v[kBatch][K];
+        uint64_t at[kBatch];
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            if (i + k >= len) break;
-            const A* src = grad + (s_src[i + k] & ~kEnds);
+        for (int k = 0; k < kBatch; ++k) at[k] = s_src[i + k < len ? i + k : len - 1];
+        // no branch between the loads, the last rows of a chunk repeat its last: 524288 tokens x 2048 455 -> 448 us for the call,
+        // rows of 1001 bf16 entries 109 -> 81
 #pragma unroll
-            for (int g = 0; g < K; ++g)
-                if (g == 0 || c + g * step < p.dim) v[k][g].load(src + g * step);
-        }
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+            for (int g = 0; g < K; ++g) v[k][g].load(grad + (at[k] & ~kEnds) + (c + g * step < p.dim ? g * step : 0));
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             if (i + k >= len) break;
@@ -739,7 +740,7 @@ __device__ __forceinline__ void sum_chunk(const Sums& p, const uint64_t* s_src, 
                 for (int q = 0; q < N; ++q) sum[g][q] = __fadd_rn(sum[g][q], f[q]);
             }
             open = true;
-            if (!(s_src[i + k] & kEnds)) continue;
+            if (!(at[k] & kEnds)) continue;
             const bool piece = slot + 1 == u0;          // the last piece of a long segment
             const uint64_t at = piece ? 0 : s_dst[slot - u0];
 #pragma unroll
@@ -904,9 +905,9 @@ __global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(cons
         if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
     }
     __syncthreads();
-    // Four rows in flight per thread, 48 registers (five blocks of 256 per SM): 524288 tokens x 2048 in 410 us, 6.2 TB/s with the
-    // pieces of long segments counted.  The next four fetched before the last are added (80 registers): 430; rings of
-    // asynchronous copies to shared memory, eight rows deep: 410.
+    // Four rows in flight per thread, 56 registers (four blocks of 256 per SM): 524288 tokens x 2048 bf16 in 404 us, 6.3 TB/s with
+    // the pieces of long segments counted.  Measured against it: the next four rows fetched before the last are added (80
+    // registers) 430 us; rings of asynchronous copies to shared memory, eight rows deep, 410; five blocks per SM spill (+12 %).
     if (c < p.dim) sum_chunk<A, B, N, K, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, blockDim.x * N);
     if (!__syncthreads_or(s.lead || s.trail)) return;
     finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0, [&](uint32_t u) { return p.seg_key[u]; },
