@@ -486,12 +486,12 @@ class Server:
 
 # ----------------------------------------------------------------------------- clipping
 
-def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-    """An output tensor that belongs to the stream its kernels run on."""
+def _empty(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """An output tensor on the device of `like` that belongs to the stream its kernels run on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape) if like.dtype == dtype else like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _element_type(t: torch.Tensor, device: int, name: str) -> int:
@@ -586,29 +586,32 @@ class Clipper:
             if grads.device != self._index:
                 raise TypeError(f"grads: need tensors on {self.device}")
             return grads.table, len(grads.grads), 1, 0, 0, grads.out
-        out = grads if out is None else out
-        e = GradTensor()
-        e.grad_type, e.out_type = _element_type(grads, self._index, "grads"), _element_type(out, self._index, "out")
-        if grads.dim() != 2 or out.shape != grads.shape:
+        kind, shape = _element_type(grads, self._index, "grads"), grads.shape
+        if out is None:
+            out, out_kind = grads, kind
+        else:
+            out_kind = _element_type(out, self._index, "out")
+        if len(shape) != 2 or out.shape != shape:
             raise ValueError("grads: need a matrix [workers, entries], and out of the same shape")
-        W, n = grads.shape
-        for t in (grads, out):
-            if (n > 1 and t.stride(1) != 1) or (W > 1 and t.stride(0) < n):
+        W, n = shape
+        strides, out_strides = grads.stride(), out.stride()
+        for apart, inner in (strides, out_strides):
+            if (n > 1 and inner != 1) or (W > 1 and apart < n):
                 raise TypeError("grads, out: need contiguous rows that do not overlap")
         if out is not grads:
             at, size, to, out_size = grads.data_ptr(), grads.element_size(), out.data_ptr(), out.element_size()
             same = at == to and grads.dtype == out.dtype and (W == 1 or grads.stride(0) == out.stride(0))
             if not same and n and at < to + ((W - 1) * out.stride(0) + n) * out_size and to < at + ((W - 1) * grads.stride(0) + n) * size:
                 raise ValueError("out: overlaps the gradients")
-        e.d_grad, e.d_out, e.n = grads.data_ptr(), out.data_ptr(), n
-        return ctypes.byref(e), 1, W, grads.stride(0) if W > 1 else 0, out.stride(0) if W > 1 else 0, out
+        e = GradTensor(grads.data_ptr(), out.data_ptr(), n, kind, out_kind)
+        return ctypes.byref(e), 1, W, strides[0] if W > 1 else 0, out_strides[0] if W > 1 else 0, out
 
     def norm(self, grads, scale: float = 1.0, norm_out: Optional[torch.Tensor] = None,
              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """|scale| times the norm over all of a worker's entries: float32 [W]."""
         table, count, W, stride, _, _ = self._given(grads)
         if norm_out is None:
-            norm_out = _empty((W,), torch.float32, self.device, stream)
+            norm_out = _empty(self.workspace, (W,), torch.float32, stream)
         elif norm_out.numel() != W:
             raise ValueError("norm_out: need one entry per worker")
         _check(_lib.adacomp_grad_norm(self._h, table, count, stride, W, float(scale), _dev(norm_out, torch.float32, "norm_out"),
@@ -621,7 +624,7 @@ class Clipper:
         themselves; ``coef_out`` [W] receives the factors."""
         table, count, W, stride, out_stride, out = self._given(grads, out)
         if norm_out is None:
-            norm_out = _empty((W,), torch.float32, self.device, stream)
+            norm_out = _empty(self.workspace, (W,), torch.float32, stream)
         for t, name in ((norm_out, "norm_out"), (coef_out, "coef_out")):
             if t is not None and t.numel() != W:
                 raise ValueError(f"{name}: need one entry per worker")
@@ -727,7 +730,7 @@ class Embedding:
         shape = (*tokens.shape, self.dim)
         ids = self._tokens(tokens)
         if out is None:
-            out = _empty(shape, dtype or table.dtype, self.device, stream)
+            out = _empty(table, shape, dtype or table.dtype, stream)
         elif out.shape != shape or (dtype is not None and out.dtype != dtype):
             raise ValueError("out: need a row for every token, and the type asked for")
         _check(_lib.adacomp_embed_lookup(self._h, ctypes.byref(self._wide(table, "table")), ctypes.byref(ids), tokens.numel(),
@@ -748,7 +751,7 @@ class Embedding:
         for t, need, name in ((rows_out, n, "rows_out"), (values_out, n * self.dim, "values_out"), (idx_out, n * self.dim, "idx_out")):
             if t is not None and t.numel() < need:
                 raise ValueError(f"{name}: too small")
-        begin = _empty((workers + 1,), torch.int64, self.device, stream)
+        begin = _empty(self.workspace, (workers + 1,), torch.int64, stream)
         kind = _element_type(values_out, self._index, "values_out")
         _check(_lib.adacomp_embed_grad_rows(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
                                             _dev(rows_out, torch.int32, "rows_out") if rows_out is not None else None,
@@ -765,9 +768,9 @@ class Embedding:
         row_begin[w + 1] of the two lists; what lies behind the last is left as it was."""
         n = tokens.numel()
         if rows_out is None:
-            rows_out = _empty((n,), torch.int32, self.device, stream)
+            rows_out = _empty(grad, (n,), torch.int32, stream)
         if values_out is None:
-            values_out = _empty((n, self.dim), dtype, self.device, stream)
+            values_out = _empty(grad, (n, self.dim), dtype, stream)
         begin = self._grad_rows(tokens, grad, scale, workers, rows_out, values_out, None, 0, stream)
         return rows_out, values_out, begin
 
@@ -779,9 +782,9 @@ class Embedding:
         update is pairs row_begin[w] * dim .. row_begin[w + 1] * dim - 1."""
         n = tokens.numel()
         if idx_out is None:
-            idx_out = _empty((n, self.dim), torch.int32, self.device, stream)
+            idx_out = _empty(grad, (n, self.dim), torch.int32, stream)
         if val_out is None:
-            val_out = _empty((n, self.dim), torch.float32, self.device, stream)
+            val_out = _empty(grad, (n, self.dim), torch.float32, stream)
         elif val_out.dtype != torch.float32:
             raise TypeError("val_out: updates are float32")
         begin = self._grad_rows(tokens, grad, scale, workers, None, val_out, idx_out, offset, stream)

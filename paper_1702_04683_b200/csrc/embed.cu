@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, R
                                                        uint32_t tiles, int wide, int passing, float scale, int* status) {
     const uint32_t t0 = blockIdx.x / tiles * (blockDim.y * R) + threadIdx.y, tile = blockIdx.x % tiles;
     const uint32_t step = blockDim.x * N, c = tile * K * step + threadIdx.x * N;
+    const bool same = table.type == out.type && scale == 1.0f;
     uint32_t v[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -101,17 +102,21 @@ __global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, R
 #pragma unroll
         for (int g = 0; g < K; ++g) {
             if (c + g * step >= dim) continue;
-            float f[N];
-            if (v[r] != 0xFFFFFFFFu) {
-                row[r][g].unpack(f);
-#pragma unroll
-                for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
-            } else {
-#pragma unroll
-                for (int k = 0; k < N; ++k) f[k] = 0.f;
-            }
             Packed<B, N> q;
-            q.pack(f);
+            if (sizeof(A) == sizeof(B) && same && v[r] != 0xFFFFFFFFu) {
+                q = *reinterpret_cast<const Packed<B, N>*>(&row[r][g]);         // nothing to convert and nothing to multiply
+            } else {
+                float f[N];
+                if (v[r] != 0xFFFFFFFFu) {
+                    row[r][g].unpack(f);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) f[k] = 0.f;
+                }
+                q.pack(f);
+            }
             if (Packed<B, N>::kVecs == 2 && wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1], l2_policy(passing != 0));
             else if (N > 1 && Packed<B, N>::kVecs == 1 && passing) __stcs(reinterpret_cast<uint4*>(dst + g * step), q.v[0]);
             else q.store(dst + g * step);
