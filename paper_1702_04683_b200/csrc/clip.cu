@@ -3,12 +3,11 @@
 //   norm_w = |s| sqrt(sum_i g_i^2),   c_w = s min(1, max_norm / (norm_w + 1e-6)),   out_i = round(g_i c_w)
 //
 // Both kernels are one pass over the data (2 and 1 operations an entry): HBM bounds them.  The tensors of a call are cut
-// into units of some 16 KB; blocks take units in turn, so short tensors next to each other in the list go to different
+// into units of 32 KB of the input (first pass) or 8192 entries (second); blocks take units in turn, so short tensors next to each other in the list go to different
 // blocks.  The second pass walks the units from the back: what the first pass read last is still in L2.
 #include <cooperative_groups.h>
 #include <math.h>
 #include <new>
-#include <vector>
 
 #include "numeric.cuh"
 
@@ -17,9 +16,8 @@ using namespace adacomp;
 struct adacomp_clip {
     int device;
     uint32_t max_workers;
-    uint32_t n_blocks;              // partial sums per worker
     int n_sms;
-    double* d_partial;              // [max_workers][n_blocks]
+    double* d_partial;              // [max_workers][kMaxBlocks]
     uint32_t* d_done;               // [max_workers] blocks that have delivered their sum
     float* d_coef;                  // [max_workers]
 };
@@ -28,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVecsPerThread = 8;
-constexpr uint32_t kUnit = kThreads * kVecsPerThread;       // vectors of 16 bytes (norm) or items (write) per unit
+constexpr uint32_t kUnit = kThreads * kVecsPerThread;       // vectors of 16 bytes per unit of the first pass
 // Blocks resident per SM.  Loads in flight count: 8 vectors a thread and 3 blocks read 6.4 GB in 866 us (7.4 TB/s), 4 and 6 in
 // 884, 4 and 8 in 937.
 constexpr int kNormBlocks = 3, kWriteBlocks = 4;

@@ -4,8 +4,8 @@
 //   gradient  dE[w][v] = s sum of the gradient rows of worker w's tokens that equal v
 //
 // The gradient sorts the pairs (worker * vocab + token, position), stable, so a row's summands stand together and in
-// order; every row is then summed by whoever owns it, without atomics.  All of it is bound by HBM (one fp32 addition per
-// entry read).
+// order; every row is then summed by whoever owns it, without floating-point atomics.  The sums and the lookup are bound by
+// HBM (one fp32 operation per entry read), the sort by latency, small calls by the launch.
 #include <cooperative_groups.h>
 #include <math.h>
 #include <new>
@@ -1095,7 +1095,8 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob 
 
 // ---------------------------------------------------------------------------------------------- host
 
-// Tokens per chunk: long enough to keep the pieces of long segments rare, short enough that all SMs have work.
+// Tokens per chunk: long enough to keep the pieces of long segments rare, short enough that all SMs have work.  With kChunkBits 21,
+// 22 and 23 an update of 32768 tokens x 1024 took 73, 64 and 67 us when this was set; later versions differ by 3 %.
 constexpr uint32_t kMinShift = 3, kMaxShift = 6;
 constexpr uint32_t kChunkBits = 22;
 uint32_t chunk_shift_of(uint64_t n, uint32_t dim) {

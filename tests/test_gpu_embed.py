@@ -337,6 +337,37 @@ def test_another_stream(binding):
     assert torch.equal(looked, grad[tokens])
 
 
+@pytest.mark.parametrize("n", [500, 20_000, 150_000])
+def test_calls_in_a_captured_graph(binding, n):
+    """One launch, a cluster, a cooperative launch; with clipping behind them.  Replays see the inputs of the time."""
+    vocab, dim = 3_000, 32
+    tokens, grad = words((n,), vocab, 1), torch.randn((n, dim), device=DEV, generator=gen(1))
+    h, clipper = binding.Embedding(vocab, dim, max_tokens=n), binding.Clipper()
+    out, clipped = torch.empty((vocab, dim), device=DEV), torch.empty((1, vocab * dim), device=DEV)
+
+    def call():
+        h.grad_dense(tokens, grad, out)
+        return clipper.clip(out.view(1, -1), 1.0, out=clipped)[1]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = call()
+    for seed in (2, 3):
+        tokens.copy_(words((n,), vocab, seed))
+        grad.copy_(torch.randn((n, dim), device=DEV, generator=gen(seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, clipped, norm)]
+        want_norm = call()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, clipped, want_norm)))
+    assert h.last_error() == 0
+
+
 def test_refusals(binding):
     lib = binding.raw()
     vocab, dim = 20, 16
