@@ -227,41 +227,6 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __gri
     }
 }
 
-// Entries [e, e + N) of a tensor of n entries at `in` that does not sit on the 16-byte grid there: the vectors around them,
-// shifted into place, if all of those lie inside the tensor.
-template <typename A, int N>
-__device__ __forceinline__ Packed<A, N> load_shifted(const A* in, int64_t e, uint64_t n) {
-    constexpr int kVecs = Packed<A, N>::kVecs, kWords = 4 * (kVecs + 1);
-    const uintptr_t a = reinterpret_cast<uintptr_t>(in + e), lo = a & ~static_cast<uintptr_t>(15);
-    const uintptr_t first = reinterpret_cast<uintptr_t>(in), end = first + n * sizeof(A);
-    Packed<A, N> p;
-    if (lo >= first && lo + 16 * (kVecs + 1) <= end) {
-        uint32_t w[kWords];
-#pragma unroll
-        for (int i = 0; i <= kVecs; ++i) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(lo + 16 * i));     // the neighbour reads it too
-            w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
-        }
-        if (a & 8)
-#pragma unroll
-            for (int i = 0; i + 2 < kWords; ++i) w[i] = w[i + 2];
-        if (a & 4)
-#pragma unroll
-            for (int i = 0; i + 1 < kWords; ++i) w[i] = w[i + 1];
-        if (a & 2)
-#pragma unroll
-            for (int i = 0; i + 1 < kWords; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) p.v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
-    } else {
-        float f[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) f[j] = to_float(in[e + j]);
-        p.pack(f);
-    }
-    return p;
-}
-
 template <typename A, typename B, int N>
 __device__ __forceinline__ void scale_store(const Packed<A, N>& p, B* out, float c, uint64_t policy) {
     float f[N];

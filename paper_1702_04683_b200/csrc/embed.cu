@@ -124,6 +124,66 @@ __global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, R
     }
 }
 
+// The same where rows do not sit on the 16-byte grid and 16-bit entries make single ones too small a load: items of eight
+// entries on the grid of each output row, taken from the two vectors of the table around them.  `total` entries lie between the table's first and its last.
+template <typename A, typename B, int R>
+__global__ void __launch_bounds__(512) k_embed_lookup_off(Rows table, Rows tokens, Rows out, uint32_t n_tokens, uint32_t vocab, uint32_t dim,
+                                                           uint32_t tiles, uint64_t total, float scale, int* status) {
+    constexpr int N = 8;
+    const uint32_t t0 = blockIdx.x / tiles * (blockDim.y * R) + threadIdx.y, tile = blockIdx.x % tiles;
+    const int64_t item = static_cast<int64_t>(tile) * blockDim.x + threadIdx.x;
+    const A* in = reinterpret_cast<const A*>(table.data);
+    uint32_t v[R];
+    int64_t e[R];
+    Packed<A, N> row[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t t = t0 + r * blockDim.y;
+        v[r] = t < n_tokens ? load_token(tokens, t, vocab) : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t t = t0 + r * blockDim.y;
+        const uintptr_t dst = reinterpret_cast<uintptr_t>(reinterpret_cast<B*>(out.data) + (t < n_tokens ? out.offset(t) : 0));
+        e[r] = item * N - static_cast<int64_t>((dst & 15) / sizeof(B));
+        if (v[r] == 0xFFFFFFFFu || e[r] >= dim) continue;
+        const A* src = in + v[r] * table.row_stride;
+        if (e[r] >= 0 && e[r] + N <= dim) {
+            row[r] = load_shifted<A, N>(in, (src - in) + e[r], total);
+        } else {                                            // a row's first and last entries
+            float f[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k) f[k] = e[r] + k >= 0 && e[r] + k < dim ? to_float(src[e[r] + k]) : 0.f;
+            row[r].pack(f);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t t = t0 + r * blockDim.y;
+        if (t >= n_tokens || e[r] >= dim) continue;
+        if (v[r] == 0xFFFFFFFFu && item == 0) record_error(status, ADACOMP_ERR_INVALID);
+        B* dst = reinterpret_cast<B*>(out.data) + out.offset(t);
+        float f[N];
+        if (v[r] != 0xFFFFFFFFu) {
+            row[r].unpack(f);
+#pragma unroll
+            for (int k = 0; k < N; ++k) f[k] = __fmul_rn(f[k], scale);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) f[k] = 0.f;
+        }
+        if (e[r] >= 0 && e[r] + N <= dim) {
+            Packed<B, N> q;
+            q.pack(f);
+            q.store(dst + e[r]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (e[r] + k >= 0 && e[r] + k < dim) dst[e[r] + k] = from_float<B>(f[k]);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- sort
 
 struct SortJob {
@@ -1233,7 +1293,23 @@ int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32
                   float scale, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
     if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16)) return launch_lookup_vec<A, B, N, 1>(table, tokens, out, n_tokens, h, scale, stream);
-    return launch_lookup_vec<A, B, 1, 4>(table, tokens, out, n_tokens, h, scale, stream);
+    // Off the grid: single entries, or for long rows of 16-bit entries items of eight.  32768 bf16 rows one way and the other: of
+    // 250 entries 15.4 and 17.2 us, of 1001 52 and 38; fp32 rows of 1001 take 49 one entry at a time (6.1 TB/s on the grid, 5.4 off it).
+    if ((sizeof(A) == 4 && sizeof(B) == 4) || h->dim < 512) return launch_lookup_vec<A, B, 1, 4>(table, tokens, out, n_tokens, h, scale, stream);
+    uint32_t x, y, tiles;
+    const uint64_t cols = (static_cast<uint64_t>(h->dim) + 7 + 7) / 8;      // wherever a row starts
+    along_row(static_cast<uint32_t>(cols), 512, &x, &y, &tiles);
+    const uint64_t total = static_cast<uint64_t>(h->vocab - 1) * table.row_stride + h->dim;
+    const dim3 block(x, y);
+    if (n_tokens * cols >= 2ull * 2048 * h->n_sms) {
+        const uint32_t grid = static_cast<uint32_t>((static_cast<uint64_t>(n_tokens) + 2 * y - 1) / (2 * y) * tiles);
+        k_embed_lookup_off<A, B, 2><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale, h->d_status);
+    } else {
+        const uint32_t grid = (n_tokens + y - 1) / y * tiles;
+        k_embed_lookup_off<A, B, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale, h->d_status);
+    }
+    ADACOMP_LAUNCH_CHECK();
+    return ADACOMP_OK;
 }
 
 // A launch whose blocks may line up while the kernel before it ends; they wait for it themselves.
