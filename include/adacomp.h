@@ -437,7 +437,8 @@ ADACOMP_API int adacomp_grad_norm(adacomp_clip_t* h, const adacomp_grad_tensor_t
  * means that nothing is clipped (the norm is still reported and scale still applied).  With a finite max_norm an infinite
  * norm gives c_w = 0 (finite entries become zeros, infinite ones NaN) and a NaN norm makes every entry NaN.  Workers do not
  * affect each other.  Where an in-place tensor meets c_w = 1 nothing is written.  out entries of worker w start
- * out_stride * w elements behind d_out.  d_coef_out (NULL or [n_workers]) receives c_w: what selected
+ * out_stride * w elements behind d_out; with several workers out_stride is at least every tensor's n, and equal to grad_stride
+ * where a tensor is clipped in place (ADACOMP_ERR_INVALID otherwise).  d_coef_out (NULL or [n_workers]) receives c_w: what selected
  * pairs have to be multiplied by when the gradients themselves are left as they are. */
 ADACOMP_API int adacomp_clip(adacomp_clip_t* h, const adacomp_grad_tensor_t* h_tensors, uint32_t n_tensors,
                              uint64_t grad_stride, uint64_t out_stride, uint32_t n_workers, float scale, float max_norm,

@@ -227,6 +227,11 @@ def test_refusals(binding):
                 dict(d_grad=g.data_ptr() + 2), dict(d_out=g.data_ptr() + 1), dict(out_type=1), dict(n=1 << 40)):
         assert clip(**bad) == binding.ERR_INVALID, bad
     assert lib.adacomp_clip(h._h, None, 1, 0, 0, 1, 1.0, 1.0, norm.data_ptr(), None, None) == binding.ERR_INVALID
+    two, to = torch.ones((2, 100), device=DEV), torch.zeros((2, 100), device=DEV)
+    for d_out, stride, out_stride, want in ((to, 100, 99, binding.ERR_INVALID), (to, 100, 0, binding.ERR_INVALID), (two, 100, 101, binding.ERR_INVALID),
+                                            (two, 100, 100, 0), (to, 0, 100, 0), (to, 100, 100, 0)):
+        e = binding.GradTensor(two.data_ptr(), d_out.data_ptr(), 100, 0, 0)
+        assert lib.adacomp_clip(h._h, ctypes.byref(e), 1, stride, out_stride, 2, 1.0, 1.0, norm.data_ptr(), None, None) == want
     assert clip() == 0 and clip(n_tensors=0) == 0
     torch.cuda.synchronize()
     for bad in (lambda: h.norm(g), lambda: h.norm([g.double()]), lambda: h.norm([g.cpu()]),
