@@ -717,8 +717,8 @@ __device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t a
     }
 }
 
-// First of the n ascending keys that is not below `bound`, by a whole warp: 32 probes a step (one at a time, 17 steps to the L2
-// and back took longer than the clearing they were for).
+// First of the n ascending keys that is not below `bound`, by whole warps (the block has no other): 32 probes a step (one at a
+// time, 17 steps to the L2 and back took longer than the clearing they were for).
 __device__ __forceinline__ uint32_t warp_lower_bound(const uint32_t* keys, uint32_t n, uint64_t bound) {
     const uint32_t lane = threadIdx.x + threadIdx.y * blockDim.x & 31;
     uint32_t lo = 0, hi = n;
@@ -742,7 +742,7 @@ __device__ void zero_gaps(const Sums& p, uint32_t block, uint32_t n_blocks) {
     for (uint64_t r = from; r < to;) {
         if (k == kKeys) {
             __syncthreads();
-            if (tid < kKeys) s_key[tid] = base + tid < n_segs ? p.seg_key[base + tid] : 0xFFFFFFFFu;
+            for (uint32_t i = tid; i < kKeys; i += n_threads) s_key[i] = base + i < n_segs ? p.seg_key[base + i] : 0xFFFFFFFFu;
             __syncthreads();
             base += kKeys;
             k = 0;
@@ -1462,6 +1462,7 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
     const uint32_t per_thread = vec ? N : K;
     along_row((p.dim + per_thread - 1) / per_thread, kSumThreads, &x, &y, &p.tiles);
     while (y > 1 && y * chunk_bytes > 32 * 1024) y /= 2;
+    while (x * y < 32) x *= 2;                              // narrow rows, long chunks: a whole warp, some of it without columns
     p.sum_blocks = (p.n_chunks + y - 1) / y * p.tiles;
     uint32_t zero_blocks = 0;
     if (clear && p.zero_first < p.zero_rows) {

@@ -306,6 +306,38 @@ def test_sorts_of_every_size(binding, n, vocab, workers):
     check_grad(binding, tokens, grad, vocab, workers=workers, pad=3)
 
 
+def whole_numbers(shape, seed, dtype=torch.float32):
+    """Gradients of -4 .. 4: every partial sum of fewer than 2^22 of them is exact in fp32, in any order."""
+    return torch.randint(-4, 5, shape, device=DEV, generator=gen(seed), dtype=torch.int8).to(dtype)
+
+
+def whole_sums(tokens, grad, vocab):
+    return torch.zeros((vocab, grad.shape[-1]), device=DEV, dtype=torch.float64).index_add_(0, tokens, grad.double()).float()
+
+
+@pytest.mark.parametrize("kind,dim,n", [(torch.bfloat16, 8, 2 ** 23 + 77), (torch.bfloat16, 8, 2 ** 24 + 5), (torch.bfloat16, 16, 2 ** 23 + 1),
+                                        (torch.float32, 4, 2 ** 24 + 3), (torch.float16, 3, 25_000_001)])
+def test_dense_tables_of_narrow_rows_and_many_tokens(binding, kind, dim, n):
+    """Long chunks and few threads along a row: the smallest blocks that sum and clear.  Half of the rows have no token, some
+    of them in long stretches; sums are exact, so they have to be equal."""
+    vocab = 600_000
+    row = torch.randperm(vocab // 2, device=DEV, generator=gen(dim)) * 2 % (vocab - vocab // 5)         # even rows of the first four fifths
+    tokens = row[words((n,), len(row), n)]
+    grad = whole_numbers((n, dim), n, kind)
+    h = binding.Embedding(vocab, dim, max_tokens=n)
+    out = torch.full((vocab, dim), 7.0, device=DEV)
+    h.grad_dense(tokens, grad, out)
+    want = whole_sums(tokens, grad, vocab)
+    assert torch.equal(out, want)
+    h.grad_dense(tokens, grad, out, accumulate=True)
+    assert torch.equal(out, 2 * want)
+    rows, values, begin = h.grad_rows(tokens, grad)
+    present = torch.bincount(tokens, minlength=vocab).nonzero().view(-1)
+    assert begin.tolist() == [0, len(present)] and torch.equal(rows[:len(present)].long(), present)
+    assert torch.equal(values[:len(present)], want[present])
+    assert h.last_error() == 0
+
+
 def test_vocabularies_of_many_bits(binding):
     for vocab, workers in ((2 ** 31 - 1, 2), (2 ** 32 - 2, 1), (2 ** 20, 4095)):
         h = binding.Embedding(vocab, 2, max_tokens=workers * 300, max_workers=workers)
