@@ -52,7 +52,7 @@ enum {
     ADACOMP_ERR_WINDOW = -4,        /* pull timestamp j > i, or j older than the kept history   */
     ADACOMP_ERR_CAPACITY = -5,      /* more pairs / updates than the server was created for     */
     ADACOMP_ERR_UNSORTED = -6,      /* an update's indices are not strictly ascending / in range */
-    ADACOMP_ERR_TIMEOUT = -7,       /* reserved: a bounded device-side wait gave up             */
+    ADACOMP_ERR_TIMEOUT = -7,       /* a bounded device-side wait gave up                       */
     ADACOMP_ERR_UNIMPLEMENTED = -8
 };
 
@@ -508,6 +508,9 @@ ADACOMP_API int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t
 ADACOMP_API int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens,
                                          uint32_t n_workers, const adacomp_rows_t* grad, float scale,
                                          const adacomp_rows_t* out, int accumulate, void* cuda_stream);
+/* How often the blocks of a large sort look for each other before they give up (4194304, some seconds, at first; 0: once, so
+ * that a program's handling of ADACOMP_ERR_TIMEOUT can be tried). */
+ADACOMP_API int adacomp_embed_set_wait_limit(adacomp_embed_t* h, uint32_t polls);
 /* Waits for cuda_stream, returns and clears the first error recorded on the device.  ADACOMP_ERR_TIMEOUT: the blocks of a large
  * sort waited for each other in vain (they run together, so this is not expected); gradients of that and later calls up to
  * this one were not written. */

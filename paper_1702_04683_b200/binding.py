@@ -111,6 +111,7 @@ def _load():
         "adacomp_embed_lookup": (i32, [vp, vp, vp, u32, f32, vp, vp]),
         "adacomp_embed_grad_rows": (i32, [vp, vp, u32, u32, vp, f32, vp, vp, vp, i32, vp, u64, vp]),
         "adacomp_embed_grad_dense": (i32, [vp, vp, u32, u32, vp, f32, vp, i32, vp]),
+        "adacomp_embed_set_wait_limit": (i32, [vp, u32]),
         "adacomp_embed_last_error": (i32, [vp, vp]),
         "adacomp_embed_destroy": (i32, [vp]),
     }
@@ -804,6 +805,10 @@ class Embedding:
                                              ctypes.byref(self._wide(out, "out")), int(accumulate), _stream_on(stream, self._index)),
                "adacomp_embed_grad_dense")
         return out
+
+    def set_wait_limit(self, polls: int) -> None:
+        """How often the blocks of a large sort look for each other before they give up (ERR_TIMEOUT); 0: once."""
+        _check(_lib.adacomp_embed_set_wait_limit(self._h, int(polls)), "adacomp_embed_set_wait_limit")
 
     def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Waits for the stream; the first error the device recorded since the last call (a token outside the vocabulary)."""

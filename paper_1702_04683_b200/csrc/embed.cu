@@ -27,6 +27,7 @@ struct adacomp_embed {
     uint32_t* d_chunk_seg;          // [chunks + 1] how many segments begin before the chunk
     uint32_t* d_n_segs;             // [2] distinct tokens, and how many tokens of the sorted list have a gradient
     uint32_t* d_order;              // [max_tokens] positions in the order of the sort
+    uint32_t wait_limit;            // polls of a barrier
     uint32_t cluster;               // blocks of the largest cluster that the device takes
     uint32_t* d_tickets;            // [levels][chunks][2][blocks along a row], all zero between calls
     uint32_t chunks;                // the most that a call has
@@ -48,7 +49,7 @@ constexpr uint32_t kSortBlocks = 128;
 constexpr int kDigitBits = 9;
 constexpr int kMaxBins = 1 << kDigitBits;
 constexpr uint32_t kClusterSmem = kClusterStep * 8 + 16 * kMaxBins * 2 + kSortWarps * kMaxBins * 2;
-constexpr uint32_t kSpinLimit = 1u << 22;                   // polls of a barrier, some seconds
+constexpr uint32_t kWaitLimit = 1u << 22;                   // polls of a barrier, some seconds
 
 // Device view of adacomp_rows_t.
 struct Rows {
@@ -199,6 +200,7 @@ struct SortJob {
     uint32_t share_shift;                                   // cluster form: log2 of the tokens of a block
     uint64_t* row_begin;                                    // or null
     uint32_t* barrier;
+    uint32_t wait_limit;
     int* status;
 };
 constexpr uint32_t kLast = 1u << 31;
@@ -211,19 +213,24 @@ __device__ __forceinline__ uint32_t load_key(const SortJob& j, uint32_t t, bool 
 }
 
 // Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
-// does not, the block says so and the caller gives up: the sums then leave its lists alone.
+// does not, the block says so and gives up: the sums then leave its lists alone.  From then on no block arrives here, in this
+// call or a later one, until the host clears the words: the arrivals that were left behind would let blocks pass before the
+// others have delivered their counts, and places made of such counts lie anywhere.
 __device__ __forceinline__ bool meet(const SortJob& j) {
     __shared__ int s_ok;
     __syncthreads();
     if (threadIdx.x == 0) {
-        __threadfence();
-        const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
-        uint32_t seen = 0, polls = __ldcg(j.barrier + 2) ? kSpinLimit : 0;      // nobody waits for a block that gave up
-        do {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
-        } while (seen < target && ++polls < kSpinLimit);
-        s_ok = seen >= target;
-        if (seen < target) j.barrier[2] = 1;
+        s_ok = 0;
+        if (__ldcg(j.barrier + 2) == 0) {
+            __threadfence();
+            const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
+            uint32_t seen = 0, polls = 0;
+            do {
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
+            } while (seen < target && ++polls < j.wait_limit);
+            s_ok = seen >= target;
+            if (seen < target) j.barrier[2] = 1;
+        }
     }
     __syncthreads();
     return s_ok != 0;
@@ -1355,6 +1362,7 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     j.chunk_shift = chunk_shift_of(j.n, h->dim);
     j.row_begin = d_row_begin;
     j.barrier = h->d_barrier;
+    j.wait_limit = h->wait_limit;
     j.status = h->d_status;
     p->order = j.order;
     p->seg_begin = j.seg_begin;
@@ -1549,6 +1557,7 @@ int adacomp_embed_create(adacomp_embed_t** h, uint32_t vocab, uint32_t dim, uint
     e->max_tokens = max_tokens;
     e->max_workers = max_workers;
     e->padding = padding_token;
+    e->wait_limit = kWaitLimit;
     carve(e, d_workspace, max_tokens, dim);
     DeviceGuard guard(device);
     cudaError_t err = guard.err;
@@ -1630,6 +1639,12 @@ int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_t* tokens, u
     p.zero_rows = static_cast<uint64_t>(n_workers) * h->vocab;
     const uint32_t out_grid = on_grid(p.out, 32) ? 32 : on_grid(p.out, 16) ? 16 : 1;
     return ADACOMP_BY_TYPE(launch_sums, p.grad.type, p.out.type, j, p, out_grid, !accumulate, h, stream);
+}
+
+int adacomp_embed_set_wait_limit(adacomp_embed_t* h, uint32_t polls) {
+    if (!h) return ADACOMP_ERR_INVALID;
+    h->wait_limit = polls;
+    return ADACOMP_OK;
 }
 
 int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream) {

@@ -338,6 +338,24 @@ def test_dense_tables_of_narrow_rows_and_many_tokens(binding, kind, dim, n):
     assert h.last_error() == 0
 
 
+@pytest.mark.parametrize("n", [66_000, 150_000, 400_001])
+def test_a_large_sort_that_gives_up(binding, n):
+    """Blocks that look for each other once only give up (none waits for anything); until the error is read, nothing is sorted or
+    written any more, however many blocks a call has; afterwards the handle goes on."""
+    vocab, dim, most = 3_000, 8, 500_000
+    h = binding.Embedding(vocab, dim, max_tokens=most)
+    rows_out = torch.full((most,), -5, dtype=torch.int32, device=DEV)
+    values_out = torch.full((most, dim), 7.0, device=DEV)
+    h.set_wait_limit(0)
+    for m in (n, 90_001, n, 300_007):
+        h.grad_rows(words((m,), vocab, m), whole_numbers((m, dim), m), rows_out=rows_out, values_out=values_out)
+        h.set_wait_limit(1 << 22)                                           # the later calls would wait, if they still met
+        assert bool((rows_out == -5).all()) and bool((values_out == 7).all())
+    assert h.last_error() == binding.ERR_TIMEOUT and h.last_error() == 0
+    check_grad(binding, words((n,), vocab, n), whole_numbers((n, dim), n), vocab, handle=h)
+    check_grad(binding, words((most,), vocab, 1), whole_numbers((most, dim), 1), vocab, handle=h)
+
+
 def test_vocabularies_of_many_bits(binding):
     for vocab, workers in ((2 ** 31 - 1, 2), (2 ** 32 - 2, 1), (2 ** 20, 4095)):
         h = binding.Embedding(vocab, 2, max_tokens=workers * 300, max_workers=workers)
