@@ -667,6 +667,8 @@ struct Sums {
     float scale;
     // rows form
     uint32_t* rows_out;
+    uint64_t* row_begin;
+    uint32_t n_workers;
     char* values;
     uint32_t* idx_out;
     uint32_t idx_offset;
@@ -945,6 +947,12 @@ __device__ __forceinline__ void finish_long(const Sums& p, const Pieces& x, uint
     }
 }
 
+// A call whose sort gave up, or that came after one: its lists read as empty.
+__device__ __forceinline__ void put_no_rows(const Sums& p) {
+    if (blockIdx.x != 0 || !p.row_begin) return;
+    for (uint32_t w = threadIdx.y * blockDim.x + threadIdx.x; w <= p.n_workers; w += blockDim.x * blockDim.y) p.row_begin[w] = 0;
+}
+
 // Sums over the sorted list, cut into chunks of 2^chunk_shift tokens.  A chunk owns the segments that begin in it, to their
 // end even if that lies in the next chunk; a segment longer than a chunk is cut at the chunks' borders, its pieces are
 // added up by finish_long.  So the work per chunk is bounded, short segments need no second pass and the tree of additions
@@ -953,7 +961,10 @@ template <typename A, typename B, int N, int K>
 __global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(const Sums p) {
     extern __shared__ uint64_t s_mem[];
     cudaGridDependencySynchronize();
-    if (*p.gave_up) return;                                 // the sort did not get through: its lists are not to be followed
+    if (*p.gave_up) {                                       // the sort did not get through: its lists are not to be followed
+        put_no_rows(p);
+        return;
+    }
     if (blockIdx.x >= p.sum_blocks) {
         zero_gaps(p, blockIdx.x - p.sum_blocks, gridDim.x - p.sum_blocks);
         return;
@@ -1116,7 +1127,12 @@ __device__ __forceinline__ void clear_small(const Sums& p, const SmallMem& m) {
 template <typename A, typename B, int N>
 __global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
     __shared__ SmallMem m;
+    const bool gave_up = *p.gave_up != 0;                   // of an earlier call: on its way while the tokens are sorted
     sort_small(j, m);
+    if (gave_up) {
+        put_no_rows(p);
+        return;
+    }
     if (blockIdx.x == 0 && j.row_begin && j.n_workers == 1) {
         if (threadIdx.x < 2) j.row_begin[threadIdx.x] = threadIdx.x ? m.n_segs : 0;
     } else if (blockIdx.x == 0 && j.row_begin) {
@@ -1374,6 +1390,8 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
     p->partial = h->d_partial;
     p->gave_up = h->d_barrier + 2;
+    p->row_begin = d_row_begin;
+    p->n_workers = n_workers;
     p->dim = h->dim;
     p->vocab = h->vocab;
     p->tickets = h->d_tickets;

@@ -356,6 +356,30 @@ def test_a_large_sort_that_gives_up(binding, n):
     check_grad(binding, words((most,), vocab, 1), whole_numbers((most, dim), 1), vocab, handle=h)
 
 
+@pytest.mark.parametrize("workers", [1, 5])
+def test_calls_after_a_sort_that_gave_up(binding, workers):
+    """Calls of every route (one launch, a cluster, many blocks) come out empty until the error is read."""
+    vocab, dim, most = 2_000, 8, 100_000
+    h = binding.Embedding(vocab, dim, max_tokens=most, max_workers=workers)
+
+    def batch(n):
+        return words((workers, n // workers), vocab, n), whole_numbers((workers, n // workers, dim), n)
+
+    h.set_wait_limit(0)
+    for n in (most, 500, 20_000, most):
+        assert h.grad_rows(*batch(n), workers=workers)[2].tolist() == [0] * (workers + 1)
+        assert h.grad_update(*batch(n), workers=workers)[2].tolist() == [0] * (workers + 1)
+        table = torch.full((workers, vocab, dim), 7.0, device=DEV)
+        h.grad_dense(*batch(n), table, workers=workers, accumulate=True)
+        assert bool((table == 7).all())
+        h.grad_dense(*batch(n), table, workers=workers)
+        assert bool(((table == 7) | (table == 0)).all())
+    assert h.last_error() == binding.ERR_TIMEOUT and h.last_error() == 0
+    h.set_wait_limit(1 << 22)
+    for n in (500, 20_000, most):
+        check_grad(binding, *batch(n), vocab, workers=workers, handle=h)
+
+
 def test_vocabularies_of_many_bits(binding):
     for vocab, workers in ((2 ** 31 - 1, 2), (2 ** 32 - 2, 1), (2 ** 20, 4095)):
         h = binding.Embedding(vocab, 2, max_tokens=workers * 300, max_workers=workers)
