@@ -376,8 +376,9 @@ int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t 
         if (t.n && (!t.d_grad || reinterpret_cast<uintptr_t>(t.d_grad) % type_size(t.grad_type))) return ADACOMP_ERR_INVALID;
         if (!write) continue;
         if (!known_type(t.out_type)) return ADACOMP_ERR_INVALID;
-        if (t.n && (!t.d_out || reinterpret_cast<uintptr_t>(t.d_out) % type_size(t.out_type))) return ADACOMP_ERR_INVALID;
-        if (t.n && t.d_out == t.d_grad && t.out_type != t.grad_type) return ADACOMP_ERR_INVALID;
+        if (t.n == 0) continue;             // its pointers and strides mean nothing
+        if (!t.d_out || reinterpret_cast<uintptr_t>(t.d_out) % type_size(t.out_type)) return ADACOMP_ERR_INVALID;
+        if (t.d_out == t.d_grad && t.out_type != t.grad_type) return ADACOMP_ERR_INVALID;
         // the workers' outputs keep clear of each other, and in place they lie where the gradients do
         if (n_workers > 1 && (out_stride < t.n || (t.d_out == t.d_grad && out_stride != in_stride))) return ADACOMP_ERR_INVALID;
     }

@@ -209,6 +209,19 @@ def test_another_stream_and_calls_in_a_row(binding):
         assert torch.equal(x, norm)
 
 
+def test_empty_tensor_without_addresses_among_several_workers(binding):
+    """An entry of n = 0 with null pointers is no tensor in place: it asks nothing of the strides."""
+    g, out = normals(2 * 110, 1).view(2, 110), torch.full((2, 130), 7.0, device=DEV)
+    norm, coef = torch.empty(2, device=DEV), torch.empty(2, device=DEV)
+    table = (binding.GradTensor * 2)(binding.GradTensor(None, None, 0, 0, 0), binding.GradTensor(g.data_ptr(), out.data_ptr(), 100, 0, 0))
+    h = binding.Clipper(max_workers=2)
+    assert binding.raw().adacomp_clip(h._h, table, 2, 110, 130, 2, 1.0, 0.1, norm.data_ptr(), coef.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out[:, :100], g[:, :100] * coef.view(2, 1)) and bool((out[:, 100:] == 7).all())
+    for w in range(2):
+        check_norm(norm[w], exact_norm([g[w, :100]]))
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)
