@@ -551,12 +551,19 @@ class GradList:
                     spans.append((to, to + n * o.element_size(), True))
         spans.sort()
         reach = reach_written = 0               # how far the tensors before extend, and those of them that are written
+        self.overlapping = False
         for begin, end, written in spans:
-            if begin < reach_written or (written and begin < reach):
-                raise ValueError("out: overlaps a gradient or another output")
+            self.overlapping |= begin < reach_written or (written and begin < reach)
             reach = max(reach, end)
             if written:
                 reach_written = max(reach_written, end)
+        if out is not None:
+            self.check_apart()
+
+    def check_apart(self):
+        """Tensors that share memory can be measured, not clipped."""
+        if self.overlapping:
+            raise ValueError("out: overlaps a gradient or another output")
 
 
 class Clipper:
@@ -577,7 +584,7 @@ class Clipper:
                                         self.device.index), "adacomp_clip_create")
         self._h = h
 
-    def _given(self, grads, out=None):
+    def _given(self, grads, out=None, write=False):
         """(table, tensors, workers, gradient stride, output stride, outputs)"""
         if not isinstance(grads, (torch.Tensor, GradList)):
             grads = GradList(grads, out)
@@ -586,6 +593,8 @@ class Clipper:
         if isinstance(grads, GradList):
             if grads.device != self._index:
                 raise TypeError(f"grads: need tensors on {self.device}")
+            if write:
+                grads.check_apart()
             return grads.table, len(grads.grads), 1, 0, 0, grads.out
         kind, shape = _element_type(grads, self._index, "grads"), grads.shape
         if out is None:
@@ -596,9 +605,10 @@ class Clipper:
             raise ValueError("grads: need a matrix [workers, entries], and out of the same shape")
         W, n = shape
         strides, out_strides = grads.stride(), out.stride()
-        for apart, inner in (strides, out_strides):
-            if (n > 1 and inner != 1) or (W > 1 and apart < n):
-                raise TypeError("grads, out: need contiguous rows that do not overlap")
+        if n > 1 and (strides[1] != 1 or out_strides[1] != 1):
+            raise TypeError("grads, out: need contiguous rows")
+        if write and W > 1 and out_strides[0] < n:
+            raise TypeError("out: need rows that do not overlap")
         if out is not grads:
             at, size, to, out_size = grads.data_ptr(), grads.element_size(), out.data_ptr(), out.element_size()
             same = at == to and grads.dtype == out.dtype and (W == 1 or grads.stride(0) == out.stride(0))
@@ -623,7 +633,7 @@ class Clipper:
              coef_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """out = grads * scale * min(1, max_norm / (norm + 1e-6)) -> (out, norm [W]).  ``out`` defaults to the gradients
         themselves; ``coef_out`` [W] receives the factors."""
-        table, count, W, stride, out_stride, out = self._given(grads, out)
+        table, count, W, stride, out_stride, out = self._given(grads, out, write=True)
         if norm_out is None:
             norm_out = _empty(self.workspace, (W,), torch.float32, stream)
         for t, name in ((norm_out, "norm_out"), (coef_out, "coef_out")):

@@ -222,6 +222,32 @@ def test_empty_tensor_without_addresses_among_several_workers(binding):
         check_norm(norm[w], exact_norm([g[w, :100]]))
 
 
+def test_norms_of_tensors_that_share_memory(binding):
+    """A norm writes to no gradient: tied tensors, overlapping ones and a row that all workers share are counted as often as they are
+    given.  Clipping them in place is refused as before."""
+    g = normals(5_000, 1)
+    h = binding.Clipper(max_workers=3)
+    for tensors in ([g, g], [g[:3_000], g[2_000:]], [g.view(50, 100), g.view(50, 100).t(), g[7:8]]):
+        check_norm(h.norm(tensors), exact_norm(tensors))
+        check_norm(h.norm(binding.GradList(tensors)), exact_norm(tensors))
+        kept = g.clone()
+        for given in (tensors, binding.GradList(tensors)):
+            with pytest.raises(ValueError):
+                h.clip(given, 1.0)
+        assert torch.equal(g, kept)
+    for rows in (g.expand(3, -1), g.as_strided((3, 1_000), (500, 1))):
+        norm = h.norm(rows)
+        assert norm.shape == (3,)
+        for w in range(3):
+            check_norm(norm[w], exact_norm([rows[w]]))
+        out = torch.empty((3, rows.shape[1]), device=DEV)
+        coef = torch.empty(3, device=DEV)
+        h.clip(rows, 0.01, out=out, coef_out=coef)
+        assert torch.equal(out, rows * coef.view(3, 1))
+        with pytest.raises(TypeError):
+            h.clip(rows, 0.01)
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)
