@@ -754,6 +754,10 @@ class Embedding:
             raise ValueError("tokens: need the same number for every worker")
         if grad.numel() != tokens.numel() * self.dim:
             raise ValueError("grad: need a row for every token")
+        if grad.dim() > 2 and tokens.dim() > 1 and grad.shape[:-1] != tokens.shape:
+            # lists of rows or of tokens are in the order of the other; two shapes have to be the same, but for ones
+            if [n for n in grad.shape[:-1] if n != 1] != [n for n in tokens.shape if n != 1]:
+                raise ValueError("grad: need the shape of the tokens")
         return self._tokens(tokens), tokens.numel() // workers, self._wide(grad, "grad")
 
     def _grad_rows(self, tokens, grad, scale, workers, rows_out, values_out, idx_out, offset, stream):

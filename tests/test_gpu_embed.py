@@ -442,6 +442,22 @@ def test_calls_in_a_captured_graph(binding, n):
     assert h.last_error() == 0
 
 
+def test_gradients_in_another_order_than_their_tokens(binding):
+    """[tokens, workers, dim] next to [workers, tokens] has as many rows, but they are other tokens' rows."""
+    tokens = words((3, 50), 20, 1)
+    grad = torch.randn((3, 50, 8), device=DEV, generator=gen(1))
+    h = binding.Embedding(20, 8, max_tokens=150, max_workers=3)
+    table = torch.empty((3, 20, 8), device=DEV)
+    for call in (lambda t, g: h.grad_rows(t, g, workers=3), lambda t, g: h.grad_update(t, g, workers=3),
+                 lambda t, g: h.grad_dense(t, g, table, workers=3)):
+        for g in (grad.transpose(0, 1), grad.transpose(0, 1).contiguous(), grad.reshape(5, 30, 8)):
+            with pytest.raises(ValueError):
+                call(tokens, g)
+    want = h.grad_dense(tokens, grad, torch.empty_like(table), workers=3)
+    for t, g in ((tokens, grad.view(150, 8)), (tokens.view(150), grad), (tokens.view(3, 1, 50), grad), (tokens, grad.view(1, 3, 50, 8))):
+        assert torch.equal(h.grad_dense(t, g, table, workers=3), want)      # the same order, in other shapes
+
+
 def test_refusals(binding):
     lib = binding.raw()
     vocab, dim = 20, 16
