@@ -67,8 +67,8 @@ __device__ __forceinline__ uint32_t load_token(const Rows& tokens, uint32_t t, u
     const uint64_t at = tokens.offset(t);
     uint64_t v;
     if (tokens.type == ADACOMP_I64) v = reinterpret_cast<const uint64_t*>(tokens.data)[at];
-    else v = reinterpret_cast<const uint32_t*>(tokens.data)[at];
-    return v < vocab ? static_cast<uint32_t>(v) : 0xFFFFFFFFu;      // negative numbers are large ones here
+    else v = static_cast<uint64_t>(static_cast<int64_t>(reinterpret_cast<const int32_t*>(tokens.data)[at]));
+    return v < vocab ? static_cast<uint32_t>(v) : 0xFFFFFFFFu;      // negative numbers are large ones here, above any vocabulary
 }
 
 // ---------------------------------------------------------------------------------------------- lookup

@@ -458,6 +458,22 @@ def test_gradients_in_another_order_than_their_tokens(binding):
         assert torch.equal(h.grad_dense(t, g, table, workers=3), want)      # the same order, in other shapes
 
 
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_negative_tokens_of_the_largest_vocabulary(binding, dtype):
+    """More than 2^31 words: a negative 32-bit number is no word of them."""
+    vocab = 2 ** 32 - 2
+    h = binding.Embedding(vocab, 2, max_tokens=6)
+    tokens = torch.tensor([-5, 3, -1, 2 ** 31 - 1, -2 ** 31, 3], device=DEV).to(dtype)
+    table = torch.tensor([[1.5, -2.5]], device=DEV).expand(vocab, 2)        # one row for all words
+    got = h.lookup(table, tokens)
+    assert torch.equal(got, torch.where((tokens >= 0).view(-1, 1), table[:6], 0.0))
+    assert h.last_error() == binding.ERR_INVALID
+    rows, values, begin = h.grad_rows(tokens, torch.arange(12.0, device=DEV).view(6, 2))
+    assert begin.tolist() == [0, 2] and rows[:2].tolist() == [3, 2 ** 31 - 1]
+    assert values[:2].tolist() == [[2 + 10, 3 + 11], [6, 7]]
+    assert h.last_error() == binding.ERR_INVALID and h.last_error() == 0
+
+
 def test_refusals(binding):
     lib = binding.raw()
     vocab, dim = 20, 16
