@@ -495,7 +495,7 @@ ADACOMP_API int adacomp_embed_lookup(adacomp_embed_t* h, const adacomp_rows_t* t
  *   d_idx_out        NULL or [.][dim]: idx_offset + token * dim + column, the index of every value in the parameter vector
  *                    whose entries idx_offset .. idx_offset + vocab * dim - 1 are the table (they must stay below 2^32):
  *                    with fp32 values (d_idx_out, d_values_out) are updates as adacomp_apply takes them.
- * What lies behind the last row is left as it was. */
+ * What lies behind the last row is left as it was.  Every list is aligned to its elements (ADACOMP_ERR_INVALID otherwise). */
 ADACOMP_API int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, uint32_t n_tokens,
                                         uint32_t n_workers, const adacomp_rows_t* grad, float scale, uint32_t* d_rows_out,
                                         uint64_t* d_row_begin_out, void* d_values_out, int values_type,

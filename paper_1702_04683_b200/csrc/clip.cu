@@ -373,11 +373,11 @@ int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t 
     for (uint32_t i = 0; i < n_tensors; ++i) {
         const adacomp_grad_tensor_t& t = ts[i];
         if (!known_type(t.grad_type) || t.n >= (1ull << 40)) return ADACOMP_ERR_INVALID;
-        if (t.n && (!t.d_grad || reinterpret_cast<uintptr_t>(t.d_grad) % type_size(t.grad_type))) return ADACOMP_ERR_INVALID;
+        if (t.n && (!t.d_grad || !aligned(t.d_grad, type_size(t.grad_type)))) return ADACOMP_ERR_INVALID;
         if (!write) continue;
         if (!known_type(t.out_type)) return ADACOMP_ERR_INVALID;
         if (t.n == 0) continue;             // its pointers and strides mean nothing
-        if (!t.d_out || reinterpret_cast<uintptr_t>(t.d_out) % type_size(t.out_type)) return ADACOMP_ERR_INVALID;
+        if (!t.d_out || !aligned(t.d_out, type_size(t.out_type))) return ADACOMP_ERR_INVALID;
         if (t.d_out == t.d_grad && t.out_type != t.grad_type) return ADACOMP_ERR_INVALID;
         // the workers' outputs keep clear of each other, and in place they lie where the gradients do
         if (n_workers > 1 && (out_stride < t.n || (t.d_out == t.d_grad && out_stride != in_stride))) return ADACOMP_ERR_INVALID;
@@ -447,6 +447,7 @@ int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, 
         uint32_t n_workers, float scale, float max_norm, float* d_norm, float* d_coef_out, bool write, void* cuda_stream) {
     if (!h || !d_norm || n_workers == 0 || n_workers > h->max_workers || !isfinite(scale)) return ADACOMP_ERR_INVALID;
     if (write && !(max_norm > 0.f)) return ADACOMP_ERR_INVALID;
+    if (!aligned(d_norm, sizeof(float)) || !aligned(d_coef_out, sizeof(float))) return ADACOMP_ERR_INVALID;
     int rc = check_tensors(ts, n_tensors, in_stride, out_stride, n_workers, write);
     if (rc != ADACOMP_OK) return rc;
     DeviceGuard guard(h->device);

@@ -1248,7 +1248,7 @@ int rows_view(const adacomp_rows_t* r, uint64_t n_rows, bool tokens, Rows* out) 
     if (!r) return ADACOMP_ERR_INVALID;
     if (tokens ? (r->type != ADACOMP_I32 && r->type != ADACOMP_I64) : !known_type(r->type)) return ADACOMP_ERR_INVALID;
     const uint32_t size = tokens ? (r->type == ADACOMP_I64 ? 8u : 4u) : type_size(r->type);
-    if (n_rows && (!r->d_data || reinterpret_cast<uintptr_t>(r->d_data) % size)) return ADACOMP_ERR_INVALID;
+    if (n_rows && (!r->d_data || !aligned(r->d_data, size))) return ADACOMP_ERR_INVALID;
     out->data = static_cast<char*>(r->d_data);
     out->type = r->type;
     out->group = r->group;
@@ -1615,7 +1615,9 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     if (rc != ADACOMP_OK) return rc;
     const uint32_t n = n_tokens * n_workers;
     if (!d_row_begin_out || !known_type(values_type) || (n && !d_values_out)) return ADACOMP_ERR_INVALID;
-    if (reinterpret_cast<uintptr_t>(d_values_out) % type_size(values_type)) return ADACOMP_ERR_INVALID;
+    if (!aligned(d_values_out, type_size(values_type)) || !aligned(d_rows_out, sizeof(uint32_t)) || !aligned(d_idx_out, sizeof(uint32_t)) ||
+        !aligned(d_row_begin_out, sizeof(uint64_t)))
+        return ADACOMP_ERR_INVALID;
     if (d_idx_out && (idx_offset >= (1ull << 32) || idx_offset + static_cast<uint64_t>(h->vocab) * h->dim > (1ull << 32))) return ADACOMP_ERR_INVALID;
     Rows k;
     Sums p = {};

@@ -9,6 +9,7 @@
 namespace adacomp {
 
 __host__ __device__ __forceinline__ uint32_t type_size(int type) { return type == ADACOMP_F32 ? 4u : 2u; }
+inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline bool known_type(int type) { return type == ADACOMP_F32 || type == ADACOMP_BF16 || type == ADACOMP_F16; }
 
 template <int TYPE> struct ElemOf;

@@ -248,6 +248,18 @@ def test_norms_of_tensors_that_share_memory(binding):
             h.clip(rows, 0.01)
 
 
+def test_misaligned_results_are_refused(binding):
+    lib = binding.raw()
+    h = binding.Clipper()
+    g = torch.ones(100, device=DEV)
+    e = binding.GradTensor(g.data_ptr(), g.data_ptr(), 100, 0, 0)
+    at = torch.zeros(64, dtype=torch.uint8, device=DEV).data_ptr()
+    for off in (1, 2, 3):
+        assert lib.adacomp_grad_norm(h._h, ctypes.byref(e), 1, 0, 1, 1.0, at + off, None) == binding.ERR_INVALID
+        assert lib.adacomp_clip(h._h, ctypes.byref(e), 1, 0, 0, 1, 1.0, 1.0, at + off, None, None) == binding.ERR_INVALID
+        assert lib.adacomp_clip(h._h, ctypes.byref(e), 1, 0, 0, 1, 1.0, 1.0, at, at + off, None) == binding.ERR_INVALID
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)

@@ -474,6 +474,20 @@ def test_negative_tokens_of_the_largest_vocabulary(binding, dtype):
     assert h.last_error() == binding.ERR_INVALID and h.last_error() == 0
 
 
+def test_misaligned_lists_are_refused(binding):
+    lib = binding.raw()
+    h = binding.Embedding(20, 16, max_tokens=100)
+    tokens, grad = torch.zeros(50, dtype=torch.int64, device=DEV), torch.zeros((50, 16), device=DEV)
+    k, g = binding.Rows(tokens.data_ptr(), 1, 0, 1, 0), binding.Rows(grad.data_ptr(), 0, 0, 16, 0)
+    at = torch.zeros(4096, dtype=torch.uint8, device=DEV).data_ptr()
+
+    def call(rows=None, begin=at, values=grad.data_ptr(), idx=None):
+        return lib.adacomp_embed_grad_rows(h._h, ctypes.byref(k), 50, 1, ctypes.byref(g), 1.0, rows, begin, values, 0, idx, 0, None)
+
+    for bad in (dict(rows=at + 2), dict(begin=at + 4), dict(values=at + 1), dict(idx=at + 2)):
+        assert call(**bad) == binding.ERR_INVALID, bad
+
+
 def test_refusals(binding):
     lib = binding.raw()
     vocab, dim = 20, 16
