@@ -487,6 +487,14 @@ class Server:
 
 # ----------------------------------------------------------------------------- clipping
 
+def _workspace(nbytes: int, device: torch.device) -> torch.Tensor:
+    """Device memory for a handle.  The allocator hands out memory that earlier work of the current stream may still write to, and
+    handles clear theirs on the default stream: that work is waited for."""
+    workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    torch.cuda.current_stream(device).synchronize()
+    return workspace
+
+
 def _empty(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """An output tensor on the device of `like` that belongs to the stream its kernels run on."""
     if stream is None:
@@ -578,7 +586,7 @@ class Clipper:
         self.max_workers = int(max_workers)
         nbytes = ctypes.c_size_t(0)
         _check(_lib.adacomp_clip_workspace_bytes(self.max_workers, ctypes.byref(nbytes)), "adacomp_clip_workspace_bytes")
-        self.workspace = torch.empty(max(int(nbytes.value), 256), dtype=torch.uint8, device=self.device)
+        self.workspace = _workspace(int(nbytes.value), self.device)
         h = ctypes.c_void_p()
         _check(_lib.adacomp_clip_create(ctypes.byref(h), self.max_workers, self.workspace.data_ptr(), self.workspace.numel(),
                                         self.device.index), "adacomp_clip_create")
@@ -706,7 +714,7 @@ class Embedding:
         nbytes = ctypes.c_size_t(0)
         _check(_lib.adacomp_embed_workspace_bytes(self.vocab, self.dim, self.max_tokens, self.max_workers, ctypes.byref(nbytes)),
                "adacomp_embed_workspace_bytes")
-        self.workspace = torch.empty(max(int(nbytes.value), 256), dtype=torch.uint8, device=self.device)
+        self.workspace = _workspace(int(nbytes.value), self.device)
         h = ctypes.c_void_p()
         _check(_lib.adacomp_embed_create(ctypes.byref(h), self.vocab, self.dim, self.max_tokens, self.max_workers, pad,
                                          self.workspace.data_ptr(), self.workspace.numel(), self.device.index),

@@ -260,6 +260,31 @@ def test_misaligned_results_are_refused(binding):
         assert lib.adacomp_clip(h._h, ctypes.byref(e), 1, 0, 0, 1, 1.0, 1.0, at, at + off, None) == binding.ERR_INVALID
 
 
+def test_handle_made_on_a_stream_whose_work_is_not_done(binding):
+    """The workspace may be memory that earlier work of the stream has still to write to."""
+    g = normals(3_000_001, 9)
+    want = exact_norm([g])
+    torch.cuda._sleep(1)                                                    # all kernels are loaded before it matters: loading waits
+    torch.empty(9, dtype=torch.uint8, device=DEV).fill_(255)
+    binding.Clipper().norm([g])
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        size = binding.Clipper().workspace.numel()
+        side.synchronize()
+        junk = torch.empty(size, dtype=torch.uint8, device=DEV)
+        at = junk.data_ptr()
+        torch.cuda._sleep(100_000_000)                                      # some 50 ms
+        junk.fill_(255)
+        del junk
+        h = binding.Clipper()
+        assert h.workspace.data_ptr() == at                                 # otherwise this shows nothing
+        norm = h.norm([g])
+    side.synchronize()
+    check_norm(norm, want)
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)
