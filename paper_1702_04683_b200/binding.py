@@ -487,14 +487,6 @@ class Server:
 
 # ----------------------------------------------------------------------------- clipping
 
-def _workspace(nbytes: int, device: torch.device) -> torch.Tensor:
-    """Device memory for a handle.  The allocator hands out memory that earlier work of the current stream may still write to, and
-    handles clear theirs on the default stream: that work is waited for."""
-    workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    torch.cuda.current_stream(device).synchronize()
-    return workspace
-
-
 def _empty(like: torch.Tensor, shape, dtype, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """An output tensor on the device of `like` that belongs to the stream its kernels run on."""
     if stream is None:
@@ -510,9 +502,25 @@ def _element_type(t: torch.Tensor, device: int, name: str) -> int:
     return kind
 
 
-def _stream_on(stream: Optional[torch.cuda.Stream], device: int) -> int:
-    """The given stream, or the device's current one (asked for without building a stream object, which costs as much as a launch)."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+class _Handle:
+    """What :class:`Clipper` and :class:`Embedding` share: a device workspace and the streams that work in it."""
+
+    def _take_workspace(self, nbytes: int) -> None:
+        """Device memory for the handle.  The allocator hands out memory that earlier work of the current stream may still write to,
+        and handles clear theirs on the default stream: that work is waited for."""
+        self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        home = torch.cuda.current_stream(self.device)
+        home.synchronize()
+        self._streams = {home.cuda_stream}
+
+    def _stream_on(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """The given stream, or the device's current one (asked for without building a stream object, which costs as much as a
+        launch).  The allocator is told of streams other than the workspace's own: a handle may be dropped while they run."""
+        raw = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
+        if raw not in self._streams:
+            self.workspace.record_stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+            self._streams.add(raw)
+        return raw
 
 
 def _is_dense(t: torch.Tensor) -> bool:
@@ -574,7 +582,7 @@ class GradList:
             raise ValueError("out: overlaps a gradient or another output")
 
 
-class Clipper:
+class Clipper(_Handle):
     """Global gradient norm and clipping; owns its device workspace.  Gradients are a :class:`GradList`, a sequence of tensors
     (one worker, any shapes), or a matrix [W, P] whose rows are the flat gradients of W workers."""
 
@@ -586,7 +594,7 @@ class Clipper:
         self.max_workers = int(max_workers)
         nbytes = ctypes.c_size_t(0)
         _check(_lib.adacomp_clip_workspace_bytes(self.max_workers, ctypes.byref(nbytes)), "adacomp_clip_workspace_bytes")
-        self.workspace = _workspace(int(nbytes.value), self.device)
+        self._take_workspace(int(nbytes.value))
         h = ctypes.c_void_p()
         _check(_lib.adacomp_clip_create(ctypes.byref(h), self.max_workers, self.workspace.data_ptr(), self.workspace.numel(),
                                         self.device.index), "adacomp_clip_create")
@@ -634,7 +642,7 @@ class Clipper:
         elif norm_out.numel() != W:
             raise ValueError("norm_out: need one entry per worker")
         _check(_lib.adacomp_grad_norm(self._h, table, count, stride, W, float(scale), _dev(norm_out, torch.float32, "norm_out"),
-                                      _stream_on(stream, self._index)), "adacomp_grad_norm")
+                                      self._stream_on(stream)), "adacomp_grad_norm")
         return norm_out
 
     def clip(self, grads, max_norm: float, scale: float = 1.0, out=None, norm_out: Optional[torch.Tensor] = None,
@@ -650,7 +658,7 @@ class Clipper:
         _check(_lib.adacomp_clip(self._h, table, count, stride, out_stride, W, float(scale), float(max_norm),
                                  _dev(norm_out, torch.float32, "norm_out"),
                                  _dev(coef_out, torch.float32, "coef_out") if coef_out is not None else None,
-                                 _stream_on(stream, self._index)), "adacomp_clip")
+                                 self._stream_on(stream)), "adacomp_clip")
         return out, norm_out
 
     def close(self):
@@ -694,7 +702,7 @@ def _rows(t: torch.Tensor, dims: int, kind: int, name: str) -> Rows:
     return r
 
 
-class Embedding:
+class Embedding(_Handle):
     """Embedding tables of `vocab` rows of `dim` entries: lookup with scaling, and the gradient by sorted tokens; owns its
     device workspace.  ``max_tokens`` bounds the tokens of a gradient call (0: lookups only)."""
 
@@ -714,7 +722,7 @@ class Embedding:
         nbytes = ctypes.c_size_t(0)
         _check(_lib.adacomp_embed_workspace_bytes(self.vocab, self.dim, self.max_tokens, self.max_workers, ctypes.byref(nbytes)),
                "adacomp_embed_workspace_bytes")
-        self.workspace = _workspace(int(nbytes.value), self.device)
+        self._take_workspace(int(nbytes.value))
         h = ctypes.c_void_p()
         _check(_lib.adacomp_embed_create(ctypes.byref(h), self.vocab, self.dim, self.max_tokens, self.max_workers, pad,
                                          self.workspace.data_ptr(), self.workspace.numel(), self.device.index),
@@ -753,7 +761,7 @@ class Embedding:
         elif out.shape != shape or (dtype is not None and out.dtype != dtype):
             raise ValueError("out: need a row for every token, and the type asked for")
         _check(_lib.adacomp_embed_lookup(self._h, ctypes.byref(self._wide(table, "table")), ctypes.byref(ids), tokens.numel(),
-                                         float(scale), ctypes.byref(self._wide(out, "out")), _stream_on(stream, self._index)),
+                                         float(scale), ctypes.byref(self._wide(out, "out")), self._stream_on(stream)),
                "adacomp_embed_lookup")
         return out
 
@@ -780,7 +788,7 @@ class Embedding:
                                             _dev(rows_out, torch.int32, "rows_out") if rows_out is not None else None,
                                             begin.data_ptr(), _dev(values_out, values_out.dtype, "values_out"), kind,
                                             _dev(idx_out, torch.int32, "idx_out") if idx_out is not None else None, int(offset),
-                                            _stream_on(stream, self._index)), "adacomp_embed_grad_rows")
+                                            self._stream_on(stream)), "adacomp_embed_grad_rows")
         return begin
 
     def grad_rows(self, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, workers: int = 1,
@@ -824,7 +832,7 @@ class Embedding:
         if out.data_ptr() == grad.data_ptr() and grad.numel():
             raise ValueError("out: overlaps the gradient")
         _check(_lib.adacomp_embed_grad_dense(self._h, ctypes.byref(ids), per_worker, workers, ctypes.byref(rows), float(scale),
-                                             ctypes.byref(self._wide(out, "out")), int(accumulate), _stream_on(stream, self._index)),
+                                             ctypes.byref(self._wide(out, "out")), int(accumulate), self._stream_on(stream)),
                "adacomp_embed_grad_dense")
         return out
 
@@ -834,7 +842,7 @@ class Embedding:
 
     def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
         """Waits for the stream; the first error the device recorded since the last call (a token outside the vocabulary)."""
-        return int(_lib.adacomp_embed_last_error(self._h, _stream_on(stream, self._index)))
+        return int(_lib.adacomp_embed_last_error(self._h, self._stream_on(stream)))
 
     def close(self):
         if getattr(self, "_h", None):

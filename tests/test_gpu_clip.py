@@ -285,6 +285,31 @@ def test_handle_made_on_a_stream_whose_work_is_not_done(binding):
     check_norm(norm, want)
 
 
+def test_handle_dropped_while_another_stream_works(binding):
+    """Its workspace must not be handed out again before that stream is through."""
+    g = normals(3_000_001, 9)
+    want = exact_norm([g])
+    torch.cuda._sleep(1)                                                    # all kernels are loaded before it matters: loading waits
+    torch.empty(9, dtype=torch.uint8, device=DEV).fill_(255)
+    binding.Clipper().norm([g])
+    side = torch.cuda.Stream()
+    for given in (True, False):
+        torch.cuda.synchronize()
+        h = binding.Clipper()
+        size = h.workspace.numel()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)                                  # some 50 ms
+            if not given:
+                norm = h.norm([g])
+        if given:
+            norm = h.norm([g], stream=side)
+        del h
+        junk = [torch.empty(size, dtype=torch.uint8, device=DEV).fill_(255) for _ in range(8)]
+        side.synchronize()
+        check_norm(norm, want)
+        del junk
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)
