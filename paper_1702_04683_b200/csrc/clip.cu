@@ -17,7 +17,7 @@ struct adacomp_clip {
     int device;
     uint32_t max_workers;
     int n_sms;
-    double* d_partial;              // [max_workers][kMaxBlocks]
+    double* d_partial;              // [workers][slots_of(blocks)] of a call
     uint32_t* d_done;               // [max_workers] blocks that have delivered their sum
     float* d_coef;                  // [max_workers]
 };
@@ -30,7 +30,10 @@ constexpr uint32_t kUnit = kThreads * kVecsPerThread;       // vectors of 16 byt
 // Blocks resident per SM.  Loads in flight count: 8 vectors a thread and 3 blocks read 6.4 GB in 866 us (7.4 TB/s), 4 and 6 in
 // 884, 4 and 8 in 937.
 constexpr int kNormBlocks = 3, kWriteBlocks = 4;
-constexpr uint32_t kMaxBlocks = 1024;                       // partial sums per worker the workspace has room for
+constexpr uint32_t kMaxBlocks = 1024;                       // blocks of a call with fewer workers; with more a worker has one
+// A worker's partial sums fill whole lines of 128 bytes, so the workers of a call need kMaxBlocks + 16 of them each at most.
+constexpr uint32_t kSlotLine = 16;
+__host__ __device__ constexpr uint32_t slots_of(uint32_t n_blocks) { return (n_blocks + kSlotLine - 1) / kSlotLine * kSlotLine; }
 // Gradients up to this many bytes: what the second pass reads and writes is given up first by L2, so that what the first pass
 // read stays until it is read again.  Measured, both passes: 102 MB of fp32 57.2 -> 53.3 us, 52 MB of fp16 44.5 -> 40.2 us;
 // but 683 MB of bf16 464 -> 471 us, where little of it can stay anyway.
@@ -203,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __gri
     const Lookup tensors(tab, job.n_tensors, s_tab);
     const double sum = block_sum(worker_squares(tensors, job, w, b, job.n_blocks), s_warp);
     if (threadIdx.x == 0) {
-        double* slot = job.partial + static_cast<uint64_t>(w) * job.n_blocks + b;
+        double* slot = job.partial + static_cast<uint64_t>(w) * slots_of(job.n_blocks) + b;
         *slot = job.first ? sum : *slot + sum;
         s_last = false;
         if (job.last) {
@@ -217,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, kNormBlocks) k_grad_norm(const __gri
     __threadfence();
     double total = 0.0;
     for (uint32_t k = threadIdx.x; k < job.n_blocks; k += kThreads)
-        total += __ldcg(job.partial + static_cast<uint64_t>(w) * job.n_blocks + k);
+        total += __ldcg(job.partial + static_cast<uint64_t>(w) * slots_of(job.n_blocks) + k);
     total = block_sum(total, s_warp);
     if (threadIdx.x == 0) {
         job.done[w] = 0;
@@ -424,15 +427,16 @@ int launch_table(const Table<kMany>& tab, const Job& job, uint32_t n_workers, Pa
 // Blocks of one worker: all of a call's are resident at once where there are not more workers than that, and none is
 // without work.
 uint32_t blocks_per_worker(const adacomp_clip_t* h, uint64_t units, uint32_t n_workers, bool write) {
-    uint64_t blocks = static_cast<uint64_t>(write ? kWriteBlocks : kNormBlocks) * h->n_sms / n_workers;
-    if (blocks > units) blocks = units;
+    uint64_t blocks = static_cast<uint64_t>(write ? kWriteBlocks : kNormBlocks) * h->n_sms;
     if (blocks > kMaxBlocks) blocks = kMaxBlocks;
+    blocks /= n_workers;
+    if (blocks > units) blocks = units;
     return blocks < 1 ? 1 : static_cast<uint32_t>(blocks);
 }
 
-size_t carve(adacomp_clip_t* h, void* ws, uint32_t max_workers, uint32_t n_blocks) {
+size_t carve(adacomp_clip_t* h, void* ws, uint32_t max_workers) {
     Carver c(ws);
-    double* partial = c.take<double>(static_cast<size_t>(max_workers) * n_blocks);
+    double* partial = c.take<double>(kMaxBlocks + static_cast<size_t>(kSlotLine) * max_workers);
     uint32_t* done = c.take<uint32_t>(max_workers);
     float* coef = c.take<float>(max_workers);
     if (h) {
@@ -500,7 +504,7 @@ extern "C" {
 
 int adacomp_clip_workspace_bytes(uint32_t max_workers, size_t* bytes_out) {
     if (!bytes_out || max_workers == 0 || max_workers > 65535) return ADACOMP_ERR_INVALID;
-    *bytes_out = carve(nullptr, nullptr, max_workers, kMaxBlocks);
+    *bytes_out = carve(nullptr, nullptr, max_workers);
     return ADACOMP_OK;
 }
 
@@ -516,7 +520,7 @@ int adacomp_clip_create(adacomp_clip_t** h, uint32_t max_workers, void* d_worksp
     if (!c) return ADACOMP_ERR_ALLOC;
     c->device = device;
     c->max_workers = max_workers;
-    carve(c, d_workspace, max_workers, kMaxBlocks);
+    carve(c, d_workspace, max_workers);
     DeviceGuard guard(device);
     cudaError_t e = guard.err;
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sms, cudaDevAttrMultiProcessorCount, device);

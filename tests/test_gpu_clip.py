@@ -310,6 +310,20 @@ def test_handle_dropped_while_another_stream_works(binding):
         del junk
 
 
+@pytest.mark.parametrize("workers", [3, 64, 444, 445, 5_000])
+def test_partial_sums_of_workers_keep_apart(binding, workers):
+    """Workers of several blocks and of one, in a workspace as small as it may be: every norm is its own worker's."""
+    n = 2_000_000 // workers + 20_000
+    g = normals(workers * n, workers).view(workers, n)
+    g *= torch.arange(1, workers + 1, device=DEV).view(-1, 1)
+    h = binding.Clipper(max_workers=workers)
+    want = (g.double() ** 2).sum(1).sqrt()
+    for _ in range(3):
+        assert bool(((h.norm(g).double() - want).abs() <= NORM_TOL * want).all())
+    longer = [g[0], *(normals(17, i) for i in range(1_000))]                # two launches, one after the other's partial sums
+    check_norm(h.norm(longer), exact_norm(longer))
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)

@@ -32,6 +32,14 @@ def test_clip_workspace_and_create(binding):
     assert h.value is None
 
 
+def test_clip_workspace_stays_small(binding):
+    """The blocks of a call share the device: many workers have few each."""
+    n = ctypes.c_size_t(0)
+    for workers in (1, 16, 1_000, 65_535):
+        assert binding.raw().adacomp_clip_workspace_bytes(workers, ctypes.byref(n)) == 0
+        assert n.value <= 16_384 + 256 * workers
+
+
 def test_clip_null_handles(binding):
     lib = binding.raw()
     t = binding.GradTensor()
