@@ -166,6 +166,82 @@ def test_lookup_keeps_infinities_and_nan(binding):
     assert torch.equal(torch.nan_to_num(got, nan=-9.0), torch.nan_to_num((table[[1, 0]] * 2).half(), nan=-9.0))
 
 
+def batch_of_tokens(n, vocab, seed, bad=0):
+    """Tokens of which the table's first and last row are some, and `bad` lie outside."""
+    ids = words((n,), vocab, seed, skew=False)
+    ids[0], ids[n // 2], ids[-1] = vocab - 1, 0, vocab - 1
+    if bad:
+        ids[torch.randperm(n, device=DEV, generator=gen(seed))[:bad]] = vocab
+    return ids
+
+
+def check_lookup(binding, table, ids, out, scale, bad=False):
+    """A lookup into `out`, a part of a larger buffer of sevens: the roundings bit for bit, and nothing beside them."""
+    vocab, dim = table.shape
+    h = binding.Embedding(vocab, dim)
+    buf = out._base if out._base is not None else out
+    buf.fill_(7.0)
+    h.lookup(table, ids, scale=scale, out=out)
+    assert h.last_error() == (binding.ERR_INVALID if bad else 0)
+    ok = (ids >= 0) & (ids < vocab)
+    want = torch.where(ok.view(-1, 1), table[ids.clamp(0, vocab - 1)].float() * scale, 0.0).to(out.dtype)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert bool((buf == 7).all())
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("to", TYPES)
+def test_lookup_of_large_batches_on_the_grid(binding, kind, to):
+    """Several tokens per thread, row strides wider than the rows, outputs on the 32-byte grid and beside it."""
+    vocab, dim, n = 3_001, 256, 80_003
+    table = (torch.randn((vocab, dim + 24), device=DEV, generator=gen(1)) * 0.02).to(kind)[:, 8:8 + dim]
+    ids = batch_of_tokens(n, vocab, 2, bad=3)
+    for pad, at in ((0, 0), (32, 16), (8, 8)):
+        out = torch.empty((n, dim + pad), device=DEV, dtype=to)[:, at:at + dim]
+        for scale in (1.0, 16.0):
+            check_lookup(binding, table, ids, out, scale, bad=True)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("to", TYPES)
+@pytest.mark.parametrize("dim", [1, 7, 250, 511])
+def test_lookup_of_large_batches_of_odd_rows(binding, kind, to, dim):
+    """Single entries, several tokens per thread."""
+    vocab, n = 3_001, 1_300_003 if dim == 1 else 700_001 if dim == 7 else 20_011
+    wide = (torch.randn((vocab, dim + 3), device=DEV, generator=gen(1)) * 0.02).to(kind)
+    for table, scale in ((wide[:, 1:1 + dim], 4.0), (wide[:, :dim].contiguous(), 1.0)):
+        check_lookup(binding, table, batch_of_tokens(n, vocab, dim, bad=2), torch.empty((n, dim + 2), device=DEV, dtype=to)[:, 1:1 + dim], scale, bad=True)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("to", TYPES)
+@pytest.mark.parametrize("n,dim", [(300, 513), (1_201, 1_001), (5_003, 1_001), (9_001, 519), (1_500, 4_099)])
+def test_lookup_of_long_rows_off_the_grid(binding, kind, to, n, dim):
+    """Few and many tokens; tables with and without gaps, their last row at the end of the memory; outputs at every offset."""
+    vocab = 601
+    for gap in (0, 3, 8):
+        memory = (torch.randn((vocab - 1) * (dim + gap) + dim + 5, device=DEV, generator=gen(gap)) * 0.02).to(kind)
+        for skip in (0, 5):
+            table = memory[skip:].as_strided((vocab, dim), (dim + gap, 1))
+            assert table.storage_offset() + (vocab - 1) * (dim + gap) + dim <= memory.numel()
+            for at in ((0, 1, 2, 3, 4, 5, 6, 7) if skip else (0, 3)):
+                out = torch.empty((n, dim + 9 - at % 2), device=DEV, dtype=to)[:, at:at + dim]
+                check_lookup(binding, table, batch_of_tokens(n, vocab, at, bad=at % 3), out, 8.0 if gap else 1.0, bad=at % 3 > 0)
+
+
+@pytest.mark.parametrize("kind,to,dim,n", [(torch.bfloat16, torch.bfloat16, 1024, 50_001), (torch.float32, torch.float32, 512, 50_001),
+                                           (torch.bfloat16, torch.float32, 512, 50_001), (torch.float32, torch.float16, 1024, 50_001),
+                                           (torch.float16, torch.float16, 1001, 51_003), (torch.float32, torch.float32, 333, 77_001)])
+def test_lookup_whose_output_exceeds_the_cache(binding, kind, to, dim, n):
+    """Above 96 MB, stores that pass L2 by; rows that start on 32 bytes and on 16 alone."""
+    vocab = 2_003
+    table = (torch.randn((vocab, dim), device=DEV, generator=gen(1)) * 0.02).to(kind)
+    for pad in (0, 8 if to != torch.float32 else 4):
+        out = torch.empty((n, dim + pad), device=DEV, dtype=to)[:, pad:]
+        check_lookup(binding, table, batch_of_tokens(n, vocab, 5), out, 1.0 if pad else 0.5)
+
+
 # --------------------------------------------------------------------------------------------- gradient
 
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 257, 1024, 1025, 2048, 2049, 8192, 8193, 20_000, 70_000])
@@ -378,6 +454,80 @@ def test_calls_after_a_sort_that_gave_up(binding, workers):
     h.set_wait_limit(1 << 22)
     for n in (500, 20_000, most):
         check_grad(binding, *batch(n), vocab, workers=workers, handle=h)
+
+
+def check_whole(binding, tokens, grad, vocab, workers=1, pad=None, table=None, out_type=torch.float32):
+    """Whole numbers: all three forms have to equal the sums, however long a segment is."""
+    n, D = tokens.numel(), grad.shape[-1]
+    h = binding.Embedding(vocab, D, max_tokens=n, max_workers=workers, padding_idx=pad)
+    flat = tokens.reshape(workers, -1)
+    key = (flat + torch.arange(workers, device=DEV).view(-1, 1) * vocab)[flat != -1 if pad is None else flat != pad]
+    rows = grad.reshape(-1, D)[(flat != -1 if pad is None else flat != pad).view(-1)]
+    want = torch.zeros((workers * vocab, D), device=DEV, dtype=torch.float64).index_add_(0, key, rows.double()).float()
+    present = torch.bincount(key, minlength=workers * vocab).nonzero().view(-1)
+    assert float(want.abs().max()) < 2 ** 24
+    got, values, begin = h.grad_rows(tokens, grad, workers=workers)
+    assert begin.tolist() == [int((present < w * vocab).sum()) for w in range(workers + 1)]
+    assert torch.equal(got[:len(present)].long(), present % vocab) and torch.equal(values[:len(present)], want[present])
+    idx, values, begin = h.grad_update(tokens, grad, workers=workers)
+    assert torch.equal(idx[:len(present)].long(), (present % vocab).view(-1, 1) * D + torch.arange(D, device=DEV))
+    assert torch.equal(values[:len(present)], want[present])
+    if table is None:
+        table = torch.full((workers, vocab, D), 7.0, device=DEV, dtype=out_type)
+    h.grad_dense(tokens, grad, table, workers=workers)
+    assert torch.equal(table, want.view(workers, vocab, D).to(table.dtype))
+    h.grad_dense(tokens, grad, table, workers=workers, accumulate=True)
+    assert torch.equal(table, (want + want.to(table.dtype).float()).view(workers, vocab, D).to(table.dtype))
+    assert h.last_error() == 0
+
+
+@pytest.mark.parametrize("n", [1, 9, 64, 500, 1_024, 1_025, 2_048, 2_049, 9_000, 65_536, 65_537, 131_073, 1_048_577, 3_000_001])
+@pytest.mark.parametrize("spread", ["one", "two runs", "a third", "runs of all lengths"])
+def test_sums_of_segments_of_any_length(binding, n, spread):
+    """Segments from one token to all of them: every level at which their pieces are joined, in every route, next to short ones."""
+    vocab, dim = 5_000, 4 if n > 100_000 else 24
+    i = torch.arange(n, device=DEV)
+    if spread == "one":
+        tokens = i * 0 + 4_321
+    elif spread == "two runs":
+        tokens = torch.where(i % 7 < 4, 17, 4_999)
+    elif spread == "a third":
+        tokens = torch.where(torch.rand(n, device=DEV, generator=gen(n)) < 0.33, 2_000, words((n,), vocab, n))
+    else:
+        tokens = (torch.log2(1.0 + i.double()) * 40).long() % vocab            # each run longer than the one before
+        tokens = tokens[torch.randperm(n, device=DEV, generator=gen(n))]
+    check_whole(binding, tokens, whole_numbers((n, dim), n), vocab)
+
+
+@pytest.mark.parametrize("kind,dim", [(torch.bfloat16, 8), (torch.bfloat16, 1000), (torch.float16, 1001), (torch.float32, 130), (torch.float32, 5000)])
+@pytest.mark.parametrize("n", [700, 30_000])
+def test_sums_of_long_segments_and_widths(binding, kind, dim, n):
+    vocab = 700
+    tokens = torch.where(torch.rand(n, device=DEV, generator=gen(n)) < 0.4, 333, words((n,), vocab, n))
+    check_whole(binding, tokens, whole_numbers((n, dim), n, kind), vocab, pad=5)
+
+
+@pytest.mark.parametrize("n,workers", [(32_768, 1), (32_769, 1), (65_536, 1), (65_537, 1), (16_384, 4), (21_846, 3), (8_192, 8)])
+def test_sorts_at_the_limit_of_a_cluster(binding, n, workers):
+    """As many tokens as one cluster of sixteen blocks takes, and one or two more; 32768 is the limit of one of eight."""
+    tokens = words((workers, n), 30_011, n)
+    check_whole(binding, tokens, whole_numbers((workers, n, 8), n, torch.bfloat16), 30_011, workers=workers, pad=1)
+
+
+@pytest.mark.parametrize("n,vocab,dim,kind,workers", [(3_000, 200_000, 256, torch.float32, 1), (70_000, 300_001, 256, torch.float32, 1),
+                                                      (5_000, 90_001, 1_000, torch.bfloat16, 2), (2_500, 60_001, 1_001, torch.float32, 1),
+                                                      (12_345, 1_500_000, 65, torch.float16, 1)])
+def test_dense_tables_that_are_cleared_during_the_sort(binding, n, vocab, dim, kind, workers):
+    """Tables of some 200 MB and more with few tokens: rows cleared next to the sort and next to the sums; in buffers with gaps."""
+    row_bytes = dim * torch.empty(0, dtype=kind).element_size()
+    assert workers * n <= workers * vocab // 4 and (16 + workers * n // 8192) * (5 << 20) // row_bytes < workers * vocab // 2
+    tokens = words((workers, n), vocab, n, skew=False)
+    tokens[:, 0], tokens[:, 1] = 0, vocab - 1
+    tokens[:, 5:n // 2] = words((workers, n // 2 - 5), 97, n)
+    buf = torch.full((workers, vocab * dim + 24), 7.0, device=DEV, dtype=kind)
+    table = buf[:, 8:8 + vocab * dim].view(workers, vocab, dim)
+    check_whole(binding, tokens, whole_numbers((workers, n, dim), n, torch.bfloat16), vocab, workers=workers, table=table)
+    assert bool((buf[:, :8] == 7).all()) and bool((buf[:, 8 + vocab * dim:] == 7).all())
 
 
 def test_vocabularies_of_many_bits(binding):
