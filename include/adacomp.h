@@ -512,9 +512,10 @@ ADACOMP_API int adacomp_embed_grad_dense(adacomp_embed_t* h, const adacomp_rows_
  * that a program's handling of ADACOMP_ERR_TIMEOUT can be tried). */
 ADACOMP_API int adacomp_embed_set_wait_limit(adacomp_embed_t* h, uint32_t polls);
 /* Waits for cuda_stream, returns and clears the first error recorded on the device.  ADACOMP_ERR_TIMEOUT: the blocks of a large
- * sort waited for each other in vain (they run together, so this is not expected).  The gradients of that and of later calls,
- * whatever their size, up to this one are missing: lists of rows are empty (d_row_begin_out holds zeros), nothing was added to a
- * table, and of a table that was to be replaced some rows may have become zeros already. */
+ * sort waited for each other in vain (they run together, so this is not expected).  The gradients of that and of later calls
+ * up to this one are missing: lists of rows are empty (d_row_begin_out holds zeros), nothing was added to a table, and of a table
+ * that was to be replaced some rows may have become zeros already.  Only calls of up to 1024 tokens are sure to be complete, those of
+ * up to 2048 may be. */
 ADACOMP_API int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream);
 ADACOMP_API int adacomp_embed_destroy(adacomp_embed_t* h);
 

@@ -213,24 +213,22 @@ __device__ __forceinline__ uint32_t load_key(const SortJob& j, uint32_t t, bool 
 }
 
 // Waits until all sorting blocks are here.  They are resident together (cooperative launch), so the wait ends; if it ever
-// does not, the block says so and gives up: the sums then leave its lists alone.  From then on no block arrives here, in this
-// call or a later one, until the host clears the words: the arrivals that were left behind would let blocks pass before the
-// others have delivered their counts, and places made of such counts lie anywhere.
+// does not, the block says so and gives up: the sums then leave its lists alone.  From then on no block passes, in this call or
+// a later one, until the host clears the words, whatever the count says: with the arrivals that were left behind it says so
+// before all have delivered their counts, and places made of such counts lie anywhere.
 __device__ __forceinline__ bool meet(const SortJob& j) {
     __shared__ int s_ok;
     __syncthreads();
     if (threadIdx.x == 0) {
-        s_ok = 0;
-        if (__ldcg(j.barrier + 2) == 0) {
-            __threadfence();
-            const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
-            uint32_t seen = 0, polls = 0;
-            do {
-                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
-            } while (seen < target && ++polls < j.wait_limit);
-            s_ok = seen >= target;
-            if (seen < target) j.barrier[2] = 1;
-        }
+        __threadfence();
+        const uint32_t target = (atomicAdd(j.barrier, 1u) / j.n_blocks + 1) * j.n_blocks;
+        const uint32_t gave_up = __ldcg(j.barrier + 2);
+        uint32_t seen = 0, polls = gave_up ? j.wait_limit : 0;
+        do {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(j.barrier) : "memory");
+        } while (seen < target && polls++ < j.wait_limit);
+        s_ok = seen >= target && gave_up == 0;
+        if (seen < target) j.barrier[2] = 1;
     }
     __syncthreads();
     return s_ok != 0;
@@ -947,7 +945,7 @@ __device__ __forceinline__ void finish_long(const Sums& p, const Pieces& x, uint
     }
 }
 
-// A call whose sort gave up, or that came after one: its lists read as empty.
+// A call whose sort gave up, or that sorts in this way after one that did: its lists read as empty.
 __device__ __forceinline__ void put_no_rows(const Sums& p) {
     if (blockIdx.x != 0 || !p.row_begin) return;
     for (uint32_t w = threadIdx.y * blockDim.x + threadIdx.x; w <= p.n_workers; w += blockDim.x * blockDim.y) p.row_begin[w] = 0;
@@ -1127,12 +1125,7 @@ __device__ __forceinline__ void clear_small(const Sums& p, const SmallMem& m) {
 template <typename A, typename B, int N>
 __global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob j, const Sums p, uint32_t x, uint32_t y) {
     __shared__ SmallMem m;
-    const bool gave_up = *p.gave_up != 0;                   // of an earlier call: on its way while the tokens are sorted
     sort_small(j, m);
-    if (gave_up) {
-        put_no_rows(p);
-        return;
-    }
     if (blockIdx.x == 0 && j.row_begin && j.n_workers == 1) {
         if (threadIdx.x < 2) j.row_begin[threadIdx.x] = threadIdx.x ? m.n_segs : 0;
     } else if (blockIdx.x == 0 && j.row_begin) {
