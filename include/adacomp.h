@@ -421,9 +421,9 @@ ADACOMP_API int adacomp_clip_create(adacomp_clip_t** h, uint32_t max_workers, vo
  *     d_norm_out[w] = |scale| * sqrt(sum of g^2),
  * scale being what the stored entries still have to be multiplied by (1 / the loss scale of half-precision
  * training; 1 otherwise).  Worker w's entries of tensor t start grad_stride * w elements behind h_tensors[t].d_grad
- * (grad_stride is in elements of each tensor's own type; 0 is legal with one worker).  Squares are summed in fp32 inside
- * groups of at most 64 entries (two chains of 32) and in 64 bits above that; groups whose sum would leave fp32's safe range are summed in 64
- * bits altogether, so neither large nor tiny entries overflow or vanish.  The order of summation is fixed: the same
+ * (grad_stride is in elements of each tensor's own type; 0: all workers share the entries).  Squares are summed in fp32 inside
+ * groups of at most 64 entries (two chains of 32) and in 64 bits above that; groups whose sum would leave fp32's safe range are
+ * summed in 64 bits altogether, so neither large nor tiny entries overflow or vanish.  The order of summation is fixed: the same
  * call on the same device gives the same bits.  An infinity gives +Inf, a NaN gives NaN, no entries at all give 0.
  * h_tensors is read before the call returns.  Errors: ADACOMP_ERR_INVALID (null pointer, unknown type, misaligned pointer,
  * n >= 2^40, n_workers = 0 or > max_workers, scale not finite), ADACOMP_ERR_CUDA. */

@@ -3,8 +3,10 @@
 //   norm_w = |s| sqrt(sum_i g_i^2),   c_w = s min(1, max_norm / (norm_w + 1e-6)),   out_i = round(g_i c_w)
 //
 // Both kernels are one pass over the data (2 and 1 operations an entry): HBM bounds them.  The tensors of a call are cut
-// into units of 32 KB of the input (first pass) or 8192 entries (second); blocks take units in turn, so short tensors next to each other in the list go to different
-// blocks.  The second pass walks the units from the back: what the first pass read last is still in L2.
+// into units of 32 KB of the input (first pass) or 8192 entries (second); blocks take units in turn, so short tensors next to
+// each other in the list go to different blocks.  The second pass walks the units from the back, where some of what the first
+// pass read last is still in L2 (38 of 102 MB; 64 MB come from HBM once more).  Of 161 tensors, 102 MB of fp32, the second pass
+// reaches 57 % of the HBM rate: a block has some five units, and nothing of the next is under way while it writes one.
 #include <cooperative_groups.h>
 #include <math.h>
 #include <new>
@@ -313,7 +315,8 @@ __global__ void __launch_bounds__(kThreads, kWriteBlocks) k_clip_write(const __g
 // shared memory.  The second read comes from L2.
 constexpr uint32_t kCluster = 8;
 template <int MAX>
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, kNormBlocks) k_clip_small(const __grid_constant__ Table<MAX> tab, const Job job) {
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, kNormBlocks)
+    k_clip_small(const __grid_constant__ Table<MAX> tab, const Job job) {
     __shared__ double s_warp[kThreads / 32];
     __shared__ double s_sums[kCluster];
     __shared__ float s_factor;
@@ -365,13 +368,15 @@ int launch(const Table<MAX>& tab, const Job& job, uint32_t n_workers, Pass pass,
     cfg.attrs = attr;
     cfg.numAttrs = pass == kWrite ? 1 : 0;
     const cudaError_t e = pass == kWrite ? cudaLaunchKernelEx(&cfg, k_clip_write<MAX>, tab, job)
-                        : pass == kNorm ? cudaLaunchKernelEx(&cfg, k_grad_norm<MAX>, tab, job) : cudaLaunchKernelEx(&cfg, k_clip_small<MAX>, tab, job);
+                        : pass == kNorm ? cudaLaunchKernelEx(&cfg, k_grad_norm<MAX>, tab, job)
+                                        : cudaLaunchKernelEx(&cfg, k_clip_small<MAX>, tab, job);
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
 
-int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t in_stride, uint64_t out_stride, uint32_t n_workers, bool write) {
+int check_tensors(const adacomp_grad_tensor_t* ts, uint32_t n_tensors, uint64_t in_stride, uint64_t out_stride, uint32_t n_workers,
+                  bool write) {
     if (!ts && n_tensors) return ADACOMP_ERR_INVALID;
     for (uint32_t i = 0; i < n_tensors; ++i) {
         const adacomp_grad_tensor_t& t = ts[i];
@@ -489,7 +494,8 @@ int run(adacomp_clip_t* h, const adacomp_grad_tensor_t* ts, uint32_t n_tensors, 
                 at = n_tensors;
             }
             job.last = at == n_tensors;
-            if (write && whole && bytes <= kSmallBytes && bytes * n_workers <= kSmallTotal) return launch_table(tab, job, n_workers, kBoth, stream);
+            if (write && whole && bytes <= kSmallBytes && bytes * n_workers <= kSmallTotal)
+                return launch_table(tab, job, n_workers, kBoth, stream);
             if (pass == 0 || job.n_tensors) rc = launch_table(tab, job, n_workers, pass == 0 ? kNorm : kWrite, stream);
             if (rc != ADACOMP_OK) return rc;
             job.first = 0;

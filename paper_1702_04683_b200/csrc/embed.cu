@@ -126,7 +126,9 @@ __global__ void __launch_bounds__(512) k_embed_lookup(Rows table, Rows tokens, R
 }
 
 // The same where rows do not sit on the 16-byte grid and 16-bit entries make single ones too small a load: items of eight
-// entries on the grid of each output row, taken from the two vectors of the table around them.  `total` entries lie between the table's first and its last.
+// entries on the grid of each output row, taken from the two vectors of the table around them.  `total` entries lie between the
+// table's first and its last.  Both ends of a row go entry by entry, and the warps that hold them wait for it: 32768 bf16 rows of
+// 1001 take 37 us, of 1024 on the grid 21.
 template <typename A, typename B, int R>
 __global__ void __launch_bounds__(512) k_embed_lookup_off(Rows table, Rows tokens, Rows out, uint32_t n_tokens, uint32_t vocab, uint32_t dim,
                                                            uint32_t tiles, uint64_t total, float scale, int* status) {
@@ -328,7 +330,8 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 
 // Sorted token i with key k between `last` and `next`, and its place in the lists that the sums read; `u` segments begin
 // before it.
-__device__ __forceinline__ void put_segment(const SortJob& j, uint64_t i, uint32_t k, uint32_t last, uint32_t next, uint32_t pos, bool head, uint32_t u) {
+__device__ __forceinline__ void put_segment(const SortJob& j, uint64_t i, uint32_t k, uint32_t last, uint32_t next, uint32_t pos, bool head,
+                                            uint32_t u) {
     if ((i & ((1u << j.chunk_shift) - 1)) == 0) j.chunk_seg[i >> j.chunk_shift] = u;
     j.order[i] = pos | (next != k ? kLast : 0u);
     if (head) {
@@ -507,10 +510,13 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
             const uint64_t t = span + i * 32;
             const uint32_t k = static_cast<uint32_t>(tok[i] >> 32);
             uint32_t last = __shfl_up_sync(0xFFFFFFFFu, k, 1), next = __shfl_down_sync(0xFFFFFFFFu, k, 1);
-            const uint32_t after = i + 1 < items ? __shfl_sync(0xFFFFFFFFu, static_cast<uint32_t>(tok[i + 1 < kItems ? i + 1 : i] >> 32), 0) : behind;
+            const uint32_t behind_row = static_cast<uint32_t>(tok[i + 1 < kItems ? i + 1 : i] >> 32);
+            const uint32_t after = i + 1 < items ? __shfl_sync(0xFFFFFFFFu, behind_row, 0) : behind;
             if (lane == 0) last = before;
             if (lane == 31) next = after;
-            if (t < to) put_segment(j, t, k, last, t + 1 < j.n ? next : j.none, static_cast<uint32_t>(tok[i]), heads[i] >> lane & 1, u + __popc(heads[i] & ((1u << lane) - 1)));
+            if (t < to)
+                put_segment(j, t, k, last, t + 1 < j.n ? next : j.none, static_cast<uint32_t>(tok[i]), heads[i] >> lane & 1,
+                            u + __popc(heads[i] & ((1u << lane) - 1)));
             u += __popc(heads[i]);
             before = __shfl_sync(0xFFFFFFFFu, k, 31);
         }
@@ -523,8 +529,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort(const SortJob j)
     }
 }
 
-// The same sort for up to kClusterStep tokens per block in one thread-block cluster: the tokens stay in registers and shared memory, a block's counts and the tokens themselves go straight to the shared memory of the block they
-// belong to, and the cluster's barrier takes the place of the one in global memory.
+// The same sort for up to kClusterStep tokens per block in one thread-block cluster: the tokens stay in registers and shared
+// memory, a block's counts and the tokens themselves go straight to the shared memory of the block they belong to, and the
+// cluster's barrier takes the place of the one in global memory.
 __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const SortJob j) {
     extern __shared__ uint64_t s_mem64[];
     __shared__ uint32_t s_base[kMaxBins];
@@ -653,7 +660,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_embed_sort_cluster(const So
 
 struct Sums {
     const uint32_t *order, *seg_begin, *seg_key, *chunk_seg, *n_segs;
-    uint32_t n, n_chunks, chunk_shift;
+    uint32_t n_chunks, chunk_shift;
     uint32_t tiles;                 // blocks along a row
     uint32_t sum_blocks;            // the blocks behind them write zeros
     float* partial;
@@ -699,7 +706,7 @@ __device__ __forceinline__ void put_row(const Sums& p, uint32_t slot, uint64_t a
             for (int k = 0; k < N; ++k) sum[k] = __fadd_rn(sum[k], old[k]);
         }
         q.pack(sum);
-                if (Packed<B, N>::kVecs == 2 && p.wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
+        if (Packed<B, N>::kVecs == 2 && p.wide) store32(dst, q.v[0], q.v[Packed<B, N>::kVecs - 1]);
         else q.store(dst);
     } else {
         if (p.accumulate) sum[0] = __fadd_rn(sum[0], to_float(*dst));
@@ -744,7 +751,8 @@ __device__ void zero_gaps(const Sums& p, uint32_t block, uint32_t n_blocks) {
     constexpr uint32_t kKeys = 64;
     __shared__ uint32_t s_key[kKeys];
     const uint32_t n_segs = p.n_segs[0], tid = threadIdx.y * blockDim.x + threadIdx.x, n_threads = blockDim.x * blockDim.y;
-    const uint64_t rows = p.zero_rows - p.zero_first, from = p.zero_first + rows * block / n_blocks, to = p.zero_first + rows * (block + 1) / n_blocks;
+    const uint64_t rows = p.zero_rows - p.zero_first;
+    const uint64_t from = p.zero_first + rows * block / n_blocks, to = p.zero_first + rows * (block + 1) / n_blocks;
     uint32_t base = warp_lower_bound(p.seg_key, n_segs, from), k = kKeys;
     for (uint64_t r = from; r < to;) {
         if (k == kKeys) {
@@ -986,20 +994,23 @@ __global__ void __launch_bounds__(kSumThreads, K == 1 ? 4 : 3) k_embed_sums(cons
         if (p.rows_out && tile == 0) p.rows_out[s.u0 + k] = key % p.vocab;
     }
     __syncthreads();
-    // Four rows in flight per thread, 56 registers (four blocks of 256 per SM): 524288 tokens x 2048 bf16 in 404 us, 6.3 TB/s with
-    // the pieces of long segments counted.  Measured against it: the next four rows fetched before the last are added (80
-    // registers) 430 us; rings of asynchronous copies to shared memory, eight rows deep, 410; five blocks per SM spill (+12 %).
+    // Four rows in flight per thread, 56 registers (four blocks of 256 per SM; from 16-bit rows to fp32 8 bytes spill, between
+    // other types none): 524288 tokens x 2048 bf16 in 404 us, 6.3 TB/s with the pieces of long segments counted.  Measured against
+    // it: the next four rows fetched before the last are added (80 registers) 430 us; rings of asynchronous copies to shared
+    // memory, eight rows deep, 410; five blocks per SM, which spill more, +12 %.  An ordinary update (4 x 8192 tokens x 1024) has
+    // 1024 blocks for 592 places and four dependent reads before a block's first sum: 167 MB in 38 us, 4.4 TB/s.
     if (c < p.dim) sum_chunk<A, B, N, K, 4>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, blockDim.x * N);
     if (!__syncthreads_or(s.lead || s.trail)) return;
-    finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0, [&](uint32_t u) { return p.seg_key[u]; },
-                         reinterpret_cast<uint32_t*>(s_src));
+    finish_long<B, N, K>(p, pieces_of(s, chunk, p.chunk_shift, p.seg_begin), chunk, tile, c, blockDim.x * N, threadIdx.x == 0,
+                         [&](uint32_t u) { return p.seg_key[u]; }, reinterpret_cast<uint32_t*>(s_src));
 }
 
 // ---------------------------------------------------------------------------------------------- few tokens
 
 // Few tokens: one launch does everything.  Every block sorts all tokens for itself in shared memory, which
 // takes less than a second kernel's start, and then sums its chunks; the block that delivers the last piece of a long segment
-// adds the pieces up.
+// adds the pieces up.  Two blocks per SM leave 64 registers a thread: 16 to 92
+// bytes spill, most with 16-bit rows.
 constexpr int kSmallThreads = 512, kSmallWarps = kSmallThreads / 32, kSmallItems = 4;
 constexpr uint32_t kSmallTokens = kSmallThreads * kSmallItems;
 constexpr uint32_t kSmallShift = 3, kSmallChunk = 1u << kSmallShift, kSmallChunks = kSmallTokens / kSmallChunk;
@@ -1147,7 +1158,8 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob 
         uint64_t* s_dst = s_src + 2 * kSmallChunk;
         Share s = {};
         if (ty < y && i0 < m.live) {
-            s = share_of(i0, kSmallChunk, m.live, m.chunk_seg[chunk], i0 + kSmallChunk < m.live ? m.chunk_seg[chunk + 1] : m.n_segs, m.seg_begin);
+            s = share_of(i0, kSmallChunk, m.live, m.chunk_seg[chunk], i0 + kSmallChunk < m.live ? m.chunk_seg[chunk + 1] : m.n_segs,
+                         m.seg_begin);
             for (uint32_t k = tx; k < s.b - s.a; k += x) {
                 const uint32_t t = s.a + k;
                 const bool ends = t + 1 == m.live || m.key(t + 1) != m.key(t);
@@ -1163,7 +1175,8 @@ __global__ void __launch_bounds__(kSmallThreads, 2) k_embed_small(const SortJob 
         if (c < p.dim) sum_chunk<A, B, N, 1, 8>(p, s_src, s_dst, s.b - s.a, s.lead ? s.u0 - 1 : s.u0, s.u0, chunk, c, x * N);
         __syncthreads();
         if (!m.any_long) continue;
-        finish_long<B, N, 1>(p, pieces_of(s, chunk, kSmallShift, m.seg_begin), chunk, tile, c, 0, tx == 0 && ty < y, [&](uint32_t u) { return m.seg_key(u); }, &m.last[ty < y ? ty : kSmallLanes]);
+        finish_long<B, N, 1>(p, pieces_of(s, chunk, kSmallShift, m.seg_begin), chunk, tile, c, 0, tx == 0 && ty < y,
+                             [&](uint32_t u) { return m.seg_key(u); }, &m.last[ty < y ? ty : kSmallLanes]);
         __syncthreads();
     }
     if (p.zero_rows) clear_small(p, m);
@@ -1295,10 +1308,12 @@ int launch_lookup_vec(const Rows& table, const Rows& tokens, const Rows& out, ui
     if (static_cast<uint64_t>(n_tokens) * cols >= 4ull * 2048 * h->n_sms) {
         const uint64_t grid = (static_cast<uint64_t>(n_tokens) + 4 * y - 1) / (4 * y) * tiles;
         if (grid > 0x7FFFFFFFull) return ADACOMP_ERR_INVALID;
-        k_embed_lookup<A, B, N, K, 4><<<static_cast<uint32_t>(grid), block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, passing, scale, h->d_status);
+        k_embed_lookup<A, B, N, K, 4><<<static_cast<uint32_t>(grid), block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles,
+                                                                                         wide, passing, scale, h->d_status);
     } else {
         const uint32_t grid = (n_tokens + y - 1) / y * tiles;
-        k_embed_lookup<A, B, N, K, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, passing, scale, h->d_status);
+        k_embed_lookup<A, B, N, K, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, wide, passing, scale,
+                                                                  h->d_status);
     }
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
@@ -1308,10 +1323,12 @@ template <typename A, typename B>
 int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32_t n_tokens, const adacomp_embed_t* h,
                   float scale, cudaStream_t stream) {
     constexpr int N = kItemElems<A, B>;
-    if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16)) return launch_lookup_vec<A, B, N, 1>(table, tokens, out, n_tokens, h, scale, stream);
+    if (h->dim % N == 0 && on_grid(table, 16) && on_grid(out, 16))
+        return launch_lookup_vec<A, B, N, 1>(table, tokens, out, n_tokens, h, scale, stream);
     // Off the grid: single entries, or for long rows of 16-bit entries items of eight.  32768 bf16 rows one way and the other: of
-    // 250 entries 15.4 and 17.2 us, of 1001 52 and 38; fp32 rows of 1001 take 49 one entry at a time (6.1 TB/s on the grid, 5.4 off it).
-    if ((sizeof(A) == 4 && sizeof(B) == 4) || h->dim < 512) return launch_lookup_vec<A, B, 1, 4>(table, tokens, out, n_tokens, h, scale, stream);
+    // 250 entries 15.4 and 17.2 us, of 1001 52 and 37; fp32 rows of 1001 take 49 one entry at a time, of 1024 on the grid 43.
+    if ((sizeof(A) == 4 && sizeof(B) == 4) || h->dim < 512)
+        return launch_lookup_vec<A, B, 1, 4>(table, tokens, out, n_tokens, h, scale, stream);
     uint32_t x, y, tiles;
     const uint64_t cols = (static_cast<uint64_t>(h->dim) + 7 + 7) / 8;      // wherever a row starts
     along_row(static_cast<uint32_t>(cols), 512, &x, &y, &tiles);
@@ -1319,10 +1336,12 @@ int launch_lookup(const Rows& table, const Rows& tokens, const Rows& out, uint32
     const dim3 block(x, y);
     if (n_tokens * cols >= 2ull * 2048 * h->n_sms) {
         const uint32_t grid = static_cast<uint32_t>((static_cast<uint64_t>(n_tokens) + 2 * y - 1) / (2 * y) * tiles);
-        k_embed_lookup_off<A, B, 2><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale, h->d_status);
+        k_embed_lookup_off<A, B, 2><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale,
+                                                                h->d_status);
     } else {
         const uint32_t grid = (n_tokens + y - 1) / y * tiles;
-        k_embed_lookup_off<A, B, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale, h->d_status);
+        k_embed_lookup_off<A, B, 1><<<grid, block, 0, stream>>>(table, tokens, out, n_tokens, h->vocab, h->dim, tiles, total, scale,
+                                                                h->d_status);
     }
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
@@ -1378,7 +1397,6 @@ SortJob describe(const adacomp_embed_t* h, const Rows& tokens, uint32_t n_tokens
     p->seg_key = j.seg_key;
     p->chunk_seg = j.chunk_seg;
     p->n_segs = j.n_segs;
-    p->n = j.n;
     p->chunk_shift = j.chunk_shift;
     p->n_chunks = static_cast<uint32_t>((static_cast<uint64_t>(j.n) + (1u << j.chunk_shift) - 1) >> j.chunk_shift);
     p->partial = h->d_partial;
@@ -1490,7 +1508,8 @@ int launch_sums(const SortJob& j, Sums p, uint32_t out_grid, bool clear, const a
         zero_blocks = static_cast<uint32_t>(left < blocks ? left : blocks);
     }
     const dim3 block(x, y);
-    return launch_after(vec ? k_embed_sums<A, B, N, 1> : k_embed_sums<A, B, 1, K>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes, stream, p);
+    return launch_after(vec ? k_embed_sums<A, B, N, 1> : k_embed_sums<A, B, 1, K>, dim3(p.sum_blocks + zero_blocks), block, y * chunk_bytes,
+                        stream, p);
 }
 
 // Calls f<A, B>() for the types' numbers.
@@ -1611,7 +1630,8 @@ int adacomp_embed_grad_rows(adacomp_embed_t* h, const adacomp_rows_t* tokens, ui
     if (!aligned(d_values_out, type_size(values_type)) || !aligned(d_rows_out, sizeof(uint32_t)) || !aligned(d_idx_out, sizeof(uint32_t)) ||
         !aligned(d_row_begin_out, sizeof(uint64_t)))
         return ADACOMP_ERR_INVALID;
-    if (d_idx_out && (idx_offset >= (1ull << 32) || idx_offset + static_cast<uint64_t>(h->vocab) * h->dim > (1ull << 32))) return ADACOMP_ERR_INVALID;
+    if (d_idx_out && (idx_offset >= (1ull << 32) || idx_offset + static_cast<uint64_t>(h->vocab) * h->dim > (1ull << 32)))
+        return ADACOMP_ERR_INVALID;
     Rows k;
     Sums p = {};
     rc = rows_view(tokens, n, true, &k);

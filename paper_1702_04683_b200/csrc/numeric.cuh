@@ -12,11 +12,6 @@ __host__ __device__ __forceinline__ uint32_t type_size(int type) { return type =
 inline bool aligned(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 inline bool known_type(int type) { return type == ADACOMP_F32 || type == ADACOMP_BF16 || type == ADACOMP_F16; }
 
-template <int TYPE> struct ElemOf;
-template <> struct ElemOf<ADACOMP_F32> { using T = float; };
-template <> struct ElemOf<ADACOMP_BF16> { using T = __nv_bfloat16; };
-template <> struct ElemOf<ADACOMP_F16> { using T = __half; };
-
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
