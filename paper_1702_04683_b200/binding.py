@@ -766,19 +766,22 @@ class Embedding(_Handle):
         return out
 
     def _batch(self, tokens: torch.Tensor, grad: torch.Tensor, workers: int):
-        if workers < 1 or tokens.numel() % workers:
+        """(tokens, tokens of a worker, gradient's rows)"""
+        n, shape = tokens.numel(), grad.shape
+        if workers < 1 or n % workers:
             raise ValueError("tokens: need the same number for every worker")
-        if grad.numel() != tokens.numel() * self.dim:
+        if grad.numel() != n * self.dim:
             raise ValueError("grad: need a row for every token")
-        if grad.dim() > 2 and tokens.dim() > 1 and grad.shape[:-1] != tokens.shape:
-            # lists of rows or of tokens are in the order of the other; two shapes have to be the same, but for ones
-            if [n for n in grad.shape[:-1] if n != 1] != [n for n in tokens.shape if n != 1]:
+        if len(shape) > 2:
+            # a list of rows or of tokens is in the order of the other; two shapes have to be the same, but for ones
+            given = tokens.shape
+            if len(given) > 1 and shape[:-1] != given and [n for n in shape[:-1] if n != 1] != [n for n in given if n != 1]:
                 raise ValueError("grad: need the shape of the tokens")
-        return self._tokens(tokens), tokens.numel() // workers, self._wide(grad, "grad")
+        return self._tokens(tokens), n // workers, self._wide(grad, "grad")
 
     def _grad_rows(self, tokens, grad, scale, workers, rows_out, values_out, idx_out, offset, stream):
         ids, per_worker, rows = self._batch(tokens, grad, workers)
-        n = tokens.numel()
+        n = per_worker * workers
         for t, need, name in ((rows_out, n, "rows_out"), (values_out, n * self.dim, "values_out"), (idx_out, n * self.dim, "idx_out")):
             if t is not None and t.numel() < need:
                 raise ValueError(f"{name}: too small")
