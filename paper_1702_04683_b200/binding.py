@@ -627,9 +627,12 @@ class Clipper(_Handle):
             raise TypeError("out: need rows that do not overlap")
         if out is not grads:
             at, size, to, out_size = grads.data_ptr(), grads.element_size(), out.data_ptr(), out.element_size()
-            same = at == to and grads.dtype == out.dtype and (W == 1 or grads.stride(0) == out.stride(0))
-            if not same and n and at < to + ((W - 1) * out.stride(0) + n) * out_size and to < at + ((W - 1) * grads.stride(0) + n) * size:
-                raise ValueError("out: overlaps the gradients")
+            apart, out_apart = strides[0] * size, out_strides[0] * out_size
+            same = at == to and grads.dtype == out.dtype and (W == 1 or apart == out_apart)
+            if not same and n and at < to + (W - 1) * out_apart + n * out_size and to < at + (W - 1) * apart + n * size:
+                # rows of one buffer may hold both, next to each other
+                if W == 1 or apart != out_apart or not n * size <= (to - at) % apart <= apart - n * out_size:
+                    raise ValueError("out: overlaps the gradients")
         e = GradTensor(grads.data_ptr(), out.data_ptr(), n, kind, out_kind)
         return ctypes.byref(e), 1, W, strides[0] if W > 1 else 0, out_strides[0] if W > 1 else 0, out
 

@@ -324,6 +324,30 @@ def test_partial_sums_of_workers_keep_apart(binding, workers):
     check_norm(h.norm(longer), exact_norm(longer))
 
 
+@pytest.mark.parametrize("kind", [torch.float32, torch.float16])
+def test_gradients_and_outputs_in_rows_of_one_buffer(binding, kind):
+    """A buffer whose rows hold a worker's gradient and the place for its clipped one: nothing overlaps unless their columns do."""
+    W, n = 5, 3_000
+    h = binding.Clipper(max_workers=W)
+    for first, second in ((0, n), (n + 16, 7), (3, n + 3)):
+        buf = normals(W * (2 * n + 16), 3, kind).view(W, 2 * n + 16)
+        kept = buf.clone()
+        coef = torch.empty(W, device=DEV)
+        h.clip(buf[:, first:first + n], 0.1, out=buf[:, second:second + n], coef_out=coef)
+        kept[:, second:second + n] = (kept[:, first:first + n].float() * coef.view(W, 1)).to(kind)
+        assert torch.equal(buf, kept)
+    for first, second in ((0, n - 1), (n, 1), (n + 16, n + 9)):
+        with pytest.raises(ValueError):
+            h.clip(buf[:, first:first + n], 0.1, out=buf[:, second:second + n])
+    shifted = buf[:-1, n + 16:], buf[1:, :n]                                # row w beside row w + 1
+    assert shifted[0].shape == shifted[1].shape
+    before = shifted[0].clone()
+    h.clip(shifted[0], float("inf"), out=shifted[1])
+    assert torch.equal(shifted[1], before)
+    with pytest.raises(ValueError):
+        h.clip(shifted[0], 0.1, out=buf[:-1, n + 10:2 * n + 10])
+
+
 def test_refusals(binding):
     lib = binding.raw()
     h = binding.Clipper(max_workers=2)

@@ -81,6 +81,10 @@ def test_embed_null_handles(binding):
     assert lib.adacomp_embed_destroy(None) == 0
 
 
+def test_wait_limit_of_no_handle(binding):
+    assert binding.raw().adacomp_embed_set_wait_limit(None, 0) == binding.ERR_INVALID
+
+
 def test_binding_refuses_host_tensors_and_unknown_types(binding):
     import torch
     with pytest.raises(TypeError):
