@@ -519,6 +519,125 @@ ADACOMP_API int adacomp_embed_set_wait_limit(adacomp_embed_t* h, uint32_t polls)
 ADACOMP_API int adacomp_embed_last_error(adacomp_embed_t* h, void* cuda_stream);
 ADACOMP_API int adacomp_embed_destroy(adacomp_embed_t* h);
 
+/* ------------------------------------------------------------------------------------------
+ * Distillation from a teacher's top logits.  A teacher sends, for every row (token position), its k largest logits as (index,
+ * value) pairs instead of all of them, as a worker sends the largest entries of its gradient; a student's loss and the gradient of
+ * its logits come from the pairs (no counterpart in the paper, whose workers learn from labels).
+ * ---------------------------------------------------------------------------------------- */
+
+typedef struct adacomp_distill adacomp_distill_t;
+
+/* A row's pairs: k token numbers (ADACOMP_I32 / ADACOMP_I64) and as many logits (any of the three types), 1 <= k <= 1024.  An
+ * entry with a negative token is not there (lists of different length are filled up with -1); one whose token is not below the
+ * vocabulary is skipped and reported by adacomp_distill_last_error; of entries with the same token the first counts.  d_lse:
+ * NULL, or for every row the logarithm of the sum of exp(l / T) over ALL of the teacher's logits (what adacomp_top_logits returns,
+ * with the temperature of the loss). */
+typedef struct {
+    adacomp_rows_t idx;
+    adacomp_rows_t val;
+    const float* d_lse;
+    uint32_t k;
+} adacomp_pairs_t;
+
+/* A handle for logits over `vocab` tokens (1 .. 1048576).  The workspace (256-byte aligned device memory) holds an error word.
+ * Creation is synchronous. */
+ADACOMP_API int adacomp_distill_workspace_bytes(uint32_t vocab, size_t* bytes_out);
+ADACOMP_API int adacomp_distill_create(adacomp_distill_t** h, uint32_t vocab, void* d_workspace, size_t workspace_bytes,
+                                       int device);
+
+/* The teacher's side.  For every one of n_rows rows (below 2^31) of `vocab` logits:
+ *   d_idx_out [n_rows][k]   the tokens of the k largest logits (1 <= k <= min(vocab, 1024)), largest first; of equal ones
+ *                           (+0 and -0 are equal) the lowest token first; a NaN counts as larger than all numbers;
+ *   d_val_out [n_rows][k]   their logits, of the logits' type, bit for bit;
+ *   d_lse_out [n_rows]      NULL, or log(sum of exp(l / temperature)): -Inf where every logit is -Inf, NaN where one is NaN or +Inf.
+ * temperature lies in 2^-20 .. 2^20 (here and below).  Outputs are aligned to their elements and do not overlap the logits. */
+ADACOMP_API int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, uint32_t k,
+                                   float temperature, int32_t* d_idx_out, void* d_val_out, float* d_lse_out, void* cuda_stream);
+
+/* The student's side.  With p = softmax(s / T) over a row's `vocab` logits s, t the teacher's listed logits and sums over the
+ * listed tokens:
+ *   d_lse = NULL:  q = softmax(t / T) over the list,               L = sum q (log q - log p);
+ *   otherwise:     q = exp(t / T - lse), r = max(0, 1 - sum q),    L = sum q (log q - log p) + r (log r - log(sum of p not listed)):
+ *                  what the teacher did not list is one more class; it is left out where the student gives it nothing
+ *                  (less than 2^-126 of its largest probability), since r cannot be told from rounding there.
+ * Terms with q = 0 are 0.  The gradient of L with respect to s_j is, with W = sum q (+ r), (W p_j - q_j) / T for a listed token and
+ * (W - r / (sum of p not listed)) p_j / T for another.  A row's loss is L; its gradient is that of d_weight[row] * L (NULL: 1), so
+ * the mean over the tokens, a loss scale or T^2 go into the weight.  Rows whose weight is 0, or without any entry, or whose q
+ * or p does not exist (all listed t -Inf without d_lse, lse = -Inf, all s -Inf) count for nothing: their loss is 0 and their gradient zeros;
+ * the logits of rows of weight 0 are not read.  NaN and +Inf (in t or s) make the row's loss and gradient NaN; -Inf in s is a
+ * token of probability 0.  Probabilities and sums are fp32, the sums over a list 64-bit; the gradient is rounded to its type once.
+ *
+ *   adacomp_distill_loss       d_loss_out [n_rows] (NULL: not wanted), and d_stats_out [n_rows][8] for adacomp_distill_grad (NULL: none;
+ *                              16-byte aligned; their meaning is the library's);
+ *   adacomp_distill_grad       the gradient, from the same logits, pairs, temperature and the stats of adacomp_distill_loss;
+ *   adacomp_distill_loss_grad  both in one pass over the logits.
+ * `out` has the logits' type and either is the logits (same address and distances: the gradient takes their place) or does not overlap
+ * any input.  Errors: ADACOMP_ERR_INVALID (null pointer, unknown type, misaligned pointer, k or temperature out of range, rows of out
+ * that overlap each other), ADACOMP_ERR_CUDA. */
+ADACOMP_API int adacomp_distill_loss(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
+                                     const adacomp_pairs_t* pairs, float temperature, const float* d_weight, float* d_loss_out,
+                                     float* d_stats_out, void* cuda_stream);
+ADACOMP_API int adacomp_distill_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
+                                     const adacomp_pairs_t* pairs, float temperature, const float* d_weight,
+                                     const float* d_stats, const adacomp_rows_t* out, void* cuda_stream);
+ADACOMP_API int adacomp_distill_loss_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
+                                          const adacomp_pairs_t* pairs, float temperature, const float* d_weight,
+                                          float* d_loss_out, const adacomp_rows_t* out, void* cuda_stream);
+/* Waits for cuda_stream, returns and clears the first error recorded on the device. */
+ADACOMP_API int adacomp_distill_last_error(adacomp_distill_t* h, void* cuda_stream);
+ADACOMP_API int adacomp_distill_destroy(adacomp_distill_t* h);
+
+/* ------------------------------------------------------------------------------------------
+ * Routing of tokens to experts, with the gradient of the router's logits.  An expert's parameters change only where tokens reach
+ * it, so their updates are sparse as an embedding table's are (no counterpart in the paper).
+ * ---------------------------------------------------------------------------------------- */
+
+typedef struct adacomp_route adacomp_route_t;
+
+enum {
+    ADACOMP_SOFTMAX = 0,            /* scores of a row: softmax over the experts */
+    ADACOMP_SIGMOID = 1             /* 1 / (1 + exp(-l)), each for itself */
+};
+
+typedef struct {
+    uint32_t experts;               /* 1 .. 1024 */
+    uint32_t top_k;                 /* 1 .. 32, at most experts / groups * top_groups */
+    uint32_t groups;                /* equal groups of consecutive experts: 1 .. 32, a divisor of experts */
+    uint32_t top_groups;            /* 1 .. groups: how many groups experts are taken from */
+    uint32_t group_terms;           /* 1 or 2: a group is rated by the sum of so many of its largest values (of all, if it has fewer) */
+    int32_t score;                  /* ADACOMP_SOFTMAX / ADACOMP_SIGMOID */
+    int32_t renormalize;            /* 1: a row's weights are divided by their sum */
+    float scale;                    /* and multiplied by this; finite */
+} adacomp_route_config_t;
+
+ADACOMP_API int adacomp_route_workspace_bytes(const adacomp_route_config_t* config, size_t* bytes_out);
+ADACOMP_API int adacomp_route_create(adacomp_route_t** h, const adacomp_route_config_t* config, void* d_workspace,
+                                     size_t workspace_bytes, int device);
+
+/* The choice.  Every expert of a row (of n_rows, below 2^31) has a score from the row's logits and a value score + d_bias[expert]
+ * (d_bias NULL: the score); an expert whose logit or bias is -Inf cannot be chosen.  The top_groups best groups are kept (of
+ * equal ones the lowest), then the top_k experts of largest value in them, largest first, of equal ones the lowest.  Comparisons are
+ * those of values computed in 64 bits.
+ *   d_experts_out [n_rows][top_k]  the experts; -1 in places that no expert is left for
+ *   d_weights_out [n_rows][top_k]  scale * score (the bias is not in it), divided by the row's sum of chosen scores if
+ *                                  renormalize is set; 0 in places without an expert
+ *   d_counts_out  [experts]        NULL, or how many places of the call name each expert (what a balancing bias is adjusted by)
+ * d_live (NULL: all; bytes, 0 or 1): rows with 0 are padding: experts -1, weights 0, not read.  A row with a NaN (in a logit
+ * or bias), or with +Inf under softmax, has no scores: experts -1, weights NaN. */
+ADACOMP_API int adacomp_route(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const float* d_bias,
+                              const uint8_t* d_live, int32_t* d_experts_out, float* d_weights_out, uint32_t* d_counts_out,
+                              void* cuda_stream);
+
+/* Gradient of the logits from that of the weights (d_grad_weights [n_rows][top_k]; entries beside an expert -1 are not used),
+ * the choice held fixed: `out` has the logits' type, and is the logits themselves (same address and distances) or does not
+ * overlap any input.  Rows without an expert get zeros.  A number in d_experts that is not below `experts` is skipped like -1 and
+ * reported by adacomp_route_last_error; an expert that a row names twice counts once, with its first place. */
+ADACOMP_API int adacomp_route_grad(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const int32_t* d_experts,
+                                   const float* d_grad_weights, const adacomp_rows_t* out, void* cuda_stream);
+/* Waits for cuda_stream, returns and clears the first error recorded on the device. */
+ADACOMP_API int adacomp_route_last_error(adacomp_route_t* h, void* cuda_stream);
+ADACOMP_API int adacomp_route_destroy(adacomp_route_t* h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -47,6 +47,15 @@ class Rows(ctypes.Structure):
                 ("row_stride", ctypes.c_uint64), ("group_stride", ctypes.c_uint64)]
 
 
+class Pairs(ctypes.Structure):
+    _fields_ = [("idx", Rows), ("val", Rows), ("d_lse", ctypes.c_void_p), ("k", ctypes.c_uint32)]
+
+
+class RouteConfig(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_uint32), ("top_k", ctypes.c_uint32), ("groups", ctypes.c_uint32), ("top_groups", ctypes.c_uint32),
+                ("group_terms", ctypes.c_uint32), ("score", ctypes.c_int32), ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 #: element types of the operators that take more than fp32, and types of token numbers
 ELEMENT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 TOKEN_TYPES = {torch.int32: 0, torch.int64: 1}
@@ -114,6 +123,20 @@ def _load():
         "adacomp_embed_set_wait_limit": (i32, [vp, u32]),
         "adacomp_embed_last_error": (i32, [vp, vp]),
         "adacomp_embed_destroy": (i32, [vp]),
+        "adacomp_distill_workspace_bytes": (i32, [u32, P(ctypes.c_size_t)]),
+        "adacomp_distill_create": (i32, [P(vp), u32, vp, ctypes.c_size_t, i32]),
+        "adacomp_top_logits": (i32, [vp, vp, u32, u32, f32, vp, vp, vp, vp]),
+        "adacomp_distill_loss": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
+        "adacomp_distill_grad": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
+        "adacomp_distill_loss_grad": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
+        "adacomp_distill_last_error": (i32, [vp, vp]),
+        "adacomp_distill_destroy": (i32, [vp]),
+        "adacomp_route_workspace_bytes": (i32, [P(RouteConfig), P(ctypes.c_size_t)]),
+        "adacomp_route_create": (i32, [P(vp), P(RouteConfig), vp, ctypes.c_size_t, i32]),
+        "adacomp_route": (i32, [vp, vp, u32, vp, vp, vp, vp, vp, vp]),
+        "adacomp_route_grad": (i32, [vp, vp, u32, vp, vp, vp, vp]),
+        "adacomp_route_last_error": (i32, [vp, vp]),
+        "adacomp_route_destroy": (i32, [vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -503,7 +526,8 @@ def _element_type(t: torch.Tensor, device: int, name: str) -> int:
 
 
 class _Handle:
-    """What :class:`Clipper` and :class:`Embedding` share: a device workspace and the streams that work in it."""
+    """What :class:`Clipper`, :class:`Embedding`, :class:`Distiller` and :class:`Router` share: a device workspace and the streams
+    that work in it."""
 
     def _take_workspace(self, nbytes: int) -> None:
         """Device memory for the handle.  The allocator hands out memory that earlier work of the current stream may still write to,
@@ -853,6 +877,261 @@ class Embedding(_Handle):
     def close(self):
         if getattr(self, "_h", None):
             _lib.adacomp_embed_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ----------------------------------------------------------------------------- distillation, routing
+
+def _logit_rows(t: torch.Tensor, width: int, device: int, name: str) -> Rows:
+    """The rows of a tensor [..., width] of one of the three element types."""
+    kind = _element_type(t, device, name)
+    shape = t.shape
+    if not shape or shape[-1] != width:
+        raise ValueError(f"{name}: need rows of {width} entries")
+    if t.is_contiguous():
+        return Rows(t.data_ptr(), kind, 0, width, 0)
+    if width > 1 and t.stride(-1) != 1:
+        raise TypeError(f"{name}: need contiguous rows")
+    return _rows(t, len(shape) - 1, kind, name)
+
+
+def _span(t: torch.Tensor):
+    """The bytes between a tensor's first entry and its last."""
+    at = t.data_ptr()
+    if t.is_contiguous():
+        return at, at + t.numel() * t.element_size()
+    return at, at + (sum(st * (n - 1) for st, n in zip(t.stride(), t.shape)) + 1) * t.element_size()
+
+
+def _gradient_for(out: Optional[torch.Tensor], logits: torch.Tensor, stream) -> torch.Tensor:
+    """Where the gradient of `logits` goes: a tensor like them, the logits themselves, or one that shares no memory with them."""
+    if out is None:
+        return _empty(logits, logits.shape, logits.dtype, stream)
+    if out is logits:
+        return out
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out: need the shape and type of the logits")
+    if out.numel() and not (out.data_ptr() == logits.data_ptr() and out.stride() == logits.stride()):
+        (a, b), (c, d) = _span(logits), _span(out)
+        if a < d and c < b:
+            raise ValueError("out: overlaps the logits")
+    return out
+
+
+def _per_row(t: Optional[torch.Tensor], dtype, rows: int, device: int, name: str) -> Optional[int]:
+    """A contiguous tensor with one entry (or `rows` of them) per row, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+        raise TypeError(f"{name}: need a contiguous tensor of {dtype} on cuda:{device}")
+    if t.numel() != rows:
+        raise ValueError(f"{name}: need {rows} entries")
+    return t.data_ptr()
+
+
+class Distiller(_Handle):
+    """Distillation from a teacher's top logits over a vocabulary of `vocab` tokens: the teacher's side (:meth:`top`) and the
+    student's loss and gradient.  Logits are tensors [..., vocab], of float32, bfloat16 or float16; a row is a token position."""
+
+    def __init__(self, vocab: int, device: Optional[torch.device] = None):
+        self.device = torch.device(device if device is not None else "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self.vocab = int(vocab)
+        if not 0 <= self.vocab < 1 << 32:
+            raise AdacompError(ERR_INVALID, "adacomp_distill_workspace_bytes")
+        nbytes = ctypes.c_size_t(0)
+        _check(_lib.adacomp_distill_workspace_bytes(self.vocab, ctypes.byref(nbytes)), "adacomp_distill_workspace_bytes")
+        self._take_workspace(int(nbytes.value))
+        h = ctypes.c_void_p()
+        _check(_lib.adacomp_distill_create(ctypes.byref(h), self.vocab, self.workspace.data_ptr(), self.workspace.numel(),
+                                           self._index), "adacomp_distill_create")
+        self._h = h
+
+    def top(self, logits: torch.Tensor, k: int, temperature: float = 1.0, idx_out: Optional[torch.Tensor] = None,
+            val_out: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None):
+        """The k largest logits of every row -> (idx int32 [..., k], val [..., k] of the logits' type, lse float32 [...]): largest
+        first, of equal ones the lowest token first; lse = log sum exp(logits / temperature) over the whole row."""
+        rows = _logit_rows(logits, self.vocab, self._index, "logits")
+        lead, k = logits.shape[:-1], int(k)
+        n = logits.numel() // self.vocab
+        if not 0 <= k < 1 << 32:
+            raise ValueError("k: out of range")
+        if idx_out is None:
+            idx_out = _empty(logits, (*lead, k), torch.int32, stream)
+        if val_out is None:
+            val_out = _empty(logits, (*lead, k), logits.dtype, stream)
+        if lse_out is None:
+            lse_out = _empty(logits, lead, torch.float32, stream)
+        _check(_lib.adacomp_top_logits(self._h, ctypes.byref(rows), n, k, float(temperature),
+                                       _per_row(idx_out, torch.int32, n * k, self._index, "idx_out"),
+                                       _per_row(val_out, logits.dtype, n * k, self._index, "val_out"),
+                                       _per_row(lse_out, torch.float32, n, self._index, "lse_out"), self._stream_on(stream)),
+               "adacomp_top_logits")
+        return idx_out, val_out, lse_out
+
+    def _given(self, logits, idx, val, lse, weight):
+        """(rows, how many, pairs, weights)"""
+        index = self._index
+        rows = _logit_rows(logits, self.vocab, index, "logits")
+        lead = logits.shape[:-1]
+        n = logits.numel() // self.vocab
+        kind = TOKEN_TYPES.get(idx.dtype)
+        if kind is None or idx.get_device() != index:
+            raise TypeError(f"idx: need an int32 or int64 tensor on {self.device}")
+        if idx.shape[:-1] != lead or val.shape != idx.shape:
+            raise ValueError("idx, val: need a list for every row of the logits")
+        k = idx.shape[-1]
+        if idx.is_contiguous():
+            tokens = Rows(idx.data_ptr(), kind, 0, k, 0)
+        elif k > 1 and idx.stride(-1) != 1:
+            raise TypeError("idx: need contiguous rows")
+        else:
+            tokens = _rows(idx, idx.dim() - 1, kind, "idx")
+        pairs = Pairs(tokens, _logit_rows(val, k, index, "val"), _per_row(lse, torch.float32, n, index, "lse"), k)
+        return rows, n, pairs, _per_row(weight, torch.float32, n, index, "weight")
+
+    def loss(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: Optional[torch.Tensor] = None,
+             temperature: float = 1.0, weight: Optional[torch.Tensor] = None, loss_out: Optional[torch.Tensor] = None,
+             stats_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """The divergence of the student's distribution from the teacher's, row by row -> (loss float32 [...], stats float32
+        [..., 8] for :meth:`grad`).  ``idx``, ``val`` [..., k]: the teacher's pairs, empty places filled up with -1; ``lse`` [...]: its
+        normalisers, with which what it did not list is one more class (None: the list alone, renormalised).  Rows of
+        ``weight`` [...] 0 are left out; other weights matter to the gradient only."""
+        rows, n, pairs, weights = self._given(logits, idx, val, lse, weight)
+        if loss_out is None:
+            loss_out = _empty(logits, logits.shape[:-1], torch.float32, stream)
+        if stats_out is None:
+            stats_out = _empty(logits, (*logits.shape[:-1], 8), torch.float32, stream)
+        _check(_lib.adacomp_distill_loss(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights,
+                                         _per_row(loss_out, torch.float32, n, self._index, "loss_out"),
+                                         _per_row(stats_out, torch.float32, 8 * n, self._index, "stats_out"),
+                                         self._stream_on(stream)), "adacomp_distill_loss")
+        return loss_out, stats_out
+
+    def grad(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stats: torch.Tensor,
+             lse: Optional[torch.Tensor] = None, temperature: float = 1.0, weight: Optional[torch.Tensor] = None,
+             out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Gradient of sum(weight * loss) with respect to the logits, from the stats of :meth:`loss`; ``out`` may be the logits
+        themselves."""
+        rows, n, pairs, weights = self._given(logits, idx, val, lse, weight)
+        out = _gradient_for(out, logits, stream)
+        _check(_lib.adacomp_distill_grad(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights,
+                                         _per_row(stats, torch.float32, 8 * n, self._index, "stats"),
+                                         ctypes.byref(_logit_rows(out, self.vocab, self._index, "out")), self._stream_on(stream)),
+               "adacomp_distill_grad")
+        return out
+
+    def loss_grad(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                  temperature: float = 1.0, weight: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                  loss_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """Loss and gradient in one pass over the logits -> (loss [...], gradient [..., vocab])."""
+        rows, n, pairs, weights = self._given(logits, idx, val, lse, weight)
+        out = _gradient_for(out, logits, stream)
+        if loss_out is None:
+            loss_out = _empty(logits, logits.shape[:-1], torch.float32, stream)
+        _check(_lib.adacomp_distill_loss_grad(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights,
+                                              _per_row(loss_out, torch.float32, n, self._index, "loss_out"),
+                                              ctypes.byref(_logit_rows(out, self.vocab, self._index, "out")), self._stream_on(stream)),
+               "adacomp_distill_loss_grad")
+        return loss_out, out
+
+    def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
+        """Waits for the stream; the first error the device recorded since the last call (a token outside the vocabulary)."""
+        return int(_lib.adacomp_distill_last_error(self._h, self._stream_on(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.adacomp_distill_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Router(_Handle):
+    """Routing of tokens to `top_k` of `experts`: scores by "softmax" or "sigmoid", experts taken from the best ``top_groups`` of
+    ``groups`` equal groups (each rated by the sum of its ``group_terms`` largest values), weights renormalised over the chosen
+    ones and scaled."""
+
+    SCORES = {"softmax": 0, "sigmoid": 1}
+
+    def __init__(self, experts: int, top_k: int, score: str = "softmax", groups: int = 1, top_groups: Optional[int] = None,
+                 group_terms: int = 1, renormalize: bool = True, scale: float = 1.0, device: Optional[torch.device] = None):
+        self.device = torch.device(device if device is not None else "cuda")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        if score not in self.SCORES:
+            raise ValueError("score: need \"softmax\" or \"sigmoid\"")
+        self.experts, self.top_k = int(experts), int(top_k)
+        sizes = (self.experts, self.top_k, int(groups), int(groups if top_groups is None else top_groups), int(group_terms))
+        if not all(0 <= n < 1 << 32 for n in sizes):
+            raise AdacompError(ERR_INVALID, "adacomp_route_workspace_bytes")
+        self.config = RouteConfig(*sizes, self.SCORES[score], int(bool(renormalize)), float(scale))
+        nbytes = ctypes.c_size_t(0)
+        _check(_lib.adacomp_route_workspace_bytes(ctypes.byref(self.config), ctypes.byref(nbytes)), "adacomp_route_workspace_bytes")
+        self._take_workspace(int(nbytes.value))
+        h = ctypes.c_void_p()
+        _check(_lib.adacomp_route_create(ctypes.byref(h), ctypes.byref(self.config), self.workspace.data_ptr(), self.workspace.numel(),
+                                         self._index), "adacomp_route_create")
+        self._h = h
+
+    def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, live: Optional[torch.Tensor] = None,
+              experts_out: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None,
+              counts_out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """logits [..., experts] -> (experts int32 [..., top_k], weights float32 [..., top_k], counts int32 [experts]).  ``bias``
+        float32 [experts] is added to the scores for the choice only; ``live`` bool [...]: rows with False are padding (experts
+        -1, weights 0); counts: how many places name each expert."""
+        rows = _logit_rows(logits, self.experts, self._index, "logits")
+        lead, k = logits.shape[:-1], self.top_k
+        n = logits.numel() // self.experts
+        if experts_out is None:
+            experts_out = _empty(logits, (*lead, k), torch.int32, stream)
+        if weights_out is None:
+            weights_out = _empty(logits, (*lead, k), torch.float32, stream)
+        if counts_out is None:
+            counts_out = _empty(logits, (self.experts,), torch.int32, stream)
+        _check(_lib.adacomp_route(self._h, ctypes.byref(rows), n, _per_row(bias, torch.float32, self.experts, self._index, "bias"),
+                                  _per_row(live, torch.bool, n, self._index, "live"),
+                                  _per_row(experts_out, torch.int32, n * k, self._index, "experts_out"),
+                                  _per_row(weights_out, torch.float32, n * k, self._index, "weights_out"),
+                                  _per_row(counts_out, torch.int32, self.experts, self._index, "counts_out"),
+                                  self._stream_on(stream)), "adacomp_route")
+        return experts_out, weights_out, counts_out
+
+    def grad(self, logits: torch.Tensor, experts: torch.Tensor, grad_weights: torch.Tensor, out: Optional[torch.Tensor] = None,
+             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Gradient of the logits from that of the weights (float32 [..., top_k]), the choice held fixed; ``out`` may be the
+        logits themselves."""
+        rows = _logit_rows(logits, self.experts, self._index, "logits")
+        n = logits.numel() // self.experts
+        out = _gradient_for(out, logits, stream)
+        _check(_lib.adacomp_route_grad(self._h, ctypes.byref(rows), n,
+                                       _per_row(experts, torch.int32, n * self.top_k, self._index, "experts"),
+                                       _per_row(grad_weights, torch.float32, n * self.top_k, self._index, "grad_weights"),
+                                       ctypes.byref(_logit_rows(out, self.experts, self._index, "out")), self._stream_on(stream)),
+               "adacomp_route_grad")
+        return out
+
+    def last_error(self, stream: Optional[torch.cuda.Stream] = None) -> int:
+        """Waits for the stream; the first error the device recorded since the last call (an expert that there is not)."""
+        return int(_lib.adacomp_route_last_error(self._h, self._stream_on(stream)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            _lib.adacomp_route_destroy(self._h)
             self._h = None
 
     def __del__(self):
