@@ -8,6 +8,7 @@
 //
 // All of it is bound by HBM: every logit is read once and, with a gradient, one entry written for it; one exponential
 // (two with a gradient) per logit.
+#include <cooperative_groups.h>
 #include <math.h>
 #include <new>
 
@@ -42,6 +43,47 @@ __device__ __forceinline__ uint4 load16_once(const void* p) {
     uint4 v;
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
+}
+
+// Two operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{ .reg .b64 a, b, c, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mov.b64 c, {%6, %7}; fma.rn.f32x2 d, a, b, c; mov.b64 {%0, %1}, d; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+// The largest of two, NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+template <typename T> __device__ __forceinline__ uint32_t max_nan_halves(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max_nan_halves<__nv_bfloat16>(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+template <> __device__ __forceinline__ uint32_t max_nan_halves<__half>(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// The largest entry of a vector, NaN if it holds one.
+template <typename T> __device__ __forceinline__ float vec_max(const uint4& v) {
+    if constexpr (sizeof(T) == 4) {
+        return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+    } else {
+        const float2 f = halves<T>(max_nan_halves<T>(max_nan_halves<T>(v.x, v.y), max_nan_halves<T>(v.z, v.w)));
+        return max_nan(f.x, f.y);
+    }
 }
 
 template <typename T> constexpr int kVec = 16 / sizeof(T);
@@ -318,7 +360,11 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
 // ---------------------------------------------------------------------------------------------- top logits
 
 constexpr int kTopThreads = 256;
+constexpr int kTopVecs = 4;                         // vectors of a thread in one step
+constexpr uint32_t kTopStep = kTopThreads * kTopVecs;
 constexpr uint32_t kCandidates = 2048;
+constexpr int kBoundBits = 16;
+constexpr uint32_t kTopCluster = 8;
 
 struct TopJob {
     Rows logits;
@@ -331,104 +377,247 @@ struct TopJob {
 };
 
 // Order of logits as whole numbers: NaN above all, +0 and -0 equal; below it the token, the lowest first.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return x != x ? 0xFFFFFFFFu : u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
 __device__ __forceinline__ uint64_t composite(float x, uint32_t token) {
-    uint32_t u = __float_as_uint(x + 0.0f);
-    u = x != x ? 0xFFFFFFFFu : u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-    return static_cast<uint64_t>(u) << 32 | (0xFFFFFFFFu - token);
+    return static_cast<uint64_t>(order_of(x)) << 32 | (0xFFFFFFFFu - token);
+}
+// A float that every entry above `bound` in order exceeds, other than by its token (NaN, which nothing fails to exceed, where there is none).
+__device__ __forceinline__ float floor_of(uint64_t bound) {
+    const uint32_t u = static_cast<uint32_t>(bound >> 32), bits = u >> 31 ? u ^ 0x80000000u : ~u;
+    return __uint_as_float(bits == 0x80000000u ? 0x80000001u : bits);      // +0 does not exceed -0
 }
 
-// Sorts s_list[0 .. n) in falling order, n a power of two.
+// Sorts s_list[0 .. n) in falling order, n a power of two.  Up to one entry a thread, distances within a warp are exchanged by
+// shuffles (256 entries: 12 barriers instead of 36).
 __device__ void sort_list(uint64_t* s_list, uint32_t n) {
-    for (uint32_t k = 2; k <= n; k *= 2)
-        for (uint32_t d = k / 2; d; d /= 2) {
-            __syncthreads();
-            for (uint32_t i = threadIdx.x; i < n / 2; i += kTopThreads) {
-                const uint32_t a = 2 * i - (i & (d - 1)), b = a + d;
-                const uint64_t x = s_list[a], y = s_list[b];
-                if ((x < y) == ((a & k) == 0)) s_list[a] = y, s_list[b] = x;
+    if (n <= kTopThreads) {
+        const uint32_t i = threadIdx.x;
+        __syncthreads();
+        uint64_t x = i < n ? s_list[i] : 0;
+        for (uint32_t k = 2; k <= n; k *= 2)
+            for (uint32_t d = k / 2; d; d /= 2) {
+                uint64_t y;
+                if (d >= 32) {
+                    if (i < n) s_list[i] = x;
+                    __syncthreads();
+                    y = i < n ? s_list[i ^ d] : 0;
+                    __syncthreads();
+                } else {
+                    y = __shfl_xor_sync(~0u, x, d);
+                }
+                const bool larger = ((i & k) == 0) == ((i & d) == 0);       // of the two, the one that this place keeps
+                x = (x > y) == larger ? x : y;
             }
-        }
+        if (i < n) s_list[i] = x;
+    } else {
+        for (uint32_t k = 2; k <= n; k *= 2)
+            for (uint32_t d = k / 2; d; d /= 2) {
+                __syncthreads();
+                for (uint32_t i = threadIdx.x; i < n / 2; i += kTopThreads) {
+                    const uint32_t a = 2 * i - (i & (d - 1)), b = a + d;
+                    const uint64_t x = s_list[a], y = s_list[b];
+                    if ((x < y) == ((a & k) == 0)) s_list[a] = y, s_list[b] = x;
+                }
+            }
+    }
     __syncthreads();
 }
 
-// One block per row; entries above the k-th largest of those seen so far are collected in a list, which is cut back to its k
-// largest when it is full.
+// The entries above the k-th largest of those seen so far are collected in a list, which is cut back to its k largest when it
+// has grown to twice that (or is full).  The first step's bound: with k of the threads' (or vectors') largest entries at or above a
+// number, k entries are.  From there on about k ln(vocab / entries of a step) entries make it to the list, so most vectors cost a
+// maximum, their exponentials and one comparison.
+//
+// A row is one block's work, or a cluster's where there are few rows: the first block then takes the others' lists through
+// their shared memory.
 template <typename T>
-__global__ void __launch_bounds__(kTopThreads) k_top_logits(const TopJob j) {
+__global__ void __launch_bounds__(kTopThreads, 4) k_top_logits(const TopJob j) {
     constexpr int N = kVec<T>;
     __shared__ uint64_t s_list[kCandidates];
-    __shared__ uint32_t s_count;
+    __shared__ uint32_t s_count, s_above[kBoundBits];
     __shared__ float s_m[kTopThreads / 32], s_s[kTopThreads / 32];
-    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    __shared__ Running s_run;
+    namespace cg = cooperative_groups;
+    const cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t ranks = cluster.num_blocks(), rank = cluster.block_rank();
+    const uint32_t row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const T* in = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
     const Cut cut = Cut::of(in, j.vocab);
+    const uint32_t per = (cut.n_vecs + ranks - 1) / ranks, from = min(rank * per, cut.n_vecs), to = min(from + per, cut.n_vecs);
+    const uint32_t trigger = min(2 * j.k + 64, kCandidates);
     uint64_t bound = 0;                             // an entry must be above it
+    float floor = NAN;
     Running r = {-INFINITY, 0.0f};
     if (tid == 0) s_count = 0;
+    if (tid < kBoundBits) s_above[tid] = 0;
     __syncthreads();
 
-    auto cut_back = [&](uint32_t keep) {            // the list sorted, and its `keep` largest kept
+    auto cut_back = [&]() {                         // the list sorted, and its k largest kept
         const uint32_t n = min(s_count, kCandidates);
         uint32_t size = 2;
         while (size < n) size *= 2;
         for (uint32_t i = n + tid; i < size; i += kTopThreads) s_list[i] = 0;
         sort_list(s_list, size);
-        if (tid == 0) s_count = min(n, keep);
-        if (n >= keep) bound = s_list[keep - 1];
+        if (tid == 0) s_count = min(n, j.k);
+        if (n >= j.k) bound = s_list[j.k - 1], floor = floor_of(bound);
         __syncthreads();
     };
-    // One step: entry e of this thread's N is f[e], token at + e, if bit e of `waiting` is set.
-    auto offer = [&](const float (&f)[N], uint32_t at, uint32_t waiting) {
-        for (;;) {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (waiting >> e & 1) {
-                    const uint64_t x = composite(f[e], at + e);
-                    bool done = x <= bound;
-                    if (!done) {
-                        const uint32_t place = atomicAdd(&s_count, 1);
-                        if (place < kCandidates) s_list[place] = x, done = true;
-                    }
-                    if (done) waiting &= ~(1u << e);
-                }
-            if (!__syncthreads_or(waiting != 0)) break;
-            cut_back(j.k);
-        }
+    bool grown = false;
+    auto taken = [&](uint64_t x) {                  // whether x needs no more care
+        if (x <= bound) return true;
+        const uint32_t place = atomicAdd(&s_count, 1);
+        grown |= place >= trigger - 1;
+        if (place >= kCandidates) return false;
+        s_list[place] = x;
+        return true;
     };
 
-    for (uint32_t v0 = 0; v0 < cut.n_vecs; v0 += kTopThreads) {
-        const uint32_t v = v0 + tid;
-        float f[N];
-        uint32_t waiting = 0;
-        if (v < cut.n_vecs) {
-            Packed<T, N> p;
-            p.v[0] = load16(in + cut.lead + v * N);
-            p.unpack(f);
-            waiting = (1u << N) - 1;
-            float most = f[0];
-#pragma unroll
-            for (int e = 1; e < N; ++e) most = fmaxf(most, f[e]);
-            r.raise(most, j.c);
-            const float base = r.base();
-#pragma unroll
-            for (int e = 0; e < N; ++e) r.s += ex2((f[e] - base) * j.c);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) f[e] = 0.0f;
-        }
-        offer(f, cut.lead + v * N, waiting);
-    }
-    {
-        float f[N] = {};
+    // entries off the grid
+    if (rank == 0) {
         const uint32_t at = tid < cut.loose ? cut.loose_at<T>(tid) : 0;
         if (tid < cut.loose) {
-            f[0] = to_float(in[at]);
-            r.raise(f[0], j.c);
-            r.s += ex2((f[0] - r.base()) * j.c);
+            const float x = to_float(in[at]);
+            r.raise(x, j.c);
+            r.s += ex2((x - r.base()) * j.c);
+            taken(composite(x, at));                // fewer than the list has room for
         }
-        offer(f, at, tid < cut.loose);
     }
-    cut_back(j.k);
+
+    uint4 next[kTopVecs];
+#pragma unroll
+    for (int i = 0; i < kTopVecs; ++i) {
+        const uint32_t v = from + i * kTopThreads + tid;
+        next[i] = v < to ? load16(in + cut.lead + v * N) : make_uint4(0, 0, 0, 0);
+    }
+    for (uint32_t v0 = from; v0 < to; v0 += kTopStep) {
+        uint4 p[kTopVecs];
+        float most[kTopVecs];
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kTopVecs; ++i) {
+            p[i] = next[i];
+            const bool here = v0 + i * kTopThreads + tid < to;
+            most[i] = here ? vec_max<T>(p[i]) : -INFINITY;
+            top = fmaxf(top, most[i]);
+            const uint32_t v = v0 + kTopStep + i * kTopThreads + tid;
+            if (v < to) next[i] = load16(in + cut.lead + v * N);
+        }
+        if (v0 == from) {
+            // bit by bit the largest number that k of the largest entries reach; its lower bits do not matter
+            uint32_t key[kTopVecs];
+            const bool fine = j.k > kTopThreads / 2;
+#pragma unroll
+            for (int i = 0; i < kTopVecs; ++i) key[i] = v0 + i * kTopThreads + tid < to ? order_of(most[i]) : 0;
+            if (!fine) {
+                key[0] = max(max(key[0], key[1]), max(key[2], key[3]));
+                key[1] = key[2] = key[3] = 0;
+            }
+            uint32_t reach = 0;
+            for (int b = 0; b < kBoundBits; ++b) {
+                const uint32_t t = reach | 0x80000000u >> b;
+                uint32_t n = __popc(__ballot_sync(~0u, key[0] >= t));
+                if (fine)
+#pragma unroll
+                    for (int i = 1; i < kTopVecs; ++i) n += __popc(__ballot_sync(~0u, key[i] >= t));
+                if (lane == 0 && n) atomicAdd(&s_above[b], n);
+                __syncthreads();
+                if (s_above[b] >= j.k) reach = t;
+            }
+            if (reach) bound = (static_cast<uint64_t>(reach) << 32) - 1, floor = floor_of(bound);
+        }
+        // the sum
+        r.raise(top, j.c);
+        const float base = r.base();
+        if (fabsf(base) < 1e30f) {
+            const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-base * j.c, -base * j.c);
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < kTopVecs; ++i) {
+                if (v0 + i * kTopThreads + tid >= to) continue;
+                Packed<T, N> q;
+                q.v[0] = p[i];
+                float f[N];
+                q.unpack(f);
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
+                    sum = add2(sum, make_float2(ex2(y.x), ex2(y.y)));
+                }
+            }
+            r.s += sum.x + sum.y;
+        } else {                                    // products with c may be too large
+#pragma unroll
+            for (int i = 0; i < kTopVecs; ++i) {
+                if (v0 + i * kTopThreads + tid >= to) continue;
+                Packed<T, N> q;
+                q.v[0] = p[i];
+                float f[N];
+                q.unpack(f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) r.s += ex2((f[e] - base) * j.c);
+            }
+        }
+        // the list
+        uint32_t waiting = 0;
+#pragma unroll
+        for (int i = 0; i < kTopVecs; ++i) {
+            const uint32_t v = v0 + i * kTopThreads + tid;
+            if (v >= to || most[i] <= floor) continue;
+            Packed<T, N> q;
+            q.v[0] = p[i];
+            float f[N];
+            q.unpack(f);
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (!(f[e] <= floor) && !taken(composite(f[e], cut.lead + v * N + e))) waiting |= 1u << (i * N + e);
+        }
+        while (__syncthreads_or(grown || waiting)) {
+            cut_back();
+            grown = false;
+            // what found no room, once more: rows in an unlucky order
+            for (uint32_t left = waiting; left; left &= left - 1) {
+                const uint32_t b = __ffs(left) - 1, at = cut.lead + (v0 + b / N * kTopThreads + tid) * N + b % N;
+                if (taken(composite(to_float(in[at]), at))) waiting &= ~(1u << b);
+            }
+        }
+    }
+    __syncthreads();
+    cut_back();
+
+    r = warp_join(r, j.c);
+    if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
+    __syncthreads();
+    if (tid == 0) {
+        r = {-INFINITY, 0.0f};
+        for (int w = 0; w < kTopThreads / 32; ++w) r.join(s_m[w], s_s[w], j.c);
+        s_run = r;
+    }
+    if (ranks > 1) {
+        cluster.sync();
+        if (rank == 0) {
+            for (uint32_t i0 = 0; i0 < (ranks - 1) * j.k; i0 += kTopThreads) {
+                const uint32_t i = i0 + tid, other = 1 + i / j.k;
+                uint64_t x = 0;
+                if (i < (ranks - 1) * j.k && i % j.k < *cluster.map_shared_rank(&s_count, other)) x = cluster.map_shared_rank(s_list, other)[i % j.k];
+                for (;;) {
+                    if (x && taken(x)) x = 0;
+                    if (!__syncthreads_or(x != 0)) break;
+                    cut_back();
+                }
+            }
+            cut_back();
+            if (tid == 0)
+                for (uint32_t o = 1; o < ranks; ++o) {
+                    const Running other = *cluster.map_shared_rank(&s_run, o);
+                    r.join(other.m, other.s, j.c);
+                }
+        }
+        cluster.sync();                             // nobody leaves while the first block reads here
+        if (rank != 0) return;
+    }
     T* val = reinterpret_cast<T*>(j.val) + static_cast<uint64_t>(row) * j.k;
     int32_t* idx = j.idx + static_cast<uint64_t>(row) * j.k;
     for (uint32_t i = tid; i < j.k; i += kTopThreads) {
@@ -436,15 +625,8 @@ __global__ void __launch_bounds__(kTopThreads) k_top_logits(const TopJob j) {
         idx[i] = static_cast<int32_t>(token);
         val[i] = in[token];
     }
-    if (!j.lse) return;
-    r = warp_join(r, j.c);
-    if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
-    __syncthreads();
-    if (tid == 0) {
-        r = {-INFINITY, 0.0f};
-        for (int w = 0; w < kTopThreads / 32; ++w) r.join(s_m[w], s_s[w], j.c);
+    if (j.lse && tid == 0)
         j.lse[row] = static_cast<float>(r.s != r.s ? static_cast<double>(r.s) : r.m == -INFINITY ? -INFINITY : r.m * j.inv_t + log(static_cast<double>(r.s)));
-    }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -492,8 +674,25 @@ int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
     return launch_distill<__half, MODE>(j, stream);
 }
 
-template <typename T> int launch_top(const TopJob& j, uint32_t n_rows, cudaStream_t stream) {
-    k_top_logits<T><<<n_rows, kTopThreads, 0, stream>>>(j);
+template <typename T> int launch_top(const TopJob& j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
+    // several blocks a row as long as all of them are on the SMs at once and each has some steps to do
+    uint32_t ranks = 1;
+    while (ranks < kTopCluster && static_cast<uint64_t>(n_rows) * ranks * 2 <= 4ull * n_sms &&
+           j.vocab * sizeof(T) / 16 >= static_cast<uint64_t>(ranks) * 2 * kTopStep)
+        ranks *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n_rows * ranks);
+    cfg.blockDim = dim3(kTopThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ranks;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ranks > 1 ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_top_logits<T>, j);
+    if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
@@ -554,9 +753,9 @@ int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint3
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (j.logits.type == ADACOMP_F32) return launch_top<float>(j, n_rows, stream);
-    if (j.logits.type == ADACOMP_BF16) return launch_top<__nv_bfloat16>(j, n_rows, stream);
-    return launch_top<__half>(j, n_rows, stream);
+    if (j.logits.type == ADACOMP_F32) return launch_top<float>(j, n_rows, h->n_sms, stream);
+    if (j.logits.type == ADACOMP_BF16) return launch_top<__nv_bfloat16>(j, n_rows, h->n_sms, stream);
+    return launch_top<__half>(j, n_rows, h->n_sms, stream);
 }
 
 int adacomp_distill_loss(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs,
