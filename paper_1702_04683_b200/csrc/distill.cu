@@ -30,7 +30,7 @@ constexpr uint32_t kMaxPairs = 1024;
 constexpr uint32_t kMaxVocab = 1u << 20;
 constexpr uint32_t kStats = 8;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
-constexpr double kLog2e = 1.4426950408889634;
+constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -103,12 +103,28 @@ struct Cut {
     template <typename T> __device__ __forceinline__ uint32_t loose_at(uint32_t i) const { return i < lead ? i : i + n_vecs * kVec<T>; }
 };
 
-// A running softmax sum: m the largest so far, s = sum exp((x - m) c) with c = log2(e) / T in base 2.
+// Exponentials are 2^(x c - R), c = log2(e) / T, relative to a largest entry `most`: R is most * c ROUNDED to fp32, so the rounding of
+// the argument is one of its own size (a fused product) and R's drops out wherever two such numbers are divided.  Only where products
+// with c might leave fp32's range (a row of the type's lowest values, say) the difference is taken first.
+constexpr float kWild = 1e30f;
+__device__ __forceinline__ float exp_from(float x, float most, float c) {
+    return ex2(fabsf(most) < kWild ? __fmaf_rn(x, c, -(most * c)) : (x - most) * c);
+}
+// log2 of 2^(-R) e^(most / T), which makes up for it: R, as a double.
+__device__ __forceinline__ double reference(float most, float c) {
+    return fabsf(most) < kWild ? static_cast<double>(most * c) : static_cast<double>(most) * c;
+}
+
+// A running softmax sum: m the largest entry so far, s the sum of exponentials relative to it.
 struct Running {
     float m, s;
+    // What a sum relative to `from` has to be multiplied by to be relative to `to`, a larger number.
+    __device__ __forceinline__ static float lowered(float from, float to, float c) {
+        return ex2(fabsf(to) < kWild && fabsf(from) < kWild ? from * c - to * c : (from - to) * c);
+    }
     __device__ __forceinline__ void raise(float to, float c) {
         if (to > m) {
-            s *= ex2((m - to) * c);
+            s *= lowered(m, to, c);
             m = to;
         }
     }
@@ -116,17 +132,11 @@ struct Running {
     __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }
     __device__ __forceinline__ void join(float m2, float s2, float c) {
         const float most = fmaxf(m, m2);
-        const float a = m == most ? s : s * ex2((m - most) * c), b = m2 == most ? s2 : s2 * ex2((m2 - most) * c);
+        const float a = m == most ? s : s * lowered(m, most, c), b = m2 == most ? s2 : s2 * lowered(m2, most, c);
         m = most;
         s = a + b;
     }
 };
-
-__device__ __forceinline__ Running warp_join(Running r, float c) {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) r.join(__shfl_xor_sync(~0u, r.m, d), __shfl_xor_sync(~0u, r.s, d), c);
-    return r;
-}
 
 template <typename V> __device__ __forceinline__ V warp_sum(V x) {
 #pragma unroll
@@ -138,6 +148,11 @@ __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
     return x;
+}
+
+__device__ __forceinline__ Running warp_join(Running r, float c) {
+    const float m = warp_max(r.m);
+    return {m, warp_sum(r.m == m ? r.s : r.s * Running::lowered(r.m, m, c))};
 }
 
 struct Job {
@@ -222,7 +237,7 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
                     listed_max = fmaxf(listed_max, x);
                 } else {
                     r.raise(x, j.c);
-                    r.s += ex2((x - r.base()) * j.c);
+                    r.s += exp_from(x, r.base(), j.c);
                 }
             }
             for (uint32_t v = tid; v < cut.n_vecs; v += kThreads) {
@@ -239,7 +254,7 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
                 const float base = r.base();
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    const float y = ex2((f[e] - base) * j.c);
+                    const float y = exp_from(f[e], base, j.c);
                     r.s += bits >> e & 1 ? 0.0f : y;
                 }
             }
@@ -262,13 +277,13 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
             for (uint32_t i = tid; i < j.k; i += kThreads) {
                 if (s_idx[i] == kNone) continue;
                 const float s = to_float(in[s_idx[i]]);
-                listed += ex2((s - base) * j.c);
+                listed += exp_from(s, base, j.c);
                 const double t = j.lse ? s_val[i] * j.inv_t - lse : (static_cast<double>(s_val[i]) - t_base) * j.inv_t;
                 // with the teacher's normaliser 1 - sum q is left over: small where the list says almost everything, so in 64 bits
                 double q = j.lse ? exp(t) : expf(static_cast<float>(t));
                 if (q > 1e300) q = NAN;
                 q_sum += q;
-                if (q != 0.0) cross += q * (t - (static_cast<double>(s) - base) * j.inv_t);
+                if (q != 0.0) cross += q * (t - (static_cast<double>(s) * j.c - reference(base, j.c)) * kLn2);
             }
             q_sum = warp_sum(q_sum), cross = warp_sum(cross), listed = warp_sum(listed);
             if (lane == 0) s_d[0][warp] = q_sum, s_d[1][warp] = cross, s_d[2][warp] = listed;
@@ -333,7 +348,7 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
         if (token[r] == kNone) continue;
         const double t = j.lse ? s_val[i] * j.inv_t - share.t_base : (static_cast<double>(s_val[i]) - share.t_base) * j.inv_t;
         const float q = expf(static_cast<float>(t)) * share.q_scale;
-        listed[r] = (ex2((to_float(in[token[r]]) - share.m) * j.c) * share.listed - q) * g;
+        listed[r] = (exp_from(to_float(in[token[r]]), share.m, j.c) * share.listed - q) * g;
     }
     __syncthreads();                                // before the gradient may take the place of a logit that is read here
     for (uint32_t v = tid; v < cut.n_vecs; v += kThreads) {
@@ -343,13 +358,13 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
         float f[N];
         p.unpack(f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = ex2((f[e] - share.m) * j.c) * rest;
+        for (int e = 0; e < N; ++e) f[e] = exp_from(f[e], share.m, j.c) * rest;
         p.pack(f);
         *reinterpret_cast<uint4*>(out + cut.lead + v * N) = p.v[0];
     }
     if (tid < cut.loose) {
         const uint32_t at = cut.loose_at<T>(tid);
-        out[at] = from_float<T>(ex2((to_float(in[at]) - share.m) * j.c) * rest);
+        out[at] = from_float<T>(exp_from(to_float(in[at]), share.m, j.c) * rest);
     }
     __syncthreads();                                // the listed ones replace what has just been written
 #pragma unroll
@@ -359,21 +374,35 @@ __global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
 
 // ---------------------------------------------------------------------------------------------- top logits
 
-constexpr int kTopThreads = 256;
-constexpr int kTopVecs = 4;                         // vectors of a thread in one step
+constexpr int kTopThreads = 128;
+constexpr int kTopVecs = 2;                         // vectors of a thread in one step: a group
 constexpr uint32_t kTopStep = kTopThreads * kTopVecs;
-constexpr uint32_t kCandidates = 2048;
-constexpr int kBoundBits = 16;
-constexpr uint32_t kTopCluster = 8;
+constexpr int kBoundBits = 12;
+constexpr uint32_t kTopClusterBits = 3;             // blocks of the largest cluster
+constexpr uint32_t kTopGroups = 32768;              // of a block
+constexpr uint32_t kHits = 512;
+
+// Shared memory of a block, no larger than it has to be: what it takes is taken from the L1 cache, which holds the loads under way
+// (with 26 KB a block instead of 9, 8192 x 50000 bf16 took 232 us instead of 206).
+struct TopShared {
+    uint32_t candidates, keys, groups, bytes;
+    TopShared(uint32_t k, uint32_t steps) {
+        candidates = 256;
+        while (candidates < 2 * k) candidates *= 2;
+        keys = candidates * sizeof(uint64_t);                        // and later the hits
+        groups = keys + kHits * sizeof(uint16_t);
+        bytes = groups + steps * kTopThreads * sizeof(uint16_t);
+    }
+};
 
 struct TopJob {
     Rows logits;
     int32_t* idx;
     void* val;
     float* lse;
-    uint32_t vocab, k;
+    uint32_t vocab, k, rank_bits;
+    uint32_t candidates, at_keys, at_groups;        // room of the list, places in shared memory
     float c;
-    double inv_t;
 };
 
 // Order of logits as whole numbers: NaN above all, +0 and -0 equal; below it the token, the lowest first.
@@ -384,16 +413,31 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ uint64_t composite(float x, uint32_t token) {
     return static_cast<uint64_t>(order_of(x)) << 32 | (0xFFFFFFFFu - token);
 }
-// A float that every entry above `bound` in order exceeds, other than by its token (NaN, which nothing fails to exceed, where there is none).
+// Entry e of a vector.
+template <typename T> __device__ __forceinline__ float pick(const uint4& v, uint32_t e) {
+    const uint32_t w = sizeof(T) == 4 ? e : e / 2;
+    const uint32_t a = w & 1 ? v.y : v.x, b = w & 1 ? v.w : v.z, word = w & 2 ? b : a;
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(word);
+    } else {
+        const float2 h = halves<T>(word);
+        return e & 1 ? h.y : h.x;
+    }
+}
+
+// A float that every entry above `bound` exceeds, and entries equal to it but for the token with them (NaN, which nothing
+// fails to exceed, where there is none).
 __device__ __forceinline__ float floor_of(uint64_t bound) {
-    const uint32_t u = static_cast<uint32_t>(bound >> 32), bits = u >> 31 ? u ^ 0x80000000u : ~u;
+    const uint32_t u = static_cast<uint32_t>(bound >> 32);
+    if (u == 0) return NAN;
+    const uint32_t below = u - 1, bits = below >> 31 ? below ^ 0x80000000u : ~below;
     return __uint_as_float(bits == 0x80000000u ? 0x80000001u : bits);      // +0 does not exceed -0
 }
 
 // Sorts s_list[0 .. n) in falling order, n a power of two.  Up to one entry a thread, distances within a warp are exchanged by
 // shuffles (256 entries: 12 barriers instead of 36).
-__device__ void sort_list(uint64_t* s_list, uint32_t n) {
-    if (n <= kTopThreads) {
+template <uint32_t THREADS> __device__ void sort_list(uint64_t* s_list, uint32_t n) {
+    if (n <= THREADS) {
         const uint32_t i = threadIdx.x;
         __syncthreads();
         uint64_t x = i < n ? s_list[i] : 0;
@@ -416,7 +460,7 @@ __device__ void sort_list(uint64_t* s_list, uint32_t n) {
         for (uint32_t k = 2; k <= n; k *= 2)
             for (uint32_t d = k / 2; d; d /= 2) {
                 __syncthreads();
-                for (uint32_t i = threadIdx.x; i < n / 2; i += kTopThreads) {
+                for (uint32_t i = threadIdx.x; i < n / 2; i += THREADS) {
                     const uint32_t a = 2 * i - (i & (d - 1)), b = a + d;
                     const uint64_t x = s_list[a], y = s_list[b];
                     if ((x < y) == ((a & k) == 0)) s_list[a] = y, s_list[b] = x;
@@ -426,207 +470,313 @@ __device__ void sort_list(uint64_t* s_list, uint32_t n) {
     __syncthreads();
 }
 
-// The entries above the k-th largest of those seen so far are collected in a list, which is cut back to its k largest when it
-// has grown to twice that (or is full).  The first step's bound: with k of the threads' (or vectors') largest entries at or above a
-// number, k entries are.  From there on about k ln(vocab / entries of a step) entries make it to the list, so most vectors cost a
-// maximum, their exponentials and one comparison.
+// Adds a vector's exponentials relative to `most` (shift = -most * c).
+template <typename T> __device__ __forceinline__ float2 vec_exps(const uint4& v, float2 sum, float c, float shift) {
+    constexpr int N = kVec<T>;
+    Packed<T, N> q;
+    q.v[0] = v;
+    float f[N];
+    q.unpack(f);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        const float2 y = fma2(make_float2(f[e], f[e + 1]), make_float2(c, c), make_float2(shift, shift));
+        sum = add2(sum, make_float2(ex2(y.x), ex2(y.y)));
+    }
+    return sum;
+}
+
+// One pass over the row computes the sum and, for every thread's share of every step (a group: kTopVecs vectors), the largest entry, which
+// stays in shared memory.  With k of the threads' largest entries at or above a number, k entries of the row are: this bound
+// leaves some k + k / 5 candidates, whose groups alone are read again (from L2) and whose places in the order are counted.
+// A list that is full (rows in which many groups hold large entries) is cut back to its k largest, which raises the bound.
 //
 // A row is one block's work, or a cluster's where there are few rows: the first block then takes the others' lists through
 // their shared memory.
 template <typename T>
-__global__ void __launch_bounds__(kTopThreads, 4) k_top_logits(const TopJob j) {
-    constexpr int N = kVec<T>;
-    __shared__ uint64_t s_list[kCandidates];
-    __shared__ uint32_t s_count, s_above[kBoundBits];
-    __shared__ float s_m[kTopThreads / 32], s_s[kTopThreads / 32];
+__global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) {
+    constexpr int N = kVec<T>, kWarps = kTopThreads / 32;
+    static_assert(kHits * sizeof(uint16_t) >= kTopThreads * sizeof(uint32_t) && kTopGroups <= 65536, "rooms");
+    extern __shared__ uint64_t s_list[];            // [candidates]
+    uint32_t* const s_key = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_list) + j.at_keys);
+    uint16_t* const s_hit = reinterpret_cast<uint16_t*>(s_key);             // [kHits], when the keys are done with
+    uint16_t* const s_group = reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(s_list) + j.at_groups);      // [steps][kTopThreads]
+    __shared__ uint32_t s_count, s_hits, s_reach, s_above[16];
+    __shared__ float s_m[kWarps], s_s[kWarps];
     __shared__ Running s_run;
-    namespace cg = cooperative_groups;
-    const cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t ranks = cluster.num_blocks(), rank = cluster.block_rank();
-    const uint32_t row = blockIdx.x / ranks, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    const uint32_t rank = blockIdx.x & ((1u << j.rank_bits) - 1);
+    const uint32_t row = blockIdx.x >> j.rank_bits, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const T* in = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
     const Cut cut = Cut::of(in, j.vocab);
-    const uint32_t per = (cut.n_vecs + ranks - 1) / ranks, from = min(rank * per, cut.n_vecs), to = min(from + per, cut.n_vecs);
-    const uint32_t trigger = min(2 * j.k + 64, kCandidates);
-    uint64_t bound = 0;                             // an entry must be above it
-    float floor = NAN;
+    const uint32_t per = (cut.n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits, from = min(rank * per, cut.n_vecs), n_here = min(from + per, cut.n_vecs) - from;
+    const uint32_t steps = (n_here + kTopStep - 1) / kTopStep;
+    const T* vecs = in + cut.lead + from * N;
     Running r = {-INFINITY, 0.0f};
-    if (tid == 0) s_count = 0;
-    if (tid < kBoundBits) s_above[tid] = 0;
+    if (tid == 0) s_count = 0, s_hits = 0;
+    if (tid < 16) s_above[tid] = 0;
+
+    // the pass over the row
+    float largest = -INFINITY;
+    auto step = [&](const uint4 (&p)[kTopVecs], uint32_t s, uint32_t have) {       // `have` of the thread's vectors are there
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kTopVecs; ++i)
+            if (i < have) top = max_nan(top, vec_max<T>(p[i]));
+        largest = max_nan(largest, top);
+        s_group[s * kTopThreads + tid] = static_cast<uint16_t>(order_of(top) >> 16);
+        r.raise(top, j.c);
+        const float base = r.base();
+        if (fabsf(base) < kWild) {
+            const float shift = -base * j.c;
+            float2 sum = make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < kTopVecs; ++i)
+                if (i < have) sum = vec_exps<T>(p[i], sum, j.c, shift);
+            r.s += sum.x + sum.y;
+        } else {                                    // products with c may be too large for fp32
+            for (uint32_t i = 0; i < have; ++i)
+                for (int e = 0; e < N; ++e) r.s += exp_from(to_float(vecs[(s * kTopStep + i * kTopThreads + tid) * N + e]), base, j.c);
+        }
+    };
+    {
+        // two buffers in turn: one step's vectors are on their way while the other's are worked on
+        const uint32_t whole = n_here / kTopStep, rest = n_here % kTopStep;
+        const uint32_t have = rest > tid ? (rest - tid + kTopThreads - 1) / kTopThreads : 0;
+        const char* at = reinterpret_cast<const char*>(vecs) + tid * 16;
+        uint4 a[kTopVecs], b[kTopVecs];
+        auto fetch = [&](uint4 (&p)[kTopVecs], uint32_t s) {
+            if (s < whole) {
+#pragma unroll
+                for (int i = 0; i < kTopVecs; ++i) p[i] = load16(at + i * kTopThreads * 16);
+            } else if (s == whole) {
+#pragma unroll
+                for (int i = 0; i < kTopVecs; ++i)
+                    if (i < have) p[i] = load16(at + i * kTopThreads * 16);
+            }
+            at += kTopStep * 16;
+        };
+        fetch(a, 0);
+        uint32_t s = 0;
+        for (; s + 1 < whole; s += 2) {
+            fetch(b, s + 1);
+            step(a, s, kTopVecs);
+            fetch(a, s + 2);
+            step(b, s + 1, kTopVecs);
+        }
+        if (s < whole) {
+            fetch(b, s + 1);
+            step(a, s, kTopVecs);
+            if (have) step(b, s + 1, have);
+        } else if (have) {
+            step(a, s, have);
+        }
+    }
+
+    // The bound: bit by bit the largest number that k of the largest entries reach, or until not many more than k do.  Up to half
+    // as many as threads, the threads' largest entries tell them apart well enough, above it the groups' do.
+    const uint32_t own = tid < n_here ? (n_here - tid + kTopStep - 1) / kTopStep : 0;      // groups of this thread
+    const uint32_t enough = j.k + j.k / 16;
+    const bool coarse = j.k <= kTopThreads / 2;
+    s_key[tid] = own ? order_of(largest) : 0;
+    r = warp_join(r, j.c);
+    if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
     __syncthreads();
+    uint32_t key[kWarps], low = ~0u, high = 0;
+    if (warp == 0 || !coarse) {
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) key[i] = s_key[i * 32 + lane], low = min(low, key[i]), high = max(high, key[i]);
+        low = __reduce_min_sync(~0u, low), high = __reduce_max_sync(~0u, high);
+        if (j.k > kTopThreads) low = 0;             // so many groups need not reach every thread's largest entry
+    }
+    if (!coarse) {
+        low >>= 16, high >>= 16;
+        const uint32_t same = __clz(low ^ high);
+        uint32_t reach = same == 32 ? high : high & ~(0xFFFFFFFFu >> same);
+        uint32_t bit = same == 32 ? 0 : 0x80000000u >> same;
+        if (min(n_here, steps * kTopThreads) < j.k) reach = bit = 0;
+        for (; bit; bit >>= 1) {
+            uint32_t n = 0, *above = &s_above[__ffs(bit) - 1];
+            for (uint32_t s = 0; s < own; ++s) n += s_group[s * kTopThreads + tid] >= (reach | bit);
+            n = __reduce_add_sync(~0u, n);
+            if (lane == 0 && n) atomicAdd(above, n);
+            __syncthreads();
+            n = *above;
+            if (n >= j.k) reach |= bit;
+            if (n >= j.k && n <= enough) break;
+        }
+        if (tid == 0) s_reach = reach << 16;
+    }
+    if (warp == 0) {
+        if (coarse) {
+            const uint32_t same = __clz(low ^ high);        // 32 where all are equal
+            uint32_t reach = same == 32 ? high : high & ~(0xFFFFFFFFu >> same);
+            uint32_t bit = same == 32 ? 0 : 0x80000000u >> same;
+            for (int b = 0; b < kBoundBits && bit; ++b, bit >>= 1) {
+                uint32_t n = 0;
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) n += __popc(__ballot_sync(~0u, key[i] >= (reach | bit)));
+                if (n >= j.k) reach |= bit;
+                if (n >= j.k && n <= enough) break;
+            }
+            if (lane == 0) s_reach = reach;
+        }
+    } else if (warp == 1) {
+        r = lane < kWarps ? Running{s_m[lane], s_s[lane]} : Running{-INFINITY, 0.0f};
+        r = warp_join(r, j.c);
+        if (lane == 0) s_run = r;
+    }
+    __syncthreads();
+    uint64_t bound = s_reach ? (static_cast<uint64_t>(s_reach) << 32) - 1 : 0;      // an entry must be above it
+    float floor = floor_of(bound);
 
     auto cut_back = [&]() {                         // the list sorted, and its k largest kept
-        const uint32_t n = min(s_count, kCandidates);
+        const uint32_t n = min(s_count, j.candidates);
         uint32_t size = 2;
         while (size < n) size *= 2;
         for (uint32_t i = n + tid; i < size; i += kTopThreads) s_list[i] = 0;
-        sort_list(s_list, size);
+        sort_list<kTopThreads>(s_list, size);
         if (tid == 0) s_count = min(n, j.k);
         if (n >= j.k) bound = s_list[j.k - 1], floor = floor_of(bound);
         __syncthreads();
     };
-    bool grown = false;
     auto taken = [&](uint64_t x) {                  // whether x needs no more care
         if (x <= bound) return true;
         const uint32_t place = atomicAdd(&s_count, 1);
-        grown |= place >= trigger - 1;
-        if (place >= kCandidates) return false;
-        s_list[place] = x;
-        return true;
+        if (place < j.candidates) s_list[place] = x;
+        return place < j.candidates;
     };
 
-    // entries off the grid
-    if (rank == 0) {
-        const uint32_t at = tid < cut.loose ? cut.loose_at<T>(tid) : 0;
-        if (tid < cut.loose) {
-            const float x = to_float(in[at]);
-            r.raise(x, j.c);
-            r.s += ex2((x - r.base()) * j.c);
-            taken(composite(x, at));                // fewer than the list has room for
+    // The groups that reach the bound, and of those the entries.  The list mostly has room for them; where it has not, all
+    // of it is done once more, as many groups at a time as there is room for and cutting the list back in between.
+    for (bool careful = false;; careful = true) {
+        bool room = true;
+        if (rank == 0 && tid < cut.loose) {         // the entries off the grid
+            const uint32_t at = cut.loose_at<T>(tid);
+            taken(composite(to_float(in[at]), at));
         }
-    }
-
-    uint4 next[kTopVecs];
+        uint32_t s = 0;
+        for (bool more = true; more;) {
+            // some of the thread's groups, one bit each; places in the list for a warp's at once
+            uint32_t mine = 0;
+            const uint32_t window = careful ? kHits / kTopThreads : 32, until = min(own, s + window), least = (bound + 1) >> 48;
+            for (uint32_t i = s; i < until; ++i) mine |= static_cast<uint32_t>(s_group[i * kTopThreads + tid] >= least) << (i - s);
+            const uint32_t count = __popc(mine);
+            uint32_t place = count;
 #pragma unroll
-    for (int i = 0; i < kTopVecs; ++i) {
-        const uint32_t v = from + i * kTopThreads + tid;
-        next[i] = v < to ? load16(in + cut.lead + v * N) : make_uint4(0, 0, 0, 0);
-    }
-    for (uint32_t v0 = from; v0 < to; v0 += kTopStep) {
-        uint4 p[kTopVecs];
-        float most[kTopVecs];
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kTopVecs; ++i) {
-            p[i] = next[i];
-            const bool here = v0 + i * kTopThreads + tid < to;
-            most[i] = here ? vec_max<T>(p[i]) : -INFINITY;
-            top = fmaxf(top, most[i]);
-            const uint32_t v = v0 + kTopStep + i * kTopThreads + tid;
-            if (v < to) next[i] = load16(in + cut.lead + v * N);
-        }
-        if (v0 == from) {
-            // bit by bit the largest number that k of the largest entries reach; its lower bits do not matter
-            uint32_t key[kTopVecs];
-            const bool fine = j.k > kTopThreads / 2;
-#pragma unroll
-            for (int i = 0; i < kTopVecs; ++i) key[i] = v0 + i * kTopThreads + tid < to ? order_of(most[i]) : 0;
-            if (!fine) {
-                key[0] = max(max(key[0], key[1]), max(key[2], key[3]));
-                key[1] = key[2] = key[3] = 0;
+            for (int d = 1; d < 32; d *= 2) {
+                const uint32_t left = __shfl_up_sync(~0u, place, d);
+                if (lane >= d) place += left;
             }
-            uint32_t reach = 0;
-            for (int b = 0; b < kBoundBits; ++b) {
-                const uint32_t t = reach | 0x80000000u >> b;
-                uint32_t n = __popc(__ballot_sync(~0u, key[0] >= t));
-                if (fine)
-#pragma unroll
-                    for (int i = 1; i < kTopVecs; ++i) n += __popc(__ballot_sync(~0u, key[i] >= t));
-                if (lane == 0 && n) atomicAdd(&s_above[b], n);
-                __syncthreads();
-                if (s_above[b] >= j.k) reach = t;
+            uint32_t begin = 0;
+            if (lane == 31 && place) begin = atomicAdd(&s_hits, place);
+            place += __shfl_sync(~0u, begin, 31) - count;
+            for (; mine; mine &= mine - 1, ++place) {
+                if (place < kHits) s_hit[place] = static_cast<uint16_t>((s + __ffs(mine) - 1) * kTopThreads + tid);
+                else room = false;
             }
-            if (reach) bound = (static_cast<uint64_t>(reach) << 32) - 1, floor = floor_of(bound);
-        }
-        // the sum
-        r.raise(top, j.c);
-        const float base = r.base();
-        if (fabsf(base) < 1e30f) {
-            const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-base * j.c, -base * j.c);
-            float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < kTopVecs; ++i) {
-                if (v0 + i * kTopThreads + tid >= to) continue;
+            s += window;
+            more = s < steps;
+            __syncthreads();
+            const uint32_t items = min(s_hits, kHits) * kTopVecs;
+            for (uint32_t h0 = careful ? 0 : warp * 32; h0 < items; h0 += kTopThreads) {
+                const uint32_t h = careful ? h0 + tid : h0 + lane, group = h < items ? s_hit[h / kTopVecs] : 0;
+                const uint32_t v = group / kTopThreads * kTopStep + h % kTopVecs * kTopThreads + group % kTopThreads;
+                uint32_t waiting = 0;
                 Packed<T, N> q;
-                q.v[0] = p[i];
-                float f[N];
-                q.unpack(f);
+                if (h < items && v < n_here) {
+                    float f[N];
+                    q.v[0] = load16(vecs + v * N);
+                    q.unpack(f);
 #pragma unroll
-                for (int e = 0; e < N; e += 2) {
-                    const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
-                    sum = add2(sum, make_float2(ex2(y.x), ex2(y.y)));
+                    for (int e = 0; e < N; ++e)
+                        if (!(f[e] <= floor)) waiting |= 1u << e;
                 }
-            }
-            r.s += sum.x + sum.y;
-        } else {                                    // products with c may be too large
-#pragma unroll
-            for (int i = 0; i < kTopVecs; ++i) {
-                if (v0 + i * kTopThreads + tid >= to) continue;
-                Packed<T, N> q;
-                q.v[0] = p[i];
-                float f[N];
-                q.unpack(f);
-#pragma unroll
-                for (int e = 0; e < N; ++e) r.s += ex2((f[e] - base) * j.c);
-            }
-        }
-        // the list
-        uint32_t waiting = 0;
-#pragma unroll
-        for (int i = 0; i < kTopVecs; ++i) {
-            const uint32_t v = v0 + i * kTopThreads + tid;
-            if (v >= to || most[i] <= floor) continue;
-            Packed<T, N> q;
-            q.v[0] = p[i];
-            float f[N];
-            q.unpack(f);
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (!(f[e] <= floor) && !taken(composite(f[e], cut.lead + v * N + e))) waiting |= 1u << (i * N + e);
-        }
-        while (__syncthreads_or(grown || waiting)) {
-            cut_back();
-            grown = false;
-            // what found no room, once more: rows in an unlucky order
-            for (uint32_t left = waiting; left; left &= left - 1) {
-                const uint32_t b = __ffs(left) - 1, at = cut.lead + (v0 + b / N * kTopThreads + tid) * N + b % N;
-                if (taken(composite(to_float(in[at]), at))) waiting &= ~(1u << b);
-            }
-        }
-    }
-    __syncthreads();
-    cut_back();
-
-    r = warp_join(r, j.c);
-    if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
-    __syncthreads();
-    if (tid == 0) {
-        r = {-INFINITY, 0.0f};
-        for (int w = 0; w < kTopThreads / 32; ++w) r.join(s_m[w], s_s[w], j.c);
-        s_run = r;
-    }
-    if (ranks > 1) {
-        cluster.sync();
-        if (rank == 0) {
-            for (uint32_t i0 = 0; i0 < (ranks - 1) * j.k; i0 += kTopThreads) {
-                const uint32_t i = i0 + tid, other = 1 + i / j.k;
-                uint64_t x = 0;
-                if (i < (ranks - 1) * j.k && i % j.k < *cluster.map_shared_rank(&s_count, other)) x = cluster.map_shared_rank(s_list, other)[i % j.k];
                 for (;;) {
-                    if (x && taken(x)) x = 0;
-                    if (!__syncthreads_or(x != 0)) break;
+                    const uint32_t first = cut.lead + (from + v) * N;
+                    for (uint32_t left = waiting; left; left &= left - 1) {
+                        const uint32_t e = __ffs(left) - 1;
+                        if (taken(composite(pick<T>(q.v[0], e), first + e))) waiting &= ~(1u << e);
+                    }
+                    if (!careful || !__syncthreads_or(waiting != 0)) break;
                     cut_back();
                 }
+                room &= waiting == 0;
             }
-            cut_back();
-            if (tid == 0)
-                for (uint32_t o = 1; o < ranks; ++o) {
-                    const Running other = *cluster.map_shared_rank(&s_run, o);
-                    r.join(other.m, other.s, j.c);
+            room = !__syncthreads_or(!room);
+            if (tid == 0) s_hits = 0;
+            if (!room) break;
+            if (more) __syncthreads();
+        }
+        if (room) break;
+        __syncthreads();
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+    }
+
+    if (j.rank_bits) {
+        const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+        cluster.sync();
+        if (rank == 0) {
+            for (uint32_t o = 1; o < 1u << j.rank_bits; ++o) {
+                const uint32_t n = min(*cluster.map_shared_rank(&s_count, o), j.candidates);
+                const uint64_t* list = cluster.map_shared_rank(s_list, o);
+                for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads) {
+                    uint64_t x = i0 + tid < n ? list[i0 + tid] : 0;
+                    for (;;) {
+                        if (x && taken(x)) x = 0;
+                        if (!__syncthreads_or(x != 0)) break;
+                        cut_back();
+                    }
                 }
+                if (tid == 0) {
+                    const Running other = *cluster.map_shared_rank(&s_run, o);
+                    s_run.join(other.m, other.s, j.c);
+                }
+            }
         }
         cluster.sync();                             // nobody leaves while the first block reads here
         if (rank != 0) return;
     }
+    // the order: places are counted where there is a thread for every candidate
     T* val = reinterpret_cast<T*>(j.val) + static_cast<uint64_t>(row) * j.k;
     int32_t* idx = j.idx + static_cast<uint64_t>(row) * j.k;
-    for (uint32_t i = tid; i < j.k; i += kTopThreads) {
-        const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(s_list[i]);
-        idx[i] = static_cast<int32_t>(token);
-        val[i] = in[token];
+    const uint32_t n = s_count;
+    if (n <= kTopThreads) {
+        if (tid == 0 && n % 2) s_list[n] = 0;
+        __syncthreads();
+        const uint64_t x = tid < n ? s_list[tid] : ~0ull;
+        uint32_t place = 0;
+        if (warp * 32 < n)
+            for (uint32_t i = 0; i < n; i += 2) {
+                const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&s_list[i]);
+                place += (y.x > x) + (y.y > x);
+            }
+        if (tid < n && place < j.k) {
+            const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(x), u = static_cast<uint32_t>(x >> 32);
+            const float f = __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u);
+            idx[place] = static_cast<int32_t>(token);
+            val[place] = f == 0.0f || f != f ? in[token] : from_float<T>(f);       // a zero's sign and a NaN's bits are not in the key
+        }
+    } else {
+        cut_back();
+        for (uint32_t i = tid; i < j.k; i += kTopThreads) {
+            const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(s_list[i]);
+            idx[i] = static_cast<int32_t>(token);
+            val[i] = in[token];
+        }
     }
-    if (j.lse && tid == 0)
-        j.lse[row] = static_cast<float>(r.s != r.s ? static_cast<double>(r.s) : r.m == -INFINITY ? -INFINITY : r.m * j.inv_t + log(static_cast<double>(r.s)));
+    if (warp == kWarps - 1 && j.lse) {
+        // the entries off the grid are in nobody's sum so far
+        r = {-INFINITY, 0.0f};
+        if (lane < cut.loose) {
+            const float x = to_float(in[cut.loose_at<T>(lane)]);
+            r.raise(x, j.c);
+            r.s = exp_from(x, r.base(), j.c);
+        }
+        r = warp_join(r, j.c);
+        r.join(s_run.m, s_run.s, j.c);
+        if (lane == 0)
+            j.lse[row] = static_cast<float>(r.s != r.s ? static_cast<double>(r.s) : r.m == -INFINITY ? -INFINITY : reference(r.m, j.c) * kLn2 + log(static_cast<double>(r.s)));
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -674,15 +824,25 @@ int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
     return launch_distill<__half, MODE>(j, stream);
 }
 
-template <typename T> int launch_top(const TopJob& j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
-    // several blocks a row as long as all of them are on the SMs at once and each has some steps to do
-    uint32_t ranks = 1;
-    while (ranks < kTopCluster && static_cast<uint64_t>(n_rows) * ranks * 2 <= 4ull * n_sms &&
-           j.vocab * sizeof(T) / 16 >= static_cast<uint64_t>(ranks) * 2 * kTopStep)
-        ranks *= 2;
+template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
+    // several blocks a row as long as all of them are on the SMs at once and each has some steps to do, or where one could
+    // not hold the groups of a row
+    const uint32_t n_vecs = j.vocab / kVec<T> + 1;
+    while (j.rank_bits < kTopClusterBits &&
+           ((n_vecs >> j.rank_bits) / kTopVecs > kTopGroups - kTopThreads ||
+            ((static_cast<uint64_t>(n_rows) << j.rank_bits) * 2 <= 4ull * n_sms && n_vecs >> j.rank_bits >= 2 * kTopStep)))
+        ++j.rank_bits;
+    const uint32_t ranks = 1u << j.rank_bits, steps = ((n_vecs + ranks - 1) / ranks + kTopStep - 1) / kTopStep;
+    const TopShared shared(j.k, steps);
+    j.candidates = shared.candidates;
+    j.at_keys = shared.keys;
+    j.at_groups = shared.groups;
+    ADACOMP_CUDA(cudaFuncSetAttribute(k_top_logits<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(TopShared(kMaxPairs, kTopGroups / kTopThreads).bytes)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_rows * ranks);
     cfg.blockDim = dim3(kTopThreads);
+    cfg.dynamicSmemBytes = shared.bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -749,7 +909,6 @@ int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint3
     j.vocab = h->vocab;
     j.k = k;
     j.c = static_cast<float>(kLog2e / temperature);
-    j.inv_t = 1.0 / temperature;
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
