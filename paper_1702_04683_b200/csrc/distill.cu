@@ -25,10 +25,14 @@ struct adacomp_distill {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMaxPairs = 1024;
 constexpr uint32_t kMaxVocab = 1u << 20;
 constexpr uint32_t kStats = 8;
+constexpr uint32_t kClusterBits = 3;               // blocks of the largest cluster
+constexpr uint32_t kChunk = 72 * 1024;              // of a row in a block's shared memory: three blocks on an SM
+constexpr uint32_t kLargestChunk = 192 * 1024;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
@@ -162,7 +166,8 @@ struct Job {
     float* loss;
     float* stats;
     int* status;
-    uint32_t n_rows, vocab, k;
+    uint32_t n_rows, vocab, k, rank_bits;
+    uint32_t at_table, table_bits;  // place in shared memory, size
     float c;                        // log2(e) / T
     double inv_t;
 };
@@ -179,197 +184,405 @@ struct Shares {
     float m, rest, listed, t_base, q_scale, live;
 };
 
+// Entry e of a vector.
+template <typename T> __device__ __forceinline__ float pick(const uint4& v, uint32_t e) {
+    const uint32_t w = sizeof(T) == 4 ? e : e / 2;
+    const uint32_t a = w & 1 ? v.y : v.x, b = w & 1 ? v.w : v.z, word = w & 2 ? b : a;
+    if constexpr (sizeof(T) == 4) {
+        return __uint_as_float(word);
+    } else {
+        const float2 h = halves<T>(word);
+        return e & 1 ? h.y : h.x;
+    }
+}
+
+// A vector whose entries e with bit e set are -Inf.
+template <typename T> __device__ __forceinline__ uint4 without(const uint4& v, uint32_t bits) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            if (bits >> i & 1) w[i] = 0xFF800000u;
+        } else {
+            const uint32_t none = pack2<T>(-INFINITY, -INFINITY);
+            const uint32_t take = (bits >> (2 * i) & 1 ? 0xFFFFu : 0u) | (bits >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
+            w[i] = (w[i] & ~take) | (none & take);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Adds a vector's exponentials relative to `most` (shift = -most * c).
+template <typename T> __device__ __forceinline__ float2 vec_exps(const uint4& v, float2 sum, float c, float shift) {
+    constexpr int N = kVec<T>;
+    Packed<T, N> q;
+    q.v[0] = v;
+    float f[N];
+    q.unpack(f);
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+        const float2 y = fma2(make_float2(f[e], f[e + 1]), make_float2(c, c), make_float2(shift, shift));
+        sum = add2(sum, make_float2(ex2(y.x), ex2(y.y)));
+    }
+    return sum;
+}
+
 enum Mode { kLoss = 0, kGrad = 1, kBoth = 2 };
 
-// One block per row, two passes over it; the second finds much of it in L2.
-template <typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) k_distill(const Job j) {
-    constexpr int N = kVec<T>;
-    extern __shared__ uint32_t s_bits[];            // one bit per token: whether it is listed
-    __shared__ uint32_t s_idx[kMaxPairs];
-    __shared__ float s_val[kMaxPairs];
-    __shared__ float s_m[kThreads / 32], s_s[kThreads / 32], s_x[kThreads / 32];
-    __shared__ double s_d[3][kThreads / 32];
+// What a warp knows of the list: the teacher's sum of exponentials relative to its largest logit (or, with a normaliser, the sum
+// of q), the student's over the listed tokens, whether any entry is there.
+struct ListPart {
+    double q;
+    float top;
+    uint32_t present;
+    Running student;
+};
+
+// What the loss is made of: the teacher's sum, what it left over, the student's sums over all and over what is not listed.
+struct Total {
+    double q, left;
+    float total, rest, top;
+};
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+
+// A row's vectors are divided among the blocks of a cluster (entries off the grid are the first block's).  A block works on its
+// vectors in two passes: the sum, of which the cluster's blocks tell each other through shared memory, and the gradient.  Every
+// block reads the whole list, while its vectors are on their way.  STAGED: a thread's vectors are copied to shared memory by
+// itself and stay there for the second pass, so that a logit crosses HBM once and nothing waits for a load but its own thread; rows
+// too long for a cluster's shared memory are read twice.
+template <typename T, int MODE, bool STAGED>
+__global__ void __launch_bounds__(kThreads, MODE == kLoss ? 6 : 4) k_distill(const Job j) {
+    constexpr int N = kVec<T>, kBatch = 4;
+    extern __shared__ uint4 s_data[];               // [vectors of a block] if STAGED, then what follows
+    __shared__ ListPart s_list[kWarps];
+    __shared__ Running s_part[1 << kClusterBits], s_warp[kWarps];
     __shared__ Shares s_share;
-    const uint32_t row = blockIdx.x, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
+    __shared__ Total s_total;
+    const uint32_t rank = blockIdx.x & ((1u << j.rank_bits) - 1), row = blockIdx.x >> j.rank_bits;
+    const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const T* in = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
     T* out = MODE == kLoss ? nullptr : reinterpret_cast<T*>(j.out.data) + j.out.offset(row);
+    const Cut cut = Cut::of(in, j.vocab);
+    const uint32_t per = (cut.n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits, from = min(rank * per, cut.n_vecs);
+    const uint32_t n_here = min(from + per, cut.n_vecs) - from, loose = rank == 0 ? cut.loose : 0;
+    const T* vecs = in + cut.lead + from * N;
     const float weight = j.weight ? j.weight[row] : 1.0f;
-    Shares share = {};
-    if (weight != 0.0f) {
-        for (uint32_t i = tid; i < (j.vocab + 31) / 32; i += kThreads) s_bits[i] = 0;
-        __syncthreads();
-        bool again = false;
-        for (uint32_t i = tid; i < j.k; i += kThreads) {
-            const uint64_t at = j.idx.offset(row) + i;
-            const int64_t v = j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at]
-                                                        : reinterpret_cast<const int32_t*>(j.idx.data)[at];
-            uint32_t token = kNone;
-            if (v >= j.vocab) record_error(j.status, ADACOMP_ERR_INVALID);
-            else if (v >= 0) token = static_cast<uint32_t>(v);
-            s_idx[i] = token;
-            s_val[i] = load_value(j.val, j.val.offset(row) + i);
-            if (token != kNone) again |= (atomicOr(&s_bits[token / 32], 1u << token % 32) >> token % 32) & 1;
-        }
-        if (__syncthreads_or(again)) {              // a token twice: the first one counts
-            bool drop[kMaxPairs / kThreads] = {};
-#pragma unroll
-            for (int r = 0; r < static_cast<int>(kMaxPairs / kThreads); ++r)
-                for (uint32_t i = tid + r * kThreads, e = 0; i < j.k && e < i; ++e) drop[r] |= s_idx[e] == s_idx[i];
-            __syncthreads();
-#pragma unroll
-            for (int r = 0; r < static_cast<int>(kMaxPairs / kThreads); ++r)
-                if (drop[r]) s_idx[tid + r * kThreads] = kNone;
-            __syncthreads();
-        }
-        if (MODE == kGrad) {
-            const float* st = j.stats + static_cast<uint64_t>(row) * kStats;
-            share = {st[0], st[1], st[2], st[3], st[4], st[5]};
+    const bool on_grid = (reinterpret_cast<uintptr_t>(in) - reinterpret_cast<uintptr_t>(out)) % 16 == 0;
+    auto store = [&](uint32_t v, const Packed<T, N>& p) {
+        T* to = out + cut.lead + (from + v) * N;
+        if (on_grid) {
+            *reinterpret_cast<uint4*>(to) = p.v[0];
         } else {
-            // the row's largest logit, and the sum over what is not listed
-            Running r = {-INFINITY, 0.0f};
-            float listed_max = -INFINITY;
-            const Cut cut = Cut::of(in, j.vocab);
-            if (tid < cut.loose) {
-                const uint32_t at = cut.loose_at<T>(tid);
-                const float x = to_float(in[at]);
-                if (s_bits[at / 32] >> at % 32 & 1) {
-                    listed_max = fmaxf(listed_max, x);
-                } else {
-                    r.raise(x, j.c);
-                    r.s += exp_from(x, r.base(), j.c);
-                }
-            }
-            for (uint32_t v = tid; v < cut.n_vecs; v += kThreads) {
-                Packed<T, N> p;
-                p.v[0] = load16_once(in + cut.lead + v * N);
-                float f[N];
-                p.unpack(f);
-                const uint32_t at = cut.lead + v * N;
-                const uint32_t bits = __funnelshift_r(s_bits[at / 32], at / 32 + 1 < (j.vocab + 31) / 32 ? s_bits[at / 32 + 1] : 0, at);
-                float most = f[0];
+            const T* e = reinterpret_cast<const T*>(&p.v[0]);
 #pragma unroll
-                for (int e = 1; e < N; ++e) most = fmaxf(most, f[e]);
-                r.raise(most, j.c);
-                const float base = r.base();
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float y = exp_from(f[e], base, j.c);
-                    r.s += bits >> e & 1 ? 0.0f : y;
-                }
-            }
-            r.raise(listed_max, j.c);               // the listed ones' sum is taken from the list
-            r = warp_join(r, j.c);
-            if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
-            __syncthreads();
-            r = warp_join({s_m[lane % (kThreads / 32)], lane < kThreads / 32 ? s_s[lane] : 0.0f}, j.c);
-            // the teacher's list
-            float top = -INFINITY;
-            for (uint32_t i = tid; i < j.k; i += kThreads)
-                if (s_idx[i] != kNone) top = fmaxf(top, s_val[i]);
-            top = warp_max(top);
-            if (lane == 0) s_x[warp] = top;
-            __syncthreads();
-            top = warp_max(s_x[lane % (kThreads / 32)]);
-            const float base = r.base(), t_base = top == -INFINITY ? 0.0f : top;
-            const double lse = j.lse ? static_cast<double>(j.lse[row]) : 0.0;
-            double q_sum = 0.0, cross = 0.0, listed = 0.0;
-            for (uint32_t i = tid; i < j.k; i += kThreads) {
-                if (s_idx[i] == kNone) continue;
-                const float s = to_float(in[s_idx[i]]);
-                listed += exp_from(s, base, j.c);
-                const double t = j.lse ? s_val[i] * j.inv_t - lse : (static_cast<double>(s_val[i]) - t_base) * j.inv_t;
-                // with the teacher's normaliser 1 - sum q is left over: small where the list says almost everything, so in 64 bits
-                double q = j.lse ? exp(t) : expf(static_cast<float>(t));
-                if (q > 1e300) q = NAN;
-                q_sum += q;
-                if (q != 0.0) cross += q * (t - (static_cast<double>(s) * j.c - reference(base, j.c)) * kLn2);
-            }
-            q_sum = warp_sum(q_sum), cross = warp_sum(cross), listed = warp_sum(listed);
-            if (lane == 0) s_d[0][warp] = q_sum, s_d[1][warp] = cross, s_d[2][warp] = listed;
-            const bool any = __syncthreads_or(top != -INFINITY);
-            bool present = false;
-            for (uint32_t i = tid; i < j.k; i += kThreads) present |= s_idx[i] != kNone;
-            present = __syncthreads_or(present);
-            if (tid == 0) {
-                q_sum = cross = listed = 0.0;
-                for (int w = 0; w < kThreads / 32; ++w) q_sum += s_d[0][w], cross += s_d[1][w], listed += s_d[2][w];
-                const double rest = r.s, total = rest + listed;
-                const bool live = present && (j.lse ? lse != -INFINITY : any || q_sum != q_sum) && total != 0.0;
-                double loss = 0.0;
-                if (live) {
-                    const double log_total = log(total);
-                    if (!j.lse) {
-                        loss = cross / q_sum + log_total - log(q_sum);
-                        share = {base, static_cast<float>(1.0 / total), static_cast<float>(1.0 / total), t_base, static_cast<float>(1.0 / q_sum), 1.0f};
-                    } else {
-                        const double left = rest > 0.0 && q_sum < 1.0 ? 1.0 - q_sum : 0.0, mass = q_sum + left;
-                        loss = cross + q_sum * log_total + (left > 0.0 ? left * (log(left) - log(rest) + log_total) : 0.0);
-                        share = {base, static_cast<float>(mass / total - (left > 0.0 ? left / rest : 0.0)), static_cast<float>(mass / total),
-                                 static_cast<float>(lse), 1.0f, 1.0f};
-                    }
-                }
-                if (q_sum != q_sum) share.rest = share.listed = NAN;
-                if (j.loss) j.loss[row] = static_cast<float>(loss);
-                s_share = share;
-                if (j.stats) {
-                    float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
-                    st[0] = make_float4(share.m, share.rest, share.listed, share.t_base);
-                    st[1] = make_float4(share.q_scale, share.live, 0.0f, 0.0f);
-                }
-            }
-            __syncthreads();
-            share = s_share;
+            for (int i = 0; i < N; ++i) to[i] = e[i];
         }
-    } else if (MODE != kGrad && tid == 0) {
-        if (j.loss) j.loss[row] = 0.0f;
-        if (j.stats) {
-            float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
-            st[0] = st[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        }
-    }
-    if (MODE == kLoss) return;
+    };
 
-    // the gradient: windows on the output's grid
-    const Cut cut = Cut::of(out, j.vocab);
-    if (share.live == 0.0f) {
-        for (uint32_t v = tid; v < cut.n_vecs; v += kThreads) *reinterpret_cast<uint4*>(out + cut.lead + v * N) = make_uint4(0, 0, 0, 0);
-        if (tid < cut.loose) out[cut.loose_at<T>(tid)] = from_float<T>(0.0f);
+    Shares share = {};
+    if (MODE == kGrad && weight != 0.0f) {
+        const float* st = j.stats + static_cast<uint64_t>(row) * kStats;
+        share = {st[0], st[1], st[2], st[3], st[4], st[5]};
+    }
+    if (weight == 0.0f || (MODE == kGrad && share.live == 0.0f)) {
+        if (MODE != kGrad && rank == 0 && tid == 0) {
+            if (j.loss) j.loss[row] = 0.0f;
+            if (MODE == kLoss && j.stats) {
+                float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
+                st[0] = st[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+        }
+        if (MODE != kLoss) {
+            Packed<T, N> zero;
+            zero.v[0] = make_uint4(0, 0, 0, 0);
+            for (uint32_t v = tid; v < n_here; v += kThreads) store(v, zero);
+            if (tid < loose) out[cut.loose_at<T>(tid)] = from_float<T>(0.0f);
+        }
         return;
     }
-    const float g = static_cast<float>(weight * j.inv_t), rest = share.rest * g;
-    const bool on_grid = (reinterpret_cast<uintptr_t>(in) - reinterpret_cast<uintptr_t>(out)) % 16 == 0;
-    uint32_t token[kMaxPairs / kThreads];
-    float listed[kMaxPairs / kThreads];
+    const bool joined = MODE != kGrad && j.rank_bits;
+    if (joined) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    // the thread's vectors in four groups of copies
+    const uint32_t turns = (n_here + kThreads - 1) / kThreads, quarter = (turns + 4 * kBatch - 1) / (4 * kBatch) * kBatch;
+    if (STAGED) {
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(s_data)) + tid * 16;
+        const uint32_t whole = n_here / kThreads;
+        const char* at = reinterpret_cast<const char*>(vecs + tid * N);
+        uint32_t i = 0;
 #pragma unroll
-    for (int r = 0; r < static_cast<int>(kMaxPairs / kThreads); ++r) {
-        const uint32_t i = tid + r * kThreads;
-        token[r] = i < j.k ? s_idx[i] : kNone;
-        if (token[r] == kNone) continue;
-        const double t = j.lse ? s_val[i] * j.inv_t - share.t_base : (static_cast<double>(s_val[i]) - share.t_base) * j.inv_t;
-        const float q = expf(static_cast<float>(t)) * share.q_scale;
-        listed[r] = (exp_from(to_float(in[token[r]]), share.m, j.c) * share.listed - q) * g;
+        for (int g = 1; g <= 4; ++g) {
+            for (const uint32_t end = min(g * quarter, whole); i < end; ++i, at += kThreads * 16) copy16(to + i * (kThreads * 16), at);
+            if (i < min(g * quarter, turns)) {
+                if (i * kThreads + tid < n_here) copy16(to + i * (kThreads * 16), at);
+                ++i;
+            }
+            copies_end();
+        }
     }
-    __syncthreads();                                // before the gradient may take the place of a logit that is read here
-    for (uint32_t v = tid; v < cut.n_vecs; v += kThreads) {
-        Packed<T, N> p;
-        if (on_grid) p.v[0] = load16_once(in + cut.lead + v * N);
-        else p = load_shifted<T, N>(in, cut.lead + static_cast<int64_t>(v) * N, j.vocab);
-        float f[N];
-        p.unpack(f);
+
+    // the list.  A table that names each token's first place finds those that stand there twice.
+    char* const s_more = reinterpret_cast<char*>(s_data) + j.at_table;
+    uint64_t* const s_table = reinterpret_cast<uint64_t*>(s_more);
+    uint32_t* const s_idx = reinterpret_cast<uint32_t*>(s_table + (1u << j.table_bits));
+    float* const s_t = reinterpret_cast<float*>(s_idx + j.k);
+    float* const s_s = s_t + j.k;
+    uint32_t* const s_bits = reinterpret_cast<uint32_t*>(s_s + j.k);        // of this block's entries, with a normaliser
+    const bool tail = j.lse != nullptr;
+    for (uint32_t i = tid; i < 1u << j.table_bits; i += kThreads) s_table[i] = ~0ull;
+    if (tail && MODE != kGrad)
+        for (uint32_t i = tid; i < (n_here * N + loose + 31) / 32; i += kThreads) s_bits[i] = 0;
+    __syncthreads();
+    for (uint32_t i = tid; i < j.k; i += kThreads) {
+        const uint64_t at = j.idx.offset(row) + i;
+        const int64_t v = j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at]
+                                                    : reinterpret_cast<const int32_t*>(j.idx.data)[at];
+        s_t[i] = load_value(j.val, j.val.offset(row) + i);
+        if (v >= j.vocab && rank == 0) record_error(j.status, ADACOMP_ERR_INVALID);
+        const uint32_t token = v >= 0 && v < j.vocab ? static_cast<uint32_t>(v) : kNone;
+        s_idx[i] = token;
+        if (token == kNone) continue;
+        s_s[i] = to_float(in[token]);
+        const uint64_t mine = static_cast<uint64_t>(token) << 32 | i;
+        for (uint32_t at = token * 2654435761u >> (32 - j.table_bits);; at = (at + 1) & ((1u << j.table_bits) - 1)) {      // half of it stays empty
+            const uint64_t there = atomicCAS(reinterpret_cast<unsigned long long*>(&s_table[at]), ~0ull, mine);
+            if (there >> 32 == token) atomicMin(reinterpret_cast<unsigned long long*>(&s_table[at]), mine);
+            if (there == ~0ull || there >> 32 == token) break;
+        }
+    }
+    __syncthreads();
+    const double lse = tail ? static_cast<double>(j.lse[row]) : 0.0;
+    {
+        ListPart part = {0.0, -INFINITY, 0, {-INFINITY, 0.0f}};
+        for (uint32_t i = tid; i < j.k; i += kThreads) {
+            const uint32_t token = s_idx[i];
+            if (token == kNone) continue;
+            uint32_t at = token * 2654435761u >> (32 - j.table_bits);
+            while (s_table[at] >> 32 != token) at = (at + 1) & ((1u << j.table_bits) - 1);
+            if (static_cast<uint32_t>(s_table[at]) != i) {
+                s_idx[i] = kNone;
+                continue;
+            }
+            if (MODE == kGrad) continue;
+            part.present = 1;
+            part.top = fmaxf(part.top, s_t[i]);
+            if (tail) {
+                part.student.raise(s_s[i], j.c);
+                part.student.s += exp_from(s_s[i], part.student.base(), j.c);
+                const uint32_t behind = token - cut.lead;
+                uint32_t bit = kNone;
+                if (token >= cut.lead && behind / N < cut.n_vecs) bit = behind / N - from < n_here ? behind - from * N : kNone;
+                else if (rank == 0) bit = n_here * N + (token < cut.lead ? token : token - cut.n_vecs * N);
+                if (bit != kNone) atomicOr(&s_bits[bit / 32], 1u << bit % 32);
+            }
+        }
+        if (MODE != kGrad && warp * 32 < j.k) {
+            part.top = warp_max(part.top);
+            const float base = part.top == -INFINITY ? 0.0f : part.top;
+            for (uint32_t i = tid; i < j.k; i += kThreads)
+                if (s_idx[i] != kNone) {
+                    // with the teacher's normaliser 1 - sum q is left over: small where the list says almost everything, so in 64 bits
+                    const double t = tail ? exp(s_t[i] * j.inv_t - lse) : expf(static_cast<float>((static_cast<double>(s_t[i]) - base) * j.inv_t));
+                    part.q += t > 1e300 ? NAN : t;
+                }
+            part.q = warp_sum(part.q);
+            part.present = __any_sync(~0u, part.present);
+            if (tail) part.student = warp_join(part.student, j.c);
+            if (lane == 0) s_list[warp] = part;
+        }
+        if (tail && MODE != kGrad) __syncthreads();         // the bits
+    }
+
+    if (MODE != kGrad) {
+        // the sum, with a normaliser over what is not listed
+        Running r = {-INFINITY, 0.0f};
+        auto vec = [&](uint32_t v) { return STAGED ? s_data[v] : load16_once(vecs + v * N); };
+        auto add = [&](auto& p, uint32_t v0) {      // vectors v0, v0 + kThreads ...
+            constexpr int kHere = sizeof(p) / sizeof(uint4);
+            float most = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = exp_from(f[e], share.m, j.c) * rest;
-        p.pack(f);
-        *reinterpret_cast<uint4*>(out + cut.lead + v * N) = p.v[0];
-    }
-    if (tid < cut.loose) {
-        const uint32_t at = cut.loose_at<T>(tid);
-        out[at] = from_float<T>(exp_from(to_float(in[at]), share.m, j.c) * rest);
-    }
-    __syncthreads();                                // the listed ones replace what has just been written
+            for (int i = 0; i < kHere; ++i) {
+                if (tail) {
+                    const uint32_t b = (v0 + i * kThreads) * N, bits = s_bits[b / 32] >> b % 32 & ((1u << N) - 1);
+                    if (bits) p[i] = without<T>(p[i], bits);
+                }
+                most = fmaxf(most, vec_max<T>(p[i]));
+            }
+            r.raise(most, j.c);
+            const float base = r.base();
+            if (fabsf(base) < kWild) {
+                const float shift = -base * j.c;
+                float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int r = 0; r < static_cast<int>(kMaxPairs / kThreads); ++r)
-        if (token[r] != kNone) out[token[r]] = from_float<T>(listed[r]);
+                for (int i = 0; i < kHere; ++i) sum = vec_exps<T>(p[i], sum, j.c, shift);
+                r.s += sum.x + sum.y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < kHere; ++i)
+#pragma unroll 1
+                    for (int e = 0; e < N; ++e) r.s += exp_from(pick<T>(p[i], e), base, j.c);
+            }
+        };
+        auto span = [&](uint32_t i, uint32_t end) {            // turns of the thread
+            const uint32_t whole = min(end, n_here / kThreads);
+            for (; i + kBatch <= whole; i += kBatch) {
+                uint4 p[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) p[u] = vec((i + u) * kThreads + tid);
+                add(p, i * kThreads + tid);
+            }
+#pragma unroll 1
+            for (; i < end && i * kThreads + tid < n_here; ++i) {
+                uint4 p[1] = {vec(i * kThreads + tid)};
+                add(p, i * kThreads + tid);
+            }
+        };
+        // (in this order without copies too: the same sums then, to the last bit)
+        if (STAGED) copies_wait<3>();
+        span(0, quarter);
+        if (STAGED) copies_wait<2>();
+        span(quarter, 2 * quarter);
+        if (STAGED) copies_wait<1>();
+        span(2 * quarter, 3 * quarter);
+        if (STAGED) copies_wait<0>();
+        span(3 * quarter, turns);
+        if (tid < loose) {
+            const float x = to_float(in[cut.loose_at<T>(tid)]);
+            const uint32_t b = n_here * N + tid;
+            r.raise(x, j.c);
+            if (!tail || !(s_bits[b / 32] >> b % 32 & 1)) r.s += exp_from(x, r.base(), j.c);
+        }
+        r = warp_join(r, j.c);
+        if (lane == 0) s_warp[warp] = r;
+        __syncthreads();
+        // the rest is the first warp's work
+        const Running none = {-INFINITY, 0.0f};
+        if (warp == 0) r = warp_join(lane < kWarps ? s_warp[lane] : none, j.c);
+        if (joined) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all blocks have started
+            if (tid < 1u << j.rank_bits) *cooperative_groups::this_cluster().map_shared_rank(&s_part[rank], tid) = r;
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (warp == 0) r = warp_join(lane < 1u << j.rank_bits ? s_part[lane] : none, j.c);
+        }
+        if (warp == 0) {
+            const bool given = lane < kWarps && lane * 32 < j.k;
+            const ListPart part = given ? s_list[lane] : ListPart{0.0, -INFINITY, 0, none};
+            const float top = warp_max(part.top);
+            const bool present = __any_sync(~0u, part.present);
+            const double q_sum = warp_sum(tail || part.top == top ? part.q : part.q * expf(static_cast<float>((static_cast<double>(part.top) - top) * j.inv_t)));
+            double left = 0.0;
+            Total all = {q_sum, 0.0, r.s, 0.0f, top};
+            if (tail) {
+                Running student = warp_join(part.student, j.c);
+                const float m = fmaxf(r.m, student.m);
+                all.rest = r.m == m ? r.s : r.s * Running::lowered(r.m, m, j.c);
+                student.join(m, 0.0f, j.c);
+                r = {m, all.rest + student.s};
+                all.total = r.s;
+                left = all.rest > 0.0f && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
+                all.left = left;
+            }
+            if (present && (tail ? lse != -INFINITY : top != -INFINITY || q_sum != q_sum) && r.s != 0.0f) {
+                const float unit = 1.0f / r.s;
+                if (tail) {
+                    const float mass = static_cast<float>(q_sum + left), over = left > 0.0 ? static_cast<float>(left) / all.rest : 0.0f;
+                    share = {r.base(), mass * unit - over, mass * unit, static_cast<float>(lse), 1.0f, 1.0f};
+                } else {
+                    share = {r.base(), unit, unit, top, 1.0f / static_cast<float>(q_sum), 1.0f};
+                }
+                if (q_sum != q_sum) share.rest = share.listed = NAN;
+            }
+            if (lane == 0) s_share = share, s_total = all;
+        }
+        __syncthreads();
+        share = s_share;
+        if (MODE == kLoss && j.stats && rank == 0 && tid == 0) {
+            float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
+            st[0] = make_float4(share.m, share.rest, share.listed, share.t_base);
+            st[1] = make_float4(share.q_scale, share.live, 0.0f, 0.0f);
+        }
+        // the loss is the last one's
+        if (rank == 0 && warp == kWarps - 1 && j.loss) {
+            double loss = 0.0;
+            if (share.live != 0.0f) {
+                const Total all = s_total;
+                const double from_m = reference(share.m, j.c);
+                double cross = 0.0, sum = 0.0;
+                for (uint32_t i = lane; i < j.k; i += 32) {
+                    if (s_idx[i] == kNone) continue;
+                    const double t = tail ? s_t[i] * j.inv_t - lse : (static_cast<double>(s_t[i]) - all.top) * j.inv_t;
+                    const double q = tail ? exp(t) : expf(static_cast<float>(t));
+                    sum += q;
+                    if (q != 0.0) cross += q * (t - (static_cast<double>(s_s[i]) * j.c - from_m) * kLn2);
+                }
+                cross = warp_sum(cross), sum = warp_sum(sum);
+                const double log_total = log(static_cast<double>(all.total));
+                if (!tail) loss = cross / sum - log(sum) + log_total;
+                else loss = cross + sum * log_total + (all.left > 0.0 ? all.left * (log(all.left) - log(static_cast<double>(all.rest)) + log_total) : 0.0);
+                if (all.q != all.q) loss = NAN;
+            }
+            if (lane == 0) j.loss[row] = static_cast<float>(loss);
+        }
+    }
+
+    if (MODE != kLoss) {
+        const float g = static_cast<float>(weight * j.inv_t), rest = share.rest * g;
+        const bool wild = !(fabsf(share.m) < kWild) || share.live == 0.0f;
+        const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-share.m * j.c, -share.m * j.c);
+        auto gradient = [&](const uint4& x, uint32_t v) {
+            Packed<T, N> p;
+            p.v[0] = x;
+            float f[N];
+            p.unpack(f);
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
+                f[e] = ex2(y.x) * rest;
+                f[e + 1] = ex2(y.y) * rest;
+            }
+            p.pack(f);
+            store(v, p);
+        };
+        auto vec = [&](uint32_t v) { return STAGED ? s_data[v] : load16_once(vecs + v * N); };
+        float off_grid = 0.0f;
+        if (tid < loose) off_grid = to_float(in[cut.loose_at<T>(tid)]);
+        if (!wild) {
+            uint32_t i = 0;
+            for (; i + kBatch <= n_here / kThreads; i += kBatch) {
+                uint4 p[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) p[u] = vec((i + u) * kThreads + tid);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) gradient(p[u], (i + u) * kThreads + tid);
+            }
+#pragma unroll 1
+            for (uint32_t v = i * kThreads + tid; v < n_here; v += kThreads) gradient(vec(v), v);
+        } else {
+#pragma unroll 1
+            for (uint32_t v = tid; v < n_here; v += kThreads) {
+                const uint4 x = vec(v);
+                T* to = out + cut.lead + (from + v) * N;
+#pragma unroll 1
+                for (int e = 0; e < N; ++e) to[e] = from_float<T>(share.live != 0.0f ? exp_from(pick<T>(x, e), share.m, j.c) * rest : 0.0f);
+            }
+        }
+        if (tid < loose) out[cut.loose_at<T>(tid)] = from_float<T>(share.live != 0.0f ? exp_from(off_grid, share.m, j.c) * rest : 0.0f);
+        __syncthreads();                            // the listed ones replace what has just been written
+        if (share.live != 0.0f)
+            for (uint32_t i = tid; i < j.k; i += kThreads) {
+                const uint32_t token = s_idx[i], behind = token - cut.lead;
+                if (token == kNone || !(token >= cut.lead && behind / N < cut.n_vecs ? behind / N - from < n_here : rank == 0)) continue;
+                const double t = tail ? s_t[i] * j.inv_t - share.t_base : (static_cast<double>(s_t[i]) - share.t_base) * j.inv_t;
+                const float q = expf(static_cast<float>(t)) * share.q_scale;
+                out[token] = from_float<T>((exp_from(s_s[i], share.m, j.c) * share.listed - q) * g);
+            }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- top logits
@@ -378,7 +591,6 @@ constexpr int kTopThreads = 128;
 constexpr int kTopVecs = 2;                         // vectors of a thread in one step: a group
 constexpr uint32_t kTopStep = kTopThreads * kTopVecs;
 constexpr int kBoundBits = 12;
-constexpr uint32_t kTopClusterBits = 3;             // blocks of the largest cluster
 constexpr uint32_t kTopGroups = 32768;              // of a block
 constexpr uint32_t kHits = 512;
 
@@ -413,18 +625,6 @@ __device__ __forceinline__ uint32_t order_of(float x) {
 __device__ __forceinline__ uint64_t composite(float x, uint32_t token) {
     return static_cast<uint64_t>(order_of(x)) << 32 | (0xFFFFFFFFu - token);
 }
-// Entry e of a vector.
-template <typename T> __device__ __forceinline__ float pick(const uint4& v, uint32_t e) {
-    const uint32_t w = sizeof(T) == 4 ? e : e / 2;
-    const uint32_t a = w & 1 ? v.y : v.x, b = w & 1 ? v.w : v.z, word = w & 2 ? b : a;
-    if constexpr (sizeof(T) == 4) {
-        return __uint_as_float(word);
-    } else {
-        const float2 h = halves<T>(word);
-        return e & 1 ? h.y : h.x;
-    }
-}
-
 // A float that every entry above `bound` exceeds, and entries equal to it but for the token with them (NaN, which nothing
 // fails to exceed, where there is none).
 __device__ __forceinline__ float floor_of(uint64_t bound) {
@@ -468,21 +668,6 @@ template <uint32_t THREADS> __device__ void sort_list(uint64_t* s_list, uint32_t
             }
     }
     __syncthreads();
-}
-
-// Adds a vector's exponentials relative to `most` (shift = -most * c).
-template <typename T> __device__ __forceinline__ float2 vec_exps(const uint4& v, float2 sum, float c, float shift) {
-    constexpr int N = kVec<T>;
-    Packed<T, N> q;
-    q.v[0] = v;
-    float f[N];
-    q.unpack(f);
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-        const float2 y = fma2(make_float2(f[e], f[e + 1]), make_float2(c, c), make_float2(shift, shift));
-        sum = add2(sum, make_float2(ex2(y.x), ex2(y.y)));
-    }
-    return sum;
 }
 
 // One pass over the row computes the sum and, for every thread's share of every step (a group: kTopVecs vectors), the largest entry, which
@@ -783,12 +968,44 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
 
 bool good_temperature(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 
-template <typename T, int MODE> int launch_distill(const Job& j, cudaStream_t stream) {
-    const size_t smem = (j.vocab + 31) / 32 * 4;
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMaxVocab / 8)));
-    k_distill<T, MODE><<<j.n_rows, kThreads, smem, stream>>>(j);
+template <typename T, int MODE, bool STAGED> int launch_shape(Job j, uint32_t chunk_vecs, cudaStream_t stream) {
+    const uint32_t data = STAGED ? chunk_vecs * 16 : 0;
+    j.at_table = data;
+    j.table_bits = 5;
+    while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
+    const uint32_t bits = j.lse && MODE != kGrad ? ((chunk_vecs + 2) * kVec<T> + 31) / 32 * 4 : 0;
+    const size_t shared = data + (8ull << j.table_bits) + j.k * 12ull + bits;
+    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(j.n_rows << j.rank_bits);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1u << j.rank_bits;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = MODE != kGrad && j.rank_bits ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_distill<T, MODE, STAGED>, j);
+    if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
+}
+
+template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_t stream) {
+    // as many blocks to a row as its chunks need, and more while the call has fewer blocks than SMs and chunks are not short
+    const uint32_t n_vecs = j.vocab / kVec<T> + 1;
+    while (j.rank_bits < kClusterBits &&
+           (n_vecs * 16ull >> j.rank_bits > kChunk ||
+            ((static_cast<uint64_t>(j.n_rows) << j.rank_bits) * 2 <= 2ull * n_sms && n_vecs >> j.rank_bits >= 4 * kThreads)))
+        ++j.rank_bits;
+    const uint32_t chunk_vecs = (n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits;
+    if constexpr (MODE == kBoth) {
+        if (chunk_vecs * 16ull <= kLargestChunk) return launch_shape<T, MODE, true>(j, chunk_vecs, stream);
+    }
+    return launch_shape<T, MODE, false>(j, chunk_vecs, stream);
 }
 
 template <int MODE>
@@ -819,16 +1036,16 @@ int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (j.logits.type == ADACOMP_F32) return launch_distill<float, MODE>(j, stream);
-    if (j.logits.type == ADACOMP_BF16) return launch_distill<__nv_bfloat16, MODE>(j, stream);
-    return launch_distill<__half, MODE>(j, stream);
+    if (j.logits.type == ADACOMP_F32) return launch_distill<float, MODE>(j, h->n_sms, stream);
+    if (j.logits.type == ADACOMP_BF16) return launch_distill<__nv_bfloat16, MODE>(j, h->n_sms, stream);
+    return launch_distill<__half, MODE>(j, h->n_sms, stream);
 }
 
 template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
     // several blocks a row as long as all of them are on the SMs at once and each has some steps to do, or where one could
     // not hold the groups of a row
     const uint32_t n_vecs = j.vocab / kVec<T> + 1;
-    while (j.rank_bits < kTopClusterBits &&
+    while (j.rank_bits < kClusterBits &&
            ((n_vecs >> j.rank_bits) / kTopVecs > kTopGroups - kTopThreads ||
             ((static_cast<uint64_t>(n_rows) << j.rank_bits) * 2 <= 4ull * n_sms && n_vecs >> j.rank_bits >= 2 * kTopStep)))
         ++j.rank_bits;
