@@ -25,13 +25,10 @@ struct adacomp_distill {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMaxPairs = 1024;
 constexpr uint32_t kMaxVocab = 1u << 20;
 constexpr uint32_t kStats = 8;
 constexpr uint32_t kClusterBits = 3;               // blocks of the largest cluster
-constexpr uint32_t kChunk = 72 * 1024;              // of a row in a block's shared memory: three blocks on an SM
 constexpr uint32_t kLargestChunk = 192 * 1024;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
@@ -59,6 +56,13 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     float2 d;
     asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; add.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{ .reg .b64 a, b, d; mov.b64 a, {%2, %3}; mov.b64 b, {%4, %5}; mul.rn.f32x2 d, a, b; mov.b64 {%0, %1}, d; }"
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
@@ -196,6 +200,10 @@ template <typename T> __device__ __forceinline__ float pick(const uint4& v, uint
     }
 }
 
+template <typename T> __device__ __forceinline__ uint32_t pack2_of(float x) {
+    if constexpr (sizeof(T) == 4) return __float_as_uint(x);
+    else return pack2<T>(x, x);
+}
 // A vector whose entries e with bit e set are -Inf.
 template <typename T> __device__ __forceinline__ uint4 without(const uint4& v, uint32_t bits) {
     uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -204,7 +212,7 @@ template <typename T> __device__ __forceinline__ uint4 without(const uint4& v, u
         if constexpr (sizeof(T) == 4) {
             if (bits >> i & 1) w[i] = 0xFF800000u;
         } else {
-            const uint32_t none = pack2<T>(-INFINITY, -INFINITY);
+            const uint32_t none = pack2_of<T>(-INFINITY);
             const uint32_t take = (bits >> (2 * i) & 1 ? 0xFFFFu : 0u) | (bits >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
             w[i] = (w[i] & ~take) | (none & take);
         }
@@ -229,90 +237,113 @@ template <typename T> __device__ __forceinline__ float2 vec_exps(const uint4& v,
 
 enum Mode { kLoss = 0, kGrad = 1, kBoth = 2 };
 
-// What a warp knows of the list: the teacher's sum of exponentials relative to its largest logit (or, with a normaliser, the sum
-// of q), the student's over the listed tokens, whether any entry is there.
-struct ListPart {
-    double q;
-    float top;
-    uint32_t present;
-    Running student;
-};
-
-// What the loss is made of: the teacher's sum, what it left over, the student's sums over all and over what is not listed.
-struct Total {
-    double q, left;
-    float total, rest, top;
-};
-
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
 
+// The first vector of a row that is block `rank`'s.
+__device__ __forceinline__ uint32_t part_begin(const Cut& cut, uint32_t rank, uint32_t rank_bits) {
+    return min(rank * ((cut.n_vecs + (1u << rank_bits) - 1) >> rank_bits), cut.n_vecs);
+}
+
+// A block's share of a row: vectors on the grid, and the first block's entries beside it.
+template <typename T, bool STAGED> struct Chunk {
+    const T* in;
+    const T* vecs;
+    const uint4* s_data;
+    const uint32_t* s_bits;         // which entries are left out of the sum, or nullptr
+    Cut cut;
+    uint32_t n, loose;
+    __device__ __forceinline__ uint4 vec(uint32_t v) const { return STAGED ? s_data[v] : load16_once(vecs + v * kVec<T>); }
+    __device__ __forceinline__ uint32_t out_bits(uint32_t v) const {        // of vector v; of the entries off the grid, v = n
+        const uint32_t b = v * kVec<T>;
+        return s_bits[b / 32] >> b % 32 & ((1u << kVec<T>) - 1);
+    }
+    __device__ __forceinline__ bool loose_out(uint32_t i) const {
+        const uint32_t b = n * kVec<T> + i;
+        return s_bits && s_bits[b / 32] >> b % 32 & 1;
+    }
+};
+
+template <uint32_t RANKS_MOST, typename V, typename F> __device__ __forceinline__ V cluster_gather(V* s_part, const V& mine, uint32_t rank, uint32_t rank_bits, V none, F join) {
+    const uint32_t lane = threadIdx.x % 32;
+    if (threadIdx.x < 1u << rank_bits) *cooperative_groups::this_cluster().map_shared_rank(&s_part[rank], threadIdx.x) = mine;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    return join(lane < 1u << rank_bits ? s_part[lane] : none);
+}
+
+// The sum relative to the largest of the entries themselves, found on the way: for rows whose logits lie so far from the listed ones
+// that the sum relative to those overflows, and for rows without numbers.
+template <typename T, bool STAGED, int THREADS>
+__device__ __noinline__ Running careful_sum(const Chunk<T, STAGED> chunk, float c, Running* s_warp, Running* s_part, uint32_t rank, uint32_t rank_bits) {
+    const uint32_t tid = threadIdx.x, lane = tid % 32;
+    Running r = {-INFINITY, 0.0f};
+#pragma unroll 1
+    for (uint32_t v = tid; v < chunk.n; v += THREADS) {
+        const uint4 x = chunk.vec(v);
+        const uint32_t out = chunk.s_bits ? chunk.out_bits(v) : 0;
+#pragma unroll 1
+        for (int e = 0; e < kVec<T>; ++e) {
+            if (out >> e & 1) continue;
+            const float f = pick<T>(x, e);
+            r.raise(f, c);
+            r.s += exp_from(f, r.base(), c);
+        }
+    }
+    if (tid < chunk.loose && !chunk.loose_out(tid)) {
+        const float f = to_float(chunk.in[chunk.cut.template loose_at<T>(tid)]);
+        r.raise(f, c);
+        r.s += exp_from(f, r.base(), c);
+    }
+    r = warp_join(r, c);
+    if (lane == 0) s_warp[tid / 32] = r;
+    __syncthreads();
+    const Running none = {-INFINITY, 0.0f};
+    r = warp_join(lane < THREADS / 32 ? s_warp[lane] : none, c);
+    if (rank_bits) r = cluster_gather<8>(s_part, r, rank, rank_bits, none, [&](const Running& x) { return warp_join(x, c); });
+    return r;
+}
+
 // A row's vectors are divided among the blocks of a cluster (entries off the grid are the first block's).  A block works on its
 // vectors in two passes: the sum, of which the cluster's blocks tell each other through shared memory, and the gradient.  Every
-// block reads the whole list, while its vectors are on their way.  STAGED: a thread's vectors are copied to shared memory by
-// itself and stay there for the second pass, so that a logit crosses HBM once and nothing waits for a load but its own thread; rows
-// too long for a cluster's shared memory are read twice.
-template <typename T, int MODE, bool STAGED>
-__global__ void __launch_bounds__(kThreads, MODE == kLoss ? 6 : 4) k_distill(const Job j) {
-    constexpr int N = kVec<T>, kBatch = 4;
+// block reads the whole list, while its vectors are on their way.  The sum is taken relative to the student's largest LISTED logit, which
+// is mostly the largest of all or near it, so that no maximum has to be looked for; where it overflows, it is taken once more with care.
+// STAGED: a thread's vectors are copied to shared memory by itself and stay there for the second pass, so that a logit crosses HBM once and
+// nothing waits for a load but its own thread; rows too long for a cluster's shared memory are read twice.
+template <typename T, int MODE, bool STAGED, int THREADS>
+__global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREADS) k_distill(const Job j) {
+    constexpr int N = kVec<T>, kBatch = 4, kWarps = THREADS / 32;
+    constexpr uint32_t kThreads = THREADS;
     extern __shared__ uint4 s_data[];               // [vectors of a block] if STAGED, then what follows
-    __shared__ ListPart s_list[kWarps];
-    __shared__ Running s_part[1 << kClusterBits], s_warp[kWarps];
-    __shared__ Shares s_share;
-    __shared__ Total s_total;
+    __shared__ float s_max[2][kWarps], s_sum[kWarps], s_listed[kWarps];
+    __shared__ double s_q[kWarps];
+    __shared__ Running s_warp[kWarps], s_part[2][1 << kClusterBits];
     const uint32_t rank = blockIdx.x & ((1u << j.rank_bits) - 1), row = blockIdx.x >> j.rank_bits;
     const uint32_t tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
     const T* in = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
     T* out = MODE == kLoss ? nullptr : reinterpret_cast<T*>(j.out.data) + j.out.offset(row);
     const Cut cut = Cut::of(in, j.vocab);
-    const uint32_t per = (cut.n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits, from = min(rank * per, cut.n_vecs);
-    const uint32_t n_here = min(from + per, cut.n_vecs) - from, loose = rank == 0 ? cut.loose : 0;
+    const uint32_t from = part_begin(cut, rank, j.rank_bits), n_here = part_begin(cut, rank + 1, j.rank_bits) - from, loose = rank == 0 ? cut.loose : 0;
     const T* vecs = in + cut.lead + from * N;
     const float weight = j.weight ? j.weight[row] : 1.0f;
     const bool on_grid = (reinterpret_cast<uintptr_t>(in) - reinterpret_cast<uintptr_t>(out)) % 16 == 0;
-    auto store = [&](uint32_t v, const Packed<T, N>& p) {
-        T* to = out + cut.lead + (from + v) * N;
-        if (on_grid) {
-            *reinterpret_cast<uint4*>(to) = p.v[0];
-        } else {
-            const T* e = reinterpret_cast<const T*>(&p.v[0]);
-#pragma unroll
-            for (int i = 0; i < N; ++i) to[i] = e[i];
-        }
-    };
+    const bool joined = MODE != kGrad && j.rank_bits;
+    if (joined) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 
     Shares share = {};
     if (MODE == kGrad && weight != 0.0f) {
         const float* st = j.stats + static_cast<uint64_t>(row) * kStats;
         share = {st[0], st[1], st[2], st[3], st[4], st[5]};
     }
-    if (weight == 0.0f || (MODE == kGrad && share.live == 0.0f)) {
-        if (MODE != kGrad && rank == 0 && tid == 0) {
-            if (j.loss) j.loss[row] = 0.0f;
-            if (MODE == kLoss && j.stats) {
-                float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
-                st[0] = st[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            }
-        }
-        if (MODE != kLoss) {
-            Packed<T, N> zero;
-            zero.v[0] = make_uint4(0, 0, 0, 0);
-            for (uint32_t v = tid; v < n_here; v += kThreads) store(v, zero);
-            if (tid < loose) out[cut.loose_at<T>(tid)] = from_float<T>(0.0f);
-        }
-        return;
-    }
-    const bool joined = MODE != kGrad && j.rank_bits;
-    if (joined) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    const bool read = weight != 0.0f && (MODE != kGrad || share.live != 0.0f);
 
     // the thread's vectors in four groups of copies
     const uint32_t turns = (n_here + kThreads - 1) / kThreads, quarter = (turns + 4 * kBatch - 1) / (4 * kBatch) * kBatch;
-    if (STAGED) {
-        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(s_data)) + tid * 16;
-        const uint32_t whole = n_here / kThreads;
+    if (STAGED && read) {
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(s_data)) + tid * 16, whole = n_here / kThreads;
         const char* at = reinterpret_cast<const char*>(vecs + tid * N);
         uint32_t i = 0;
 #pragma unroll
@@ -334,254 +365,239 @@ __global__ void __launch_bounds__(kThreads, MODE == kLoss ? 6 : 4) k_distill(con
     float* const s_s = s_t + j.k;
     uint32_t* const s_bits = reinterpret_cast<uint32_t*>(s_s + j.k);        // of this block's entries, with a normaliser
     const bool tail = j.lse != nullptr;
-    for (uint32_t i = tid; i < 1u << j.table_bits; i += kThreads) s_table[i] = ~0ull;
-    if (tail && MODE != kGrad)
-        for (uint32_t i = tid; i < (n_here * N + loose + 31) / 32; i += kThreads) s_bits[i] = 0;
-    __syncthreads();
-    for (uint32_t i = tid; i < j.k; i += kThreads) {
-        const uint64_t at = j.idx.offset(row) + i;
-        const int64_t v = j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at]
-                                                    : reinterpret_cast<const int32_t*>(j.idx.data)[at];
-        s_t[i] = load_value(j.val, j.val.offset(row) + i);
-        if (v >= j.vocab && rank == 0) record_error(j.status, ADACOMP_ERR_INVALID);
-        const uint32_t token = v >= 0 && v < j.vocab ? static_cast<uint32_t>(v) : kNone;
-        s_idx[i] = token;
-        if (token == kNone) continue;
-        s_s[i] = to_float(in[token]);
-        const uint64_t mine = static_cast<uint64_t>(token) << 32 | i;
-        for (uint32_t at = token * 2654435761u >> (32 - j.table_bits);; at = (at + 1) & ((1u << j.table_bits) - 1)) {      // half of it stays empty
-            const uint64_t there = atomicCAS(reinterpret_cast<unsigned long long*>(&s_table[at]), ~0ull, mine);
-            if (there >> 32 == token) atomicMin(reinterpret_cast<unsigned long long*>(&s_table[at]), mine);
-            if (there == ~0ull || there >> 32 == token) break;
-        }
-    }
-    __syncthreads();
-    const double lse = tail ? static_cast<double>(j.lse[row]) : 0.0;
-    {
-        ListPart part = {0.0, -INFINITY, 0, {-INFINITY, 0.0f}};
-        for (uint32_t i = tid; i < j.k; i += kThreads) {
-            const uint32_t token = s_idx[i];
-            if (token == kNone) continue;
-            uint32_t at = token * 2654435761u >> (32 - j.table_bits);
-            while (s_table[at] >> 32 != token) at = (at + 1) & ((1u << j.table_bits) - 1);
-            if (static_cast<uint32_t>(s_table[at]) != i) {
-                s_idx[i] = kNone;
-                continue;
-            }
-            if (MODE == kGrad) continue;
-            part.present = 1;
-            part.top = fmaxf(part.top, s_t[i]);
-            if (tail) {
-                part.student.raise(s_s[i], j.c);
-                part.student.s += exp_from(s_s[i], part.student.base(), j.c);
-                const uint32_t behind = token - cut.lead;
-                uint32_t bit = kNone;
-                if (token >= cut.lead && behind / N < cut.n_vecs) bit = behind / N - from < n_here ? behind - from * N : kNone;
-                else if (rank == 0) bit = n_here * N + (token < cut.lead ? token : token - cut.n_vecs * N);
-                if (bit != kNone) atomicOr(&s_bits[bit / 32], 1u << bit % 32);
-            }
-        }
-        if (MODE != kGrad && warp * 32 < j.k) {
-            part.top = warp_max(part.top);
-            const float base = part.top == -INFINITY ? 0.0f : part.top;
-            for (uint32_t i = tid; i < j.k; i += kThreads)
-                if (s_idx[i] != kNone) {
-                    // with the teacher's normaliser 1 - sum q is left over: small where the list says almost everything, so in 64 bits
-                    const double t = tail ? exp(s_t[i] * j.inv_t - lse) : expf(static_cast<float>((static_cast<double>(s_t[i]) - base) * j.inv_t));
-                    part.q += t > 1e300 ? NAN : t;
-                }
-            part.q = warp_sum(part.q);
-            part.present = __any_sync(~0u, part.present);
-            if (tail) part.student = warp_join(part.student, j.c);
-            if (lane == 0) s_list[warp] = part;
-        }
-        if (tail && MODE != kGrad) __syncthreads();         // the bits
-    }
-
-    if (MODE != kGrad) {
-        // the sum, with a normaliser over what is not listed
-        Running r = {-INFINITY, 0.0f};
-        auto vec = [&](uint32_t v) { return STAGED ? s_data[v] : load16_once(vecs + v * N); };
-        auto add = [&](auto& p, uint32_t v0) {      // vectors v0, v0 + kThreads ...
-            constexpr int kHere = sizeof(p) / sizeof(uint4);
-            float most = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kHere; ++i) {
-                if (tail) {
-                    const uint32_t b = (v0 + i * kThreads) * N, bits = s_bits[b / 32] >> b % 32 & ((1u << N) - 1);
-                    if (bits) p[i] = without<T>(p[i], bits);
-                }
-                most = fmaxf(most, vec_max<T>(p[i]));
-            }
-            r.raise(most, j.c);
-            const float base = r.base();
-            if (fabsf(base) < kWild) {
-                const float shift = -base * j.c;
-                float2 sum = make_float2(0.0f, 0.0f);
-#pragma unroll
-                for (int i = 0; i < kHere; ++i) sum = vec_exps<T>(p[i], sum, j.c, shift);
-                r.s += sum.x + sum.y;
-            } else {
-#pragma unroll
-                for (int i = 0; i < kHere; ++i)
-#pragma unroll 1
-                    for (int e = 0; e < N; ++e) r.s += exp_from(pick<T>(p[i], e), base, j.c);
-            }
-        };
-        auto span = [&](uint32_t i, uint32_t end) {            // turns of the thread
-            const uint32_t whole = min(end, n_here / kThreads);
-            for (; i + kBatch <= whole; i += kBatch) {
-                uint4 p[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) p[u] = vec((i + u) * kThreads + tid);
-                add(p, i * kThreads + tid);
-            }
-#pragma unroll 1
-            for (; i < end && i * kThreads + tid < n_here; ++i) {
-                uint4 p[1] = {vec(i * kThreads + tid)};
-                add(p, i * kThreads + tid);
-            }
-        };
-        // (in this order without copies too: the same sums then, to the last bit)
-        if (STAGED) copies_wait<3>();
-        span(0, quarter);
-        if (STAGED) copies_wait<2>();
-        span(quarter, 2 * quarter);
-        if (STAGED) copies_wait<1>();
-        span(2 * quarter, 3 * quarter);
-        if (STAGED) copies_wait<0>();
-        span(3 * quarter, turns);
-        if (tid < loose) {
-            const float x = to_float(in[cut.loose_at<T>(tid)]);
-            const uint32_t b = n_here * N + tid;
-            r.raise(x, j.c);
-            if (!tail || !(s_bits[b / 32] >> b % 32 & 1)) r.s += exp_from(x, r.base(), j.c);
-        }
-        r = warp_join(r, j.c);
-        if (lane == 0) s_warp[warp] = r;
+    const uint32_t parts = min((j.k + 31) / 32, static_cast<uint32_t>(kWarps));          // warps with a part of the list
+    const double lse = tail && read ? static_cast<double>(j.lse[row]) : 0.0;
+    float top = -INFINITY, base = -INFINITY;        // the largest listed logits of the teacher's, of the student's
+    bool present = false;
+    if (read) {
+        for (uint32_t i = tid; i < 1u << j.table_bits; i += kThreads) s_table[i] = ~0ull;
+        if (tail && MODE != kGrad)
+            for (uint32_t i = tid; i < (n_here * N + loose + 31) / 32; i += kThreads) s_bits[i] = 0;
         __syncthreads();
-        // the rest is the first warp's work
-        const Running none = {-INFINITY, 0.0f};
-        if (warp == 0) r = warp_join(lane < kWarps ? s_warp[lane] : none, j.c);
-        if (joined) {
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all blocks have started
-            if (tid < 1u << j.rank_bits) *cooperative_groups::this_cluster().map_shared_rank(&s_part[rank], tid) = r;
-            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            if (warp == 0) r = warp_join(lane < 1u << j.rank_bits ? s_part[lane] : none, j.c);
-        }
-        if (warp == 0) {
-            const bool given = lane < kWarps && lane * 32 < j.k;
-            const ListPart part = given ? s_list[lane] : ListPart{0.0, -INFINITY, 0, none};
-            const float top = warp_max(part.top);
-            const bool present = __any_sync(~0u, part.present);
-            const double q_sum = warp_sum(tail || part.top == top ? part.q : part.q * expf(static_cast<float>((static_cast<double>(part.top) - top) * j.inv_t)));
-            double left = 0.0;
-            Total all = {q_sum, 0.0, r.s, 0.0f, top};
-            if (tail) {
-                Running student = warp_join(part.student, j.c);
-                const float m = fmaxf(r.m, student.m);
-                all.rest = r.m == m ? r.s : r.s * Running::lowered(r.m, m, j.c);
-                student.join(m, 0.0f, j.c);
-                r = {m, all.rest + student.s};
-                all.total = r.s;
-                left = all.rest > 0.0f && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
-                all.left = left;
+        for (uint32_t i = tid; i < j.k; i += kThreads) {
+            const uint64_t at = j.idx.offset(row) + i;
+            const int64_t v = j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at]
+                                                        : reinterpret_cast<const int32_t*>(j.idx.data)[at];
+            s_t[i] = load_value(j.val, j.val.offset(row) + i);
+            if (v >= j.vocab && rank == 0) record_error(j.status, ADACOMP_ERR_INVALID);
+            const uint32_t token = v >= 0 && v < j.vocab ? static_cast<uint32_t>(v) : kNone;
+            s_idx[i] = token;
+            if (token == kNone) continue;
+            s_s[i] = to_float(in[token]);
+            const uint64_t mine = static_cast<uint64_t>(token) << 32 | i;
+            for (uint32_t at = token * 2654435761u >> (32 - j.table_bits);; at = (at + 1) & ((1u << j.table_bits) - 1)) {      // half of it stays empty
+                const uint64_t there = atomicCAS(reinterpret_cast<unsigned long long*>(&s_table[at]), ~0ull, mine);
+                if (there >> 32 == token) atomicMin(reinterpret_cast<unsigned long long*>(&s_table[at]), mine);
+                if (there == ~0ull || there >> 32 == token) break;
             }
-            if (present && (tail ? lse != -INFINITY : top != -INFINITY || q_sum != q_sum) && r.s != 0.0f) {
-                const float unit = 1.0f / r.s;
+        }
+        __syncthreads();
+        if (warp < parts) {
+            for (uint32_t i = tid; i < j.k; i += kThreads) {
+                const uint32_t token = s_idx[i];
+                if (token == kNone) continue;
+                uint32_t at = token * 2654435761u >> (32 - j.table_bits);
+                while (s_table[at] >> 32 != token) at = (at + 1) & ((1u << j.table_bits) - 1);
+                if (static_cast<uint32_t>(s_table[at]) != i) {
+                    s_idx[i] = kNone;
+                    continue;
+                }
+                present = true;
+                top = fmaxf(top, s_t[i]);
+                base = fmaxf(base, s_s[i]);
+                if (tail && MODE != kGrad) {
+                    const uint32_t behind = token - cut.lead;
+                    uint32_t bit = kNone;
+                    if (token >= cut.lead && behind / N < cut.n_vecs) bit = behind / N - from < n_here ? behind - from * N : kNone;
+                    else if (rank == 0) bit = n_here * N + (token < cut.lead ? token : token - cut.n_vecs * N);
+                    if (bit != kNone) atomicOr(&s_bits[bit / 32], 1u << bit % 32);
+                }
+            }
+            if (MODE != kGrad) {
+                top = warp_max(top);
+                base = warp_max(base);
+                if (lane == 0) s_max[0][warp] = top, s_max[1][warp] = base;
+            }
+        }
+    }
+    if (MODE != kGrad) {
+        present = __syncthreads_or(present);        // (nobody's where the row is not read)
+        if (present) {
+            for (uint32_t w = 0; w < parts; ++w) top = fmaxf(top, s_max[0][w]), base = fmaxf(base, s_max[1][w]);
+            if (warp < parts) {                     // the teacher's sum (with a normaliser that of q), the student's over the list
+                const float t_base = top == -INFINITY ? 0.0f : top, s_base = base == -INFINITY ? 0.0f : base;
+                double q = 0.0;
+                float listed = 0.0f;
+                for (uint32_t i = tid; i < j.k; i += kThreads)
+                    if (s_idx[i] != kNone) {
+                        // with a normaliser 1 - sum q is left over: small where the list says almost everything, so in 64 bits
+                        const double x = tail ? exp(s_t[i] * j.inv_t - lse) : expf(static_cast<float>((static_cast<double>(s_t[i]) - t_base) * j.inv_t));
+                        q += x > 1e300 ? NAN : x;
+                        if (tail) listed += exp_from(s_s[i], s_base, j.c);
+                    }
+                q = warp_sum(q);
+                listed = warp_sum(listed);
+                if (lane == 0) s_q[warp] = q, s_listed[warp] = listed;
+            }
+            // the sum, with a normaliser over what is not listed
+            Chunk<T, STAGED> chunk = {in, vecs, s_data, tail ? s_bits : nullptr, cut, n_here, loose};
+            const float shift = -base * j.c;
+            const uint32_t lowest = pack2_of<T>(-INFINITY);
+            float2 sum = make_float2(0.0f, 0.0f);
+            auto span = [&](uint32_t i, uint32_t end) {            // turns of the thread, kBatch at a time
+#pragma unroll 1
+                for (; i < end; i += kBatch) {
+                    const uint32_t v0 = i * kThreads + tid;
+                    uint4 p[kBatch];
+                    if (v0 + (kBatch - 1) * kThreads < n_here) {
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u) p[u] = chunk.vec(v0 + u * kThreads);
+                    } else {                        // nothing adds nothing
+#pragma unroll
+                        for (int u = 0; u < kBatch; ++u) {
+                            p[u] = make_uint4(lowest, lowest, lowest, lowest);
+                            if (v0 + u * kThreads < n_here) p[u] = chunk.vec(v0 + u * kThreads);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        if (tail) {
+                            const uint32_t bits = chunk.out_bits(min(v0 + u * kThreads, n_here));
+                            if (bits) p[u] = without<T>(p[u], bits);
+                        }
+                        sum = vec_exps<T>(p[u], sum, j.c, shift);
+                    }
+                }
+            };
+            if (STAGED) copies_wait<3>();
+            span(0, min(quarter, turns));
+            if (STAGED) copies_wait<2>();
+            span(quarter, min(2 * quarter, turns));
+            if (STAGED) copies_wait<1>();
+            span(2 * quarter, min(3 * quarter, turns));
+            if (STAGED) copies_wait<0>();
+            span(3 * quarter, turns);
+            if (tid < loose && !chunk.loose_out(tid)) sum.x += exp_from(to_float(in[cut.loose_at<T>(tid)]), base, j.c);
+            float rest = warp_sum(sum.x + sum.y);
+            if (lane == 0) s_sum[warp] = rest;
+            __syncthreads();
+            rest = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) rest += s_sum[w];
+            if (joined) {
+                asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all blocks have started
+                rest = cluster_gather<8>(s_part[0], Running{0.0f, rest}, rank, j.rank_bits, Running{0.0f, 0.0f},
+                                         [](const Running& x) { return Running{0.0f, warp_sum(x.s)}; }).s;
+            }
+            double q_sum = 0.0, left = 0.0;
+            for (uint32_t w = 0; w < parts; ++w) q_sum += s_q[w];
+            float listed = 0.0f, total = rest;
+            if (tail) {
+                for (uint32_t w = 0; w < parts; ++w) listed += s_listed[w];
+                total = rest + listed;
+            }
+            if (!(total < INFINITY) || !(fabsf(base) < kWild)) {
+                const Running r = careful_sum<T, STAGED, THREADS>(chunk, j.c, s_warp, s_part[1], rank, j.rank_bits);
+                const float m = tail ? fmaxf(r.m, base) : r.m;
+                rest = r.m == m ? r.s : r.s * Running::lowered(r.m, m, j.c);
+                if (tail && base != m) listed *= Running::lowered(base, m, j.c);
+                base = m;
+                total = tail ? rest + listed : rest;
+            }
+            if ((tail ? lse != -INFINITY : top != -INFINITY || q_sum != q_sum) && total != 0.0f) {
+                const float unit = 1.0f / total;
+                base = base == -INFINITY ? 0.0f : base;
                 if (tail) {
-                    const float mass = static_cast<float>(q_sum + left), over = left > 0.0 ? static_cast<float>(left) / all.rest : 0.0f;
-                    share = {r.base(), mass * unit - over, mass * unit, static_cast<float>(lse), 1.0f, 1.0f};
+                    left = rest > 0.0f && q_sum < 1.0 ? 1.0 - q_sum : 0.0;
+                    const float mass = static_cast<float>(q_sum + left), over = left > 0.0 ? static_cast<float>(left) / rest : 0.0f;
+                    share = {base, mass * unit - over, mass * unit, static_cast<float>(lse), 1.0f, 1.0f};
                 } else {
-                    share = {r.base(), unit, unit, top, 1.0f / static_cast<float>(q_sum), 1.0f};
+                    share = {base, unit, unit, top, 1.0f / static_cast<float>(q_sum), 1.0f};
                 }
                 if (q_sum != q_sum) share.rest = share.listed = NAN;
             }
-            if (lane == 0) s_share = share, s_total = all;
+            // the loss is one warp's work
+            if (rank == 0 && warp == kWarps - 1 && j.loss) {
+                double loss = 0.0;
+                if (share.live != 0.0f) {
+                    const double from_m = reference(share.m, j.c);
+                    double cross = 0.0;
+                    for (uint32_t i = lane; i < j.k; i += 32) {
+                        if (s_idx[i] == kNone) continue;
+                        const double t = tail ? s_t[i] * j.inv_t - lse : (static_cast<double>(s_t[i]) - top) * j.inv_t;
+                        const double q = tail ? exp(t) : expf(static_cast<float>(t));
+                        if (q != 0.0) cross += q * (t - (static_cast<double>(s_s[i]) * j.c - from_m) * kLn2);
+                    }
+                    cross = warp_sum(cross);
+                    const double log_total = log(static_cast<double>(total));
+                    if (!tail) loss = cross / q_sum - log(q_sum) + log_total;
+                    else loss = cross + q_sum * log_total + (left > 0.0 ? left * (log(left) - log(static_cast<double>(rest)) + log_total) : 0.0);
+                    if (q_sum != q_sum) loss = NAN;
+                }
+                if (lane == 0) j.loss[row] = static_cast<float>(loss);
+            }
+        } else {
+            if (rank == 0 && tid == 0 && j.loss) j.loss[row] = 0.0f;
+            if (joined) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (STAGED) copies_wait<0>();
         }
-        __syncthreads();
-        share = s_share;
         if (MODE == kLoss && j.stats && rank == 0 && tid == 0) {
             float4* st = reinterpret_cast<float4*>(j.stats + static_cast<uint64_t>(row) * kStats);
             st[0] = make_float4(share.m, share.rest, share.listed, share.t_base);
             st[1] = make_float4(share.q_scale, share.live, 0.0f, 0.0f);
         }
-        // the loss is the last one's
-        if (rank == 0 && warp == kWarps - 1 && j.loss) {
-            double loss = 0.0;
-            if (share.live != 0.0f) {
-                const Total all = s_total;
-                const double from_m = reference(share.m, j.c);
-                double cross = 0.0, sum = 0.0;
-                for (uint32_t i = lane; i < j.k; i += 32) {
-                    if (s_idx[i] == kNone) continue;
-                    const double t = tail ? s_t[i] * j.inv_t - lse : (static_cast<double>(s_t[i]) - all.top) * j.inv_t;
-                    const double q = tail ? exp(t) : expf(static_cast<float>(t));
-                    sum += q;
-                    if (q != 0.0) cross += q * (t - (static_cast<double>(s_s[i]) * j.c - from_m) * kLn2);
-                }
-                cross = warp_sum(cross), sum = warp_sum(sum);
-                const double log_total = log(static_cast<double>(all.total));
-                if (!tail) loss = cross / sum - log(sum) + log_total;
-                else loss = cross + sum * log_total + (all.left > 0.0 ? all.left * (log(all.left) - log(static_cast<double>(all.rest)) + log_total) : 0.0);
-                if (all.q != all.q) loss = NAN;
-            }
-            if (lane == 0) j.loss[row] = static_cast<float>(loss);
-        }
     }
 
     if (MODE != kLoss) {
+        const bool live = share.live != 0.0f;
+        const Chunk<T, STAGED> chunk = {in, vecs, s_data, nullptr, cut, n_here, loose};
         const float g = static_cast<float>(weight * j.inv_t), rest = share.rest * g;
-        const bool wild = !(fabsf(share.m) < kWild) || share.live == 0.0f;
-        const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-share.m * j.c, -share.m * j.c);
-        auto gradient = [&](const uint4& x, uint32_t v) {
-            Packed<T, N> p;
-            p.v[0] = x;
-            float f[N];
-            p.unpack(f);
-#pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
-                f[e] = ex2(y.x) * rest;
-                f[e + 1] = ex2(y.y) * rest;
-            }
-            p.pack(f);
-            store(v, p);
-        };
-        auto vec = [&](uint32_t v) { return STAGED ? s_data[v] : load16_once(vecs + v * N); };
+        T* to = out + cut.lead + from * N;
         float off_grid = 0.0f;
-        if (tid < loose) off_grid = to_float(in[cut.loose_at<T>(tid)]);
-        if (!wild) {
-            uint32_t i = 0;
-            for (; i + kBatch <= n_here / kThreads; i += kBatch) {
-                uint4 p[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) p[u] = vec((i + u) * kThreads + tid);
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u) gradient(p[u], (i + u) * kThreads + tid);
-            }
+        if (live && tid < loose) off_grid = to_float(in[cut.loose_at<T>(tid)]);
+        if (MODE == kGrad && read) __syncthreads();         // the list's logits have been read: in place the gradient overwrites them
+        if (live && on_grid && fabsf(share.m) < kWild) {
+            const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-share.m * j.c, -share.m * j.c), rest2 = make_float2(rest, rest);
 #pragma unroll 1
-            for (uint32_t v = i * kThreads + tid; v < n_here; v += kThreads) gradient(vec(v), v);
-        } else {
+            for (uint32_t v0 = tid; v0 < n_here; v0 += kBatch * kThreads) {
+                Packed<T, N> p[kBatch];
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u)
+                    if (v0 + u * kThreads < n_here) p[u].v[0] = chunk.vec(v0 + u * kThreads);
+#pragma unroll
+                for (int u = 0; u < kBatch; ++u) {
+                    float f[N];
+                    p[u].unpack(f);
+#pragma unroll
+                    for (int e = 0; e < N; e += 2) {
+                        const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
+                        const float2 z = mul2(make_float2(ex2(y.x), ex2(y.y)), rest2);
+                        f[e] = z.x, f[e + 1] = z.y;
+                    }
+                    p[u].pack(f);
+                    if (v0 + u * kThreads < n_here) *reinterpret_cast<uint4*>(to + (v0 + u * kThreads) * N) = p[u].v[0];
+                }
+            }
+        } else if (!live && on_grid) {
+            for (uint32_t v = tid; v < n_here; v += kThreads) *reinterpret_cast<uint4*>(to + v * N) = make_uint4(0, 0, 0, 0);
+        } else {                                    // rows of huge numbers, outputs on another grid
 #pragma unroll 1
             for (uint32_t v = tid; v < n_here; v += kThreads) {
-                const uint4 x = vec(v);
-                T* to = out + cut.lead + (from + v) * N;
+                const uint4 x = live ? chunk.vec(v) : make_uint4(0, 0, 0, 0);
 #pragma unroll 1
-                for (int e = 0; e < N; ++e) to[e] = from_float<T>(share.live != 0.0f ? exp_from(pick<T>(x, e), share.m, j.c) * rest : 0.0f);
+                for (int e = 0; e < N; ++e) to[v * N + e] = from_float<T>(live ? exp_from(pick<T>(x, e), share.m, j.c) * rest : 0.0f);
             }
         }
-        if (tid < loose) out[cut.loose_at<T>(tid)] = from_float<T>(share.live != 0.0f ? exp_from(off_grid, share.m, j.c) * rest : 0.0f);
+        if (tid < loose) out[cut.loose_at<T>(tid)] = from_float<T>(live ? exp_from(off_grid, share.m, j.c) * rest : 0.0f);
+        if (!live) return;
         __syncthreads();                            // the listed ones replace what has just been written
-        if (share.live != 0.0f)
-            for (uint32_t i = tid; i < j.k; i += kThreads) {
-                const uint32_t token = s_idx[i], behind = token - cut.lead;
-                if (token == kNone || !(token >= cut.lead && behind / N < cut.n_vecs ? behind / N - from < n_here : rank == 0)) continue;
-                const double t = tail ? s_t[i] * j.inv_t - share.t_base : (static_cast<double>(s_t[i]) - share.t_base) * j.inv_t;
-                const float q = expf(static_cast<float>(t)) * share.q_scale;
-                out[token] = from_float<T>((exp_from(s_s[i], share.m, j.c) * share.listed - q) * g);
-            }
+        for (uint32_t i = tid; i < j.k; i += kThreads) {
+            const uint32_t token = s_idx[i], behind = token - cut.lead;
+            if (token == kNone || !(token >= cut.lead && behind / N < cut.n_vecs ? behind / N - from < n_here : rank == 0)) continue;
+            const double t = tail ? s_t[i] * j.inv_t - share.t_base : (static_cast<double>(s_t[i]) - share.t_base) * j.inv_t;
+            const float q = expf(static_cast<float>(t)) * share.q_scale;
+            out[token] = from_float<T>((exp_from(s_s[i], share.m, j.c) * share.listed - q) * g);
+        }
     }
 }
 
@@ -968,17 +984,17 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
 
 bool good_temperature(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 
-template <typename T, int MODE, bool STAGED> int launch_shape(Job j, uint32_t chunk_vecs, cudaStream_t stream) {
+template <typename T, int MODE, bool STAGED, int THREADS> int launch_shape(Job j, uint32_t chunk_vecs, cudaStream_t stream) {
     const uint32_t data = STAGED ? chunk_vecs * 16 : 0;
     j.at_table = data;
     j.table_bits = 5;
     while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
     const uint32_t bits = j.lse && MODE != kGrad ? ((chunk_vecs + 2) * kVec<T> + 31) / 32 * 4 : 0;
     const size_t shared = data + (8ull << j.table_bits) + j.k * 12ull + bits;
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
+    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, STAGED, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(j.n_rows << j.rank_bits);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -988,24 +1004,28 @@ template <typename T, int MODE, bool STAGED> int launch_shape(Job j, uint32_t ch
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = MODE != kGrad && j.rank_bits ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_distill<T, MODE, STAGED>, j);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_distill<T, MODE, STAGED, THREADS>, j);
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
 
+constexpr uint32_t kChunk = 104 * 1024;
+constexpr uint32_t kSmallChunk = 72 * 1024;
+
 template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_t stream) {
     // as many blocks to a row as its chunks need, and more while the call has fewer blocks than SMs and chunks are not short
     const uint32_t n_vecs = j.vocab / kVec<T> + 1;
     while (j.rank_bits < kClusterBits &&
-           (n_vecs * 16ull >> j.rank_bits > kChunk ||
-            ((static_cast<uint64_t>(j.n_rows) << j.rank_bits) * 2 <= 2ull * n_sms && n_vecs >> j.rank_bits >= 4 * kThreads)))
+           ((MODE == kBoth && n_vecs * 16ull >> j.rank_bits > kChunk) || (n_vecs >> j.rank_bits) * kVec<T> > kMaxVocab / 4 ||
+            ((static_cast<uint64_t>(j.n_rows) << j.rank_bits) * 2 <= 2ull * n_sms && n_vecs >> j.rank_bits >= 1024)))
         ++j.rank_bits;
     const uint32_t chunk_vecs = (n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits;
     if constexpr (MODE == kBoth) {
-        if (chunk_vecs * 16ull <= kLargestChunk) return launch_shape<T, MODE, true>(j, chunk_vecs, stream);
+        if (chunk_vecs * 16ull <= kSmallChunk) return launch_shape<T, MODE, true, 256>(j, chunk_vecs, stream);
+        if (chunk_vecs * 16ull <= kLargestChunk) return launch_shape<T, MODE, true, 512>(j, chunk_vecs, stream);
     }
-    return launch_shape<T, MODE, false>(j, chunk_vecs, stream);
+    return launch_shape<T, MODE, false, 256>(j, chunk_vecs, stream);
 }
 
 template <int MODE>
