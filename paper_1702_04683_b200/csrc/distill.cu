@@ -29,7 +29,6 @@ constexpr uint32_t kMaxPairs = 1024;
 constexpr uint32_t kMaxVocab = 1u << 20;
 constexpr uint32_t kStats = 8;
 constexpr uint32_t kClusterBits = 3;               // blocks of the largest cluster
-constexpr uint32_t kLargestChunk = 192 * 1024;
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 constexpr double kLog2e = 1.4426950408889634, kLn2 = 0.6931471805599453;
 
@@ -172,6 +171,7 @@ struct Job {
     int* status;
     uint32_t n_rows, vocab, k, rank_bits;
     uint32_t at_table, table_bits;  // place in shared memory, size
+    uint32_t staged;                // vectors of a block that are copied to shared memory
     float c;                        // log2(e) / T
     double inv_t;
 };
@@ -248,15 +248,35 @@ __device__ __forceinline__ uint32_t part_begin(const Cut& cut, uint32_t rank, ui
     return min(rank * ((cut.n_vecs + (1u << rank_bits) - 1) >> rank_bits), cut.n_vecs);
 }
 
+// Where the sums' and the gradient's logits come from: device memory both times, shared memory, or that as far as it reaches.
+enum Place { kDevice = 0, kShared = 1, kPartly = 2 };
+
 // A block's share of a row: vectors on the grid, and the first block's entries beside it.
-template <typename T, bool STAGED> struct Chunk {
+template <typename T, int PLACE> struct Chunk {
     const T* in;
     const T* vecs;
     const uint4* s_data;
     const uint32_t* s_bits;         // which entries are left out of the sum, or nullptr
     Cut cut;
-    uint32_t n, loose;
-    __device__ __forceinline__ uint4 vec(uint32_t v) const { return STAGED ? s_data[v] : load16_once(vecs + v * kVec<T>); }
+    uint32_t n, loose, staged;      // vectors, entries beside them, vectors in shared memory
+    __device__ __forceinline__ bool shared(uint32_t v) const { return PLACE == kShared || (PLACE == kPartly && v < staged); }
+    __device__ __forceinline__ uint4 vec(uint32_t v) const { return shared(v) ? s_data[v] : load16_once(vecs + v * kVec<T>); }
+    // Vectors v0, v0 + THREADS ... as far as there are any, from one place or the other (staged is a multiple of their number).
+    template <int BATCH, int THREADS> __device__ __forceinline__ void batch(uint4 (&p)[BATCH], uint32_t v0, uint32_t otherwise) const {
+        const bool whole = v0 + (BATCH - 1) * THREADS < n;
+        if (!whole)
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) p[u] = make_uint4(otherwise, otherwise, otherwise, otherwise);
+        if (shared(v0)) {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u)
+                if (whole || v0 + u * THREADS < n) p[u] = s_data[v0 + u * THREADS];
+        } else {
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u)
+                if (whole || v0 + u * THREADS < n) p[u] = load16_once(vecs + (v0 + u * THREADS) * kVec<T>);
+        }
+    }
     __device__ __forceinline__ uint32_t out_bits(uint32_t v) const {        // of vector v; of the entries off the grid, v = n
         const uint32_t b = v * kVec<T>;
         return s_bits[b / 32] >> b % 32 & ((1u << kVec<T>) - 1);
@@ -277,8 +297,8 @@ template <uint32_t RANKS_MOST, typename V, typename F> __device__ __forceinline_
 
 // The sum relative to the largest of the entries themselves, found on the way: for rows whose logits lie so far from the listed ones
 // that the sum relative to those overflows, and for rows without numbers.
-template <typename T, bool STAGED, int THREADS>
-__device__ __noinline__ Running careful_sum(const Chunk<T, STAGED> chunk, float c, Running* s_warp, Running* s_part, uint32_t rank, uint32_t rank_bits) {
+template <typename T, int PLACE, int THREADS>
+__device__ __noinline__ Running careful_sum(const Chunk<T, PLACE> chunk, float c, Running* s_warp, Running* s_part, uint32_t rank, uint32_t rank_bits) {
     const uint32_t tid = threadIdx.x, lane = tid % 32;
     Running r = {-INFINITY, 0.0f};
 #pragma unroll 1
@@ -311,11 +331,12 @@ __device__ __noinline__ Running careful_sum(const Chunk<T, STAGED> chunk, float 
 // vectors in two passes: the sum, of which the cluster's blocks tell each other through shared memory, and the gradient.  Every
 // block reads the whole list, while its vectors are on their way.  The sum is taken relative to the student's largest LISTED logit, which
 // is mostly the largest of all or near it, so that no maximum has to be looked for; where it overflows, it is taken once more with care.
-// STAGED: a thread's vectors are copied to shared memory by itself and stay there for the second pass, so that a logit crosses HBM once and
-// nothing waits for a load but its own thread; rows too long for a cluster's shared memory are read twice.
-template <typename T, int MODE, bool STAGED, int THREADS>
+// PLACE: a thread's vectors are copied to shared memory by itself and stay there for the second pass, so that a logit crosses HBM once and
+// nothing waits for a load but its own thread; of rows too long for that the rest is read twice.
+template <typename T, int MODE, int PLACE, int THREADS>
 __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREADS) k_distill(const Job j) {
     constexpr int N = kVec<T>, kBatch = 4, kWarps = THREADS / 32;
+    constexpr bool STAGED = PLACE != kDevice;
     constexpr uint32_t kThreads = THREADS;
     extern __shared__ uint4 s_data[];               // [vectors of a block] if STAGED, then what follows
     __shared__ float s_max[2][kWarps], s_sum[kWarps], s_listed[kWarps];
@@ -341,16 +362,17 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
     const bool read = weight != 0.0f && (MODE != kGrad || share.live != 0.0f);
 
     // the thread's vectors in four groups of copies
-    const uint32_t turns = (n_here + kThreads - 1) / kThreads, quarter = (turns + 4 * kBatch - 1) / (4 * kBatch) * kBatch;
+    const uint32_t staged = PLACE == kPartly ? j.staged : 0, n_staged = PLACE == kPartly ? min(n_here, staged) : n_here;
+    const uint32_t turns = (n_staged + kThreads - 1) / kThreads, quarter = (turns + 4 * kBatch - 1) / (4 * kBatch) * kBatch;
     if (STAGED && read) {
-        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(s_data)) + tid * 16, whole = n_here / kThreads;
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(s_data)) + tid * 16, whole = n_staged / kThreads;
         const char* at = reinterpret_cast<const char*>(vecs + tid * N);
         uint32_t i = 0;
 #pragma unroll
         for (int g = 1; g <= 4; ++g) {
             for (const uint32_t end = min(g * quarter, whole); i < end; ++i, at += kThreads * 16) copy16(to + i * (kThreads * 16), at);
             if (i < min(g * quarter, turns)) {
-                if (i * kThreads + tid < n_here) copy16(to + i * (kThreads * 16), at);
+                if (i * kThreads + tid < n_staged) copy16(to + i * (kThreads * 16), at);
                 ++i;
             }
             copies_end();
@@ -440,7 +462,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
                 if (lane == 0) s_q[warp] = q, s_listed[warp] = listed;
             }
             // the sum, with a normaliser over what is not listed
-            Chunk<T, STAGED> chunk = {in, vecs, s_data, tail ? s_bits : nullptr, cut, n_here, loose};
+            Chunk<T, PLACE> chunk = {in, vecs, s_data, tail ? s_bits : nullptr, cut, n_here, loose, staged};
             const float shift = -base * j.c;
             const uint32_t lowest = pack2_of<T>(-INFINITY);
             float2 sum = make_float2(0.0f, 0.0f);
@@ -449,16 +471,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
                 for (; i < end; i += kBatch) {
                     const uint32_t v0 = i * kThreads + tid;
                     uint4 p[kBatch];
-                    if (v0 + (kBatch - 1) * kThreads < n_here) {
-#pragma unroll
-                        for (int u = 0; u < kBatch; ++u) p[u] = chunk.vec(v0 + u * kThreads);
-                    } else {                        // nothing adds nothing
-#pragma unroll
-                        for (int u = 0; u < kBatch; ++u) {
-                            p[u] = make_uint4(lowest, lowest, lowest, lowest);
-                            if (v0 + u * kThreads < n_here) p[u] = chunk.vec(v0 + u * kThreads);
-                        }
-                    }
+                    chunk.template batch<kBatch, THREADS>(p, v0, lowest);          // nothing adds nothing
 #pragma unroll
                     for (int u = 0; u < kBatch; ++u) {
                         if (tail) {
@@ -469,14 +482,17 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
                     }
                 }
             };
-            if (STAGED) copies_wait<3>();
-            span(0, min(quarter, turns));
-            if (STAGED) copies_wait<2>();
-            span(quarter, min(2 * quarter, turns));
-            if (STAGED) copies_wait<1>();
-            span(2 * quarter, min(3 * quarter, turns));
-            if (STAGED) copies_wait<0>();
-            span(3 * quarter, turns);
+            if (STAGED) {
+                copies_wait<3>();
+                span(0, min(quarter, turns));
+                copies_wait<2>();
+                span(quarter, min(2 * quarter, turns));
+                copies_wait<1>();
+                span(2 * quarter, min(3 * quarter, turns));
+                copies_wait<0>();
+                span(3 * quarter, turns);
+            }
+            if (PLACE != kShared) span(STAGED ? turns : 0, (n_here + kThreads - 1) / kThreads);
             if (tid < loose && !chunk.loose_out(tid)) sum.x += exp_from(to_float(in[cut.loose_at<T>(tid)]), base, j.c);
             float rest = warp_sum(sum.x + sum.y);
             if (lane == 0) s_sum[warp] = rest;
@@ -497,7 +513,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
                 total = rest + listed;
             }
             if (!(total < INFINITY) || !(fabsf(base) < kWild)) {
-                const Running r = careful_sum<T, STAGED, THREADS>(chunk, j.c, s_warp, s_part[1], rank, j.rank_bits);
+                const Running r = careful_sum<T, PLACE, THREADS>(chunk, j.c, s_warp, s_part[1], rank, j.rank_bits);
                 const float m = tail ? fmaxf(r.m, base) : r.m;
                 rest = r.m == m ? r.s : r.s * Running::lowered(r.m, m, j.c);
                 if (tail && base != m) listed *= Running::lowered(base, m, j.c);
@@ -550,7 +566,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
 
     if (MODE != kLoss) {
         const bool live = share.live != 0.0f;
-        const Chunk<T, STAGED> chunk = {in, vecs, s_data, nullptr, cut, n_here, loose};
+        const Chunk<T, PLACE> chunk = {in, vecs, s_data, nullptr, cut, n_here, loose, staged};
         const float g = static_cast<float>(weight * j.inv_t), rest = share.rest * g;
         T* to = out + cut.lead + from * N;
         float off_grid = 0.0f;
@@ -558,24 +574,27 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREA
         if (MODE == kGrad && read) __syncthreads();         // the list's logits have been read: in place the gradient overwrites them
         if (live && on_grid && fabsf(share.m) < kWild) {
             const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-share.m * j.c, -share.m * j.c), rest2 = make_float2(rest, rest);
+            const uint32_t batches = (n_here + kBatch * kThreads - 1) / (kBatch * kThreads);
 #pragma unroll 1
-            for (uint32_t v0 = tid; v0 < n_here; v0 += kBatch * kThreads) {
-                Packed<T, N> p[kBatch];
-#pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-                    if (v0 + u * kThreads < n_here) p[u].v[0] = chunk.vec(v0 + u * kThreads);
+            for (uint32_t i = 0; i < batches; ++i) {
+                // from the back where anything is read a second time: first what was read last
+                const uint32_t v0 = (PLACE == kPartly ? batches - 1 - i : i) * (kBatch * kThreads) + tid;
+                uint4 x[kBatch];
+                chunk.template batch<kBatch, THREADS>(x, v0, 0u);
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     float f[N];
-                    p[u].unpack(f);
+                    Packed<T, N> p;
+                    p.v[0] = x[u];
+                    p.unpack(f);
 #pragma unroll
                     for (int e = 0; e < N; e += 2) {
                         const float2 y = fma2(make_float2(f[e], f[e + 1]), c2, shift);
                         const float2 z = mul2(make_float2(ex2(y.x), ex2(y.y)), rest2);
                         f[e] = z.x, f[e + 1] = z.y;
                     }
-                    p[u].pack(f);
-                    if (v0 + u * kThreads < n_here) *reinterpret_cast<uint4*>(to + (v0 + u * kThreads) * N) = p[u].v[0];
+                    p.pack(f);
+                    if (v0 + u * kThreads < n_here) *reinterpret_cast<uint4*>(to + (v0 + u * kThreads) * N) = p.v[0];
                 }
             }
         } else if (!live && on_grid) {
@@ -984,14 +1003,16 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
 
 bool good_temperature(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 
-template <typename T, int MODE, bool STAGED, int THREADS> int launch_shape(Job j, uint32_t chunk_vecs, cudaStream_t stream) {
-    const uint32_t data = STAGED ? chunk_vecs * 16 : 0;
+// Rows of loss_grad stay in shared memory as far as they find room there, next to those of the SM's other blocks.
+constexpr uint32_t kRoom = 110 * 1024;              // of a block of 512 threads, two on an SM
+constexpr uint32_t kSmallRoom = 74 * 1024;          // of one of 256, three on an SM
+
+template <typename T, int MODE, int PLACE, int THREADS> int launch_shape(Job j, uint32_t chunk_vecs, uint32_t beside, cudaStream_t stream) {
+    j.staged = PLACE == kPartly ? (kRoom - beside) / 16 / (4 * THREADS) * (4 * THREADS) : chunk_vecs;
+    const uint32_t data = PLACE == kDevice ? 0 : j.staged * 16;
     j.at_table = data;
-    j.table_bits = 5;
-    while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
-    const uint32_t bits = j.lse && MODE != kGrad ? ((chunk_vecs + 2) * kVec<T> + 31) / 32 * 4 : 0;
-    const size_t shared = data + (8ull << j.table_bits) + j.k * 12ull + bits;
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, STAGED, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
+    const size_t shared = data + beside;
+    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, PLACE, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(j.n_rows << j.rank_bits);
     cfg.blockDim = dim3(THREADS);
@@ -1004,28 +1025,32 @@ template <typename T, int MODE, bool STAGED, int THREADS> int launch_shape(Job j
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = MODE != kGrad && j.rank_bits ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_distill<T, MODE, STAGED, THREADS>, j);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_distill<T, MODE, PLACE, THREADS>, j);
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
 
-constexpr uint32_t kChunk = 104 * 1024;
-constexpr uint32_t kSmallChunk = 72 * 1024;
-
 template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_t stream) {
-    // as many blocks to a row as its chunks need, and more while the call has fewer blocks than SMs and chunks are not short
+    // several blocks to a row while the call has fewer blocks than SMs and their shares are not short, or where the bits of one
+    // would be too many
     const uint32_t n_vecs = j.vocab / kVec<T> + 1;
     while (j.rank_bits < kClusterBits &&
-           ((MODE == kBoth && n_vecs * 16ull >> j.rank_bits > kChunk) || (n_vecs >> j.rank_bits) * kVec<T> > kMaxVocab / 4 ||
+           ((n_vecs >> j.rank_bits) * kVec<T> > kMaxVocab / 4 ||
             ((static_cast<uint64_t>(j.n_rows) << j.rank_bits) * 2 <= 2ull * n_sms && n_vecs >> j.rank_bits >= 1024)))
         ++j.rank_bits;
     const uint32_t chunk_vecs = (n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits;
+    j.table_bits = 5;
+    while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
+    const uint32_t bits = j.lse && MODE != kGrad ? ((chunk_vecs + 2) * kVec<T> + 31) / 32 * 4 : 0;
+    const uint32_t beside = (8u << j.table_bits) + j.k * 12 + bits;         // the table, the list, the bits
     if constexpr (MODE == kBoth) {
-        if (chunk_vecs * 16ull <= kSmallChunk) return launch_shape<T, MODE, true, 256>(j, chunk_vecs, stream);
-        if (chunk_vecs * 16ull <= kLargestChunk) return launch_shape<T, MODE, true, 512>(j, chunk_vecs, stream);
+        if (chunk_vecs * 16ull + beside <= kSmallRoom) return launch_shape<T, MODE, kShared, 256>(j, chunk_vecs, beside, stream);
+        if (chunk_vecs * 16ull + beside <= kRoom) return launch_shape<T, MODE, kShared, 512>(j, chunk_vecs, beside, stream);
+        return launch_shape<T, MODE, kPartly, 512>(j, chunk_vecs, beside, stream);
+    } else {
+        return launch_shape<T, MODE, kDevice, 256>(j, chunk_vecs, beside, stream);
     }
-    return launch_shape<T, MODE, false, 256>(j, chunk_vecs, stream);
 }
 
 template <int MODE>
