@@ -7,8 +7,7 @@
 //   ds_i = d_i, or (d_i - (sum d s) / S) / S;      dl_i = ds_i s_i (1 - s_i)  (sigmoid)
 //   softmax: dl_e = s_e (ds_e - sum ds s); renormalised this vanishes outside of the chosen ones and is a softmax's over those
 //
-// A row is a warp's work.  Rows are short: large calls are bound by instruction issue (the rounds of the choice), small ones
-// by the launch.
+// Rows are short: large calls are bound by instruction issue (the rounds of the choice), small ones by the launch.
 #include <math.h>
 #include <new>
 
@@ -27,10 +26,12 @@ struct adacomp_route {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
 constexpr uint32_t kMaxExperts = 1024;
 constexpr uint32_t kMaxChosen = 32;
 constexpr uint32_t kMaxGroups = 32;
+constexpr double kLog2e = 1.4426950408889634;
 
 struct Job {
     Rows logits, out;
@@ -44,6 +45,7 @@ struct Job {
     uint32_t* ticket;
     int* status;
     uint32_t n_rows;
+    bool wide;                      // rows are on the 16-byte grid and E a whole number of lanes' shares
 };
 
 template <typename V> __device__ __forceinline__ V warp_sum(V x) {
@@ -61,62 +63,114 @@ template <typename V> __device__ __forceinline__ V warp_max(V x) {
     return x;
 }
 
-// The choice among a row's values s_v[0 .. experts) (-Inf: cannot be chosen), which are used up.  Lane i < top_k returns its place's
-// expert, or -1.  The result tells whether two candidates that a decision hung on lie within `tol` of each other, other than by having
-// the same logit and bias, which makes the decision one for a finer computation.
-template <typename V, typename T>
-__device__ bool choose(V* s_v, const T* logits, const float* bias, const adacomp_route_config_t& cfg, V tol, int* expert) {
-    const uint32_t lane = threadIdx.x % 32, size = cfg.experts / cfg.groups;
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Order of values as whole numbers; nothing that is a number comes out as 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.0f);           // -0 becomes +0
+    return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t u) { return __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u); }
+
+// Whether this lane's group, rated `rating` (lanes from `cfg.groups` on have none), is among the best top_groups, and whether that hung on
+// less than 2 tol (`least`: the lowest rating among the best).
+template <typename V> __device__ __forceinline__ uint32_t best_groups(V rating, const adacomp_route_config_t& cfg, V tol, bool* close, V* least_out) {
+    const uint32_t lane = threadIdx.x % 32;
     const V none = -INFINITY;
-    uint32_t kept = ~0u;
-    bool close = false;
-    if (cfg.top_groups < cfg.groups) {
-        V rating = none;
-        if (lane < cfg.groups) {
-            V first = none, second = none;
-            for (uint32_t e = lane * size; e < (lane + 1) * size; ++e) {
-                const V v = s_v[e];
-                if (v > first) second = first, first = v;
-                else if (v > second) second = v;
-            }
-            rating = cfg.group_terms == 2 && second != none ? first + second : first;
-        }
-        uint32_t better = 0;
-        for (uint32_t g = 0; g < cfg.groups; ++g) {
-            const V other = __shfl_sync(~0u, rating, g);
-            better += other > rating || (other == rating && g < lane);
-        }
-        const bool in = lane < cfg.groups && better < cfg.top_groups;
-        kept = __ballot_sync(~0u, in);
-        const V least = -warp_max(in ? -rating : none), most = warp_max(lane < cfg.groups && !in ? rating : none);
-        close = least - most <= 2 * tol;
+    uint32_t better = 0;
+    for (uint32_t g = 0; g < cfg.groups; ++g) {
+        const V other = __shfl_sync(~0u, rating, g);
+        better += other > rating || (other == rating && g < lane);
     }
-    V mine = none, last = none;
-    int id = -1, last_id = -1;
-    const uint32_t rounds = min(cfg.top_k + (tol > 0), cfg.experts);
-    for (uint32_t r = 0; r < rounds; ++r) {
-        V best = none;
+    const bool in = lane < cfg.groups && better < cfg.top_groups;
+    const V least = -warp_max(in ? -rating : none), most = warp_max(lane < cfg.groups && !in ? rating : none);
+    *close = least - most <= 2 * tol;
+    *least_out = least;
+    return __ballot_sync(~0u, in);
+}
+
+// Whether other logits than `x` may have the same score in 64 bits: a softmax's smallest ones, a sigmoid's largest and smallest.
+__device__ __forceinline__ bool tied_in_64(float x, float base, bool soft) { return soft ? x < base - 700.0f : x > 16.0f || x < -700.0f; }
+
+// A group's rating from the values s_v of its `size` experts (-Inf: cannot be chosen).
+template <typename V> __device__ __forceinline__ V rate(const V* s_v, uint32_t size, uint32_t terms) {
+    const V none = -INFINITY;
+    V first = none, second = none;
+    for (uint32_t e = 0; e < size; ++e) {
+        const V v = s_v[e];
+        if (v > first) second = first, first = v;
+        else if (v > second) second = v;
+    }
+    return terms == 2 && second != none ? first + second : first;
+}
+
+// The choice in 64 bits, a lane's place in its result: for rows in which fp32 does not tell candidates apart.  s_v: room for a row.
+template <typename T>
+__device__ __noinline__ int choose_careful(double* s_v, const T* l, const float* bias, const adacomp_route_config_t& cfg) {
+    const uint32_t lane = threadIdx.x % 32, size = cfg.experts / cfg.groups;
+    const bool soft = cfg.score == ADACOMP_SOFTMAX;
+    float most = -INFINITY;
+    for (uint32_t e = lane; e < cfg.experts; e += 32) most = fmaxf(most, to_float(l[e]));
+    most = warp_max(most);
+    const double base = most == -INFINITY ? 0.0 : most, none = -INFINITY;
+    double sum = 0.0;
+    __syncwarp();
+    for (uint32_t e = lane; e < cfg.experts; e += 32) {
+        const double x = to_float(l[e]), y = soft ? exp(x - base) : 1.0 / (1.0 + exp(-x));
+        sum += y;
+        s_v[e] = x == -INFINITY ? none : y;
+    }
+    sum = warp_sum(sum);
+    for (uint32_t e = lane; e < cfg.experts; e += 32) s_v[e] = (soft ? s_v[e] / sum : s_v[e]) + (bias ? static_cast<double>(bias[e]) : 0.0);
+    __syncwarp();
+    uint32_t kept = ~0u;
+    if (cfg.top_groups < cfg.groups) {
+        bool close;
+        double least;
+        kept = best_groups(lane < cfg.groups ? rate(s_v + lane * size, size, cfg.group_terms) : none, cfg, 0.0, &close, &least);
+    }
+    int id = -1;
+    for (uint32_t r = 0; r < cfg.top_k; ++r) {
+        double best = none;
         int at = INT_MAX;
         for (uint32_t e = lane; e < cfg.experts; e += 32)
             if (kept >> (e / size) & 1 && s_v[e] > best) best = s_v[e], at = static_cast<int>(e);
 #pragma unroll
         for (int d = 16; d; d >>= 1) {
-            const V v = __shfl_xor_sync(~0u, best, d);
+            const double v = __shfl_xor_sync(~0u, best, d);
             const int a = __shfl_xor_sync(~0u, at, d);
             if (v > best || (v == best && a < at)) best = v, at = a;
         }
         if (best == none) break;
-        // candidates come in falling order: close ones are neighbours
-        if (r > 0 && last - best <= tol)
-            close |= !(to_float(logits[at]) == to_float(logits[last_id]) && (!bias || bias[at] == bias[last_id]));
-        last = best, last_id = at;
-        if (lane == r) mine = best, id = at;
+        if (lane == r) id = at;
         __syncwarp();
         if (lane == 0) s_v[at] = none;
         __syncwarp();
     }
-    *expert = lane < cfg.top_k && mine != none ? id : -1;
-    return close;
+    return id;
+}
+
+// V consecutive entries; beyond `n` there is -Inf.
+template <typename T, int V> __device__ __forceinline__ void load_row(const T* p, uint32_t first, uint32_t n, bool wide, float (&x)[V]) {
+    if constexpr (V * sizeof(T) >= 16) {
+        if (wide) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = -INFINITY;
+            if (first < n) {
+                Packed<T, V> q;
+#pragma unroll
+                for (int i = 0; i < Packed<T, V>::kVecs; ++i) q.v[i] = reinterpret_cast<const uint4*>(p + first)[i];
+                q.unpack(x);
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = first + i < n ? to_float(p[first + i]) : -INFINITY;
 }
 
 // A chosen expert's score s (logit x; -Inf in lanes without one) divided by the sum over the warp.  Sigmoids that fp32 has no
@@ -131,83 +185,182 @@ __device__ __forceinline__ float quotient(float s, float x, bool soft) {
     return sum > 0.0f ? s / sum : 0.0f;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) k_route(const Job j) {
-    extern __shared__ double s_rows[];                      // a row of values per warp, then the counts
+// One warp per row, V consecutive experts per lane.  Every lane keeps the two best of its experts that are left at hand; a round
+// takes the best of the lanes' first ones (one reduction, one ballot: of equal ones the lowest lane has the lowest expert).
+//
+// What is compared is the logit itself where scores rise with it and nothing is added to them; otherwise fp32 values, and a row in which
+// two candidates lie closer than those can tell (and do not have the same logit and bias) is decided in 64 bits.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job j) {
+    extern __shared__ double s_rows[];                      // a row of values per warp then the counts
     __shared__ bool s_last;
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, E = j.cfg.experts, K = j.cfg.top_k;
+    const adacomp_route_config_t& cfg = j.cfg;
+    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, E = cfg.experts, K = cfg.top_k, first = lane * V, size = E / cfg.groups;
     double* s_wide = s_rows + warp * E;
-    float* s_v = reinterpret_cast<float*>(s_wide);
     uint32_t* s_counts = reinterpret_cast<uint32_t*>(s_rows + kWarps * E);
-    for (uint32_t e = threadIdx.x; e < E; e += kWarps * 32) s_counts[e] = 0;
+    for (uint32_t e = threadIdx.x; e < E; e += kThreads) s_counts[e] = 0;
     __syncthreads();
-    const bool soft = j.cfg.score == ADACOMP_SOFTMAX;
+    const bool soft = cfg.score == ADACOMP_SOFTMAX, in_groups = cfg.top_groups < cfg.groups;
+    const bool by_logit = !j.bias && (!in_groups || cfg.group_terms == 1);
+    // lanes of a group, where groups are whole lanes and their number a power of two; 0 otherwise
+    const uint32_t team = size % V == 0 && (size / V & (size / V - 1)) == 0 && E == 32 * V ? size / V : 0;
+    float bias[V], bias_most = 0.0f;
+    bool bad_bias = false;
+    if (j.bias) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            bias[i] = first + i < E ? j.bias[first + i] : 0.0f;
+            bad_bias |= bias[i] != bias[i];
+            if (bias[i] != -INFINITY) bias_most = fmaxf(bias_most, fabsf(bias[i]));
+        }
+        bias_most = warp_max(bias_most);
+    }
     for (uint32_t row = blockIdx.x * kWarps + warp; row < j.n_rows; row += gridDim.x * kWarps) {
         int id = -1;
         float w = 0.0f;
         if (!j.live || j.live[row]) {
             const T* l = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
-            float most = -INFINITY, bias_most = 0.0f, total = 0.0f;
-            bool bad = false;
-            for (uint32_t e = lane; e < E; e += 32) {
-                const float x = to_float(l[e]), b = j.bias ? j.bias[e] : 0.0f;
-                bad |= x != x || b != b || (soft && x == INFINITY);
-                most = fmaxf(most, x);
-                if (b != -INFINITY) bias_most = fmaxf(bias_most, fabsf(b));
-                s_v[e] = x;
+            float x[V];
+            load_row<T, V>(l, first, E, j.wide, x);
+            float most = -INFINITY;
+            bool bad = bad_bias;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                most = fmaxf(most, x[i]);
+                bad |= x[i] != x[i];
             }
-            bad = __any_sync(~0u, bad);
+            most = warp_max(most);
+            bad = __any_sync(~0u, bad) || (soft && most == INFINITY);
             if (!bad) {
-                most = warp_max(most);
-                bias_most = warp_max(bias_most);
                 const float base = most == -INFINITY ? 0.0f : most;
-                for (uint32_t e = lane; e < E; e += 32) {
-                    const float x = s_v[e], y = soft ? expf(x - base) : 1.0f / (1.0f + expf(-x));
-                    total += y;
-                    s_v[e] = x == -INFINITY ? -INFINITY : y;
+                float total = 1.0f, tol = 0.0f;
+                uint32_t key[V];
+                if (soft && (!by_logit || !cfg.renormalize)) {
+                    total = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) total += !cfg.renormalize ? expf(x[i] - base) : exp2_of((x[i] - base) * static_cast<float>(kLog2e));
+                    total = warp_sum(total);
                 }
-                total = warp_sum(total);
-                const float unit = soft ? 1.0f / total : 1.0f;
-                for (uint32_t e = lane; e < E; e += 32) s_v[e] = s_v[e] * unit + (j.bias ? j.bias[e] : 0.0f);
-                __syncwarp();
-                // scores are off by some rounding steps of the largest: 16 of them are allowed for
-                const float tol = (unit + bias_most) * 0x1p-20f;
-                if (choose<float, T>(s_v, l, j.bias, j.cfg, tol, &id)) {
-                    double sum = 0.0;
-                    __syncwarp();
-                    for (uint32_t e = lane; e < E; e += 32) {
-                        const double x = to_float(l[e]), y = soft ? exp(x - base) : 1.0 / (1.0 + exp(-x));
-                        sum += y;
-                        s_wide[e] = x == -INFINITY ? -INFINITY : y;
+                if (by_logit) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) key[i] = x[i] == -INFINITY ? 0 : order_of(x[i]);
+                } else {
+                    // a score is off by a few rounding steps of the largest, and all of a row's by those of its sum (37 additions at most)
+                    const float unit = soft ? 1.0f / total : 1.0f;
+                    tol = (unit + bias_most) * (soft ? 0x1p-18f : 0x1p-20f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float s = soft ? exp2_of((x[i] - base) * static_cast<float>(kLog2e)) * unit
+                                             : __fdividef(1.0f, 1.0f + exp2_of(x[i] * -static_cast<float>(kLog2e)));
+                        const float v = j.bias ? s + bias[i] : s;
+                        key[i] = x[i] == -INFINITY || v == -INFINITY ? 0 : order_of(v);
                     }
-                    sum = warp_sum(sum);
-                    for (uint32_t e = lane; e < E; e += 32)
-                        s_wide[e] = (soft ? s_wide[e] / sum : s_wide[e]) + (j.bias ? static_cast<double>(j.bias[e]) : 0.0);
-                    __syncwarp();
-                    choose<double, T>(s_wide, l, j.bias, j.cfg, 0.0, &id);
                 }
-                const float x = id >= 0 ? to_float(l[id]) : -INFINITY;
+                bool close = false;
+                if (in_groups) {
+                    float rating;
+                    if (team) {
+                        uint32_t one = 0, two = 0;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            two = max(two, min(one, key[i]));
+                            one = max(one, key[i]);
+                        }
+                        for (uint32_t d = team / 2; d; d /= 2) {
+                            const uint32_t other = __shfl_xor_sync(~0u, one, d), second = __shfl_xor_sync(~0u, two, d);
+                            two = max(max(two, second), min(one, other));
+                            one = max(one, other);
+                        }
+                        rating = one == 0 ? -INFINITY : cfg.group_terms == 2 && two ? value_of(one) + value_of(two) : value_of(one);
+                        rating = __shfl_sync(~0u, rating, lane * team);             // lane g: group g's
+                        if (lane >= cfg.groups) rating = -INFINITY;
+                    } else {
+                        float* s_v = reinterpret_cast<float*>(s_wide);
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            if (first + i < E) s_v[first + i] = key[i] ? value_of(key[i]) : -INFINITY;
+                        __syncwarp();
+                        rating = lane < cfg.groups ? rate(s_v + lane * size, size, cfg.group_terms) : -INFINITY;
+                    }
+                    bool border;
+                    float least;
+                    const uint32_t kept = best_groups(rating, cfg, tol, &border, &least);
+                    close |= by_logit ? tied_in_64(least, base, soft) || tied_in_64(most, base, soft) : border;
+                    if (team) {
+                        if (!(kept >> (lane / team) & 1))
+#pragma unroll
+                            for (int i = 0; i < V; ++i) key[i] = 0;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < V; ++i)
+                            if (first + i >= E || !(kept >> ((first + i) / size) & 1)) key[i] = 0;
+                    }
+                }
+                // the rounds
+                uint32_t one = 0, two = 0, at_one = 0, at_two = 0, taken = 0, mine = 0, last = 0;
+                auto at_hand = [&] {
+                    one = two = 0;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const uint32_t u = taken >> i & 1 ? 0 : key[i];
+                        if (u > one) two = one, at_two = at_one, one = u, at_one = i;
+                        else if (u > two) two = u, at_two = i;
+                    }
+                };
+                at_hand();
+                const uint32_t rounds = min(K + 1, E);
+                for (uint32_t r = 0; r < rounds; ++r) {
+                    const uint32_t best = __reduce_max_sync(~0u, one);
+                    if (best == 0) break;
+                    const uint32_t from = __ffs(__ballot_sync(~0u, one == best)) - 1;
+                    const uint32_t e = __shfl_sync(~0u, first + at_one, from);
+                    if (lane == r) mine = best, id = static_cast<int>(e);
+                    last = r < K ? 0 : best;
+                    if (lane == from) {
+                        taken |= 1u << at_one;
+                        one = two, at_one = at_two, two = 0;
+                        if (one == 0) at_hand();
+                    }
+                }
+                // candidates come in falling order, so close ones are neighbours; the one after the last place counts too
+                if (id >= 0 && lane > K) id = -1;
+                const float chosen = id >= 0 ? to_float(l[id]) : -INFINITY;
+                bool doubt = false;
+                if (by_logit) {
+                    doubt = id >= 0 && tied_in_64(chosen, base, soft);
+                } else {
+                    const float b = id >= 0 && j.bias ? j.bias[id] : 0.0f;
+                    uint32_t next = __shfl_down_sync(~0u, mine, 1);
+                    const float next_l = __shfl_down_sync(~0u, chosen, 1), next_b = __shfl_down_sync(~0u, b, 1);
+                    if (lane == 31) next = K == 32 ? last : 0;
+                    const bool same = lane < 31 && chosen == next_l && b == next_b;
+                    doubt = lane < K && mine && next && value_of(mine) - value_of(next) <= tol && !same;
+                }
+                close |= __any_sync(~0u, doubt);
+                if (lane >= K) id = -1;
+                if (close) id = choose_careful<T>(s_wide, l, j.bias, cfg);
+                const float xs = id < 0 ? -INFINITY : close ? to_float(l[id]) : chosen;
                 float s;
-                if (!soft) s = 1.0f / (1.0f + expf(-x));
-                else if (j.cfg.renormalize) s = expf(x - warp_max(x));           // relative to the largest chosen one
-                else s = expf(x - base) / total;
+                if (!soft) s = 1.0f / (1.0f + expf(-xs));
+                else if (cfg.renormalize) s = expf(xs - warp_max(xs));              // relative to the largest chosen one
+                else s = expf(xs - base) / total;
                 if (id < 0) s = 0.0f;
-                if (j.cfg.renormalize) s = quotient(s, x, soft);
-                w = s * j.cfg.scale;
+                if (cfg.renormalize) s = quotient(s, xs, soft);
+                w = s * cfg.scale;
             } else {
                 w = NAN;
             }
-            __syncwarp();
         }
         if (lane < K) {
             j.experts[static_cast<uint64_t>(row) * K + lane] = id;
             j.weights[static_cast<uint64_t>(row) * K + lane] = w;
-            if (id >= 0) atomicAdd(&s_counts[id], 1u);
+            if (id >= 0 && j.counts_out) atomicAdd(&s_counts[id], 1u);
         }
     }
     if (!j.counts_out) return;
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < E; e += kWarps * 32)
+    for (uint32_t e = threadIdx.x; e < E; e += kThreads)
         if (s_counts[e]) atomicAdd(&j.counts[e], s_counts[e]);
     __threadfence();
     __syncthreads();
@@ -215,63 +368,112 @@ __global__ void __launch_bounds__(kWarps * 32) k_route(const Job j) {
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    for (uint32_t e = threadIdx.x; e < E; e += kWarps * 32) {
+    for (uint32_t e = threadIdx.x; e < E; e += kThreads) {
         j.counts_out[e] = __ldcg(&j.counts[e]);
         j.counts[e] = 0;
     }
     if (threadIdx.x == 0) *j.ticket = 0;
 }
 
+template <typename V> __device__ __forceinline__ V part_sum(V x, uint32_t width) {
+    for (uint32_t d = width / 2; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
+    return x;
+}
+__device__ __forceinline__ float part_max(float x, uint32_t width) {
+    for (uint32_t d = width / 2; d; d /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+    return x;
+}
+
+// Zeros in a row of n entries, then whatever else its warp writes there.
+template <typename T> __device__ __forceinline__ void clear_row(T* out, uint32_t n, bool wide, uint32_t lane) {
+    if (wide) {
+        for (uint32_t v = lane; v < n / (16 / sizeof(T)); v += 32) reinterpret_cast<uint4*>(out)[v] = make_uint4(0, 0, 0, 0);
+    } else {
+        for (uint32_t e = lane; e < n; e += 32) out[e] = from_float<T>(0.0f);
+    }
+}
+
+// A place's expert as far as it counts: one that there is, named for the first time in its row (`width` lanes).
+__device__ __forceinline__ int counting(int id, uint32_t experts, uint32_t width, int* status) {
+    const uint32_t lane = threadIdx.x % 32, begin = lane / width * width;
+    if (id >= static_cast<int>(experts)) record_error(status, ADACOMP_ERR_INVALID), id = -1;
+    __syncwarp();
+    // lanes of other rows, and places without an expert, match nobody
+    const uint32_t same = __match_any_sync(~0u, id < 0 ? -1 - static_cast<int>(lane) : id) & (width == 32 ? ~0u : ((1u << width) - 1) << begin);
+    return id < 0 || lane != static_cast<uint32_t>(__ffs(same)) - 1 ? -1 : id;
+}
+
+// The gradient where only the chosen experts have one: as many rows per warp as their places allow.
 template <typename T>
-__global__ void __launch_bounds__(kWarps * 32) k_route_grad(const Job j) {
-    extern __shared__ float s_grads[];
-    const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, E = j.cfg.experts, K = j.cfg.top_k;
-    float* s_g = s_grads + warp * E;
+__global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__ Job j, uint32_t width) {
+    const uint32_t lane = threadIdx.x % 32, E = j.cfg.experts, K = j.cfg.top_k, rows = 32 / width, slot = lane % width;
     const bool soft = j.cfg.score == ADACOMP_SOFTMAX;
-    for (uint32_t row = blockIdx.x * kWarps + warp; row < j.n_rows; row += gridDim.x * kWarps) {
+    for (uint64_t row0 = static_cast<uint64_t>(blockIdx.x * kWarps + threadIdx.x / 32) * rows; row0 < j.n_rows; row0 += static_cast<uint64_t>(gridDim.x) * kWarps * rows) {
+        const uint64_t row = row0 + lane / width;
+        const bool here = row < j.n_rows && slot < K;
+        const int id = counting(here ? j.experts[row * K + slot] : -1, E, width, j.status);
+        float x = -INFINITY, d = 0.0f;
+        if (id >= 0) {
+            x = to_float(reinterpret_cast<const T*>(j.logits.data)[j.logits.offset(static_cast<uint32_t>(row)) + id]);
+            d = j.weights[row * K + slot] * j.cfg.scale;
+        }
+        __syncwarp();                                       // in place, the rows' logits are gone from here on
+        for (uint32_t r = 0; r < rows && row0 + r < j.n_rows; ++r)
+            clear_row(reinterpret_cast<T*>(j.out.data) + j.out.offset(static_cast<uint32_t>(row0 + r)), E, j.wide, lane);
+        float s = id < 0 ? 0.0f : 1.0f / (1.0f + expf(-x));
+        const float rest = soft ? 1.0f : 1.0f / (1.0f + expf(x));
+        if (j.cfg.renormalize) {
+            const float top = part_max(x, width);
+            float sum = part_sum(s, width);
+            if (soft || sum < 0x1p-90f) s = id < 0 ? 0.0f : expf(x - top);          // see quotient()
+            sum = part_sum(s, width);
+            s = sum > 0.0f ? s / sum : 0.0f;
+            d -= part_sum(d * s, width);
+        }
+        __syncwarp();
+        if (id >= 0) reinterpret_cast<T*>(j.out.data)[j.out.offset(static_cast<uint32_t>(row)) + id] = from_float<T>(d * s * rest);
+        __syncwarp();
+    }
+}
+
+// The gradient through a whole row's softmax: one warp per row, V consecutive experts per lane.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads) k_route_grad_dense(const __grid_constant__ Job j) {
+    const uint32_t lane = threadIdx.x % 32, E = j.cfg.experts, K = j.cfg.top_k, first = lane * V;
+    for (uint32_t row = blockIdx.x * kWarps + threadIdx.x / 32; row < j.n_rows; row += gridDim.x * kWarps) {
         const T* l = reinterpret_cast<const T*>(j.logits.data) + j.logits.offset(row);
         T* out = reinterpret_cast<T*>(j.out.data) + j.out.offset(row);
-        int id = lane < K ? j.experts[static_cast<uint64_t>(row) * K + lane] : -1;
-        if (id >= static_cast<int>(E)) record_error(j.status, ADACOMP_ERR_INVALID), id = -1;
-        __syncwarp();
-        const uint32_t same = __match_any_sync(~0u, id >= 0 ? id : -1 - static_cast<int>(lane));
-        if (id < 0 || lane != static_cast<uint32_t>(__ffs(same)) - 1) id = -1;
-        const float x = id >= 0 ? to_float(l[id]) : -INFINITY;
-        const float d = id >= 0 ? j.weights[static_cast<uint64_t>(row) * K + lane] * j.cfg.scale : 0.0f;
-        const bool any = __any_sync(~0u, id >= 0), dense = any && soft && !j.cfg.renormalize;
-        float total = 1.0f, base = 0.0f, common = 0.0f;
-        if (dense) {
-            float most = -INFINITY;
-            for (uint32_t e = lane; e < E; e += 32) most = fmaxf(most, to_float(l[e]));
-            most = warp_max(most);
-            base = most == -INFINITY ? 0.0f : most;
-            total = 0.0f;
-            for (uint32_t e = lane; e < E; e += 32) total += expf(to_float(l[e]) - base);
-            total = warp_sum(total);
+        const int id = counting(lane < K ? j.experts[static_cast<uint64_t>(row) * K + lane] : -1, E, 32, j.status);
+        if (!__any_sync(~0u, id >= 0)) {
+            clear_row(out, E, j.wide, lane);
+            continue;
         }
-        float g = 0.0f;
-        if (!soft) {
-            float s = id >= 0 ? 1.0f / (1.0f + expf(-x)) : 0.0f;
-            const float rest = 1.0f / (1.0f + expf(x));
-            if (j.cfg.renormalize) {
-                s = quotient(s, x, false);
-                g = (d - warp_sum(d * s)) * s * rest;
-            } else {
-                g = d * s * rest;
+        const float chosen = id >= 0 ? to_float(l[id]) : -INFINITY, d = id >= 0 ? j.weights[static_cast<uint64_t>(row) * K + lane] * j.cfg.scale : 0.0f;
+        float x[V], most = -INFINITY, total = 0.0f;
+        load_row<T, V>(l, first, E, j.wide, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) most = fmaxf(most, x[i]);
+        most = warp_max(most);
+        const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = expf(x[i] - base), total += x[i];
+        total = warp_sum(total);
+        const float s = id >= 0 ? expf(chosen - base) / total : 0.0f, common = warp_sum(d * s), unit = -common / total;
+        if (V * sizeof(T) >= 16 && j.wide) {
+            if constexpr (V * sizeof(T) >= 16) {
+                Packed<T, V> q;
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] *= unit;
+                q.pack(x);
+                if (first < E) q.store(out + first);
             }
-        } else if (j.cfg.renormalize) {
-            const float top = warp_max(x), s = quotient(id >= 0 ? expf(x - top) : 0.0f, x, true);
-            g = s * (d - warp_sum(d * s));
         } else {
-            const float s = id >= 0 ? expf(x - base) / total : 0.0f;
-            common = warp_sum(d * s);
-            g = s * (d - common);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (first + i < E) out[first + i] = from_float<T>(x[i] * unit);
         }
-        for (uint32_t e = lane; e < E; e += 32) s_g[e] = dense ? -(expf(to_float(l[e]) - base) / total) * common : 0.0f;
         __syncwarp();
-        if (id >= 0) s_g[id] = g;
-        __syncwarp();
-        for (uint32_t e = lane; e < E; e += 32) out[e] = from_float<T>(s_g[e]);
+        if (id >= 0) out[id] = from_float<T>(s * (d - common));
         __syncwarp();
     }
 }
@@ -297,22 +499,61 @@ size_t carve(adacomp_route_t* h, void* base, uint32_t experts) {
     return c.used;
 }
 
-uint32_t grid_of(const adacomp_route_t* h, uint32_t n_rows) {
-    const uint32_t most = static_cast<uint32_t>(h->n_sms) * 8, need = (n_rows + kWarps - 1) / kWarps;
-    return need < most ? need : most;
+uint32_t grid_of(int n_sms, uint64_t n_rows, uint32_t rows_per_block, uint32_t per_sm) {
+    const uint64_t most = static_cast<uint64_t>(n_sms) * per_sm, need = (n_rows + rows_per_block - 1) / rows_per_block;
+    return static_cast<uint32_t>(need < most ? need : most);
 }
 
-template <typename T> int launch_route(const Job& j, uint32_t blocks, cudaStream_t stream) {
+// Experts per lane.
+uint32_t share_of(uint32_t experts) {
+    uint32_t v = 1;
+    while (32 * v < experts) v *= 2;
+    return v;
+}
+
+template <typename T, int V> int launch_route(const Job& j, int n_sms, cudaStream_t stream) {
     const size_t smem = kWarps * j.cfg.experts * sizeof(double) + j.cfg.experts * sizeof(uint32_t);
-    k_route<T><<<blocks, kWarps * 32, smem, stream>>>(j);
+    ADACOMP_CUDA(cudaFuncSetAttribute(k_route<T, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    k_route<T, V><<<grid_of(n_sms, j.n_rows, kWarps, 6), kThreads, smem, stream>>>(j);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
 
-template <typename T> int launch_grad(const Job& j, uint32_t blocks, cudaStream_t stream) {
-    k_route_grad<T><<<blocks, kWarps * 32, kWarps * j.cfg.experts * sizeof(float), stream>>>(j);
+template <typename T, int V> int launch_dense(const Job& j, int n_sms, cudaStream_t stream) {
+    k_route_grad_dense<T, V><<<grid_of(n_sms, j.n_rows, kWarps, 8), kThreads, 0, stream>>>(j);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
+}
+
+#define ADACOMP_BY_SHARE(fn, T, experts, ...)               \
+    [&]() -> int {                                          \
+        switch (share_of(experts)) {                        \
+            case 1: return fn<T, 1>(__VA_ARGS__);           \
+            case 2: return fn<T, 2>(__VA_ARGS__);           \
+            case 4: return fn<T, 4>(__VA_ARGS__);           \
+            case 8: return fn<T, 8>(__VA_ARGS__);           \
+            case 16: return fn<T, 16>(__VA_ARGS__);         \
+            default: return fn<T, 32>(__VA_ARGS__);         \
+        }                                                   \
+    }()
+
+template <typename T> int route(const Job& j, int n_sms, cudaStream_t stream) {
+    return ADACOMP_BY_SHARE(launch_route, T, j.cfg.experts, j, n_sms, stream);
+}
+
+template <typename T> int route_grad(const Job& j, int n_sms, cudaStream_t stream) {
+    if (j.cfg.score == ADACOMP_SOFTMAX && !j.cfg.renormalize) return ADACOMP_BY_SHARE(launch_dense, T, j.cfg.experts, j, n_sms, stream);
+    uint32_t width = 1;
+    while (width < j.cfg.top_k) width *= 2;
+    k_route_grad<T><<<grid_of(n_sms, j.n_rows, kWarps * (32 / width), 8), kThreads, 0, stream>>>(j, width);
+    ADACOMP_LAUNCH_CHECK();
+    return ADACOMP_OK;
+}
+
+// Whether lanes can load their shares of a row as whole vectors.
+bool wide_rows(const Rows& r, uint32_t experts) {
+    const uint32_t share = share_of(experts), bytes = share * type_size(r.type);
+    return bytes >= 16 && experts % share == 0 && on_grid(r, 16);
 }
 
 }  // namespace
@@ -378,10 +619,10 @@ int adacomp_route(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_t n_r
     j.ticket = h->d_ticket;
     j.status = h->d_status;
     j.n_rows = n_rows;
-    const uint32_t blocks = grid_of(h, n_rows);
-    if (j.logits.type == ADACOMP_F32) return launch_route<float>(j, blocks, stream);
-    if (j.logits.type == ADACOMP_BF16) return launch_route<__nv_bfloat16>(j, blocks, stream);
-    return launch_route<__half>(j, blocks, stream);
+    j.wide = wide_rows(j.logits, j.cfg.experts);
+    if (j.logits.type == ADACOMP_F32) return route<float>(j, h->n_sms, stream);
+    if (j.logits.type == ADACOMP_BF16) return route<__nv_bfloat16>(j, h->n_sms, stream);
+    return route<__half>(j, h->n_sms, stream);
 }
 
 int adacomp_route_grad(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const int32_t* d_experts,
@@ -402,11 +643,13 @@ int adacomp_route_grad(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_
     j.n_rows = n_rows;
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
-    const uint32_t blocks = grid_of(h, n_rows);
+    const bool dense = j.cfg.score == ADACOMP_SOFTMAX && !j.cfg.renormalize;
+    j.wide = dense ? wide_rows(j.logits, j.cfg.experts) && wide_rows(j.out, j.cfg.experts)
+                   : on_grid(j.out, 16) && j.cfg.experts * type_size(j.out.type) % 16 == 0;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (j.logits.type == ADACOMP_F32) return launch_grad<float>(j, blocks, stream);
-    if (j.logits.type == ADACOMP_BF16) return launch_grad<__nv_bfloat16>(j, blocks, stream);
-    return launch_grad<__half>(j, blocks, stream);
+    if (j.logits.type == ADACOMP_F32) return route_grad<float>(j, h->n_sms, stream);
+    if (j.logits.type == ADACOMP_BF16) return route_grad<__nv_bfloat16>(j, h->n_sms, stream);
+    return route_grad<__half>(j, h->n_sms, stream);
 }
 
 int adacomp_route_last_error(adacomp_route_t* h, void* cuda_stream) {
