@@ -69,10 +69,17 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
-// Order of values as whole numbers; nothing that is a number comes out as 0.
+__device__ __forceinline__ float reciprocal_of(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Order of values as whole numbers.  What cannot be chosen is -Inf, or 0 once it has been left out.
+constexpr uint32_t kNothing = 0x007FFFFFu;                  // -Inf
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);           // -0 becomes +0
-    return u ^ (u >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+    return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t u) { return __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u); }
 
@@ -87,7 +94,13 @@ template <typename V> __device__ __forceinline__ uint32_t best_groups(V rating, 
         better += other > rating || (other == rating && g < lane);
     }
     const bool in = lane < cfg.groups && better < cfg.top_groups;
-    const V least = -warp_max(in ? -rating : none), most = warp_max(lane < cfg.groups && !in ? rating : none);
+    V least, most;
+    if constexpr (sizeof(V) == 4) {
+        least = value_of(__reduce_min_sync(~0u, in ? order_of(rating) : ~0u));
+        most = value_of(__reduce_max_sync(~0u, lane < cfg.groups && !in ? order_of(rating) : kNothing));
+    } else {
+        least = -warp_max(in ? -rating : none), most = warp_max(lane < cfg.groups && !in ? rating : none);
+    }
     *close = least - most <= 2 * tol;
     *least_out = least;
     return __ballot_sync(~0u, in);
@@ -173,25 +186,37 @@ template <typename T, int V> __device__ __forceinline__ void load_row(const T* p
     for (int i = 0; i < V; ++i) x[i] = first + i < n ? to_float(p[first + i]) : -INFINITY;
 }
 
-// A chosen expert's score s (logit x; -Inf in lanes without one) divided by the sum over the warp.  Sigmoids that fp32 has no
+template <typename V> __device__ __forceinline__ V part_sum(V x, uint32_t width) {
+    for (uint32_t d = width / 2; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
+    return x;
+}
+__device__ __forceinline__ float part_max(float x, uint32_t width) {
+    for (uint32_t d = width / 2; d; d /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+    return x;
+}
+
+// A chosen expert's score s (logit x; -Inf in lanes without one) divided by the sum over the first `width` lanes.  Sigmoids that fp32 has no
 // numbers for, or few bits, are exp(x) to all of its bits: their quotients are those of exp(x - the largest x).
-__device__ __forceinline__ float quotient(float s, float x, bool soft) {
-    float sum = warp_sum(s);
+__device__ __forceinline__ float quotient(float s, float x, bool soft, uint32_t width) {
+    float sum = __shfl_sync(~0u, part_sum(s, width), 0);
     if (!soft && sum < 0x1p-90f) {
-        const float top = warp_max(x);
+        const float top = part_max(x, width);
         s = x == -INFINITY ? 0.0f : expf(x - top);
-        sum = warp_sum(s);
+        sum = __shfl_sync(~0u, part_sum(s, width), 0);
     }
     return sum > 0.0f ? s / sum : 0.0f;
 }
 
-// One warp per row, V consecutive experts per lane.  Every lane keeps the two best of its experts that are left at hand; a round
-// takes the best of the lanes' first ones (one reduction, one ballot: of equal ones the lowest lane has the lowest expert).
+// One warp per row, V consecutive experts per lane.  Where a row has more candidates than a warp lanes (ties, long choices), every lane
+// keeps the two best of its experts that are left at hand, and a round takes the best of the lanes' first ones (one reduction, one
+// ballot: of equal ones the lowest lane has the lowest expert).
 //
 // What is compared is the logit itself where scores rise with it and nothing is added to them; otherwise fp32 values, and a row in which
 // two candidates lie closer than those can tell (and do not have the same logit and bias) is decided in 64 bits.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job j) {
+    __shared__ uint2 s_places[kWarps][kMaxChosen + 1];      // a row's choice: order of the value, expert
+    __shared__ uint64_t s_lists[kWarps][32];                // its candidates
     extern __shared__ double s_rows[];                      // a row of values per warp then the counts
     __shared__ bool s_last;
     const adacomp_route_config_t& cfg = j.cfg;
@@ -203,6 +228,9 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
     const bool soft = cfg.score == ADACOMP_SOFTMAX, in_groups = cfg.top_groups < cfg.groups;
     const bool by_logit = !j.bias && (!in_groups || cfg.group_terms == 1);
     // lanes of a group, where groups are whole lanes and their number a power of two; 0 otherwise
+    uint32_t width = 1;                                     // lanes that hold a row's places
+    while (width < K) width *= 2;
+    const uint32_t below = (1u << lane) - 1, rounds = by_logit ? K : K + 1;
     const uint32_t team = size % V == 0 && (size / V & (size / V - 1)) == 0 && E == 32 * V ? size / V : 0;
     float bias[V], bias_most = 0.0f;
     bool bad_bias = false;
@@ -229,7 +257,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                 most = fmaxf(most, x[i]);
                 bad |= x[i] != x[i];
             }
-            most = warp_max(most);
+            most = value_of(__reduce_max_sync(~0u, order_of(most)));
             bad = __any_sync(~0u, bad) || (soft && most == INFINITY);
             if (!bad) {
                 const float base = most == -INFINITY ? 0.0f : most;
@@ -243,7 +271,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                 }
                 if (by_logit) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) key[i] = x[i] == -INFINITY ? 0 : order_of(x[i]);
+                    for (int i = 0; i < V; ++i) key[i] = order_of(x[i]);
                 } else {
                     // a score is off by a few rounding steps of the largest, and all of a row's by those of its sum (37 additions at most)
                     const float unit = soft ? 1.0f / total : 1.0f;
@@ -251,9 +279,9 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float s = soft ? exp2_of((x[i] - base) * static_cast<float>(kLog2e)) * unit
-                                             : __fdividef(1.0f, 1.0f + exp2_of(x[i] * -static_cast<float>(kLog2e)));
+                                             : reciprocal_of(1.0f + exp2_of(x[i] * -static_cast<float>(kLog2e)));
                         const float v = j.bias ? s + bias[i] : s;
-                        key[i] = x[i] == -INFINITY || v == -INFINITY ? 0 : order_of(v);
+                        key[i] = x[i] == -INFINITY ? 0 : order_of(v);
                     }
                 }
                 bool close = false;
@@ -271,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                             two = max(max(two, second), min(one, other));
                             one = max(one, other);
                         }
-                        rating = one == 0 ? -INFINITY : cfg.group_terms == 2 && two ? value_of(one) + value_of(two) : value_of(one);
+                        rating = one <= kNothing ? -INFINITY : cfg.group_terms == 2 && two > kNothing ? value_of(one) + value_of(two) : value_of(one);
                         rating = __shfl_sync(~0u, rating, lane * team);             // lane g: group g's
                         if (lane >= cfg.groups) rating = -INFINITY;
                     } else {
@@ -279,7 +307,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                         __syncwarp();
 #pragma unroll
                         for (int i = 0; i < V; ++i)
-                            if (first + i < E) s_v[first + i] = key[i] ? value_of(key[i]) : -INFINITY;
+                            if (first + i < E) s_v[first + i] = key[i] > kNothing ? value_of(key[i]) : -INFINITY;
                         __syncwarp();
                         rating = lane < cfg.groups ? rate(s_v + lane * size, size, cfg.group_terms) : -INFINITY;
                     }
@@ -297,56 +325,112 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                             if (first + i >= E || !(kept >> ((first + i) / size) & 1)) key[i] = 0;
                     }
                 }
-                // the rounds
-                uint32_t one = 0, two = 0, at_one = 0, at_two = 0, taken = 0, mine = 0, last = 0;
-                auto at_hand = [&] {
-                    one = two = 0;
+                // The candidates: the lanes' best ones, one after the other, give a number that one more than top_k experts reach; what
+                // lies that high (or too little below to tell) is mostly fewer than a warp has lanes, and places are counted.
+                uint32_t one = 0;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const uint32_t u = taken >> i & 1 ? 0 : key[i];
-                        if (u > one) two = one, at_two = at_one, one = u, at_one = i;
-                        else if (u > two) two = u, at_two = i;
-                    }
-                };
-                at_hand();
-                const uint32_t rounds = min(K + 1, E);
-                for (uint32_t r = 0; r < rounds; ++r) {
-                    const uint32_t best = __reduce_max_sync(~0u, one);
-                    if (best == 0) break;
-                    const uint32_t from = __ffs(__ballot_sync(~0u, one == best)) - 1;
-                    const uint32_t e = __shfl_sync(~0u, first + at_one, from);
-                    if (lane == r) mine = best, id = static_cast<int>(e);
-                    last = r < K ? 0 : best;
-                    if (lane == from) {
-                        taken |= 1u << at_one;
-                        one = two, at_one = at_two, two = 0;
-                        if (one == 0) at_hand();
+                for (int i = 0; i < V; ++i) one = max(one, key[i]);
+                uint32_t floor = 0;
+                for (uint32_t r = 0, left = one; r < rounds; ++r) {
+                    floor = __reduce_max_sync(~0u, left);
+                    if (left == floor) left = 0;
+                }
+                floor = max(floor, kNothing + 1);
+                if (!by_logit) floor = max(order_of(value_of(floor) - tol), kNothing + 1);
+                uint64_t* const list = s_lists[warp];
+                uint32_t n = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const uint32_t there = __ballot_sync(~0u, key[i] >= floor), place = n + __popc(there & below);
+                    if (key[i] >= floor && place < 32) list[place] = static_cast<uint64_t>(key[i]) << 32 | (0xFFFFFFFFu - (first + i));
+                    n += __popc(there);
+                }
+                uint2* const places = s_places[warp];
+                __syncwarp();
+                uint64_t mine = 0;
+                if (n <= 32) {
+                    mine = lane < n ? list[lane] : 0;
+                    uint32_t place = 0;
+                    for (uint32_t i = 0; i < n; ++i) place += list[i] > mine;
+                    if (lane < n && place < rounds) places[place] = make_uint2(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
+                    if (lane >= n && lane < rounds) places[lane] = make_uint2(0, 0);
+                } else {                                    // by rounds
+                    uint32_t two = 0, at_one = 0, at_two = 0, taken = 0;
+                    auto at_hand = [&] {
+                        one = two = 0;
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const uint32_t u = taken >> i & 1 ? 0 : key[i];
+                            if (u > one) two = one, at_two = at_one, one = u, at_one = i;
+                            else if (u > two) two = u, at_two = i;
+                        }
+                    };
+                    at_hand();
+#pragma unroll 1
+                    for (uint32_t r = 0; r < rounds; ++r) {
+                        const uint32_t best = __reduce_max_sync(~0u, one);
+                        const uint32_t firsts = __ballot_sync(~0u, one == best);
+                        if (one == best && !(firsts & below)) {
+                            places[r] = make_uint2(best, first + at_one);
+                            taken |= 1u << at_one;
+                            one = two, at_one = at_two, two = 0;
+                            if (one == 0) at_hand();
+                        }
                     }
                 }
-                // candidates come in falling order, so close ones are neighbours; the one after the last place counts too
-                if (id >= 0 && lane > K) id = -1;
-                const float chosen = id >= 0 ? to_float(l[id]) : -INFINITY;
+                __syncwarp();
+                // candidates stand in falling order, so close ones are neighbours; the one after the last place counts too
+                const uint2 given = lane < rounds ? places[lane] : make_uint2(0, 0);
+                id = given.x > kNothing ? static_cast<int>(given.y) : -1;
+                float chosen = -INFINITY;
                 bool doubt = false;
                 if (by_logit) {
+                    if (id >= 0) chosen = value_of(given.x);
                     doubt = id >= 0 && tied_in_64(chosen, base, soft);
                 } else {
-                    const float b = id >= 0 && j.bias ? j.bias[id] : 0.0f;
-                    uint32_t next = __shfl_down_sync(~0u, mine, 1);
-                    const float next_l = __shfl_down_sync(~0u, chosen, 1), next_b = __shfl_down_sync(~0u, b, 1);
-                    if (lane == 31) next = K == 32 ? last : 0;
-                    const bool same = lane < 31 && chosen == next_l && b == next_b;
-                    doubt = lane < K && mine && next && value_of(mine) - value_of(next) <= tol && !same;
+                    if (id >= 0) chosen = to_float(l[id]);
+                    const uint2 next = lane + 1 < rounds ? places[lane + 1] : make_uint2(0, 0);
+                    if (lane < K && next.x > kNothing && value_of(given.x) - value_of(next.x) <= tol)
+                        doubt = chosen != to_float(l[next.y]) || (j.bias && j.bias[id] != j.bias[next.y]);
                 }
-                close |= __any_sync(~0u, doubt);
+                __syncwarp();
+                if (__any_sync(~0u, doubt) && !close) {
+                    if (n > 32 || by_logit) {
+                        close = true;
+                    } else {                                // the order of the candidates alone, in 64 bits
+                        double value = -INFINITY, sum = 0.0;
+                        const uint32_t e = 0xFFFFFFFFu - static_cast<uint32_t>(mine);
+                        if (soft)
+#pragma unroll 1
+                            for (uint32_t i = lane; i < E; i += 32) sum += exp(static_cast<double>(to_float(l[i])) - base);
+                        sum = warp_sum(sum);
+                        if (lane < n) {
+                            const double xe = to_float(l[e]);
+                            value = (soft ? exp(xe - base) / sum : 1.0 / (1.0 + exp(-xe))) + (j.bias ? static_cast<double>(j.bias[e]) : 0.0);
+                        }
+                        uint32_t place = 0;
+#pragma unroll 1
+                        for (uint32_t i = 0; i < n; ++i) {
+                            const double other = __shfl_sync(~0u, value, i);
+                            const uint32_t at = __shfl_sync(~0u, e, i);
+                            place += other > value || (other == value && at < e);
+                        }
+                        if (lane < n && place < K) places[place].y = e;
+                        __syncwarp();
+                        id = lane < min(K, n) ? static_cast<int>(places[lane].y) : -1;
+                        chosen = id >= 0 ? to_float(l[id]) : -INFINITY;
+                        __syncwarp();
+                    }
+                }
                 if (lane >= K) id = -1;
                 if (close) id = choose_careful<T>(s_wide, l, j.bias, cfg);
                 const float xs = id < 0 ? -INFINITY : close ? to_float(l[id]) : chosen;
                 float s;
                 if (!soft) s = 1.0f / (1.0f + expf(-xs));
-                else if (cfg.renormalize) s = expf(xs - warp_max(xs));              // relative to the largest chosen one
+                else if (cfg.renormalize) s = expf(xs - (by_logit && !close ? __shfl_sync(~0u, xs, 0) : warp_max(xs)));    // relative to the largest chosen one
                 else s = expf(xs - base) / total;
                 if (id < 0) s = 0.0f;
-                if (cfg.renormalize) s = quotient(s, xs, soft);
+                if (cfg.renormalize) s = quotient(s, xs, soft, width);
                 w = s * cfg.scale;
             } else {
                 w = NAN;
@@ -373,15 +457,6 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
         j.counts[e] = 0;
     }
     if (threadIdx.x == 0) *j.ticket = 0;
-}
-
-template <typename V> __device__ __forceinline__ V part_sum(V x, uint32_t width) {
-    for (uint32_t d = width / 2; d; d /= 2) x += __shfl_xor_sync(~0u, x, d);
-    return x;
-}
-__device__ __forceinline__ float part_max(float x, uint32_t width) {
-    for (uint32_t d = width / 2; d; d /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
-    return x;
 }
 
 // Zeros in a row of n entries, then whatever else its warp writes there.
