@@ -917,11 +917,26 @@ def _gradient_for(out: Optional[torch.Tensor], logits: torch.Tensor, stream) -> 
         return out
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out: need the shape and type of the logits")
-    if out.numel() and not (out.data_ptr() == logits.data_ptr() and out.stride() == logits.stride()):
+    at, to = logits.data_ptr(), out.data_ptr()
+    if logits.is_contiguous() and out.is_contiguous():
+        if at != to and abs(at - to) < out.numel() * out.element_size():
+            raise ValueError("out: overlaps the logits")
+    elif out.numel() and not (to == at and out.stride() == logits.stride()):
         (a, b), (c, d) = _span(logits), _span(out)
         if a < d and c < b:
             raise ValueError("out: overlaps the logits")
     return out
+
+
+def _result(t: Optional[torch.Tensor], like: torch.Tensor, shape, dtype, rows: int, device: int, name: str, stream):
+    """The tensor a result goes to, a new one of that shape if none is given, and its address."""
+    if t is not None:
+        return t, _per_row(t, dtype, rows, device, name)
+    if stream is not None:
+        t = _empty(like, shape, dtype, stream)
+    else:
+        t = like.new_empty(shape) if like.dtype == dtype else like.new_empty(shape, dtype=dtype)
+    return t, t.data_ptr()
 
 
 def _per_row(t: Optional[torch.Tensor], dtype, rows: int, device: int, name: str) -> Optional[int]:
@@ -965,17 +980,12 @@ class Distiller(_Handle):
         n = logits.numel() // self.vocab
         if not 0 <= k < 1 << 32:
             raise ValueError("k: out of range")
-        if idx_out is None:
-            idx_out = _empty(logits, (*lead, k), torch.int32, stream)
-        if val_out is None:
-            val_out = _empty(logits, (*lead, k), logits.dtype, stream)
-        if lse_out is None:
-            lse_out = _empty(logits, lead, torch.float32, stream)
-        _check(_lib.adacomp_top_logits(self._h, ctypes.byref(rows), n, k, float(temperature),
-                                       _per_row(idx_out, torch.int32, n * k, self._index, "idx_out"),
-                                       _per_row(val_out, logits.dtype, n * k, self._index, "val_out"),
-                                       _per_row(lse_out, torch.float32, n, self._index, "lse_out"), self._stream_on(stream)),
-               "adacomp_top_logits")
+        index, shape = self._index, (*lead, k)
+        idx_out, idx_at = _result(idx_out, logits, shape, torch.int32, n * k, index, "idx_out", stream)
+        val_out, val_at = _result(val_out, logits, shape, logits.dtype, n * k, index, "val_out", stream)
+        lse_out, lse_at = _result(lse_out, logits, lead, torch.float32, n, index, "lse_out", stream)
+        _check(_lib.adacomp_top_logits(self._h, ctypes.byref(rows), n, k, float(temperature), idx_at, val_at, lse_at,
+                                       self._stream_on(stream)), "adacomp_top_logits")
         return idx_out, val_out, lse_out
 
     def _given(self, logits, idx, val, lse, weight):
@@ -1007,14 +1017,11 @@ class Distiller(_Handle):
         normalisers, with which what it did not list is one more class (None: the list alone, renormalised).  Rows of
         ``weight`` [...] 0 are left out; other weights matter to the gradient only."""
         rows, n, pairs, weights = self._given(logits, idx, val, lse, weight)
-        if loss_out is None:
-            loss_out = _empty(logits, logits.shape[:-1], torch.float32, stream)
-        if stats_out is None:
-            stats_out = _empty(logits, (*logits.shape[:-1], 8), torch.float32, stream)
-        _check(_lib.adacomp_distill_loss(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights,
-                                         _per_row(loss_out, torch.float32, n, self._index, "loss_out"),
-                                         _per_row(stats_out, torch.float32, 8 * n, self._index, "stats_out"),
-                                         self._stream_on(stream)), "adacomp_distill_loss")
+        lead = logits.shape[:-1]
+        loss_out, loss_at = _result(loss_out, logits, lead, torch.float32, n, self._index, "loss_out", stream)
+        stats_out, stats_at = _result(stats_out, logits, (*lead, 8), torch.float32, 8 * n, self._index, "stats_out", stream)
+        _check(_lib.adacomp_distill_loss(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights, loss_at,
+                                         stats_at, self._stream_on(stream)), "adacomp_distill_loss")
         return loss_out, stats_out
 
     def grad(self, logits: torch.Tensor, idx: torch.Tensor, val: torch.Tensor, stats: torch.Tensor,
@@ -1036,10 +1043,8 @@ class Distiller(_Handle):
         """Loss and gradient in one pass over the logits -> (loss [...], gradient [..., vocab])."""
         rows, n, pairs, weights = self._given(logits, idx, val, lse, weight)
         out = _gradient_for(out, logits, stream)
-        if loss_out is None:
-            loss_out = _empty(logits, logits.shape[:-1], torch.float32, stream)
-        _check(_lib.adacomp_distill_loss_grad(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights,
-                                              _per_row(loss_out, torch.float32, n, self._index, "loss_out"),
+        loss_out, loss_at = _result(loss_out, logits, logits.shape[:-1], torch.float32, n, self._index, "loss_out", stream)
+        _check(_lib.adacomp_distill_loss_grad(self._h, ctypes.byref(rows), n, ctypes.byref(pairs), float(temperature), weights, loss_at,
                                               ctypes.byref(_logit_rows(out, self.vocab, self._index, "out")), self._stream_on(stream)),
                "adacomp_distill_loss_grad")
         return loss_out, out
@@ -1097,17 +1102,12 @@ class Router(_Handle):
         rows = _logit_rows(logits, self.experts, self._index, "logits")
         lead, k = logits.shape[:-1], self.top_k
         n = logits.numel() // self.experts
-        if experts_out is None:
-            experts_out = _empty(logits, (*lead, k), torch.int32, stream)
-        if weights_out is None:
-            weights_out = _empty(logits, (*lead, k), torch.float32, stream)
-        if counts_out is None:
-            counts_out = _empty(logits, (self.experts,), torch.int32, stream)
-        _check(_lib.adacomp_route(self._h, ctypes.byref(rows), n, _per_row(bias, torch.float32, self.experts, self._index, "bias"),
-                                  _per_row(live, torch.bool, n, self._index, "live"),
-                                  _per_row(experts_out, torch.int32, n * k, self._index, "experts_out"),
-                                  _per_row(weights_out, torch.float32, n * k, self._index, "weights_out"),
-                                  _per_row(counts_out, torch.int32, self.experts, self._index, "counts_out"),
+        index, shape = self._index, (*lead, k)
+        experts_out, experts_at = _result(experts_out, logits, shape, torch.int32, n * k, index, "experts_out", stream)
+        weights_out, weights_at = _result(weights_out, logits, shape, torch.float32, n * k, index, "weights_out", stream)
+        counts_out, counts_at = _result(counts_out, logits, (self.experts,), torch.int32, self.experts, index, "counts_out", stream)
+        _check(_lib.adacomp_route(self._h, ctypes.byref(rows), n, _per_row(bias, torch.float32, self.experts, index, "bias"),
+                                  _per_row(live, torch.bool, n, index, "live"), experts_at, weights_at, counts_at,
                                   self._stream_on(stream)), "adacomp_route")
         return experts_out, weights_out, counts_out
 

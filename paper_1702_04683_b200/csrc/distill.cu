@@ -633,8 +633,8 @@ constexpr uint32_t kHits = 512;
 // (with 26 KB a block instead of 9, 8192 x 50000 bf16 took 232 us instead of 206).
 struct TopShared {
     uint32_t candidates, keys, groups, bytes;
-    TopShared(uint32_t k, uint32_t steps) {
-        candidates = 256;
+    TopShared(uint32_t k, uint32_t steps, uint32_t rank_bits) {
+        candidates = rank_bits ? 1024 : 256;        // a cluster's first block takes the others' lists
         while (candidates < 2 * k) candidates *= 2;
         keys = candidates * sizeof(uint64_t);                        // and later the hits
         groups = keys + kHits * sizeof(uint16_t);
@@ -705,6 +705,48 @@ template <uint32_t THREADS> __device__ void sort_list(uint64_t* s_list, uint32_t
     __syncthreads();
 }
 
+// Cuts s_list[0 .. n), n <= 8 kTopThreads, down to the entries whose value is among the k largest ones' (k, some more, and ties),
+// in any order; returns how many.  s_words: 34 of them.
+__device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k, uint32_t* s_words) {
+    const uint32_t tid = threadIdx.x, lane = tid % 32;
+    uint64_t x[8];
+    uint32_t low = ~0u, high = 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        x[u] = tid + u * kTopThreads < n ? s_list[tid + u * kTopThreads] : 0;
+        high = max(high, static_cast<uint32_t>(x[u] >> 32));
+        if (x[u]) low = min(low, static_cast<uint32_t>(x[u] >> 32));
+    }
+    if (tid < 32) s_words[tid] = 0;
+    if (tid == 0) s_words[32] = 0, s_words[33] = ~0u;
+    __syncthreads();
+    low = __reduce_min_sync(~0u, low), high = __reduce_max_sync(~0u, high);
+    if (lane == 0) atomicMax(&s_words[32], high), atomicMin(&s_words[33], low);
+    __syncthreads();
+    high = s_words[32], low = s_words[33];
+    const uint32_t same = __clz(low ^ high);
+    uint32_t reach = same == 32 ? high : high & ~(0xFFFFFFFFu >> same);
+    for (uint32_t bit = same == 32 ? 0 : 0x80000000u >> same; bit; bit >>= 1) {
+        uint32_t there = 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) there += static_cast<uint32_t>(x[u] >> 32) >= (reach | bit);
+        there = __reduce_add_sync(~0u, there);
+        if (lane == 0 && there) atomicAdd(&s_words[__ffs(bit) - 1], there);
+        __syncthreads();
+        there = s_words[__ffs(bit) - 1];
+        if (there >= k) reach |= bit;
+        if (there >= k && there <= k + k / 16) break;
+    }
+    __syncthreads();
+    if (tid == 0) s_words[32] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+        if (x[u] && static_cast<uint32_t>(x[u] >> 32) >= reach) s_list[atomicAdd(&s_words[32], 1)] = x[u];
+    __syncthreads();
+    return s_words[32];
+}
+
 // One pass over the row computes the sum and, for every thread's share of every step (a group: kTopVecs vectors), the largest entry, which
 // stays in shared memory.  With k of the threads' largest entries at or above a number, k entries of the row are: this bound
 // leaves some k + k / 5 candidates, whose groups alone are read again (from L2) and whose places in the order are counted.
@@ -720,7 +762,7 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
     uint32_t* const s_key = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_list) + j.at_keys);
     uint16_t* const s_hit = reinterpret_cast<uint16_t*>(s_key);             // [kHits], when the keys are done with
     uint16_t* const s_group = reinterpret_cast<uint16_t*>(reinterpret_cast<char*>(s_list) + j.at_groups);      // [steps][kTopThreads]
-    __shared__ uint32_t s_count, s_hits, s_reach, s_above[16];
+    __shared__ uint32_t s_count, s_hits, s_reach, s_above[34];
     __shared__ float s_m[kWarps], s_s[kWarps];
     __shared__ Running s_run;
     const uint32_t rank = blockIdx.x & ((1u << j.rank_bits) - 1);
@@ -731,6 +773,8 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
     const uint32_t steps = (n_here + kTopStep - 1) / kTopStep;
     const T* vecs = in + cut.lead + from * N;
     Running r = {-INFINITY, 0.0f};
+    if (j.rank_bits)                                // few rows: all of a block's lines on their way at once
+        for (uint32_t i = tid; i < n_here / 8; i += kTopThreads) asm volatile("prefetch.global.L2 [%0];" :: "l"(vecs + i * 8 * N));
     if (tid == 0) s_count = 0, s_hits = 0;
     if (tid < 16) s_above[tid] = 0;
 
@@ -936,50 +980,80 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
         const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
         cluster.sync();
         if (rank == 0) {
-            for (uint32_t o = 1; o < 1u << j.rank_bits; ++o) {
-                const uint32_t n = min(*cluster.map_shared_rank(&s_count, o), j.candidates);
-                const uint64_t* list = cluster.map_shared_rank(s_list, o);
-                for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads) {
-                    uint64_t x = i0 + tid < n ? list[i0 + tid] : 0;
-                    for (;;) {
-                        if (x && taken(x)) x = 0;
-                        if (!__syncthreads_or(x != 0)) break;
-                        cut_back();
-                    }
+            // where the others' entries begin when they are counted through
+            if (warp == 0) {
+                const bool there = lane && lane < 1u << j.rank_bits;
+                uint32_t end = there ? *cluster.map_shared_rank(&s_count, lane) : 0;
+                const Running other = lane < 1u << j.rank_bits ? *cluster.map_shared_rank(&s_run, lane) : Running{-INFINITY, 0.0f};
+#pragma unroll
+                for (int d = 1; d < 1 << kClusterBits; d *= 2) {
+                    const uint32_t left = __shfl_up_sync(~0u, end, d);
+                    if (lane >= d) end += left;
                 }
-                if (tid == 0) {
-                    const Running other = *cluster.map_shared_rank(&s_run, o);
-                    s_run.join(other.m, other.s, j.c);
+                if (lane < 1u << kClusterBits) s_above[lane] = end;
+                r = warp_join(other, j.c);
+                if (lane == 0) s_run = r;
+            }
+            __syncthreads();
+            const uint32_t n = s_above[(1u << kClusterBits) - 1], had = s_count;
+            __syncthreads();
+            if (had + n <= j.candidates) {
+#pragma unroll 4
+                for (uint32_t i = tid; i < n; i += kTopThreads) {
+                    uint32_t o = 1;
+                    while (i >= s_above[o]) ++o;
+                    s_list[had + i] = cluster.map_shared_rank(s_list, o)[i - s_above[o - 1]];
+                }
+                if (tid == 0) s_count = had + n;
+            } else for (uint32_t i0 = 0; i0 < n; i0 += kTopThreads) {
+                const uint32_t i = i0 + tid;
+                uint64_t x = 0;
+                if (i < n) {
+                    uint32_t o = 1;
+                    while (i >= s_above[o]) ++o;
+                    x = cluster.map_shared_rank(s_list, o)[i - s_above[o - 1]];
+                }
+                for (;;) {
+                    if (x && taken(x)) x = 0;
+                    if (!__syncthreads_or(x != 0)) break;
+                    cut_back();
                 }
             }
         }
         cluster.sync();                             // nobody leaves while the first block reads here
         if (rank != 0) return;
     }
-    // the order: places are counted where there is a thread for every candidate
+    // the order: places are counted, unless the candidates are very many
     T* val = reinterpret_cast<T*>(j.val) + static_cast<uint64_t>(row) * j.k;
     int32_t* idx = j.idx + static_cast<uint64_t>(row) * j.k;
-    const uint32_t n = s_count;
-    if (n <= kTopThreads) {
+    uint32_t n = s_count;
+    if (n > kTopThreads && n > 2 * j.k && n <= 8 * kTopThreads) n = narrow(s_list, n, j.k, s_above);
+    if (n <= 3 * kTopThreads) {
         if (tid == 0 && n % 2) s_list[n] = 0;
         __syncthreads();
-        const uint64_t x = tid < n ? s_list[tid] : ~0ull;
-        uint32_t place = 0;
-        if (warp * 32 < n)
+        for (uint32_t i0 = warp * 32; i0 < n; i0 += kTopThreads) {
+            const uint64_t x = i0 + lane < n ? s_list[i0 + lane] : ~0ull;
+            uint32_t place = 0;
+#pragma unroll 4
             for (uint32_t i = 0; i < n; i += 2) {
                 const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&s_list[i]);
                 place += (y.x > x) + (y.y > x);
             }
-        if (tid < n && place < j.k) {
-            const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(x), u = static_cast<uint32_t>(x >> 32);
-            const float f = __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u);
-            idx[place] = static_cast<int32_t>(token);
-            val[place] = f == 0.0f || f != f ? in[token] : from_float<T>(f);       // a zero's sign and a NaN's bits are not in the key
+            if (i0 + lane < n && place < j.k) {
+                const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(x), u = static_cast<uint32_t>(x >> 32);
+                const float f = __uint_as_float(u >> 31 ? u ^ 0x80000000u : ~u);
+                idx[place] = static_cast<int32_t>(token);
+                val[place] = f == 0.0f || f != f ? in[token] : from_float<T>(f);   // a zero's sign and a NaN's bits are not in the key
+            }
         }
     } else {
+        __syncthreads();
+        if (tid == 0) s_count = n;
+        __syncthreads();
         cut_back();
         for (uint32_t i = tid; i < j.k; i += kTopThreads) {
             const uint32_t token = 0xFFFFFFFFu - static_cast<uint32_t>(s_list[i]);
+            if (token >= j.vocab) continue;         // (there are at least k candidates)
             idx[i] = static_cast<int32_t>(token);
             val[i] = in[token];
         }
@@ -1012,7 +1086,7 @@ template <typename T, int MODE, int PLACE, int THREADS> int launch_shape(Job j, 
     const uint32_t data = PLACE == kDevice ? 0 : j.staged * 16;
     j.at_table = data;
     const size_t shared = data + beside;
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, PLACE, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
+    if (shared > 46 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_distill<T, MODE, PLACE, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(j.n_rows << j.rank_bits);
     cfg.blockDim = dim3(THREADS);
@@ -1087,20 +1161,21 @@ int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
 }
 
 template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
-    // several blocks a row as long as all of them are on the SMs at once and each has some steps to do, or where one could
+    // several blocks a row as long as that makes no more than eight to an SM and each has some steps to do (300 x 131072 bf16: 37 us, 44
+    // with one block a row), or where one could
     // not hold the groups of a row
     const uint32_t n_vecs = j.vocab / kVec<T> + 1;
     while (j.rank_bits < kClusterBits &&
            ((n_vecs >> j.rank_bits) / kTopVecs > kTopGroups - kTopThreads ||
-            ((static_cast<uint64_t>(n_rows) << j.rank_bits) * 2 <= 4ull * n_sms && n_vecs >> j.rank_bits >= 2 * kTopStep)))
+            ((static_cast<uint64_t>(n_rows) << j.rank_bits) * 2 <= 8ull * n_sms && n_vecs >> j.rank_bits >= 2 * kTopStep)))
         ++j.rank_bits;
     const uint32_t ranks = 1u << j.rank_bits, steps = ((n_vecs + ranks - 1) / ranks + kTopStep - 1) / kTopStep;
-    const TopShared shared(j.k, steps);
+    const TopShared shared(j.k, steps, j.rank_bits);
     j.candidates = shared.candidates;
     j.at_keys = shared.keys;
     j.at_groups = shared.groups;
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_top_logits<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      static_cast<int>(TopShared(kMaxPairs, kTopGroups / kTopThreads).bytes)));
+    if (shared.bytes > 46 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_top_logits<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(TopShared(kMaxPairs, kTopGroups / kTopThreads, 0).bytes)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_rows * ranks);
     cfg.blockDim = dim3(kTopThreads);

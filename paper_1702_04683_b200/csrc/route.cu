@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
         for (int i = 0; i < V; ++i) {
             bias[i] = first + i < E ? j.bias[first + i] : 0.0f;
             bad_bias |= bias[i] != bias[i];
-            if (bias[i] != -INFINITY) bias_most = fmaxf(bias_most, fabsf(bias[i]));
+            if (fabsf(bias[i]) < INFINITY) bias_most = fmaxf(bias_most, fabsf(bias[i]));
         }
         bias_most = warp_max(bias_most);
     }
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                     uint32_t place = 0;
                     for (uint32_t i = 0; i < n; ++i) place += list[i] > mine;
                     if (lane < n && place < rounds) places[place] = make_uint2(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
-                    if (lane >= n && lane < rounds) places[lane] = make_uint2(0, 0);
+                    if (n + lane < rounds) places[n + lane] = make_uint2(0, 0);
                 } else {                                    // by rounds
                     uint32_t two = 0, at_one = 0, at_two = 0, taken = 0;
                     auto at_hand = [&] {
@@ -588,7 +588,7 @@ uint32_t share_of(uint32_t experts) {
 
 template <typename T, int V> int launch_route(const Job& j, int n_sms, cudaStream_t stream) {
     const size_t smem = kWarps * j.cfg.experts * sizeof(double) + j.cfg.experts * sizeof(uint32_t);
-    ADACOMP_CUDA(cudaFuncSetAttribute(k_route<T, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    if (smem > 44 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_route<T, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     k_route<T, V><<<grid_of(n_sms, j.n_rows, kWarps, 6), kThreads, smem, stream>>>(j);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;

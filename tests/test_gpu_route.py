@@ -336,3 +336,21 @@ def test_refusals(binding):
     with pytest.raises(binding.AdacompError):
         h.grad(x, experts, weights, out=torch.zeros(40, device="cuda").as_strided((4, 8), (4, 1)))
     assert h.last_error() == 0
+
+
+def test_rows_with_exactly_a_warps_candidates(binding):
+    """32 experts to choose from and 32 places: nothing stands behind the last one."""
+    for experts, groups in ((32, 1), (96, 3), (1024, 32)):
+        bias = torch.randn(experts, device="cuda", generator=gen(experts)) * 0.05
+        for score in ("softmax", "sigmoid"):
+            check(binding, rows(300, experts, "f32", experts), bias, top_k=32, score=score, groups=groups, top_groups=1, group_terms=2)
+
+
+def test_infinite_biases(binding):
+    """+Inf: chosen before all others, of several the lowest first; -Inf: never."""
+    bias = torch.zeros(64, device="cuda")
+    bias[[50, 9, 33]] = math.inf
+    bias[:5] = -math.inf
+    for score in ("softmax", "sigmoid"):
+        experts, _, _, _ = check(binding, rows(40, 64, "bf16", 3), bias, top_k=5, score=score)
+        assert bool((experts[:, :3] == torch.tensor([9, 33, 50], device="cuda", dtype=torch.int32)).all()) and bool((experts >= 5).all())
