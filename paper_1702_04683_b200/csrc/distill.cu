@@ -16,6 +16,7 @@
 
 using namespace adacomp;
 
+// (The tests of arguments make such objects themselves, to do without a GPU: new members go to the end.)
 struct adacomp_distill {
     int device;
     uint32_t vocab;

@@ -15,6 +15,7 @@
 
 using namespace adacomp;
 
+// (The tests of arguments make such objects themselves, to do without a GPU: new members go to the end.)
 struct adacomp_route {
     int device;
     adacomp_route_config_t config;
