@@ -758,7 +758,7 @@ __device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k
 template <typename T>
 __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) {
     constexpr int N = kVec<T>, kWarps = kTopThreads / 32;
-    static_assert(kHits * sizeof(uint16_t) >= kTopThreads * sizeof(uint32_t) && kTopGroups <= 65536, "rooms");
+    static_assert(kHits * sizeof(uint16_t) >= 2 * kTopThreads * sizeof(uint32_t) && kTopGroups <= 65536, "rooms");
     extern __shared__ uint64_t s_list[];            // [candidates]
     uint32_t* const s_key = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_list) + j.at_keys);
     uint16_t* const s_hit = reinterpret_cast<uint16_t*>(s_key);             // [kHits], when the keys are done with
@@ -780,8 +780,8 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
     if (tid < 16) s_above[tid] = 0;
 
     // the pass over the row
-    float largest = -INFINITY;
-    auto step = [&](const uint4 (&p)[kTopVecs], uint32_t s, uint32_t have) {       // `have` of the thread's vectors are there
+    float even = -INFINITY, odd = -INFINITY;        // the thread's largest entries, of its even and odd steps
+    auto step = [&](const uint4 (&p)[kTopVecs], float& largest, uint32_t s, uint32_t have) {       // `have` of the thread's vectors are there
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kTopVecs; ++i)
@@ -823,37 +823,38 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
         uint32_t s = 0;
         for (; s + 1 < whole; s += 2) {
             fetch(b, s + 1);
-            step(a, s, kTopVecs);
+            step(a, even, s, kTopVecs);
             fetch(a, s + 2);
-            step(b, s + 1, kTopVecs);
+            step(b, odd, s + 1, kTopVecs);
         }
         if (s < whole) {
             fetch(b, s + 1);
-            step(a, s, kTopVecs);
-            if (have) step(b, s + 1, have);
+            step(a, even, s, kTopVecs);
+            if (have) step(b, odd, s + 1, have);
         } else if (have) {
-            step(a, s, have);
+            step(a, even, s, have);
         }
     }
 
-    // The bound: bit by bit the largest number that k of the largest entries reach, or until not many more than k do.  Up to half
-    // as many as threads, the threads' largest entries tell them apart well enough, above it the groups' do.
+    // The bound: bit by bit the largest number that k of the largest entries reach, or until not many more than k do.  Up to as
+    // many as threads, the threads' two largest entries tell them apart well enough, above it the groups' do.
     const uint32_t own = tid < n_here ? (n_here - tid + kTopStep - 1) / kTopStep : 0;      // groups of this thread
     const uint32_t enough = j.k + j.k / 16;
-    const bool coarse = j.k <= kTopThreads / 2;
-    s_key[tid] = own ? order_of(largest) : 0;
+    const bool coarse = j.k <= kTopThreads;
+    s_key[tid] = own ? order_of(even) : 0;
+    s_key[kTopThreads + tid] = own > 1 ? order_of(odd) : 0;
     r = warp_join(r, j.c);
     if (lane == 0) s_m[warp] = r.m, s_s[warp] = r.s;
     __syncthreads();
-    uint32_t key[kWarps], low = ~0u, high = 0;
+    constexpr int kKeys = 2 * kWarps;
+    uint32_t key[kKeys], low = ~0u, high = 0;
     if (warp == 0 || !coarse) {
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) key[i] = s_key[i * 32 + lane], low = min(low, key[i]), high = max(high, key[i]);
+        for (int i = 0; i < kKeys; ++i) key[i] = s_key[i * 32 + lane], low = min(low, key[i]), high = max(high, key[i]);
         low = __reduce_min_sync(~0u, low), high = __reduce_max_sync(~0u, high);
-        if (j.k > kTopThreads) low = 0;             // so many groups need not reach every thread's largest entry
     }
     if (!coarse) {
-        low >>= 16, high >>= 16;
+        low = 0, high >>= 16;                       // (so many groups need not reach every thread's largest entry)
         const uint32_t same = __clz(low ^ high);
         uint32_t reach = same == 32 ? high : high & ~(0xFFFFFFFFu >> same);
         uint32_t bit = same == 32 ? 0 : 0x80000000u >> same;
@@ -878,7 +879,8 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
             for (int b = 0; b < kBoundBits && bit; ++b, bit >>= 1) {
                 uint32_t n = 0;
 #pragma unroll
-                for (int i = 0; i < kWarps; ++i) n += __popc(__ballot_sync(~0u, key[i] >= (reach | bit)));
+                for (int i = 0; i < kKeys; ++i) n += key[i] >= (reach | bit);
+                n = __reduce_add_sync(~0u, n);
                 if (n >= j.k) reach |= bit;
                 if (n >= j.k && n <= enough) break;
             }
