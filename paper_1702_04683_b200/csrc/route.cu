@@ -33,6 +33,9 @@ constexpr uint32_t kMaxExperts = 1024;
 constexpr uint32_t kMaxChosen = 32;
 constexpr uint32_t kMaxGroups = 32;
 constexpr double kLog2e = 1.4426950408889634;
+// Blocks of the choice on an SM, and as many in the grid: with four 16384 x 256 in groups, 20001 x 60 and 65536 x 128 (both with their
+// gradient) took 38, 28 and 60 us, with five 34, 29 and 61, with six 34, 30 and 66.
+constexpr int kRouteBlocks = 5;
 
 struct Job {
     Rows logits, out;
@@ -70,6 +73,7 @@ __device__ __forceinline__ float exp2_of(float x) {
     return y;
 }
 
+// One unit in the last place off at most; an infinity's is 0.
 __device__ __forceinline__ float reciprocal_of(float x) {
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -122,9 +126,9 @@ template <typename V> __device__ __forceinline__ V rate(const V* s_v, uint32_t s
     return terms == 2 && second != none ? first + second : first;
 }
 
-// The choice in 64 bits, a lane's place in its result: for rows in which fp32 does not tell candidates apart.  s_v: room for a row.
+// A row's values in 64 bits, and its best groups by them, for rows in which fp32 does not tell those apart.  s_v: room for a row.
 template <typename T>
-__device__ __noinline__ int choose_careful(double* s_v, const T* l, const float* bias, const adacomp_route_config_t& cfg) {
+__device__ __noinline__ uint32_t groups_careful(double* s_v, const T* l, const float* bias, const adacomp_route_config_t& cfg) {
     const uint32_t lane = threadIdx.x % 32, size = cfg.experts / cfg.groups;
     const bool soft = cfg.score == ADACOMP_SOFTMAX;
     float most = -INFINITY;
@@ -141,12 +145,17 @@ __device__ __noinline__ int choose_careful(double* s_v, const T* l, const float*
     sum = warp_sum(sum);
     for (uint32_t e = lane; e < cfg.experts; e += 32) s_v[e] = (soft ? s_v[e] / sum : s_v[e]) + (bias ? static_cast<double>(bias[e]) : 0.0);
     __syncwarp();
-    uint32_t kept = ~0u;
-    if (cfg.top_groups < cfg.groups) {
-        bool close;
-        double least;
-        kept = best_groups(lane < cfg.groups ? rate(s_v + lane * size, size, cfg.group_terms) : none, cfg, 0.0, &close, &least);
-    }
+    if (cfg.top_groups == cfg.groups) return ~0u;
+    bool close;
+    double least;
+    return best_groups(lane < cfg.groups ? rate(s_v + lane * size, size, cfg.group_terms) : none, cfg, 0.0, &close, &least);
+}
+
+// The choice in 64 bits, a lane's place in its result.
+template <typename T>
+__device__ __noinline__ int choose_careful(double* s_v, const T* l, const float* bias, const adacomp_route_config_t& cfg) {
+    const uint32_t lane = threadIdx.x % 32, size = cfg.experts / cfg.groups, kept = groups_careful<T>(s_v, l, bias, cfg);
+    const double none = -INFINITY;
     int id = -1;
     for (uint32_t r = 0; r < cfg.top_k; ++r) {
         double best = none;
@@ -205,7 +214,7 @@ __device__ __forceinline__ float quotient(float s, float x, bool soft, uint32_t 
         s = x == -INFINITY ? 0.0f : expf(x - top);
         sum = __shfl_sync(~0u, part_sum(s, width), 0);
     }
-    return sum > 0.0f ? s / sum : 0.0f;
+    return sum > 0.0f ? s * reciprocal_of(sum) : 0.0f;
 }
 
 // One warp per row, V consecutive experts per lane.  Where a row has more candidates than a warp lanes (ties, long choices), every lane
@@ -215,9 +224,9 @@ __device__ __forceinline__ float quotient(float s, float x, bool soft, uint32_t 
 // What is compared is the logit itself where scores rise with it and nothing is added to them; otherwise fp32 values, and a row in which
 // two candidates lie closer than those can tell (and do not have the same logit and bias) is decided in 64 bits.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job j) {
+__global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(const __grid_constant__ Job j) {
     __shared__ uint2 s_places[kWarps][kMaxChosen + 1];      // a row's choice: order of the value, expert
-    __shared__ uint64_t s_lists[kWarps][32];                // its candidates
+    __shared__ __align__(16) uint64_t s_lists[kWarps][32];                // its candidates
     extern __shared__ double s_rows[];                      // a row of values per warp then the counts
     __shared__ bool s_last;
     const adacomp_route_config_t& cfg = j.cfg;
@@ -314,8 +323,9 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                     }
                     bool border;
                     float least;
-                    const uint32_t kept = best_groups(rating, cfg, tol, &border, &least);
-                    close |= by_logit ? tied_in_64(least, base, soft) || tied_in_64(most, base, soft) : border;
+                    uint32_t kept = best_groups(rating, cfg, tol, &border, &least);
+                    if (by_logit) close = tied_in_64(least, base, soft) || tied_in_64(most, base, soft);
+                    else if (border) kept = groups_careful<T>(s_wide, l, j.bias, cfg);
                     if (team) {
                         if (!(kept >> (lane / team) & 1))
 #pragma unroll
@@ -332,7 +342,9 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
 #pragma unroll
                 for (int i = 0; i < V; ++i) one = max(one, key[i]);
                 uint32_t floor = 0;
-                for (uint32_t r = 0, left = one; r < rounds; ++r) {
+                uint32_t left = one;
+#pragma unroll 4
+                for (uint32_t r = 0; r < rounds; ++r) {
                     floor = __reduce_max_sync(~0u, left);
                     if (left == floor) left = 0;
                 }
@@ -346,13 +358,17 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                     if (key[i] >= floor && place < 32) list[place] = static_cast<uint64_t>(key[i]) << 32 | (0xFFFFFFFFu - (first + i));
                     n += __popc(there);
                 }
+                if (lane == 0 && n < 32) list[n] = 0;
                 uint2* const places = s_places[warp];
                 __syncwarp();
                 uint64_t mine = 0;
                 if (n <= 32) {
                     mine = lane < n ? list[lane] : 0;
                     uint32_t place = 0;
-                    for (uint32_t i = 0; i < n; ++i) place += list[i] > mine;
+                    for (uint32_t i = 0; i < n; i += 2) {   // (an odd one's neighbour is made nothing)
+                        const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&list[i]);
+                        place += (two.x > mine) + (two.y > mine);
+                    }
                     if (lane < n && place < rounds) places[place] = make_uint2(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
                     if (n + lane < rounds) places[n + lane] = make_uint2(0, 0);
                 } else {                                    // by rounds
@@ -427,9 +443,9 @@ __global__ void __launch_bounds__(kThreads) k_route(const __grid_constant__ Job 
                 if (close) id = choose_careful<T>(s_wide, l, j.bias, cfg);
                 const float xs = id < 0 ? -INFINITY : close ? to_float(l[id]) : chosen;
                 float s;
-                if (!soft) s = 1.0f / (1.0f + expf(-xs));
+                if (!soft) s = reciprocal_of(1.0f + expf(-xs));
                 else if (cfg.renormalize) s = expf(xs - (by_logit && !close ? __shfl_sync(~0u, xs, 0) : warp_max(xs)));    // relative to the largest chosen one
-                else s = expf(xs - base) / total;
+                else s = expf(xs - base) * reciprocal_of(total);
                 if (id < 0) s = 0.0f;
                 if (cfg.renormalize) s = quotient(s, xs, soft, width);
                 w = s * cfg.scale;
@@ -496,14 +512,14 @@ __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__
         __syncwarp();                                       // in place, the rows' logits are gone from here on
         for (uint32_t r = 0; r < rows && row0 + r < j.n_rows; ++r)
             clear_row(reinterpret_cast<T*>(j.out.data) + j.out.offset(static_cast<uint32_t>(row0 + r)), E, j.wide, lane);
-        float s = id < 0 ? 0.0f : 1.0f / (1.0f + expf(-x));
-        const float rest = soft ? 1.0f : 1.0f / (1.0f + expf(x));
+        float s = id < 0 ? 0.0f : reciprocal_of(1.0f + expf(-x));
+        const float rest = soft ? 1.0f : reciprocal_of(1.0f + expf(x));
         if (j.cfg.renormalize) {
             const float top = part_max(x, width);
             float sum = part_sum(s, width);
             if (soft || sum < 0x1p-90f) s = id < 0 ? 0.0f : expf(x - top);          // see quotient()
             sum = part_sum(s, width);
-            s = sum > 0.0f ? s / sum : 0.0f;
+            s = sum > 0.0f ? s * reciprocal_of(sum) : 0.0f;
             d -= part_sum(d * s, width);
         }
         __syncwarp();
@@ -590,7 +606,7 @@ uint32_t share_of(uint32_t experts) {
 template <typename T, int V> int launch_route(const Job& j, int n_sms, cudaStream_t stream) {
     const size_t smem = kWarps * j.cfg.experts * sizeof(double) + j.cfg.experts * sizeof(uint32_t);
     if (smem > 44 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_route<T, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    k_route<T, V><<<grid_of(n_sms, j.n_rows, kWarps, 6), kThreads, smem, stream>>>(j);
+    k_route<T, V><<<grid_of(n_sms, j.n_rows, kWarps, V <= 8 ? kRouteBlocks : 2), kThreads, smem, stream>>>(j);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
 }
