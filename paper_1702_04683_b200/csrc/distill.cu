@@ -335,7 +335,7 @@ __device__ __noinline__ Running careful_sum(const Chunk<T, PLACE> chunk, float c
 // PLACE: a thread's vectors are copied to shared memory by itself and stay there for the second pass, so that a logit crosses HBM once and
 // nothing waits for a load but its own thread; of rows too long for that the rest is read twice.
 template <typename T, int MODE, int PLACE, int THREADS>
-__global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : 1024) / THREADS) k_distill(const Job j) {
+__global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 384 ? 1152 : 1024) / THREADS) k_distill(const Job j) {
     constexpr int N = kVec<T>, kBatch = 4, kWarps = THREADS / 32;
     constexpr bool STAGED = PLACE != kDevice;
     constexpr uint32_t kThreads = THREADS;
@@ -1081,11 +1081,15 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
 bool good_temperature(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 
 // Rows of loss_grad stay in shared memory as far as they find room there, next to those of the SM's other blocks.
+// Three blocks of 384 threads for rows longer than what they find, unless much of that is taken by the list: 4096 x 131072 bf16 499 us, two
+// of 512 539 (with the rest as a class, whose bits take 16 KB, 579 and 539); 2048 x 65536 fp32 256 and 267.  Rows that find room in one of
+// 512 altogether: 8192 x 50000 bf16 385, three of 384 411.
 constexpr uint32_t kRoom = 110 * 1024;              // of a block of 512 threads, two on an SM
-constexpr uint32_t kSmallRoom = 74 * 1024;          // of one of 256, three on an SM
+constexpr uint32_t kSmallRoom = 74 * 1024;          // of one of 256 or 384, three on an SM
+constexpr uint32_t kLargeList = 12 * 1024;
 
 template <typename T, int MODE, int PLACE, int THREADS> int launch_shape(Job j, uint32_t chunk_vecs, uint32_t beside, cudaStream_t stream) {
-    j.staged = PLACE == kPartly ? (kRoom - beside) / 16 / (4 * THREADS) * (4 * THREADS) : chunk_vecs;
+    j.staged = PLACE == kPartly ? ((THREADS == 512 ? kRoom : kSmallRoom) - beside) / 16 / (4 * THREADS) * (4 * THREADS) : chunk_vecs;
     const uint32_t data = PLACE == kDevice ? 0 : j.staged * 16;
     j.at_table = data;
     const size_t shared = data + beside;
@@ -1124,6 +1128,7 @@ template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_
     if constexpr (MODE == kBoth) {
         if (chunk_vecs * 16ull + beside <= kSmallRoom) return launch_shape<T, MODE, kShared, 256>(j, chunk_vecs, beside, stream);
         if (chunk_vecs * 16ull + beside <= kRoom) return launch_shape<T, MODE, kShared, 512>(j, chunk_vecs, beside, stream);
+        if (beside <= kLargeList) return launch_shape<T, MODE, kPartly, 384>(j, chunk_vecs, beside, stream);
         return launch_shape<T, MODE, kPartly, 512>(j, chunk_vecs, beside, stream);
     } else {
         return launch_shape<T, MODE, kDevice, 256>(j, chunk_vecs, beside, stream);
