@@ -552,14 +552,14 @@ ADACOMP_API int adacomp_distill_create(adacomp_distill_t** h, uint32_t vocab, vo
  *   d_lse_out [n_rows]      NULL, or log(sum of exp(l / temperature)): -Inf where every logit is -Inf, NaN where one is NaN or +Inf.
  * temperature lies in 2^-20 .. 2^20 (here and below).  Outputs are aligned to their elements and do not overlap the logits. */
 ADACOMP_API int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, uint32_t k,
-                                   float temperature, int32_t* d_idx_out, void* d_val_out, float* d_lse_out, void* cuda_stream);
+                                   double temperature, int32_t* d_idx_out, void* d_val_out, float* d_lse_out, void* cuda_stream);
 
 /* The student's side.  With p = softmax(s / T) over a row's `vocab` logits s, t the teacher's listed logits and sums over the
  * listed tokens:
  *   d_lse = NULL:  q = softmax(t / T) over the list,               L = sum q (log q - log p);
  *   otherwise:     q = exp(t / T - lse), r = max(0, 1 - sum q),    L = sum q (log q - log p) + r (log r - log(sum of p not listed)):
  *                  what the teacher did not list is one more class; it is left out where the student gives it nothing
- *                  (less than 2^-126 of its largest probability), since r cannot be told from rounding there.
+ *                  (less than 2^-126 of its largest listed probability), since r cannot be told from rounding there.
  * Terms with q = 0 are 0.  The gradient of L with respect to s_j is, with W = sum q (+ r), (W p_j - q_j) / T for a listed token and
  * (W - r / (sum of p not listed)) p_j / T for another.  A row's loss is L; its gradient is that of d_weight[row] * L (NULL: 1), so
  * the mean over the tokens, a loss scale or T^2 go into the weight.  Rows whose weight is 0, or without any entry, or whose q
@@ -575,13 +575,13 @@ ADACOMP_API int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* l
  * any input.  Errors: ADACOMP_ERR_INVALID (null pointer, unknown type, misaligned pointer, k or temperature out of range, rows of out
  * that overlap each other), ADACOMP_ERR_CUDA. */
 ADACOMP_API int adacomp_distill_loss(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
-                                     const adacomp_pairs_t* pairs, float temperature, const float* d_weight, float* d_loss_out,
+                                     const adacomp_pairs_t* pairs, double temperature, const float* d_weight, float* d_loss_out,
                                      float* d_stats_out, void* cuda_stream);
 ADACOMP_API int adacomp_distill_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
-                                     const adacomp_pairs_t* pairs, float temperature, const float* d_weight,
+                                     const adacomp_pairs_t* pairs, double temperature, const float* d_weight,
                                      const float* d_stats, const adacomp_rows_t* out, void* cuda_stream);
 ADACOMP_API int adacomp_distill_loss_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
-                                          const adacomp_pairs_t* pairs, float temperature, const float* d_weight,
+                                          const adacomp_pairs_t* pairs, double temperature, const float* d_weight,
                                           float* d_loss_out, const adacomp_rows_t* out, void* cuda_stream);
 /* Waits for cuda_stream, returns and clears the first error recorded on the device. */
 ADACOMP_API int adacomp_distill_last_error(adacomp_distill_t* h, void* cuda_stream);
@@ -622,6 +622,7 @@ ADACOMP_API int adacomp_route_create(adacomp_route_t** h, const adacomp_route_co
  *   d_weights_out [n_rows][top_k]  scale * score (the bias is not in it), divided by the row's sum of chosen scores if
  *                                  renormalize is set; 0 in places without an expert
  *   d_counts_out  [experts]        NULL, or how many places of the call name each expert (what a balancing bias is adjusted by)
+ * (none of which overlaps the inputs).
  * d_live (NULL: all; bytes, 0 or 1): rows with 0 are padding: experts -1, weights 0, not read.  A row with a NaN (in a logit
  * or bias), or with +Inf under softmax, has no scores: experts -1, weights NaN. */
 ADACOMP_API int adacomp_route(adacomp_route_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const float* d_bias,

@@ -67,7 +67,7 @@ def _load():
             f"{LIB_PATH} is missing: build it with `python -m paper_1702_04683_b200.build` "
             "(nvcc, sm_100a). There is no fallback implementation.")
     L = ctypes.CDLL(LIB_PATH)
-    vp, u32, u64, i32, f32 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int, ctypes.c_float
+    vp, u32, u64, i32, f32, f64 = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_int, ctypes.c_float, ctypes.c_double
     P = ctypes.POINTER
     sig = {
         "adacomp_status_string": (ctypes.c_char_p, [i32]),
@@ -125,10 +125,10 @@ def _load():
         "adacomp_embed_destroy": (i32, [vp]),
         "adacomp_distill_workspace_bytes": (i32, [u32, P(ctypes.c_size_t)]),
         "adacomp_distill_create": (i32, [P(vp), u32, vp, ctypes.c_size_t, i32]),
-        "adacomp_top_logits": (i32, [vp, vp, u32, u32, f32, vp, vp, vp, vp]),
-        "adacomp_distill_loss": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
-        "adacomp_distill_grad": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
-        "adacomp_distill_loss_grad": (i32, [vp, vp, u32, vp, f32, vp, vp, vp, vp]),
+        "adacomp_top_logits": (i32, [vp, vp, u32, u32, f64, vp, vp, vp, vp]),
+        "adacomp_distill_loss": (i32, [vp, vp, u32, vp, f64, vp, vp, vp, vp]),
+        "adacomp_distill_grad": (i32, [vp, vp, u32, vp, f64, vp, vp, vp, vp]),
+        "adacomp_distill_loss_grad": (i32, [vp, vp, u32, vp, f64, vp, vp, vp, vp]),
         "adacomp_distill_last_error": (i32, [vp, vp]),
         "adacomp_distill_destroy": (i32, [vp]),
         "adacomp_route_workspace_bytes": (i32, [P(RouteConfig), P(ctypes.c_size_t)]),
@@ -901,6 +901,13 @@ def _logit_rows(t: torch.Tensor, width: int, device: int, name: str) -> Rows:
     return _rows(t, len(shape) - 1, kind, name)
 
 
+def _row_count(logits: torch.Tensor, width: int) -> int:
+    n = logits.numel() // width
+    if n >= 1 << 31:
+        raise ValueError("logits: too many rows")
+    return n
+
+
 def _span(t: torch.Tensor):
     """The bytes between a tensor's first entry and its last."""
     at = t.data_ptr()
@@ -977,7 +984,7 @@ class Distiller(_Handle):
         first, of equal ones the lowest token first; lse = log sum exp(logits / temperature) over the whole row."""
         rows = _logit_rows(logits, self.vocab, self._index, "logits")
         lead, k = logits.shape[:-1], int(k)
-        n = logits.numel() // self.vocab
+        n = _row_count(logits, self.vocab)
         if not 0 <= k < 1 << 32:
             raise ValueError("k: out of range")
         index, shape = self._index, (*lead, k)
@@ -993,7 +1000,7 @@ class Distiller(_Handle):
         index = self._index
         rows = _logit_rows(logits, self.vocab, index, "logits")
         lead = logits.shape[:-1]
-        n = logits.numel() // self.vocab
+        n = _row_count(logits, self.vocab)
         kind = TOKEN_TYPES.get(idx.dtype)
         if kind is None or idx.get_device() != index:
             raise TypeError(f"idx: need an int32 or int64 tensor on {self.device}")
@@ -1101,7 +1108,7 @@ class Router(_Handle):
         -1, weights 0); counts: how many places name each expert."""
         rows = _logit_rows(logits, self.experts, self._index, "logits")
         lead, k = logits.shape[:-1], self.top_k
-        n = logits.numel() // self.experts
+        n = _row_count(logits, self.experts)
         index, shape = self._index, (*lead, k)
         experts_out, experts_at = _result(experts_out, logits, shape, torch.int32, n * k, index, "experts_out", stream)
         weights_out, weights_at = _result(weights_out, logits, shape, torch.float32, n * k, index, "weights_out", stream)
@@ -1116,7 +1123,7 @@ class Router(_Handle):
         """Gradient of the logits from that of the weights (float32 [..., top_k]), the choice held fixed; ``out`` may be the
         logits themselves."""
         rows = _logit_rows(logits, self.experts, self._index, "logits")
-        n = logits.numel() // self.experts
+        n = _row_count(logits, self.experts)
         out = _gradient_for(out, logits, stream)
         _check(_lib.adacomp_route_grad(self._h, ctypes.byref(rows), n,
                                        _per_row(experts, torch.int32, n * self.top_k, self._index, "experts"),

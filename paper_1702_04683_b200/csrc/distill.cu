@@ -9,6 +9,7 @@
 // All of it is bound by HBM: every logit is read once and, with a gradient, one entry written for it; one exponential
 // (two with a gradient) per logit.
 #include <cooperative_groups.h>
+#include <limits.h>
 #include <math.h>
 #include <new>
 
@@ -651,6 +652,7 @@ struct TopJob {
     uint32_t vocab, k, rank_bits;
     uint32_t candidates, at_keys, at_groups;        // room of the list, places in shared memory
     float c;
+    double inv_t;
 };
 
 // Order of logits as whole numbers: NaN above all, +0 and -0 equal; below it the token, the lowest first.
@@ -1072,13 +1074,14 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
         r = warp_join(r, j.c);
         r.join(s_run.m, s_run.s, j.c);
         if (lane == 0)
-            j.lse[row] = static_cast<float>(r.s != r.s ? static_cast<double>(r.s) : r.m == -INFINITY ? -INFINITY : reference(r.m, j.c) * kLn2 + log(static_cast<double>(r.s)));
+            j.lse[row] = static_cast<float>(r.s != r.s ? static_cast<double>(r.s) : r.m == -INFINITY ? -INFINITY
+                                                    : r.m * j.inv_t + (reference(r.m, j.c) - static_cast<double>(r.m) * j.c) * kLn2 + log(static_cast<double>(r.s)));      // (c is rounded, 1 / T is not)
     }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
 
-bool good_temperature(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
+bool good_temperature(double t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 
 // Rows of loss_grad stay in shared memory as far as they find room there, next to those of the SM's other blocks.
 // Three blocks of 384 threads for rows longer than what they find, unless much of that is taken by the list: 4096 x 131072 bf16 499 us, two
@@ -1120,6 +1123,7 @@ template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_
            ((n_vecs >> j.rank_bits) * kVec<T> > kMaxVocab / 4 ||
             ((static_cast<uint64_t>(j.n_rows) << j.rank_bits) * 2 <= 2ull * n_sms && n_vecs >> j.rank_bits >= 1024)))
         ++j.rank_bits;
+    if (static_cast<uint64_t>(j.n_rows) << j.rank_bits > INT_MAX) return ADACOMP_ERR_INVALID;     // more blocks than a grid has
     const uint32_t chunk_vecs = (n_vecs + (1u << j.rank_bits) - 1) >> j.rank_bits;
     j.table_bits = 5;
     while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
@@ -1136,7 +1140,7 @@ template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_
 }
 
 template <int MODE>
-int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs, float temperature,
+int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs, double temperature,
             const float* d_weight, float* d_loss, float* d_stats, const adacomp_rows_t* out, void* cuda_stream) {
     if (!h || !pairs || !good_temperature(temperature) || n_rows >= (1u << 31)) return ADACOMP_ERR_INVALID;
     if (pairs->k == 0 || pairs->k > kMaxPairs) return ADACOMP_ERR_INVALID;
@@ -1177,6 +1181,7 @@ template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaS
            ((n_vecs >> j.rank_bits) / kTopVecs > kTopGroups - kTopThreads ||
             ((static_cast<uint64_t>(n_rows) << j.rank_bits) * 2 <= 8ull * n_sms && n_vecs >> j.rank_bits >= 2 * kTopStep)))
         ++j.rank_bits;
+    if (static_cast<uint64_t>(n_rows) << j.rank_bits > INT_MAX) return ADACOMP_ERR_INVALID;       // more blocks than a grid has
     const uint32_t ranks = 1u << j.rank_bits, steps = ((n_vecs + ranks - 1) / ranks + kTopStep - 1) / kTopStep;
     const TopShared shared(j.k, steps, j.rank_bits);
     j.candidates = shared.candidates;
@@ -1238,7 +1243,7 @@ int adacomp_distill_create(adacomp_distill_t** h, uint32_t vocab, void* d_worksp
     return ADACOMP_OK;
 }
 
-int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, uint32_t k, float temperature,
+int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, uint32_t k, double temperature,
                        int32_t* d_idx_out, void* d_val_out, float* d_lse_out, void* cuda_stream) {
     if (!h || n_rows >= (1u << 31) || !good_temperature(temperature)) return ADACOMP_ERR_INVALID;
     if (k == 0 || k > kMaxPairs || k > h->vocab) return ADACOMP_ERR_INVALID;
@@ -1254,6 +1259,7 @@ int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint3
     j.vocab = h->vocab;
     j.k = k;
     j.c = static_cast<float>(kLog2e / temperature);
+    j.inv_t = 1.0 / temperature;
     DeviceGuard guard(h->device);
     ADACOMP_CUDA(guard.err);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
@@ -1263,17 +1269,17 @@ int adacomp_top_logits(adacomp_distill_t* h, const adacomp_rows_t* logits, uint3
 }
 
 int adacomp_distill_loss(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs,
-                         float temperature, const float* d_weight, float* d_loss_out, float* d_stats_out, void* cuda_stream) {
+                         double temperature, const float* d_weight, float* d_loss_out, float* d_stats_out, void* cuda_stream) {
     return distill<kLoss>(h, logits, n_rows, pairs, temperature, d_weight, d_loss_out, d_stats_out, nullptr, cuda_stream);
 }
 
 int adacomp_distill_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs,
-                         float temperature, const float* d_weight, const float* d_stats, const adacomp_rows_t* out, void* cuda_stream) {
+                         double temperature, const float* d_weight, const float* d_stats, const adacomp_rows_t* out, void* cuda_stream) {
     return distill<kGrad>(h, logits, n_rows, pairs, temperature, d_weight, nullptr, const_cast<float*>(d_stats), out, cuda_stream);
 }
 
 int adacomp_distill_loss_grad(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows, const adacomp_pairs_t* pairs,
-                              float temperature, const float* d_weight, float* d_loss_out, const adacomp_rows_t* out, void* cuda_stream) {
+                              double temperature, const float* d_weight, float* d_loss_out, const adacomp_rows_t* out, void* cuda_stream) {
     return distill<kBoth>(h, logits, n_rows, pairs, temperature, d_weight, d_loss_out, nullptr, out, cuda_stream);
 }
 

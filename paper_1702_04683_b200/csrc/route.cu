@@ -8,6 +8,7 @@
 //   softmax: dl_e = s_e (ds_e - sum ds s); renormalised this vanishes outside of the chosen ones and is a softmax's over those
 //
 // Rows are short: large calls are bound by instruction issue (the rounds of the choice), small ones by the launch.
+#include <limits.h>
 #include <math.h>
 #include <new>
 
@@ -225,7 +226,7 @@ __device__ __forceinline__ float quotient(float s, float x, bool soft, uint32_t 
 // two candidates lie closer than those can tell (and do not have the same logit and bias) is decided in 64 bits.
 template <typename T, int V>
 __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(const __grid_constant__ Job j) {
-    __shared__ uint2 s_places[kWarps][kMaxChosen + 1];      // a row's choice: order of the value, expert
+    __shared__ uint2 s_places[kWarps][kMaxChosen];      // a row's choice: order of the value, expert
     __shared__ __align__(16) uint64_t s_lists[kWarps][32];                // its candidates
     extern __shared__ double s_rows[];                      // a row of values per warp then the counts
     __shared__ bool s_last;
@@ -240,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
     // lanes of a group, where groups are whole lanes and their number a power of two; 0 otherwise
     uint32_t width = 1;                                     // lanes that hold a row's places
     while (width < K) width *= 2;
-    const uint32_t below = (1u << lane) - 1, rounds = by_logit ? K : K + 1;
+    const uint32_t below = (1u << lane) - 1;
     const uint32_t team = size % V == 0 && (size / V & (size / V - 1)) == 0 && E == 32 * V ? size / V : 0;
     float bias[V], bias_most = 0.0f;
     bool bad_bias = false;
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                             if (first + i >= E || !(kept >> ((first + i) / size) & 1)) key[i] = 0;
                     }
                 }
-                // The candidates: the lanes' best ones, one after the other, give a number that one more than top_k experts reach; what
+                // The candidates: the lanes' best ones, one after the other, give a number that top_k experts reach; what
                 // lies that high (or too little below to tell) is mostly fewer than a warp has lanes, and places are counted.
                 uint32_t one = 0;
 #pragma unroll
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                 uint32_t floor = 0;
                 uint32_t left = one;
 #pragma unroll 4
-                for (uint32_t r = 0; r < rounds; ++r) {
+                for (uint32_t r = 0; r < K; ++r) {
                     floor = __reduce_max_sync(~0u, left);
                     if (left == floor) left = 0;
                 }
@@ -369,8 +370,8 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                         const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(&list[i]);
                         place += (two.x > mine) + (two.y > mine);
                     }
-                    if (lane < n && place < rounds) places[place] = make_uint2(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
-                    if (n + lane < rounds) places[n + lane] = make_uint2(0, 0);
+                    if (lane < n && place < K) places[place] = make_uint2(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
+                    if (n + lane < K) places[n + lane] = make_uint2(0, 0);
                 } else {                                    // by rounds
                     uint32_t two = 0, at_one = 0, at_two = 0, taken = 0;
                     auto at_hand = [&] {
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                     };
                     at_hand();
 #pragma unroll 1
-                    for (uint32_t r = 0; r < rounds; ++r) {
+                    for (uint32_t r = 0; r < K; ++r) {
                         const uint32_t best = __reduce_max_sync(~0u, one);
                         const uint32_t firsts = __ballot_sync(~0u, one == best);
                         if (one == best && !(firsts & below)) {
@@ -396,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                     }
                 }
                 __syncwarp();
-                // candidates stand in falling order, so close ones are neighbours; the one after the last place counts too
-                const uint2 given = lane < rounds ? places[lane] : make_uint2(0, 0);
+                // the chosen stand in falling order, so close ones are neighbours
+                const uint2 given = lane < K ? places[lane] : make_uint2(0, 0);
                 id = given.x > kNothing ? static_cast<int>(given.y) : -1;
                 float chosen = -INFINITY;
                 bool doubt = false;
@@ -406,9 +407,23 @@ __global__ void __launch_bounds__(kThreads, V <= 8 ? kRouteBlocks : 1) k_route(c
                     doubt = id >= 0 && tied_in_64(chosen, base, soft);
                 } else {
                     if (id >= 0) chosen = to_float(l[id]);
-                    const uint2 next = lane + 1 < rounds ? places[lane + 1] : make_uint2(0, 0);
+                    const uint2 next = lane + 1 < K ? places[lane + 1] : make_uint2(0, 0), end = places[K - 1];
                     if (lane < K && next.x > kNothing && value_of(given.x) - value_of(next.x) <= tol)
                         doubt = chosen != to_float(l[next.y]) || (j.bias && j.bias[id] != j.bias[next.y]);
+                    // and what is as close to the last place as that, on either side of it
+                    if (end.x > kNothing) {
+                        const float at_end = value_of(end.x), end_l = to_float(l[end.y]), end_b = j.bias ? j.bias[end.y] : 0.0f;
+                        auto close_to_end = [&](uint32_t order, uint32_t e) {
+                            return order > kNothing && fabsf(value_of(order) - at_end) <= tol && (to_float(l[e]) != end_l || (j.bias && j.bias[e] != end_b));
+                        };
+                        if (n <= 32) {
+                            if (lane < n) doubt |= close_to_end(static_cast<uint32_t>(mine >> 32), 0xFFFFFFFFu - static_cast<uint32_t>(mine));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < V; ++i)
+                                if (key[i]) doubt |= close_to_end(key[i], first + i);
+                        }
+                    }
                 }
                 __syncwarp();
                 if (__any_sync(~0u, doubt) && !close) {

@@ -495,3 +495,24 @@ def test_refusals(binding):
         with pytest.raises(binding.AdacompError):
             binding.Distiller(vocab)
     assert d.last_error() == 0
+    with pytest.raises(ValueError):                 # more rows than a call takes
+        binding.Distiller(1).top(torch.zeros((1, 1), device="cuda").expand(1 << 31, 1), 1)
+
+
+def test_two_streams_at_once(binding):
+    """Two handles, each on a stream of its own, neither waiting for the other."""
+    n, vocab, k = 500, 20011, 30
+    x, y = logits_like(n, vocab, "bf16", 1), logits_like(n, vocab, "bf16", 2)
+    handles, streams = [binding.Distiller(vocab) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    alone = handles[0].top(x, k)
+    want = handles[0].loss_grad(y, *alone)
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for h, s, g in zip(handles, streams, got):
+            pairs = h.top(x, k, stream=s)
+            g.append((pairs, h.loss_grad(y, *pairs, stream=s)))
+    torch.cuda.synchronize()
+    for g in got:
+        for pairs, result in g:
+            assert all(torch.equal(a, b) for a, b in zip(pairs, alone)) and all(torch.equal(a, b) for a, b in zip(result, want))

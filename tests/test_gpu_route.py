@@ -354,3 +354,19 @@ def test_infinite_biases(binding):
     for score in ("softmax", "sigmoid"):
         experts, _, _, _ = check(binding, rows(40, 64, "bf16", 3), bias, top_k=5, score=score)
         assert bool((experts[:, :3] == torch.tensor([9, 33, 50], device="cuda", dtype=torch.int32)).all()) and bool((experts >= 5).all())
+
+
+@pytest.mark.parametrize("experts", [40, 748])
+def test_close_ones_behind_equal_ones(binding, experts):
+    """Sigmoids that are 1 in fp32: two equal logits stand before a larger one, which 64 bits choose."""
+    x = rows(60, experts, "f32", 4)
+    x[:, [3, 20]] = 18.0
+    x[:, 31] = 19.0
+    x[30:, 5:15] = 18.0
+    zero = torch.zeros(experts, device="cuda")
+    for k in (1, 2, 3):
+        experts_, _, _, _ = check(binding, x, zero, top_k=k, score="sigmoid")
+        assert bool((experts_[:, 0] == 31).all())
+    many = torch.full((20, experts), 18.0, device="cuda")       # more equal ones than a warp has lanes
+    many[:, 35] = 19.0
+    check(binding, many, zero, top_k=2, score="sigmoid")
