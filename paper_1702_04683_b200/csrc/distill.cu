@@ -289,7 +289,8 @@ template <typename T, int PLACE> struct Chunk {
     }
 };
 
-template <uint32_t RANKS_MOST, typename V, typename F> __device__ __forceinline__ V cluster_gather(V* s_part, const V& mine, uint32_t rank, uint32_t rank_bits, V none, F join) {
+// Every block's part, told to all blocks of the cluster and joined by every warp.
+template <typename V, typename F> __device__ __forceinline__ V cluster_gather(V* s_part, const V& mine, uint32_t rank, uint32_t rank_bits, V none, F join) {
     const uint32_t lane = threadIdx.x % 32;
     if (threadIdx.x < 1u << rank_bits) *cooperative_groups::this_cluster().map_shared_rank(&s_part[rank], threadIdx.x) = mine;
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -325,7 +326,7 @@ __device__ __noinline__ Running careful_sum(const Chunk<T, PLACE> chunk, float c
     __syncthreads();
     const Running none = {-INFINITY, 0.0f};
     r = warp_join(lane < THREADS / 32 ? s_warp[lane] : none, c);
-    if (rank_bits) r = cluster_gather<8>(s_part, r, rank, rank_bits, none, [&](const Running& x) { return warp_join(x, c); });
+    if (rank_bits) r = cluster_gather(s_part, r, rank, rank_bits, none, [&](const Running& x) { return warp_join(x, c); });
     return r;
 }
 
@@ -363,6 +364,20 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
     }
     const bool read = weight != 0.0f && (MODE != kGrad || share.live != 0.0f);
 
+    // The thread's first entry of the list, in blocks of 512 on its way before all else: a logit has to be looked up with it, and two blocks on
+    // an SM hide little (8192 x 50000 bf16 385 -> 364 us; with three and more blocks it only takes registers, 256 -> 269 us for 2048 x 65536 fp32).
+    constexpr bool kEarly = THREADS == 512;
+    auto token_at = [&](uint32_t i) -> int64_t {
+        const uint64_t at = j.idx.offset(row) + i;
+        return j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at] : reinterpret_cast<const int32_t*>(j.idx.data)[at];
+    };
+    int64_t first_token = -1;
+    float first_t = 0.0f;
+    if (kEarly && read && tid < j.k) {
+        first_token = token_at(tid);
+        first_t = load_value(j.val, j.val.offset(row) + tid);
+    }
+
     // the thread's vectors in four groups of copies
     const uint32_t staged = PLACE == kPartly ? j.staged : 0, n_staged = PLACE == kPartly ? min(n_here, staged) : n_here;
     const uint32_t turns = (n_staged + kThreads - 1) / kThreads, quarter = (turns + 4 * kBatch - 1) / (4 * kBatch) * kBatch;
@@ -399,21 +414,21 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
             for (uint32_t i = tid; i < (n_here * N + loose + 31) / 32; i += kThreads) s_bits[i] = 0;
         __syncthreads();
         for (uint32_t i = tid; i < j.k; i += kThreads) {
-            const uint64_t at = j.idx.offset(row) + i;
-            const int64_t v = j.idx.type == ADACOMP_I64 ? reinterpret_cast<const int64_t*>(j.idx.data)[at]
-                                                        : reinterpret_cast<const int32_t*>(j.idx.data)[at];
-            s_t[i] = load_value(j.val, j.val.offset(row) + i);
+            const int64_t v = kEarly && i == tid ? first_token : token_at(i);
+            s_t[i] = kEarly && i == tid ? first_t : load_value(j.val, j.val.offset(row) + i);
             if (v >= j.vocab && rank == 0) record_error(j.status, ADACOMP_ERR_INVALID);
             const uint32_t token = v >= 0 && v < j.vocab ? static_cast<uint32_t>(v) : kNone;
             s_idx[i] = token;
             if (token == kNone) continue;
-            s_s[i] = to_float(in[token]);
+            const T s = in[token];
+            if (!kEarly) s_s[i] = to_float(s);
             const uint64_t mine = static_cast<uint64_t>(token) << 32 | i;
             for (uint32_t at = token * 2654435761u >> (32 - j.table_bits);; at = (at + 1) & ((1u << j.table_bits) - 1)) {      // half of it stays empty
                 const uint64_t there = atomicCAS(reinterpret_cast<unsigned long long*>(&s_table[at]), ~0ull, mine);
                 if (there >> 32 == token) atomicMin(reinterpret_cast<unsigned long long*>(&s_table[at]), mine);
                 if (there == ~0ull || there >> 32 == token) break;
             }
+            if (kEarly) s_s[i] = to_float(s);
         }
         __syncthreads();
         if (warp < parts) {
@@ -504,7 +519,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
             for (int w = 0; w < kWarps; ++w) rest += s_sum[w];
             if (joined) {
                 asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all blocks have started
-                rest = cluster_gather<8>(s_part[0], Running{0.0f, rest}, rank, j.rank_bits, Running{0.0f, 0.0f},
+                rest = cluster_gather(s_part[0], Running{0.0f, rest}, rank, j.rank_bits, Running{0.0f, 0.0f},
                                          [](const Running& x) { return Running{0.0f, warp_sum(x.s)}; }).s;
             }
             double q_sum = 0.0, left = 0.0;
@@ -566,6 +581,9 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
         }
     }
 
+    // While the last warp works out the loss, the others write the gradient (with the rest as a class 8192 x 50000 bf16 430 us, 445 where it
+    // writes too; rows that are read twice are 1 % the worse for it).
+    constexpr uint32_t kWriters = PLACE == kShared ? THREADS - 32 : THREADS;
     if (MODE != kLoss) {
         const bool live = share.live != 0.0f;
         const Chunk<T, PLACE> chunk = {in, vecs, s_data, nullptr, cut, n_here, loose, staged};
@@ -576,13 +594,13 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
         if (MODE == kGrad && read) __syncthreads();         // the list's logits have been read: in place the gradient overwrites them
         if (live && on_grid && fabsf(share.m) < kWild) {
             const float2 c2 = make_float2(j.c, j.c), shift = make_float2(-share.m * j.c, -share.m * j.c), rest2 = make_float2(rest, rest);
-            const uint32_t batches = (n_here + kBatch * kThreads - 1) / (kBatch * kThreads);
+            const uint32_t batches = (n_here + kBatch * kWriters - 1) / (kBatch * kWriters);
 #pragma unroll 1
-            for (uint32_t i = 0; i < batches; ++i) {
+            for (uint32_t i = 0; i < (tid < kWriters ? batches : 0); ++i) {
                 // from the back where anything is read a second time: first what was read last
-                const uint32_t v0 = (PLACE == kPartly ? batches - 1 - i : i) * (kBatch * kThreads) + tid;
+                const uint32_t v0 = (PLACE == kPartly ? batches - 1 - i : i) * (kBatch * kWriters) + tid;
                 uint4 x[kBatch];
-                chunk.template batch<kBatch, THREADS>(x, v0, 0u);
+                chunk.template batch<kBatch, kWriters>(x, v0, 0u);
 #pragma unroll
                 for (int u = 0; u < kBatch; ++u) {
                     float f[N];
@@ -596,7 +614,7 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
                         f[e] = z.x, f[e + 1] = z.y;
                     }
                     p.pack(f);
-                    if (v0 + u * kThreads < n_here) *reinterpret_cast<uint4*>(to + (v0 + u * kThreads) * N) = p.v[0];
+                    if (v0 + u * kWriters < n_here) *reinterpret_cast<uint4*>(to + (v0 + u * kWriters) * N) = p.v[0];
                 }
             }
         } else if (!live && on_grid) {
