@@ -336,6 +336,10 @@ __device__ __noinline__ Running careful_sum(const Chunk<T, PLACE> chunk, float c
 // is mostly the largest of all or near it, so that no maximum has to be looked for; where it overflows, it is taken once more with care.
 // PLACE: a thread's vectors are copied to shared memory by itself and stay there for the second pass, so that a logit crosses HBM once and
 // nothing waits for a load but its own thread; of rows too long for that the rest is read twice.
+//
+// Bound by a block's phases, which leave HBM idle between them, and by the MUFU and shared-memory queues within them (two
+// exponentials a logit are 60 % of MUFU's time): 8192 x 50000 bf16 366 us, 4.5 TB/s read and written, 4096 x 131072 with the rest as a
+// class 528 (4.1).  The loss alone is bound by HBM: 138 us, 6.0 TB/s.
 template <typename T, int MODE, int PLACE, int THREADS>
 __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 384 ? 1152 : 1024) / THREADS) k_distill(const Job j) {
     constexpr int N = kVec<T>, kBatch = 4, kWarps = THREADS / 32;
@@ -650,7 +654,7 @@ constexpr uint32_t kTopGroups = 32768;              // of a block
 constexpr uint32_t kHits = 512;
 
 // Shared memory of a block, no larger than it has to be: what it takes is taken from the L1 cache, which holds the loads under way
-// (with 26 KB a block instead of 9, 8192 x 50000 bf16 took 232 us instead of 206).
+// (with 26 KB a block instead of 9, 8192 x 50000 bf16 took 232 us instead of 193).
 struct TopShared {
     uint32_t candidates, keys, groups, bytes;
     TopShared(uint32_t k, uint32_t steps, uint32_t rank_bits) {
@@ -690,8 +694,8 @@ __device__ __forceinline__ float floor_of(uint64_t bound) {
     return __uint_as_float(bits == 0x80000000u ? 0x80000001u : bits);      // +0 does not exceed -0
 }
 
-// Sorts s_list[0 .. n) in falling order, n a power of two.  Up to one entry a thread, distances within a warp are exchanged by
-// shuffles (256 entries: 12 barriers instead of 36).
+// Sorts s_list[0 .. n) in falling order, n a power of two (bitonic).  Up to one entry a thread, distances within a warp are exchanged
+// by shuffles.
 template <uint32_t THREADS> __device__ void sort_list(uint64_t* s_list, uint32_t n) {
     if (n <= THREADS) {
         const uint32_t i = threadIdx.x;
@@ -768,13 +772,16 @@ __device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k
     return s_words[32];
 }
 
-// One pass over the row computes the sum and, for every thread's share of every step (a group: kTopVecs vectors), the largest entry, which
-// stays in shared memory.  With k of the threads' largest entries at or above a number, k entries of the row are: this bound
-// leaves some k + k / 5 candidates, whose groups alone are read again (from L2) and whose places in the order are counted.
+// One pass over the row computes the sum and, for every thread's share of every step (a group: kTopVecs vectors), the largest entry, of which
+// 16 bits stay in shared memory.  With k of the threads' largest entries at or above a number, k entries of the row are: this bound
+// leaves some k + k / 8 candidates, whose groups alone are read again (from L2) and whose places in the order are counted.
 // A list that is full (rows in which many groups hold large entries) is cut back to its k largest, which raises the bound.
 //
 // A row is one block's work, or a cluster's where there are few rows: the first block then takes the others' lists through
 // their shared memory.
+//
+// The pass alone takes what HBM does: 120 us for 8192 x 50000 bf16, 6.8 TB/s.  The whole kernel 175 (4.7 TB/s): twelve small blocks an SM, so
+// that the bound (10 us), the candidates and the order (45 us together) of some overlap others' passes; issue is 57 % busy.
 template <typename T>
 __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) {
     constexpr int N = kVec<T>, kWarps = kTopThreads / 32;
@@ -1108,6 +1115,13 @@ bool good_temperature(double t) { return t >= 0x1p-20f && t <= 0x1p20f; }
 constexpr uint32_t kRoom = 110 * 1024;              // of a block of 512 threads, two on an SM
 constexpr uint32_t kSmallRoom = 74 * 1024;          // of one of 256 or 384, three on an SM
 constexpr uint32_t kLargeList = 12 * 1024;
+// Many short rows in smaller blocks: 20000 x 1000 and x 4000 bf16 71 and 108 us with 64 threads, 122 and 139 with 128, 232 and 249 with
+// 256; 8192 x 20000 155 with 128, 167 with 256.
+constexpr uint32_t kShortRoom = 46 * 1024;          // of a block of 128 threads
+constexpr uint32_t kTinyRoom = 12 * 1024;           // of one of 64
+// Loss and gradient apart: 64 and 128 threads a row for many rows of up to 16 and 128 KB, 256 otherwise.  Loss alone of 8192 x 50000 bf16 138
+// us with 128, 158 with 256, of 500 of them 24 and 21, of 2048 x 65536 fp32 108 and 100; both of 10000 x 8000 bf16 104 with 64, 121 with 128.
+constexpr uint32_t kShortRow = 8192, kTinyRow = 1024;       // vectors
 
 template <typename T, int MODE, int PLACE, int THREADS> int launch_shape(Job j, uint32_t chunk_vecs, uint32_t beside, cudaStream_t stream) {
     j.staged = PLACE == kPartly ? ((THREADS == 512 ? kRoom : kSmallRoom) - beside) / 16 / (4 * THREADS) * (4 * THREADS) : chunk_vecs;
@@ -1147,12 +1161,17 @@ template <typename T, int MODE> int launch_distill(Job j, int n_sms, cudaStream_
     while (1u << j.table_bits < 2 * j.k) ++j.table_bits;
     const uint32_t bits = j.lse && MODE != kGrad ? ((chunk_vecs + 2) * kVec<T> + 31) / 32 * 4 : 0;
     const uint32_t beside = (8u << j.table_bits) + j.k * 12 + bits;         // the table, the list, the bits
+    const bool many = j.n_rows >= 4u * n_sms;
     if constexpr (MODE == kBoth) {
+        if (many && chunk_vecs * 16ull + beside <= kTinyRoom) return launch_shape<T, MODE, kShared, 64>(j, chunk_vecs, beside, stream);
+        if (many && chunk_vecs * 16ull + beside <= kShortRoom) return launch_shape<T, MODE, kShared, 128>(j, chunk_vecs, beside, stream);
         if (chunk_vecs * 16ull + beside <= kSmallRoom) return launch_shape<T, MODE, kShared, 256>(j, chunk_vecs, beside, stream);
         if (chunk_vecs * 16ull + beside <= kRoom) return launch_shape<T, MODE, kShared, 512>(j, chunk_vecs, beside, stream);
         if (beside <= kLargeList) return launch_shape<T, MODE, kPartly, 384>(j, chunk_vecs, beside, stream);
         return launch_shape<T, MODE, kPartly, 512>(j, chunk_vecs, beside, stream);
     } else {
+        if (many && n_vecs <= kTinyRow) return launch_shape<T, MODE, kDevice, 64>(j, chunk_vecs, beside, stream);
+        if (many && n_vecs <= kShortRow) return launch_shape<T, MODE, kDevice, 128>(j, chunk_vecs, beside, stream);
         return launch_shape<T, MODE, kDevice, 256>(j, chunk_vecs, beside, stream);
     }
 }

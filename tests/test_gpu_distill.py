@@ -516,3 +516,28 @@ def test_two_streams_at_once(binding):
     for g in got:
         for pairs, result in g:
             assert all(torch.equal(a, b) for a, b in zip(pairs, alone)) and all(torch.equal(a, b) for a, b in zip(result, want))
+
+
+@pytest.mark.parametrize("vocab,kind", [(500, "bf16"), (1501, "f32"), (7000, "f16"), (15001, "bf16"), (20000, "f32"), (30000, "bf16"), (52001, "f16"),
+                                        (70000, "bf16"), (40003, "f32")])
+@pytest.mark.parametrize("tail", [False, True])
+def test_many_rows_of_every_length(binding, vocab, kind, tail):
+    """Rows that blocks of every size take, whole or in part, and the same in place."""
+    n, k = 601, 30
+    teacher = logits_like(n, vocab, kind, 1)
+    student = (teacher.float() + logits_like(n, vocab, "f32", 2, 0.5)).to(TYPES[kind])
+    idx, val, lse = pairs_of(teacher, k)
+    idx[3, 5] = idx[3, 0]
+    idx[4, ::2] = -1
+    weight = torch.rand(n, device="cuda", generator=gen(3)) + 0.1
+    weight[::50] = 0.0
+    lse = lse if tail else None
+    _, grad = check_loss(binding, student, idx, val, lse, 1.0, weight)
+    d = binding.Distiller(vocab)
+    again = student.clone()
+    d.loss_grad(again, idx, val, lse, weight=weight, out=again)
+    assert torch.equal(again, grad)
+    _, stats = d.loss(student, idx, val, lse, weight=weight)
+    two = d.grad(student, idx, val, stats, lse, weight=weight)
+    again = student.clone()
+    assert torch.equal(d.grad(again, idx, val, stats, lse, weight=weight, out=again), two)
