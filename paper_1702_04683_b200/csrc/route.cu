@@ -513,8 +513,8 @@ __device__ __forceinline__ int counting(int id, uint32_t experts, uint32_t width
     return id < 0 || lane != static_cast<uint32_t>(__ffs(same)) - 1 ? -1 : id;
 }
 
-// The gradient where only the chosen experts have one: as many rows per warp as their places allow.  65536 x 128 fp32, k 8: 15 us, 2.6 TB/s
-// of zeros and places written; each row is a chain of load, lookup, sums and store.
+// The gradient where only the chosen experts have one: as many rows per warp as their places allow.  65536 x 128 fp32, k 8: 15 us, 2.5 TB/s
+// read and written; each row is a chain of load, lookup, sums and store.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_route_grad(const __grid_constant__ Job j, uint32_t width) {
     const uint32_t lane = threadIdx.x % 32, E = j.cfg.experts, K = j.cfg.top_k, rows = 32 / width, slot = lane % width;
