@@ -31,7 +31,8 @@ def gen(seed):
 def plain_choice(x, bias, cfg):
     """x [N, E] in 64 bits on the CPU -> experts [N, k], -1 where none is left."""
     N, E = x.shape
-    scores = torch.softmax(x, 1) if cfg["score"] == "softmax" else torch.sigmoid(x)
+    # (on the GPU: there equal logits have equal scores, the CPU's vectors and their remainders differ in the last bit)
+    scores = (torch.softmax(x.cuda(), 1) if cfg["score"] == "softmax" else torch.sigmoid(x.cuda())).cpu()
     value = scores + (0.0 if bias is None else bias.double().cpu())
     value = torch.where(x == -math.inf, -math.inf, value)
     bad = value.isnan().any(1) | x.isnan().any(1)
