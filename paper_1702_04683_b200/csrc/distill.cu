@@ -646,23 +646,22 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
 
 // ---------------------------------------------------------------------------------------------- top logits
 
-constexpr int kTopThreads = 128;
 constexpr int kTopVecs = 2;                         // vectors of a thread in one step: a group
-constexpr uint32_t kTopStep = kTopThreads * kTopVecs;
 constexpr int kBoundBits = 12;
 constexpr uint32_t kTopGroups = 32768;              // of a block
 constexpr uint32_t kHits = 512;
+constexpr uint32_t kShortTop = 1024, kShortList = 64;       // vectors of a row, pairs that blocks of 64 threads take
 
 // Shared memory of a block, no larger than it has to be: what it takes is taken from the L1 cache, which holds the loads under way
 // (with 26 KB a block instead of 9, 8192 x 50000 bf16 took 232 us instead of 193).
 struct TopShared {
     uint32_t candidates, keys, groups, bytes;
-    TopShared(uint32_t k, uint32_t steps, uint32_t rank_bits) {
+    TopShared(uint32_t k, uint32_t threads, uint32_t steps, uint32_t rank_bits) {
         candidates = rank_bits ? 1024 : 256;        // a cluster's first block takes the others' lists
         while (candidates < 2 * k) candidates *= 2;
         keys = candidates * sizeof(uint64_t);                        // and later the hits
         groups = keys + kHits * sizeof(uint16_t);
-        bytes = groups + steps * kTopThreads * sizeof(uint16_t);
+        bytes = groups + steps * threads * sizeof(uint16_t);
     }
 };
 
@@ -730,15 +729,15 @@ template <uint32_t THREADS> __device__ void sort_list(uint64_t* s_list, uint32_t
     __syncthreads();
 }
 
-// Cuts s_list[0 .. n), n <= 8 kTopThreads, down to the entries whose value is among the k largest ones' (k, some more, and ties),
+// Cuts s_list[0 .. n), n <= 8 THREADS, down to the entries whose value is among the k largest ones' (k, some more, and ties),
 // in any order; returns how many.  s_words: 34 of them.
-__device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k, uint32_t* s_words) {
+template <uint32_t THREADS> __device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k, uint32_t* s_words) {
     const uint32_t tid = threadIdx.x, lane = tid % 32;
     uint64_t x[8];
     uint32_t low = ~0u, high = 0;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-        x[u] = tid + u * kTopThreads < n ? s_list[tid + u * kTopThreads] : 0;
+        x[u] = tid + u * THREADS < n ? s_list[tid + u * THREADS] : 0;
         high = max(high, static_cast<uint32_t>(x[u] >> 32));
         if (x[u]) low = min(low, static_cast<uint32_t>(x[u] >> 32));
     }
@@ -782,9 +781,10 @@ __device__ __noinline__ uint32_t narrow(uint64_t* s_list, uint32_t n, uint32_t k
 //
 // The pass alone takes what HBM does: 120 us for 8192 x 50000 bf16, 6.8 TB/s.  The whole kernel 175 (4.7 TB/s): twelve small blocks an SM, so
 // that the bound (10 us), the candidates and the order (45 us together) of some overlap others' passes; issue is 57 % busy.
-template <typename T>
-__global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) {
-    constexpr int N = kVec<T>, kWarps = kTopThreads / 32;
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_top_logits(const TopJob j) {
+    constexpr int N = kVec<T>, kWarps = THREADS / 32;
+    constexpr uint32_t kTopThreads = THREADS, kTopStep = THREADS * kTopVecs;
     static_assert(kHits * sizeof(uint16_t) >= 2 * kTopThreads * sizeof(uint32_t) && kTopGroups <= 65536, "rooms");
     extern __shared__ uint64_t s_list[];            // [candidates]
     uint32_t* const s_key = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_list) + j.at_keys);
@@ -1057,7 +1057,7 @@ __global__ void __launch_bounds__(kTopThreads, 12) k_top_logits(const TopJob j) 
     T* val = reinterpret_cast<T*>(j.val) + static_cast<uint64_t>(row) * j.k;
     int32_t* idx = j.idx + static_cast<uint64_t>(row) * j.k;
     uint32_t n = s_count;
-    if (n > kTopThreads && n > 2 * j.k && n <= 8 * kTopThreads) n = narrow(s_list, n, j.k, s_above);
+    if (n > kTopThreads && n > 2 * j.k && n <= 8 * kTopThreads) n = narrow<kTopThreads>(s_list, n, j.k, s_above);
     if (n <= 3 * kTopThreads) {
         if (tid == 0 && n % 2) s_list[n] = 0;
         __syncthreads();
@@ -1209,7 +1209,8 @@ int distill(adacomp_distill_t* h, const adacomp_rows_t* logits, uint32_t n_rows,
     return launch_distill<__half, MODE>(j, h->n_sms, stream);
 }
 
-template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
+template <typename T, int THREADS> int launch_top_shape(TopJob j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
+    constexpr uint32_t kTopThreads = THREADS, kTopStep = THREADS * kTopVecs;
     // several blocks a row as long as that makes no more than eight to an SM and each has some steps to do (300 x 131072 bf16: 37 us, 44
     // with one block a row), or where one could
     // not hold the groups of a row
@@ -1220,12 +1221,12 @@ template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaS
         ++j.rank_bits;
     if (static_cast<uint64_t>(n_rows) << j.rank_bits > INT_MAX) return ADACOMP_ERR_INVALID;       // more blocks than a grid has
     const uint32_t ranks = 1u << j.rank_bits, steps = ((n_vecs + ranks - 1) / ranks + kTopStep - 1) / kTopStep;
-    const TopShared shared(j.k, steps, j.rank_bits);
+    const TopShared shared(j.k, THREADS, steps, j.rank_bits);
     j.candidates = shared.candidates;
     j.at_keys = shared.keys;
     j.at_groups = shared.groups;
-    if (shared.bytes > 46 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_top_logits<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      static_cast<int>(TopShared(kMaxPairs, kTopGroups / kTopThreads, 0).bytes)));
+    if (shared.bytes > 46 * 1024) ADACOMP_CUDA(cudaFuncSetAttribute(k_top_logits<T, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(TopShared(kMaxPairs, THREADS, kTopGroups / THREADS, 0).bytes)));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_rows * ranks);
     cfg.blockDim = dim3(kTopThreads);
@@ -1238,10 +1239,16 @@ template <typename T> int launch_top(TopJob j, uint32_t n_rows, int n_sms, cudaS
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = ranks > 1 ? 1 : 0;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_top_logits<T>, j);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_top_logits<T, THREADS>, j);
     if (e != cudaSuccess) return cuda_fail(e);
     ADACOMP_LAUNCH_CHECK();
     return ADACOMP_OK;
+}
+
+template <typename T> int launch_top(const TopJob& j, uint32_t n_rows, int n_sms, cudaStream_t stream) {
+    // many short rows in blocks of 64 threads, twice as many on an SM: 20000 x 4000 bf16, 20 of each row, 75 us, 91 with 128
+    if (j.vocab <= kShortTop * kVec<T> && n_rows >= 8u * n_sms && j.k <= kShortList) return launch_top_shape<T, 64>(j, n_rows, n_sms, stream);
+    return launch_top_shape<T, 128>(j, n_rows, n_sms, stream);
 }
 
 }  // namespace

@@ -541,3 +541,14 @@ def test_many_rows_of_every_length(binding, vocab, kind, tail):
     two = d.grad(student, idx, val, stats, lse, weight=weight)
     again = student.clone()
     assert torch.equal(d.grad(again, idx, val, stats, lse, weight=weight, out=again), two)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n,vocab,k", [(1300, 4000, 20), (1201, 901, 64), (1184, 64, 64), (1500, 7777, 1), (1300, 4000, 65)])
+def test_top_of_many_short_rows(binding, n, vocab, k, kind):
+    x = logits_like(n, vocab, kind, vocab)
+    check_top(binding, x, k)
+    check_top(binding, (x * 0.4).round(), k, temperature=2.0)         # ties
+    x[::3, vocab // 3:] = -math.inf
+    x[5] = 1.0
+    check_top(binding, x, k)
