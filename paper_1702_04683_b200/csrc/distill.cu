@@ -566,7 +566,8 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
                         if (q != 0.0) cross += q * (t - (static_cast<double>(s_s[i]) * j.c - from_m) * kLn2);
                     }
                     cross = warp_sum(cross);
-                    const double log_total = log(static_cast<double>(total));
+                    // (not from the rounded total: where the list holds little, log rest nearly takes it away again)
+                    const double log_total = log(tail ? static_cast<double>(rest) + listed : static_cast<double>(total));
                     if (!tail) loss = cross / q_sum - log(q_sum) + log_total;
                     else loss = cross + q_sum * log_total + (left > 0.0 ? left * (log(left) - log(static_cast<double>(rest)) + log_total) : 0.0);
                     if (q_sum != q_sum) loss = NAN;
