@@ -558,16 +558,19 @@ __global__ void __launch_bounds__(THREADS, (MODE == kLoss ? 1536 : THREADS == 38
                 double loss = 0.0;
                 if (share.live != 0.0f) {
                     const double from_m = reference(share.m, j.c);
-                    double cross = 0.0;
+                    // the listed tokens' own terms of the sum once more, exactly: of a small loss their rounding is a part
+                    double cross = 0.0, exact = 0.0;
                     for (uint32_t i = lane; i < j.k; i += 32) {
                         if (s_idx[i] == kNone) continue;
                         const double t = tail ? s_t[i] * j.inv_t - lse : (static_cast<double>(s_t[i]) - top) * j.inv_t;
                         const double q = tail ? exp(t) : expf(static_cast<float>(t));
-                        if (q != 0.0) cross += q * (t - (static_cast<double>(s_s[i]) * j.c - from_m) * kLn2);
+                        const double y = static_cast<double>(s_s[i]) * j.c - from_m;
+                        if (q != 0.0) cross += q * (t - y * kLn2);
+                        exact += tail ? exp2(y) : exp2(y) - exp_from(s_s[i], share.m, j.c);
                     }
-                    cross = warp_sum(cross);
+                    cross = warp_sum(cross), exact = warp_sum(exact);
                     // (not from the rounded total: where the list holds little, log rest nearly takes it away again)
-                    const double log_total = log(tail ? static_cast<double>(rest) + listed : static_cast<double>(total));
+                    const double log_total = log((tail ? static_cast<double>(rest) : static_cast<double>(total)) + exact);
                     if (!tail) loss = cross / q_sum - log(q_sum) + log_total;
                     else loss = cross + q_sum * log_total + (left > 0.0 ? left * (log(left) - log(static_cast<double>(rest)) + log_total) : 0.0);
                     if (q_sum != q_sum) loss = NAN;
